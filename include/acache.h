@@ -67,6 +67,7 @@ typedef enum {
 /* bits of the device status word returned by acache_poll_status */
 #define ACACHE_FLAG_BAD_INDEX   0x1u  /* an anchor / masked / extra index was out of range; row skipped */
 #define ACACHE_FLAG_WAIT_EXPIRED 0x2u /* a bounded wait inside a kernel gave up                          */
+#define ACACHE_FLAG_NONFINITE   0x4u  /* a row written to an 8-bit cache held an infinity or a NaN       */
 
 /* flags of acache_layer_step */
 #define ACACHE_F_SCORE            0x1u /* form Q for the masked rows from x and run the scoring (Eq. 4-5) */
@@ -117,6 +118,26 @@ typedef struct {
     int64_t batch_stride;
     int32_t ctx_capacity;
 } acache_kv;
+
+/* formats of the codes of an 8-bit cache */
+#define ACACHE_KV8_E4M3 0   /* floating point, 4 exponent and 3 mantissa bits, no infinities */
+#define ACACHE_KV8_INT8 1   /* whole numbers -127 .. 127                                     */
+
+/* One layer's KV cache held in 8 bits (the paper has no counterpart; half the memory of acache_kv and half the bytes of every
+ * pass over it).  DEVICE codes [B, Hkv, ctx_capacity, d], a (request, head)'s tokens side by side, K after the rotary
+ * embedding; DEVICE exponent bytes [B, Hkv, ctx_capacity / block], one for each block of `block` tokens and head: a code c under
+ * the exponent byte e stands for c * 2^(e - 127), which is exact in bf16.  e = 0: the block holds nothing and reads as
+ * zero; a new cache is one whose exponent bytes are 0.
+ * batch_stride: codes between two requests (normally Hkv * ctx_capacity * d; a multiple of 16); exponents of the requests follow
+ * each other.  0: one cache shared by the batch, for the calls that only read it. */
+typedef struct {
+    void    *k, *v;
+    uint8_t *k_exp, *v_exp;
+    int64_t  batch_stride;
+    int32_t  ctx_capacity;          /* a multiple of block */
+    int32_t  block;                 /* 16, 32, 64 or 128 tokens */
+    int32_t  format;                /* ACACHE_KV8_E4M3 or ACACHE_KV8_INT8 */
+} acache_kv8;
 
 /* The request batch: every request shares the layout (ctx_len, affix span, m, e). */
 typedef struct {
@@ -302,6 +323,51 @@ acache_status acache_layer_step(acache_ctx *ctx, const acache_layer_weights *w,
                                 const acache_request *req, acache_kv *kv,
                                 const void *x, int x_is_compact, double ratio, uint32_t flags,
                                 float *scores, int32_t *anchor_idx, void *y, acache_stream_t stream);
+
+/* Writes rows into an 8-bit cache, quantising them: row i of request b goes to position pos[b, i] (DEVICE int32 [B, n_rows]),
+ * or to start + i where pos is NULL.  Of a block that is written to, for K and V and every head by itself:
+ *   e_rows = exponent field of the largest finite |x| of the written rows - 6 (int8) or - 7 (e4m3), at least 16
+ *            (0 where they are all zero or below the normal numbers)
+ *   e      = max(e_rows, its exponent so far) if the block has other rows below ctx_len, which stay; else e_rows
+ *   code   = x * 2^(127 - e) rounded to the nearest code, ties to the even one
+ * The rows that stay keep their codes bit for bit while e does not grow; where it does, their codes are rounded to the new
+ * scale.  Positions of the block from ctx_len on are cleared.  Other blocks are left as they are.
+ * int8: -127 .. 127, infinities saturate and a NaN becomes 0.  e4m3: both become NaN.  Either raises ACACHE_FLAG_NONFINITE.
+ * A position outside [0, ctx_len) raises ACACHE_FLAG_BAD_INDEX and its row is skipped; of two rows of one position the last
+ * is written.
+ *   k_rows, v_rows: DEVICE bf16 [B, n_rows, Hkv, d], requests rows_batch_stride elements apart (a multiple of 8; 0: the same
+ *   rows for every request); they may be rows of an acache_kv cache.  ctx_len: length of the context, at most ctx_capacity.
+ * Bits are reproducible and do not depend on the order of the list. */
+acache_status acache_kv8_write(acache_ctx *ctx, acache_kv8 *kv, int32_t batch, int32_t ctx_len, const void *k_rows,
+                               const void *v_rows, int64_t rows_batch_stride, int32_t n_rows, const int32_t *pos, int32_t start,
+                               acache_stream_t stream);
+
+/* Reads rows of an 8-bit cache back as bf16, exactly: k_out, v_out DEVICE bf16 [B, n_rows, Hkv, d] (either may be NULL),
+ * positions as in acache_kv8_write.  A position outside [0, ctx_len) raises ACACHE_FLAG_BAD_INDEX and reads as zero. */
+acache_status acache_kv8_read(acache_ctx *ctx, const acache_kv8 *kv, int32_t batch, int32_t ctx_len, void *k_out, void *v_out,
+                              int32_t n_rows, const int32_t *pos, int32_t start, acache_stream_t stream);
+
+/* Bidirectional attention over an 8-bit cache:
+ *   o[b, i, h] = sum_j softmax_j(q[b, i, h] . K[b, j, kv(h)] / sqrt(d)) V[b, j, kv(h)],   lse[b, i, h] = log sum_j exp(...)
+ * over the positions j < lens[b] (DEVICE int32 [B]; NULL: ctx_len) that exist: bit j % 32 of key_drop[b, j / 32] is clear
+ * (DEVICE uint32 [B, ceil(ctx_len / 32)]; NULL: all).  Where there is none, o = 0 and lse = -inf.  What the cache holds in
+ * places that do not count is of no account, NaN included.  A length outside [0, ctx_len] raises ACACHE_FLAG_BAD_INDEX and is
+ * taken as the nearer end.
+ *   q, o: DEVICE bf16 [B, n_rows, H, d], n_rows from one (a single token) to many; lse: DEVICE fp32 [B, n_rows, H], natural
+ *   logarithm, may be NULL (with it, results over several caches can be put together).
+ * Logits, softmax and sums in fp32; probabilities and queries enter the products with 11 bits, codes exactly.  The scales of
+ * one head's values may differ by a factor of 2^100. */
+acache_status acache_kv8_attention(acache_ctx *ctx, const acache_kv8 *kv, int32_t batch, int32_t n_rows, int32_t ctx_len,
+                                   const void *q, const int32_t *lens, const uint32_t *key_drop, void *o, float *lse,
+                                   acache_stream_t stream);
+
+/* acache_layer_step on an 8-bit cache: scores are taken on the affix keys read back, the fresh K/V of the rows of R are
+ * written into the cache as acache_kv8_write does, and their attention is acache_kv8_attention over the cache as it then is
+ * (so rows of R see their own K/V quantised too).  A row that stays in the cache keeps its codes unless a refreshed row of its
+ * block is too large for the block's scale.  Flags and other arguments as acache_layer_step. */
+acache_status acache_layer_step_kv8(acache_ctx *ctx, const acache_layer_weights *w, const acache_request *req, acache_kv8 *kv,
+                                    const void *x, int x_is_compact, double ratio, uint32_t flags, float *scores,
+                                    int32_t *anchor_idx, void *y, acache_stream_t stream);
 
 /* Predict-then-commit on the current block (Section 3.1, Eq. 2-3, with the confidence-threshold
  * commit rule the paper's set-up uses, threshold 0.9 in Section 5):

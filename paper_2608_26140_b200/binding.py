@@ -15,7 +15,8 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libacache.so")
 
 OK, ERR_INVALID_ARG, ERR_UNSUPPORTED_SHAPE, ERR_WORKSPACE, ERR_CUDA, ERR_TIMEOUT = range(6)
-FLAG_BAD_INDEX, FLAG_WAIT_EXPIRED = 0x1, 0x2
+FLAG_BAD_INDEX, FLAG_WAIT_EXPIRED, FLAG_NONFINITE = 0x1, 0x2, 0x4
+KV8_FORMATS = {"e4m3": 0, "int8": 1}
 F_SCORE, F_SELECT, F_ACCUMULATE, F_SCORE_NORM_FULL, F_NO_RECOMPUTE, F_DROP_NON_ANCHOR = 0x1, 0x2, 0x4, 0x8, 0x10, 0x20
 
 EXPORTS = ["acache_create", "acache_workspace_bytes", "acache_set_workspace", "acache_destroy",
@@ -25,7 +26,8 @@ EXPORTS = ["acache_create", "acache_workspace_bytes", "acache_set_workspace", "a
            "acache_score_anchors_static", "acache_predict_commit", "acache_denoise_step", "acache_probe_select",
            "acache_commit_update", "acache_generate_block", "acache_denoise_step_shared", "acache_recompute_rows_shared",
            "acache_decode_step_shared", "acache_generate_block_shared", "acache_layer_step_shared",
-           "acache_host_x_in_place", "acache_score_kv_deviation", "acache_debug_expire_next_wait"]
+           "acache_host_x_in_place", "acache_score_kv_deviation", "acache_debug_expire_next_wait",
+           "acache_kv8_write", "acache_kv8_read", "acache_kv8_attention", "acache_layer_step_kv8"]
 
 STAGES = ["mask_q", "score", "topk", "gather_norm", "qkv", "attention", "oproj", "mlp_norm", "gate_up", "down"]
 
@@ -45,6 +47,11 @@ class LayerWeights(C.Structure):
 
 class KV(C.Structure):
     _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("batch_stride", C.c_int64), ("ctx_capacity", C.c_int32)]
+
+
+class KV8(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_exp", C.c_void_p), ("v_exp", C.c_void_p), ("batch_stride", C.c_int64),
+                ("ctx_capacity", C.c_int32), ("block", C.c_int32), ("format", C.c_int32)]
 
 
 class Request(C.Structure):
@@ -146,6 +153,15 @@ def load_library(path: Optional[str] = None) -> C.CDLL:
                                                  C.POINTER(Request), vp, vp, i32, C.POINTER(vp), C.POINTER(vp), vp, vp, vp, vp,
                                                  i32, vp, vp, i32, C.c_float, i32, i32, vp, vp, vp, vp, C.POINTER(i32), vp]
     lib.acache_generate_block_shared.restype = C.c_int
+    lib.acache_kv8_write.argtypes = [vp, C.POINTER(KV8), i32, i32, vp, vp, i64, i32, vp, i32, vp]
+    lib.acache_kv8_write.restype = C.c_int
+    lib.acache_kv8_read.argtypes = [vp, C.POINTER(KV8), i32, i32, vp, vp, i32, vp, i32, vp]
+    lib.acache_kv8_read.restype = C.c_int
+    lib.acache_kv8_attention.argtypes = [vp, C.POINTER(KV8), i32, i32, i32, vp, vp, vp, vp, vp, vp]
+    lib.acache_kv8_attention.restype = C.c_int
+    lib.acache_layer_step_kv8.argtypes = [vp, C.POINTER(LayerWeights), C.POINTER(Request), C.POINTER(KV8), vp, C.c_int,
+                                          C.c_double, u32, vp, vp, vp, vp]
+    lib.acache_layer_step_kv8.restype = C.c_int
     lib.acache_stage_timing.argtypes = [vp, C.c_int]
     lib.acache_stage_timing.restype = C.c_int
     lib.acache_read_stage_times.argtypes = [vp, C.POINTER(C.c_float)]
@@ -239,6 +255,38 @@ class Context:
         return KV(cache_k.data_ptr(), cache_v.data_ptr(), cap * hkv * d, cap)
 
     @staticmethod
+    def kv8(codes_k, codes_v, exp_k, exp_v, block, fmt, shared=False) -> KV8:
+        """8-bit cache over one-byte codes [B, Hkv, capacity, d] and exponent bytes [B, Hkv, capacity / block]; fmt: a value of
+        KV8_FORMATS.  Requests may lie further apart than their codes take.  shared: one request's cache for every request."""
+        _, hkv, cap, d = codes_k.shape
+        for c, e in ((codes_k, exp_k), (codes_v, exp_v)):
+            if c.element_size() != 1 or e.element_size() != 1:
+                raise ValueError("codes and exponents are bytes")
+            if c.shape != codes_k.shape or tuple(e.shape) != (c.shape[0], hkv, cap // block):
+                raise ValueError(f"codes {tuple(c.shape)} and exponents {tuple(e.shape)} do not go together with blocks of {block}")
+            if c.stride()[1:] != (cap * d, d, 1) or not e.is_contiguous() or c.stride(0) != codes_k.stride(0):
+                raise ValueError("the codes of a request and all exponents are contiguous")
+        return KV8(_ptr(codes_k), _ptr(codes_v), _ptr(exp_k), _ptr(exp_v), 0 if shared else codes_k.stride(0), cap, block, fmt)
+
+    def new_kv8(self, batch, ctx_capacity, block=64, fmt="e4m3"):
+        """An empty 8-bit cache for this context's shape: (tensors to keep alive: codes k, v, exponents k, v; the KV8)."""
+        import torch
+        hkv, d = self.desc.n_kv_heads, self.desc.head_dim
+        cap = -(-ctx_capacity // block) * block
+        t = [torch.zeros((batch, hkv, cap, d), dtype=torch.uint8, device=self.device) for _ in range(2)]
+        t += [torch.zeros((batch, hkv, cap // block), dtype=torch.uint8, device=self.device) for _ in range(2)]
+        return t, self.kv8(*t, block, KV8_FORMATS[fmt])
+
+    @staticmethod
+    def pack_key_drop(drop):
+        """Boolean [B, T] (True: the position does not exist as a key) as the bit mask of kv8_attention, int32 [B, ceil(T / 32)]."""
+        import torch
+        import torch.nn.functional as F
+        B, T = drop.shape
+        bits = F.pad(drop.to(torch.int64), (0, -T % 32)).view(B, -1, 32) << torch.arange(32, device=drop.device)
+        return bits.sum(-1).to(torch.uint32).view(torch.int32)
+
+    @staticmethod
     def request(batch, ctx_len, affix_start, affix_len, masked_pos, extra_rows, rope_cos, rope_sin,
                 token_ids=None, n_embed=0) -> Request:
         nm = 0 if masked_pos is None else int(masked_pos.shape[1])
@@ -302,6 +350,59 @@ class Context:
         self._check(self.lib.acache_layer_step(self.h, C.byref(w), C.byref(req), C.byref(kv), _ptr(x),
                                                int(x_is_compact), float(ratio), int(flags), _ptr(scores),
                                                _ptr(anchor_idx), _ptr(y), _stream()))
+
+    def kv8_write(self, cache: KV8, batch, ctx_len, k_rows, v_rows, start=0, pos=None):
+        """Rows [B, n, Hkv, d] (bf16; requests may lie further apart) to positions start .. or pos [B, n] (int32)."""
+        stride = self._check_rows(k_rows, batch, pos)
+        if self._check_rows(v_rows, batch, pos) != stride or v_rows.shape != k_rows.shape:
+            raise ValueError("k_rows and v_rows differ in shape or stride")
+        self._check(self.lib.acache_kv8_write(self.h, C.byref(cache), batch, ctx_len, _ptr(k_rows), _ptr(v_rows), stride,
+                                              k_rows.shape[1], _ptr(pos), start, _stream()))
+
+    def kv8_read(self, cache: KV8, batch, ctx_len, k_out, v_out, start=0, pos=None):
+        """Rows at positions start .. or pos [B, n] into k_out, v_out [B, n, Hkv, d] (contiguous; either may be None)."""
+        n = None
+        for t in (k_out, v_out):
+            if t is not None:
+                self._check_rows(t, batch, pos)
+                if not t.is_contiguous() or n not in (None, t.shape[1]):
+                    raise ValueError("k_out and v_out are contiguous and of one length")
+                n = t.shape[1]
+        if n is None:
+            raise AcacheError(ERR_INVALID_ARG, "neither k_out nor v_out is given")
+        self._check(self.lib.acache_kv8_read(self.h, C.byref(cache), batch, ctx_len, _ptr(k_out), _ptr(v_out), n, _ptr(pos),
+                                             start, _stream()))
+
+    def kv8_attention(self, cache: KV8, batch, ctx_len, q, o, lse=None, lens=None, key_drop=None):
+        """q, o: bf16 [B, n, H, d]; lse: fp32 [B, n, H]; lens: int32 [B]; key_drop: int32 [B, ceil(ctx_len / 32)] (pack_key_drop)."""
+        import torch
+        B, n, H, d = q.shape
+        if (B, H, d) != (batch, self.desc.n_heads, self.desc.head_dim) or o.shape != q.shape:
+            raise ValueError(f"q {tuple(q.shape)} or o {tuple(o.shape)} is not [batch, n, H, d]")
+        want = [(q, torch.bfloat16, q.shape), (o, torch.bfloat16, q.shape), (lse, torch.float32, (B, n, H)),
+                (lens, torch.int32, (B,)), (key_drop, torch.int32, (B, -(-ctx_len // 32)))]
+        for t, dtype, shape in want:
+            if t is not None and (t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous()):
+                raise ValueError(f"a tensor {tuple(t.shape)} of {t.dtype} where contiguous {tuple(shape)} of {dtype} is wanted")
+        self._check(self.lib.acache_kv8_attention(self.h, C.byref(cache), batch, n, ctx_len, _ptr(q), _ptr(lens), _ptr(key_drop),
+                                                  _ptr(o), _ptr(lse), _stream()))
+
+    def layer_step_kv8(self, w: LayerWeights, req: Request, cache: KV8, x, x_is_compact, ratio, flags, scores, anchor_idx, y):
+        """The layer-step on an 8-bit cache."""
+        self._check(self.lib.acache_layer_step_kv8(self.h, C.byref(w), C.byref(req), C.byref(cache), _ptr(x), int(x_is_compact),
+                                                   float(ratio), int(flags), _ptr(scores), _ptr(anchor_idx), _ptr(y), _stream()))
+
+    def _check_rows(self, t, batch, pos) -> int:
+        """Elements between the requests of rows [B, n, Hkv, d]."""
+        import torch
+        B, n, hkv, d = t.shape
+        if t.dtype != torch.bfloat16 or (B, hkv, d) != (batch, self.desc.n_kv_heads, self.desc.head_dim):
+            raise ValueError(f"rows {tuple(t.shape)} of {t.dtype} are not bf16 [batch, n, Hkv, d]")
+        if n and t.stride()[1:] != (hkv * d, d, 1):
+            raise ValueError("the rows of a request are contiguous")
+        if pos is not None and (pos.dtype != torch.int32 or tuple(pos.shape) != (B, n) or not pos.is_contiguous()):
+            raise ValueError("pos is int32 [batch, n], contiguous")
+        return t.stride(0) if B > 1 else n * hkv * d
 
     def predict_commit(self, h, h_rows, block_rows, batch, n_blk, final_norm_g, w_lm, vocab, threshold, token,
                        confidence, commit):

@@ -24,7 +24,7 @@ struct acache_ctx {
     size_t o_status, o_row_pos, o_row_src, o_xn, o_q, o_o, o_h1, o_xn2, o_act, o_knew, o_vnew;
     size_t o_mrow_pos, o_mrow_src, o_xn_mask, o_qmask, o_stats, o_partial, o_slot;
     size_t o_rowmask, partial_bytes;
-    size_t o_xstage, o_ystage, o_sstage, o_astage, o_gemm, o_attn, o_gridbar, o_mcidx, o_lstats, o_lxn, o_keymask;
+    size_t o_xstage, o_ystage, o_sstage, o_astage, o_gemm, o_attn, o_gridbar, o_mcidx, o_lstats, o_lxn, o_keymask, o_arrived;
     std::string err;
     uint64_t launches = 0;
     void* stash_rows = nullptr;   // set for the duration of a host-buffer call: device copy of the gathered rows of x
@@ -114,6 +114,83 @@ acache_status check_weights(acache_ctx* c, const acache_layer_weights* w, bool q
     return ACACHE_OK;
 }
 
+// The 8-bit cache of a call.  writes: the call stores into it, so every request needs its own.
+acache_status check_kv8(acache_ctx* c, const acache_kv8* kv, int32_t batch, int32_t ctx_len, bool writes) {
+    const acache_model_desc& d = c->d;
+    if (!c->ws) return fail(c, ACACHE_ERR_WORKSPACE, "workspace not set");
+    if (!kv) return fail(c, ACACHE_ERR_INVALID_ARG, "kv8 is NULL");
+    if (batch < 0 || batch > d.max_batch) return fail(c, ACACHE_ERR_INVALID_ARG, "batch %d outside [0, %d]", batch, d.max_batch);
+    if (ctx_len < 0 || ctx_len > d.max_ctx) return fail(c, ACACHE_ERR_INVALID_ARG, "ctx_len %d outside [0, %d]", ctx_len, d.max_ctx);
+    if (!kv->k || !kv->v || !kv->k_exp || !kv->v_exp || !aligned16(kv->k) || !aligned16(kv->v))
+        return fail(c, ACACHE_ERR_INVALID_ARG, "cache pointer NULL or misaligned");
+    if (kv->format != ACACHE_KV8_E4M3 && kv->format != ACACHE_KV8_INT8) return fail(c, ACACHE_ERR_INVALID_ARG, "format %d is neither e4m3 nor int8", kv->format);
+    if (kv->block != 16 && kv->block != 32 && kv->block != 64 && kv->block != 128)
+        return fail(c, ACACHE_ERR_UNSUPPORTED_SHAPE, "block %d is not 16, 32, 64 or 128 tokens", kv->block);
+    if (kv->ctx_capacity < ctx_len || kv->ctx_capacity <= 0 || kv->ctx_capacity % kv->block)
+        return fail(c, ACACHE_ERR_INVALID_ARG, "ctx_capacity %d smaller than ctx_len %d or not whole blocks of %d", kv->ctx_capacity, ctx_len, kv->block);
+    if (kv->batch_stride == 0) {
+        if (writes) return fail(c, ACACHE_ERR_INVALID_ARG, "batch_stride 0 (one cache shared by the batch) is only valid for calls that do not write the cache");
+    } else if (kv->batch_stride < (int64_t)kv->ctx_capacity * d.n_kv_heads * d.head_dim || (kv->batch_stride & 15)) {
+        return fail(c, ACACHE_ERR_INVALID_ARG, "batch_stride smaller than one request's cache or not a multiple of 16");
+    }
+    if ((int64_t)batch * d.n_kv_heads > 65535) return fail(c, ACACHE_ERR_UNSUPPORTED_SHAPE, "batch * n_kv_heads above 65535");
+    return ACACHE_OK;
+}
+
+int log2_of(int block) { return block == 16 ? 4 : block == 32 ? 5 : block == 64 ? 6 : 7; }
+
+// rows k_rows / v_rows [B, n, Hkv, d] at positions pos (or start ..) of the cache
+void run_kv8_write(acache_ctx* c, const acache_kv8* kv, int32_t batch, int32_t ctx_len, const void* k_rows, const void* v_rows,
+                   int64_t rows_batch_stride, int32_t n, const int32_t* pos, int32_t start, cudaStream_t st) {
+    Kv8WriteArgs a{};
+    a.k = static_cast<uint8_t*>(kv->k); a.v = static_cast<uint8_t*>(kv->v); a.k_exp = kv->k_exp; a.v_exp = kv->v_exp;
+    a.batch_stride = kv->batch_stride; a.capacity = kv->ctx_capacity; a.n_blocks = kv->ctx_capacity / kv->block; a.block = kv->block;
+    a.format = kv->format;
+    a.batch = batch; a.n_kv_heads = c->d.n_kv_heads; a.head_dim = c->d.head_dim; a.ctx_len = ctx_len;
+    a.k_rows = k_rows; a.v_rows = v_rows; a.rows_batch_stride = rows_batch_stride; a.n = n; a.pos = pos; a.start = start;
+    a.status = wsp<uint32_t>(c, c->o_status);
+    launch_kv8_write(a, st);
+    c->launches += 1;
+}
+
+// rows at positions pos (or start ..) of the cache to k_out / v_out [B, n, Hkv, d]; either may be null
+void run_kv8_read(acache_ctx* c, const acache_kv8* kv, int32_t batch, int32_t ctx_len, void* k_out, void* v_out,
+                  int64_t out_batch_stride, int32_t n, const int32_t* pos, int32_t start, cudaStream_t st) {
+    Kv8ReadArgs a{};
+    a.k = static_cast<const uint8_t*>(kv->k); a.v = static_cast<const uint8_t*>(kv->v); a.k_exp = kv->k_exp; a.v_exp = kv->v_exp;
+    a.batch_stride = kv->batch_stride; a.shared = kv->batch_stride == 0; a.capacity = kv->ctx_capacity;
+    a.n_blocks = kv->ctx_capacity / kv->block; a.log2_block = log2_of(kv->block); a.format = kv->format;
+    a.batch = batch; a.n_kv_heads = c->d.n_kv_heads; a.head_dim = c->d.head_dim; a.ctx_len = ctx_len;
+    a.k_out = k_out; a.v_out = v_out; a.out_batch_stride = out_batch_stride; a.n = n; a.pos = pos; a.start = start;
+    a.status = wsp<uint32_t>(c, c->o_status);
+    launch_kv8_read(a, st);
+    c->launches += 1;
+}
+
+acache_status run_kv8_attention(acache_ctx* c, const acache_kv8* kv, int32_t batch, int32_t n, int32_t ctx_len, const void* q, void* o,
+                                float* lse, const int32_t* lens, const uint32_t* key_drop, cudaStream_t st) {
+    const acache_model_desc& d = c->d;
+    Kv8AttnArgs a{};
+    a.q = q; a.o = o; a.lse = lse;
+    a.k = static_cast<const uint8_t*>(kv->k); a.v = static_cast<const uint8_t*>(kv->v); a.k_exp = kv->k_exp; a.v_exp = kv->v_exp;
+    a.batch_stride = kv->batch_stride; a.shared = kv->batch_stride == 0; a.capacity = kv->ctx_capacity;
+    a.n_blocks = kv->ctx_capacity / kv->block; a.log2_block = log2_of(kv->block); a.format = kv->format;
+    a.batch = batch; a.n = n; a.ctx_len = ctx_len; a.n_heads = d.n_heads; a.n_kv_heads = d.n_kv_heads; a.head_dim = d.head_dim;
+    a.lens = lens; a.key_drop = key_drop; a.drop_words = (ctx_len + 31) / 32;
+    a.scale_log2e = 1.4426950408889634f / sqrtf((float)d.head_dim);
+    a.part = wsp<float>(c, c->o_gemm);           // the projections' partial tiles: no projection runs beside an attention
+    a.arrived = wsp<unsigned int>(c, c->o_arrived);
+    a.status = wsp<uint32_t>(c, c->o_status);
+    if (a.shared && !lens && !key_drop) {        // one cache and one set of keys: the batch's rows are rows of one request
+        a.n *= a.batch;
+        a.batch = 1;
+    }
+    const int nl = launch_kv8_attention(a, st);
+    if (nl < 0) return check_cuda(c, "8-bit attention") == ACACHE_OK ? fail(c, ACACHE_ERR_CUDA, "8-bit attention launch failed") : ACACHE_ERR_CUDA;
+    c->launches += nl;
+    return check_cuda(c, "8-bit attention");
+}
+
 // Q for the masked rows, then Eq. 4-5.
 acache_status run_score(acache_ctx* c, const acache_request* r, const void* q_mask, const acache_kv* kv,
                         float* scores, int accumulate, int norm_full, int defer_head_sum, cudaStream_t st, int early_k = 0) {
@@ -168,7 +245,8 @@ acache_status run_recompute(acache_ctx* c, const acache_layer_weights* w, const 
                             const int32_t* anchor_idx, int k, void* k_new, void* v_new, void* y, cudaStream_t st,
                             const PrivateRows* priv = nullptr, MapReuse maps = MapReuse{false}, bool drop_non_anchor = false,
                             const FusedScore* fs = nullptr,
-                            const std::function<acache_status()>& after_qkv = std::function<acache_status()>()) {
+                            const std::function<acache_status()>& after_qkv = std::function<acache_status()>(),
+                            const acache_kv8* kv8 = nullptr) {
     const acache_model_desc& d = c->d;
     const int rows = k + r->n_extra, n = r->batch * rows;
     if (n == 0) {
@@ -211,7 +289,7 @@ acache_status run_recompute(acache_ctx* c, const acache_layer_weights* w, const 
     g.head_dim = d.head_dim; g.rope_segments = 2;
     g.out[0] = q; g.out[1] = k_new; g.out[2] = v_new;
     if (fuse_scatter) { g.cache_k = kv->k; g.cache_v = kv->v; }
-    g.kv_batch_stride = kv->batch_stride; g.rows_per_req = rows;
+    g.kv_batch_stride = kv ? kv->batch_stride : 0; g.rows_per_req = rows;
     if (priv) { g.kv_out_rows = priv->out_rows; g.kv_out_stride = priv->k + priv->e; }
     g.partial = partial; g.status = status; g.grid_bar = grid_bar;
     g.debug_expire = c->debug_expire_once;
@@ -219,12 +297,14 @@ acache_status run_recompute(acache_ctx* c, const acache_layer_weights* w, const 
     { int nl = launch_gemm(g, st); if (nl < 0) return check_cuda(c, "qkv projection") == ACACHE_OK ? fail(c, ACACHE_ERR_CUDA, "qkv projection launch failed") : ACACHE_ERR_CUDA;
     c->launches += nl; }
 
+    if (kv8) run_kv8_write(c, kv8, r->batch, r->ctx_len, k_new, v_new, (int64_t)rows * kvd, rows, row_pos, 0, st);
     if (after_qkv) {            // work of the caller that wants the fresh K/V in place but precedes the attention
         const acache_status sq = after_qkv();
         if (sq != ACACHE_OK) return sq;
     }
     mark(c, ACACHE_STAGE_ATTENTION, st);
     AttnArgs at{};
+    if (!kv8) {
     at.q = q; at.cache_k = kv->k; at.cache_v = kv->v; at.kv_batch_stride = kv->batch_stride;
     if (!fuse_scatter) {
         // the rows that serve their positions from k_new / v_new: the rows recomputed now, or the whole private
@@ -245,6 +325,7 @@ acache_status run_recompute(acache_ctx* c, const acache_layer_weights* w, const 
             c->launches += 1;
         }
     }
+    }
     if (drop_non_anchor) {
         // DropNA layout (Section 5.3): the affix positions that are not anchors do not exist as keys.  The bits
         // live behind the two masks of the two-source attention; with fresh rows as a second source they are also
@@ -252,10 +333,14 @@ acache_status run_recompute(acache_ctx* c, const acache_layer_weights* w, const 
         const int words = (r->ctx_len + 31) / 32;
         uint32_t* km = wsp<uint32_t>(c, c->o_keymask);
         uint32_t* kd = km + (size_t)r->batch * (words + (d.max_rows + 31) / 32 + 2);
-        launch_drop_mask(anchor_idx, k, r->affix_start, r->affix_len, r->ctx_len, r->batch, kd, fuse_scatter ? nullptr : km, words, st);
+        launch_drop_mask(anchor_idx, k, r->affix_start, r->affix_len, r->ctx_len, r->batch, kd, fuse_scatter || kv8 ? nullptr : km, words, st);
         c->launches += 1;
         at.key_drop = kd; at.excl_words = words;
     }
+    if (kv8) {
+        const acache_status sa = run_kv8_attention(c, kv8, r->batch, rows, r->ctx_len, q, o, nullptr, nullptr, at.key_drop, st);
+        if (sa != ACACHE_OK) return sa;
+    } else {
     at.batch = r->batch; at.n = rows; at.ctx_len = r->ctx_len;
     at.n_heads = d.n_heads; at.n_kv_heads = d.n_kv_heads; at.head_dim = d.head_dim;
     at.o = o;
@@ -267,6 +352,7 @@ acache_status run_recompute(acache_ctx* c, const acache_layer_weights* w, const 
         at.affix_start = r->affix_start; at.affix_len = r->affix_len; at.score_norm_full = fs->norm_full;
     }
     c->launches += launch_attention(at, st);
+    }
     if (fs) {
         launch_score_reduce_tiles(wsp<float>(c, c->o_partial), fs->rowmask, fs->rm_words, fs->scores, r->batch, d.n_heads,
                                   (rows + 127) / 128, r->affix_len, fs->accumulate, st);
@@ -371,8 +457,10 @@ acache_status acache_create(const acache_model_desc* desc, acache_ctx** out) {
     }
     c->o_rowmask = take(cur, (size_t)d.max_batch * ((d.max_rows + 31) / 32 + 8) * 4);
     c->o_slot = take(cur, (size_t)d.max_batch * d.max_ctx * 4);
+    c->o_arrived = take(cur, kKv8Counters * 4);
     c->o_keymask = take(cur, (size_t)d.max_batch * (2 * ((d.max_ctx + 31) / 32) + (d.max_rows + 31) / 32 + 4) * 4);
-    c->o_xstage = take(cur, (size_t)d.max_batch * d.max_ctx * d.hidden * 2);
+    // x of the host-buffer call, or the affix keys read back from an 8-bit cache
+    c->o_xstage = take(cur, (size_t)d.max_batch * d.max_ctx * std::max(d.hidden, kvd) * 2);
     c->o_ystage = take(cur, nr * d.hidden * 2);
     c->o_sstage = take(cur, (size_t)d.max_batch * d.max_affix * 4);
     c->o_astage = take(cur, (size_t)d.max_batch * d.max_affix * 4);
@@ -383,6 +471,7 @@ acache_status acache_create(const acache_model_desc* desc, acache_ctx** out) {
         pb = std::max(pb, gemm_partial_bytes(nri, d.hidden, d.ffn, true));
         pb = std::max(pb, gemm_partial_bytes(nri, d.ffn, d.hidden, false));
         pb = std::max(pb, gemm_partial_bytes(nmi, d.hidden, qd, false));
+        pb = std::max(pb, kv8_attention_scratch_bytes(d.head_dim));
         c->o_gemm = take(cur, pb);
     }
     c->o_attn = take(cur, attention_scratch_bytes(d.head_dim));
@@ -405,8 +494,10 @@ acache_status acache_set_workspace(acache_ctx* ctx, void* dev_ptr, size_t bytes,
     if (bytes < ctx->ws_need) return fail(ctx, ACACHE_ERR_WORKSPACE, "workspace %zu < %zu bytes", bytes, ctx->ws_need);
     ctx->ws = static_cast<unsigned char*>(dev_ptr);
     ctx->ws_have = bytes;
-    // status word and grid-barrier words are adjacent: clear both
-    if (cudaMemsetAsync(ctx->ws + ctx->o_status, 0, 512, stream) != cudaSuccess) return check_cuda(ctx, "memset");
+    // status word and grid-barrier words are adjacent: clear both; counters of the split attention
+    if (cudaMemsetAsync(ctx->ws + ctx->o_status, 0, 512, stream) != cudaSuccess ||
+        cudaMemsetAsync(ctx->ws + ctx->o_arrived, 0, kKv8Counters * 4, stream) != cudaSuccess)
+        return check_cuda(ctx, "memset");
     return ACACHE_OK;
 }
 
@@ -456,8 +547,9 @@ acache_status acache_poll_status(acache_ctx* ctx, acache_stream_t stream, uint32
         return check_cuda(ctx, "poll_status") == ACACHE_OK ? fail(ctx, ACACHE_ERR_CUDA, "poll_status failed") : ACACHE_ERR_CUDA;
     *host_flags = v;
     if (v & ACACHE_FLAG_WAIT_EXPIRED) {
-        // a kernel gave up half way: its grid-barrier words are stale, re-arm them
+        // a kernel gave up half way: its grid-barrier words and counters are stale, re-arm them
         cudaMemsetAsync(ctx->ws + ctx->o_gridbar, 0, 256, stream);
+        cudaMemsetAsync(ctx->ws + ctx->o_arrived, 0, kKv8Counters * 4, stream);
         cudaStreamSynchronize(stream);
         return fail(ctx, ACACHE_ERR_TIMEOUT, "a bounded device-side wait expired");
     }
@@ -557,15 +649,16 @@ namespace {
 acache_status layer_step_impl(acache_ctx* ctx, const acache_layer_weights* w, const acache_request* req,
                               const acache_kv* kv, const void* x, int x_is_compact, double ratio, uint32_t flags,
                               float* scores, int32_t* anchor_idx, void* k_new, void* v_new, void* y,
-                              acache_stream_t stream) {
+                              acache_stream_t stream, const acache_kv8* kv8 = nullptr) {
     if (!ctx) return ACACHE_ERR_INVALID_ARG;
-    if (!kv) return fail(ctx, ACACHE_ERR_INVALID_ARG, "kv is NULL");
+    if (!kv && !kv8) return fail(ctx, ACACHE_ERR_INVALID_ARG, "kv is NULL");
     if (!req) return fail(ctx, ACACHE_ERR_INVALID_ARG, "request is NULL");
     const acache_model_desc& d = ctx->d;
     const int k = acache_k_from_ratio(req->affix_len, ratio);
-    const bool to_slots = k_new != nullptr;
+    const bool to_slots = k_new != nullptr && !kv8;
     acache_status s = check_request(ctx, req, kv, k, true, to_slots);
     if (s != ACACHE_OK) return s;
+    if (kv8 && (s = check_kv8(ctx, kv8, req->batch, req->ctx_len, true)) != ACACHE_OK) return s;
     const bool do_score = flags & ACACHE_F_SCORE, do_select = flags & ACACHE_F_SELECT;
     const bool do_recompute = !(flags & ACACHE_F_NO_RECOMPUTE);
     if ((s = check_weights(ctx, w, !do_recompute)) != ACACHE_OK) return s;
@@ -583,7 +676,7 @@ acache_status layer_step_impl(acache_ctx* ctx, const acache_layer_weights* w, co
     FusedScore fs{};
     bool score_in_attention = false;
     static const bool attn_tc_on = [] { const char* e = getenv("ACACHE_ATTN_TC"); return !(e && e[0] == '0'); }();
-    if (fuse_on && attn_tc_on && !to_slots && do_score && !do_select && do_recompute && k == 0 && d.head_dim == 128 &&
+    if (fuse_on && attn_tc_on && !to_slots && !kv8 && do_score && !do_select && do_recompute && k == 0 && d.head_dim == 128 &&
         req->batch > 0 && req->affix_len > 0 && req->n_masked > 0 && req->n_extra > 0 && (kv->batch_stride & 7) == 0 &&
         (size_t)req->batch * d.n_heads * ((req->n_extra + 127) / 128) * req->affix_len * 4 <= ctx->partial_bytes) {
         fs.rm_words = (req->n_extra + 31) / 32;
@@ -602,6 +695,18 @@ acache_status layer_step_impl(acache_ctx* ctx, const acache_layer_weights* w, co
     auto score_now = [&]() -> acache_status {
         if (do_score && !score_in_attention && req->batch > 0 && req->affix_len > 0) {
             void* qmask = wsp<void>(ctx, ctx->o_qmask);
+            acache_kv read_back{};
+            const acache_kv* keys = kv;
+            if (kv8) {
+                // the keys that the scores (and with the full normaliser, their softmax) are about, as bf16 in their places
+                const bool all = flags & ACACHE_F_SCORE_NORM_FULL;
+                const int kvd = d.n_kv_heads * d.head_dim, first = all ? 0 : req->affix_start;
+                char* at = wsp<char>(ctx, ctx->o_xstage);
+                read_back = acache_kv{at, at, (int64_t)req->ctx_len * kvd, req->ctx_len};
+                run_kv8_read(ctx, kv8, req->batch, req->ctx_len, at + (size_t)first * kvd * 2, nullptr, read_back.batch_stride,
+                             all ? req->ctx_len : req->affix_len, nullptr, first, stream);
+                keys = &read_back;
+            }
             mark(ctx, ACACHE_STAGE_MASK_Q, stream);
             if (req->n_masked > 0) {
                 int32_t* mpos = wsp<int32_t>(ctx, ctx->o_mrow_pos);
@@ -645,8 +750,8 @@ acache_status layer_step_impl(acache_ctx* ctx, const acache_layer_weights* w, co
             fused_head_sum = do_select && k > 0 && req->n_masked > 0 && (int64_t)req->affix_len * d.n_heads <= 65536;
             // the masked rows' projection was launched just above: nothing that writes the cache is the scoring kernels'
             // direct predecessor, so they may request their first key tiles early
-            s = run_score(ctx, req, qmask, kv, scores, (flags & ACACHE_F_ACCUMULATE) ? 1 : 0,
-                          (flags & ACACHE_F_SCORE_NORM_FULL) ? 1 : 0, fused_head_sum ? 1 : 0, stream, req->n_masked > 0 ? 1 : 0);
+            s = run_score(ctx, req, qmask, keys, scores, (flags & ACACHE_F_ACCUMULATE) ? 1 : 0,
+                          (flags & ACACHE_F_SCORE_NORM_FULL) ? 1 : 0, fused_head_sum ? 1 : 0, stream, req->n_masked > 0 && !kv8 ? 1 : 0);
             if (s != ACACHE_OK) return s;
         }
         return ACACHE_OK;
@@ -662,9 +767,9 @@ acache_status layer_step_impl(acache_ctx* ctx, const acache_layer_weights* w, co
         ctx->launches += 1;
     }
     if (do_recompute)
-        return run_recompute(ctx, w, req, kv, !to_slots, x, x_is_compact, anchor_idx, k, k_new, v_new, y, stream, nullptr,
+        return run_recompute(ctx, w, req, kv, !to_slots && !kv8, x, x_is_compact, anchor_idx, k, k_new, v_new, y, stream, nullptr,
                              MapReuse{false}, (flags & ACACHE_F_DROP_NON_ANCHOR) != 0, score_in_attention ? &fs : nullptr,
-                             score_late ? std::function<acache_status()>(score_now) : std::function<acache_status()>());
+                             score_late ? std::function<acache_status()>(score_now) : std::function<acache_status()>(), kv8);
     mark(ctx, ACACHE_N_STAGES, stream);
     return check_cuda(ctx, "layer_step");
 }
@@ -688,6 +793,60 @@ acache_status acache_layer_step_shared(acache_ctx* ctx, const acache_layer_weigh
     static char dummy;        // a scoring-only call stores no K/V: any non-NULL value selects the read-only path
     return layer_step_impl(ctx, w, req, kv, x, x_is_compact, ratio, flags, scores, anchor_idx, k_new ? k_new : &dummy,
                            v_new ? v_new : &dummy, y, stream);
+}
+
+acache_status acache_layer_step_kv8(acache_ctx* ctx, const acache_layer_weights* w, const acache_request* req, acache_kv8* kv,
+                                    const void* x, int x_is_compact, double ratio, uint32_t flags, float* scores,
+                                    int32_t* anchor_idx, void* y, acache_stream_t stream) {
+    if (!ctx) return ACACHE_ERR_INVALID_ARG;
+    if (!kv) return fail(ctx, ACACHE_ERR_INVALID_ARG, "kv8 is NULL");
+    if (!ctx->ws) return fail(ctx, ACACHE_ERR_WORKSPACE, "workspace not set");
+    // the fresh rows in bf16, on their way into the cache
+    return layer_step_impl(ctx, w, req, nullptr, x, x_is_compact, ratio, flags, scores, anchor_idx, wsp<void>(ctx, ctx->o_knew),
+                           wsp<void>(ctx, ctx->o_vnew), y, stream, kv);
+}
+
+acache_status acache_kv8_write(acache_ctx* ctx, acache_kv8* kv, int32_t batch, int32_t ctx_len, const void* k_rows,
+                               const void* v_rows, int64_t rows_batch_stride, int32_t n_rows, const int32_t* pos, int32_t start,
+                               acache_stream_t stream) {
+    if (!ctx) return ACACHE_ERR_INVALID_ARG;
+    acache_status s = check_kv8(ctx, kv, batch, ctx_len, true);
+    if (s != ACACHE_OK) return s;
+    if (n_rows < 0 || (!pos && (start < 0 || (int64_t)start + n_rows > ctx_len)))
+        return fail(ctx, ACACHE_ERR_INVALID_ARG, "rows [%d, +%d) outside the context of %d", start, n_rows, ctx_len);
+    if (rows_batch_stride < 0 || (rows_batch_stride & 7) ||
+        (rows_batch_stride != 0 && rows_batch_stride < (int64_t)n_rows * ctx->d.n_kv_heads * ctx->d.head_dim))
+        return fail(ctx, ACACHE_ERR_INVALID_ARG, "rows_batch_stride smaller than one request's rows or not a multiple of 8");
+    if (batch == 0 || n_rows == 0) return ACACHE_OK;
+    if (!k_rows || !v_rows || !aligned16(k_rows) || !aligned16(v_rows)) return fail(ctx, ACACHE_ERR_INVALID_ARG, "k_rows / v_rows NULL or misaligned");
+    run_kv8_write(ctx, kv, batch, ctx_len, k_rows, v_rows, rows_batch_stride, n_rows, pos, start, stream);
+    return check_cuda(ctx, "kv8 write");
+}
+
+acache_status acache_kv8_read(acache_ctx* ctx, const acache_kv8* kv, int32_t batch, int32_t ctx_len, void* k_out, void* v_out,
+                              int32_t n_rows, const int32_t* pos, int32_t start, acache_stream_t stream) {
+    if (!ctx) return ACACHE_ERR_INVALID_ARG;
+    acache_status s = check_kv8(ctx, kv, batch, ctx_len, false);
+    if (s != ACACHE_OK) return s;
+    if (n_rows < 0 || (!pos && (start < 0 || (int64_t)start + n_rows > ctx_len)))
+        return fail(ctx, ACACHE_ERR_INVALID_ARG, "rows [%d, +%d) outside the context of %d", start, n_rows, ctx_len);
+    if (batch == 0 || n_rows == 0) return ACACHE_OK;
+    if ((!k_out && !v_out) || !aligned16(k_out) || !aligned16(v_out)) return fail(ctx, ACACHE_ERR_INVALID_ARG, "k_out and v_out NULL, or misaligned");
+    run_kv8_read(ctx, kv, batch, ctx_len, k_out, v_out, (int64_t)n_rows * ctx->d.n_kv_heads * ctx->d.head_dim, n_rows, pos, start, stream);
+    return check_cuda(ctx, "kv8 read");
+}
+
+acache_status acache_kv8_attention(acache_ctx* ctx, const acache_kv8* kv, int32_t batch, int32_t n_rows, int32_t ctx_len, const void* q,
+                                   const int32_t* lens, const uint32_t* key_drop, void* o, float* lse, acache_stream_t stream) {
+    if (!ctx) return ACACHE_ERR_INVALID_ARG;
+    acache_status s = check_kv8(ctx, kv, batch, ctx_len, false);
+    if (s != ACACHE_OK) return s;
+    if (n_rows < 0) return fail(ctx, ACACHE_ERR_INVALID_ARG, "n_rows %d is negative", n_rows);
+    if (batch == 0 || n_rows == 0) return ACACHE_OK;
+    if ((int64_t)batch * n_rows * (ctx->d.n_heads / ctx->d.n_kv_heads) > (1 << 19))
+        return fail(ctx, ACACHE_ERR_UNSUPPORTED_SHAPE, "more than 2^19 query rows per KV head");
+    if (!q || !o || !aligned16(q) || !aligned16(o)) return fail(ctx, ACACHE_ERR_INVALID_ARG, "q / o NULL or misaligned");
+    return run_kv8_attention(ctx, kv, batch, n_rows, ctx_len, q, o, lse, lens, key_drop, stream);
 }
 
 acache_status acache_predict_commit(acache_ctx* ctx, const void* h, int32_t h_rows, const int32_t* block_rows,

@@ -8,6 +8,7 @@ namespace acache {
 
 constexpr uint32_t kFlagBadIndex = 0x1u;
 constexpr uint32_t kFlagWaitExpired = 0x2u;
+constexpr uint32_t kFlagNonFinite = 0x4u;
 
 // ---- small PTX wrappers ---------------------------------------------------------------
 __device__ __forceinline__ uint32_t smem_u32(const void* p) {

@@ -206,4 +206,57 @@ int launch_attention_tc(const AttnArgs& a, uint32_t* status, cudaStream_t stream
 size_t attention_scratch_bytes(int head_dim);   // bytes for part_o followed by part_ml
 int launch_attention(const AttnArgs& a, cudaStream_t stream);
 
+// ---- kv8.cu: the cache held in 8 bits (kv8.cuh: what a code stands for) -------------------
+// codes [B, Hkv, capacity, d], exponent bytes [B, Hkv, n_blocks]; batch_stride in codes, 0 with `shared`
+struct Kv8WriteArgs {
+    uint8_t *k, *v, *k_exp, *v_exp;
+    int64_t batch_stride;
+    int shared, capacity, n_blocks, block, format;
+    int batch, n_kv_heads, head_dim, ctx_len;
+    const void *k_rows, *v_rows;    // bf16 [B, n, Hkv, d], requests rows_batch_stride elements apart
+    int64_t rows_batch_stride;
+    int n;
+    const int32_t* pos;             // [B, n] positions, or null: start .. start + n - 1
+    int start;
+    int first_block, by_row;        // set by the launcher
+    uint32_t* status;
+};
+void launch_kv8_write(Kv8WriteArgs a, cudaStream_t stream);
+
+struct Kv8ReadArgs {
+    const uint8_t *k, *v, *k_exp, *v_exp;
+    int64_t batch_stride;
+    int shared, capacity, n_blocks, log2_block, format;
+    int batch, n_kv_heads, head_dim, ctx_len;
+    void *k_out, *v_out;            // bf16 [B, n, Hkv, d]; either may be null
+    int64_t out_batch_stride;
+    int n;
+    const int32_t* pos;
+    int start;
+    uint32_t* status;
+};
+void launch_kv8_read(const Kv8ReadArgs& a, cudaStream_t stream);
+
+// ---- kv8_attn.cu ------------------------------------------------------------------------
+struct Kv8AttnArgs {
+    const void* q;                  // bf16 [B, n, H, d]
+    void* o;                        // bf16 [B, n, H, d]
+    float* lse;                     // fp32 [B, n, H] or null
+    const uint8_t *k, *v, *k_exp, *v_exp;
+    int64_t batch_stride;
+    int shared, capacity, n_blocks, log2_block, format;
+    int batch, n, ctx_len, n_heads, n_kv_heads, head_dim;
+    const int32_t* lens;            // [B] or null: keys of each request
+    const uint32_t* key_drop;       // [B, drop_words] or null: bit t = position t does not exist as a key
+    int drop_words;
+    float scale_log2e;              // log2(e) / sqrt(d)
+    float* part;                    // scratch of kv8_attention_scratch_bytes()
+    unsigned int* arrived;          // kKv8Counters words that are zero between launches
+    uint32_t* status;
+    int splits, split_keys;         // set by the launchers: CTAs per item, keys of each
+};
+constexpr int kKv8Counters = 4096;
+size_t kv8_attention_scratch_bytes(int head_dim);
+int launch_kv8_attention(const Kv8AttnArgs& a, cudaStream_t stream);     // kernels launched, or -1
+
 }  // namespace acache

@@ -1,0 +1,77 @@
+// Device helpers of the 8-bit cache: what a code and an exponent byte stand for, and conversions both ways.
+//
+// A (request, KV head, block of tokens) has one exponent byte e; its code c stands for c * 2^(e - 127).  e = 0: the block
+// holds nothing and reads as zero whatever its codes.  Powers of two cost int8 at most one of its 8 bits against a free
+// scale (e4m3 none: a floating-point code is as exact at any scale) and make everything else exact: x * 2^(127 - e) before
+// the rounding, code * 2^(e - 127) in bf16, a code by itself in f16.
+#pragma once
+#include <cuda_fp16.h>
+
+#include "common.cuh"
+
+namespace acache {
+
+constexpr int kKv8E4m3 = 0, kKv8Int8 = 1;
+constexpr int kKv8MinExp = 16;      // lowest exponent of a block that holds something: its smallest code is a normal number in bf16
+// A block's largest value lands in [2^top, 2^(top + 1)) scales.  int8: 64 to 127 (127.5 saturates, half a step like any
+// other rounding).  e4m3: 128 to 256, so that nothing saturates; the codes above, up to 448, would give no bit.
+template <int FMT>
+__host__ __device__ constexpr int kv8_top() { return FMT == kKv8Int8 ? 6 : 7; }
+
+// 2^(e - 127) for e in 1 .. 254, 0 for e = 0 (and below: a factor too small to matter)
+__device__ __forceinline__ float kv8_scale(int e) { return e > 0 ? __int_as_float(e << 23) : 0.f; }
+
+// ---- codes to f16 (exact) ---------------------------------------------------------------
+// 4 codes -> (codes 0, 1), (codes 2, 3)
+template <int FMT>
+__device__ __forceinline__ void kv8_to_f16(uint32_t w, uint32_t& lo, uint32_t& hi) {
+    if constexpr (FMT == kKv8Int8) {
+        // the byte as the low bits of 1024 + (code + 128), then minus 1152
+        const uint32_t u = w ^ 0x80808080u;
+        const uint32_t l = __byte_perm(u, 0x64646464u, 0x4140), h = __byte_perm(u, 0x64646464u, 0x4342);
+        asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(lo) : "r"(l), "r"(0x64806480u));
+        asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(hi) : "r"(h), "r"(0x64806480u));
+    } else {
+        asm("{\n\t.reg .b16 a, b;\n\t"
+            "mov.b32 {a, b}, %2;\n\t"
+            "cvt.rn.f16x2.e4m3x2 %0, a;\n\t"
+            "cvt.rn.f16x2.e4m3x2 %1, b;\n\t}"
+            : "=r"(lo), "=r"(hi)
+            : "r"(w));
+    }
+}
+
+__device__ __forceinline__ float2 f16x2_to_f32(uint32_t h) { return __half22float2(*reinterpret_cast<const __half2*>(&h)); }
+
+// ---- values (in scales) to codes --------------------------------------------------------
+// 4 finite values -> 4 codes; int8 saturates, e4m3 values stay below 256
+template <int FMT>
+__device__ __forceinline__ uint32_t kv8_round(float a, float b, float c, float d) {
+    if constexpr (FMT == kKv8Int8) {
+        // clamped, then rounded to the nearest even whole number by the addition of 1.5 * 2^23: the low byte is the code
+        auto r = [](float x) { return __float_as_uint(fminf(fmaxf(x, -127.f), 127.f) + 12582912.f); };
+        return __byte_perm(__byte_perm(r(a), r(b), 0x0040), __byte_perm(r(c), r(d), 0x0040), 0x5410);
+    } else {
+        uint32_t w;
+        asm("{\n\t.reg .b16 a, b;\n\t"
+            "cvt.rn.satfinite.e4m3x2.f32 a, %2, %1;\n\t"
+            "cvt.rn.satfinite.e4m3x2.f32 b, %4, %3;\n\t"
+            "mov.b32 %0, {a, b};\n\t}"
+            : "=r"(w)
+            : "f"(a), "f"(b), "f"(c), "f"(d));
+        return w;
+    }
+}
+// The same for values that need care: not finite (int8: NaN is 0, an infinity the largest code; e4m3: both are NaN), or of
+// the block at the top of bf16's range, whose largest values would round past it (limit: the largest code to be used).
+template <int FMT>
+__device__ __forceinline__ uint32_t kv8_round_careful(float a, float b, float c, float d, float limit) {
+    auto mend = [limit](float x) {
+        if constexpr (FMT == kKv8Int8) return x != x ? 0.f : x;
+        if (!(fabsf(x) < INFINITY)) return __int_as_float(0x7FC00000);
+        return fminf(fmaxf(x, -limit), limit);
+    };
+    return kv8_round<FMT>(mend(a), mend(b), mend(c), mend(d));
+}
+
+}  // namespace acache
