@@ -254,6 +254,7 @@ struct Kv8AttnArgs {
     unsigned int* arrived;          // kKv8Counters words that are zero between launches
     uint32_t* status;
     int splits, split_keys;         // set by the launchers: CTAs per item, keys of each
+    int cluster;                    // CTAs of a cluster, which add their results up before the rest is
 };
 constexpr int kKv8Counters = 4096;
 size_t kv8_attention_scratch_bytes(int head_dim);

@@ -74,4 +74,48 @@ __device__ __forceinline__ uint32_t kv8_round_careful(float a, float b, float c,
     return kv8_round<FMT>(mend(a), mend(b), mend(c), mend(d));
 }
 
+// ---- what the attention kernels share ----------------------------------------------------
+constexpr float kRaise = 15.f, kHeadroom = 4.f;      // log2 units: p stays below 2^15; a new reference is above the largest logit
+constexpr int kFarApart = 100;                       // most by which E0 is above an ev
+
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+__device__ __forceinline__ float ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+// of another CTA of the cluster
+__device__ __forceinline__ float ld_peer(uint32_t addr) {
+    float v;
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
+    return v;
+}
+__device__ __forceinline__ float4 ld_peer4(uint32_t addr) {
+    float4 v;
+    asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
+    return v;
+}
+// Results over several sets of keys, each with the log2 of its denominator, put together.
+struct Sum {
+    float mx = -INFINITY, den = 0.f;
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    __device__ __forceinline__ void add(float x, const float4& w) {
+        if (x == -INFINITY) return;                              // no keys
+        const float m = fmaxf(mx, x);                            // (a NaN comes through by fp)
+        const float fo = mx == -INFINITY ? 0.f : ex2(mx - m), fp = ex2(x - m);
+        mx = m;
+        den = fmaf(den, fo, fp);
+        v.x = fmaf(v.x, fo, fp * w.x); v.y = fmaf(v.y, fo, fp * w.y); v.z = fmaf(v.z, fo, fp * w.z); v.w = fmaf(v.w, fo, fp * w.w);
+    }
+    __device__ __forceinline__ float4 mean() const {
+        const float i = den == 0.f ? 0.f : 1.f / den;
+        return make_float4(v.x * i, v.y * i, v.z * i, v.w * i);
+    }
+    __device__ __forceinline__ float lse2() const { return den == 0.f ? -INFINITY : mx + log2f(den); }
+};
+
 }  // namespace acache

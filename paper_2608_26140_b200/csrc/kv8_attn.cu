@@ -16,52 +16,59 @@
 // free, so a thread's 16 contiguous bytes of a key row serve as its fragment of four products:
 //   S^T = K Q^T (keys x rows)   O^T += V^T P^T (d x rows): keys and d are the long sides of both products, so up to 8 rows cost
 //   one instruction, and P only has to be transposed in 8 x 8 blocks (movmatrix).
-// The reference M moves only when a logit passes it by 2^8, found by a vote; then maxima are exchanged and O is scaled.
+// The reference M moves only when a logit passes it by 2^15 (f16 ends at 2^16), found by a vote; then maxima are exchanged and O is scaled.
+#include <algorithm>
+#include <climits>
+
 #include "kernels.h"
 #include "kv8.cuh"
 #include "launch.h"
+#include "tc_ptx.cuh"
 
 namespace acache {
+
+// kernels launched, 0: it would take longer than `limit` ns, -1: failed
+int launch_kv8_attention_tc(const Kv8AttnArgs& a, int64_t limit, cudaStream_t stream);
 
 namespace {
 
 constexpr int RW = 4;                    // warps of a CTA
-constexpr int RSTEP = 32;                // keys of a warp's step (two 16-key tiles)
+constexpr int MT = 2;                    // 16-key tiles of a warp's step
+constexpr int RSTEP = 16 * MT;
 constexpr int RSTAGES = 3;
-constexpr float kRaise = 8.f;            // log2 units
-constexpr int kFarApart = 100;           // most by which E0 is above an ev
+constexpr int kMinSplit = 256;           // keys
+constexpr int kSlots = 2;                // CTAs of an SM
+// tenths of a nanosecond that a key takes a CTA
+template <int D, int NT>
+constexpr int kKeyNs = (NT == 4 ? 175 : 130) * D / 128;
 
 __device__ __forceinline__ void mma_f16_16816(float* c, const uint32_t* a, uint32_t b0, uint32_t b1) {
-    asm volatile(
-        "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};\n"
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};\n"
         : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 __device__ __forceinline__ uint32_t transpose8(uint32_t v) {
     uint32_t r;
-    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
     return r;
-}
-__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
-    uint32_t r;
-    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-    return r;
-}
-__device__ __forceinline__ float ex2(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
 }
 template <int BYTES>
 __device__ __forceinline__ void cp_async(uint32_t dst, const void* src, bool on) {
-    if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;\n" ::"r"(dst), "l"(src), "r"(on ? 16 : 0));
-    else asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;\n" ::"r"(dst), "l"(src), "r"(on ? 8 : 0));
+    if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;\n" ::"r"(dst), "l"(src), "r"(on ? 16 : 0) : "memory");
+    else asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;\n" ::"r"(dst), "l"(src), "r"(on ? 8 : 0) : "memory");
 }
+// the copies asked for are there but for the newest N groups; what is read from them stays behind this
+template <int N>
+__device__ __forceinline__ void ring_wait() { asm volatile("cp.async.wait_group %0;\n" ::"n"(N) : "memory"); }
 template <int WORDS>
-__device__ __forceinline__ void lds(uint32_t addr, uint32_t* w) {
-    if constexpr (WORDS == 4)
-        asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(addr));
-    else asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(addr));
+__device__ __forceinline__ void lds(const unsigned char* from, uint32_t* w) {
+    if constexpr (WORDS == 4) {
+        const uint4 v = *reinterpret_cast<const uint4*>(from);
+        w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
+    } else {
+        const uint2 v = *reinterpret_cast<const uint2*>(from);
+        w[0] = v.x; w[1] = v.y;
+    }
 }
 
 template <int D, int NT>
@@ -69,18 +76,17 @@ struct RowsLayout {
     static constexpr int ROWS = 8 * NT;
     static constexpr int KCH = D / 64;                       // 16-byte pieces of a key row per thread
     static constexpr int VB = D / 8;                         // bytes of a value row per thread (8 threads share a row)
-    static constexpr int K_SLOTS = 2 * 2 * KCH, V_SLOTS = 2 * 4;
-    static constexpr int K_BYTES = K_SLOTS * 16 * 32, V_BYTES = V_SLOTS * VB * 32;   // of a warp's stage
-    static constexpr int STAGE = K_BYTES + V_BYTES;
+    static constexpr int HALF = RSTEP * D;                   // bytes of a warp's stage: keys, then values
+    static constexpr int STAGE = 2 * HALF;
     static constexpr int RING = RW * RSTAGES * STAGE;
-    static constexpr int MERGE = RW * ROWS * (D + 4) * 4;    // the warps' results, after the loop
+    static constexpr int MERGE = (RW * ROWS * (D + 4) + ROWS * (D + 1)) * 4;    // after the loop: the warps' results, the CTA's
     static constexpr int SMEM = RING > MERGE ? RING : MERGE;
 };
 
 // item = (request, KV head, tile of 8 NT rows); rows of a KV head: query row i, head g of its group -> i G + g.
 // grid (splits, row tiles, B Hkv).  The keys of a split are dealt out to the warps step by step.
 template <int D, int NT, int FMT>
-__global__ void __launch_bounds__(RW * 32) kv8_attn_rows_kernel(const Kv8AttnArgs a) {
+__global__ void __launch_bounds__(RW * 32, NT < 4 ? kSlots : 1) kv8_attn_rows_kernel(const Kv8AttnArgs a) {
     using L = RowsLayout<D, NT>;
     extern __shared__ __align__(16) unsigned char smem[];
     __shared__ float stat[2][RW][8 * NT];                    // reference, denominator
@@ -102,28 +108,25 @@ __global__ void __launch_bounds__(RW * 32) kv8_attn_rows_kernel(const Kv8AttnArg
     const int steps = key_hi > key_lo ? (key_hi - key_lo + RSTEP - 1) / RSTEP : 0;
     const int64_t cache_at = (int64_t)b * a.batch_stride + (int64_t)kvh * a.capacity * D;
     const uint8_t *kb = a.k + cache_at, *vb = a.v + cache_at;
-    const uint32_t ring = smem_u32(smem) + warp * (RSTAGES * L::STAGE) + lane * 16;
-    const uint32_t vring = smem_u32(smem) + warp * (RSTAGES * L::STAGE) + L::K_BYTES + lane * L::VB;
+    const unsigned char* ring = smem + warp * (RSTAGES * L::STAGE);
+    // A warp's copies take whole rows, side by side; where a row's 16-byte pieces lie in the ring depends on the row, so that the
+    // fragments' reads (other rows in other threads) meet different banks.  Pieces per row: 8, at head dimension 64 4.
+    constexpr int PIECES = D / 16;
+    auto k_at = [](int row, int piece) { return row * D + ((D == 128 ? piece ^ ((row & 1) << 2) : piece ^ ((row >> 1) & 3)) << 4); };
+    auto v_at = [](int row, int piece) { return row * D + ((D == 128 ? piece ^ (row & 6) : piece ^ ((row >> 1) & 3)) << 4); };
 
     auto fetch = [&](int step) {         // this warp's `step`-th step into its ring
         const int s = warp + step * RW;
         if (s < steps) {
             const int key0 = key_lo + s * RSTEP;
-            const uint32_t st = (step % RSTAGES) * L::STAGE;
+            const uint32_t st = smem_u32(ring) + (step % RSTAGES) * L::STAGE;
 #pragma unroll
-            for (int mt = 0; mt < 2; ++mt) {
-#pragma unroll
-                for (int r = 0; r < 2; ++r)
-#pragma unroll
-                    for (int c = 0; c < L::KCH; ++c) {
-                        const int key = key0 + mt * 16 + r * 8 + g;
-                        cp_async<16>(ring + st + ((mt * 2 + r) * L::KCH + c) * 512, kb + (int64_t)min(key, key_hi - 1) * D + c * 64 + t * 16, key < key_hi);
-                    }
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int key = key0 + mt * 16 + 2 * t + (j & 1) + (j >> 1) * 8;
-                    cp_async<L::VB>(vring + st + (mt * 4 + j) * (L::VB * 32), vb + (int64_t)min(key, key_hi - 1) * D + g * L::VB, key < key_hi);
-                }
+            for (int i = 0; i < RSTEP * PIECES / 32; ++i) {
+                const int row = (i * 32 + lane) / PIECES, piece = lane % PIECES;
+                const bool on = key0 + row < key_hi;
+                const int64_t at = (int64_t)(on ? key0 + row : key_lo) * D + piece * 16;
+                cp_async<16>(st + k_at(row, piece), kb + at, on);
+                cp_async<16>(st + L::HALF + v_at(row, piece), vb + at, on);
             }
         }
         cp_async_commit();
@@ -133,20 +136,22 @@ __global__ void __launch_bounds__(RW * 32) kv8_attn_rows_kernel(const Kv8AttnArg
 
     // exponent bytes of a step's two 16-key tiles: K, K, V, V (a block holds whole tiles)
     const int64_t exps_at = ((int64_t)(a.shared ? 0 : b) * a.n_kv_heads + kvh) * a.n_blocks;
-    auto exponents = [&](int step, int (&e)[4]) {
+    auto exponents = [&](int step, int (&e)[2 * MT]) {
         const int key0 = key_lo + min(warp + step * RW, steps - 1) * RSTEP;
 #pragma unroll
-        for (int mt = 0; mt < 2; ++mt) {
+        for (int mt = 0; mt < MT; ++mt) {
             const int64_t at = exps_at + (min(key0 + mt * 16, key_hi - 1) >> a.log2_block);
             e[mt] = __ldg(a.k_exp + at);
-            e[2 + mt] = __ldg(a.v_exp + at);
+            e[MT + mt] = __ldg(a.v_exp + at);
         }
     };
-    int e_next[4] = {0, 0, 0, 0};
+    int e_next[2 * MT] = {};
     if (warp < steps) exponents(0, e_next);
-    // q as f16, each row over a power of two of its own
-    uint32_t qf[NT][D / 16][2];
-    float rq[NT][2];                     // what a product of row 2 t (+ 1) is multiplied by, times the key's scale
+    // q as f16, each row over a power of two of its own; kept in shared memory where the registers are needed for the sums
+    constexpr bool Q_SMEM = NT * D > 256;
+    __shared__ uint2 qs[Q_SMEM ? (D / 16) * NT * 32 : 1];
+    uint32_t qf[Q_SMEM ? 1 : NT][D / 16][2];
+    float2 rq[NT];                       // what a product of row 2 t (+ 1) is multiplied by, times the key's scale
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
         const int r = tile * L::ROWS + nt * 8 + g;
@@ -170,21 +175,29 @@ __global__ void __launch_bounds__(RW * 32) kv8_attn_rows_kernel(const Kv8AttnArg
         const float inv = __int_as_float((254 - field) << 23);
 #pragma unroll
         for (int ks = 0; ks < D / 16; ++ks) {
-            qf[nt][ks][0] = pack_f16(bf16_lo(raw[2 * ks]) * inv, bf16_hi(raw[2 * ks]) * inv);
-            qf[nt][ks][1] = pack_f16(bf16_lo(raw[2 * ks + 1]) * inv, bf16_hi(raw[2 * ks + 1]) * inv);
+            const uint32_t q0 = pack_f16(bf16_lo(raw[2 * ks]) * inv, bf16_hi(raw[2 * ks]) * inv);
+            const uint32_t q1 = pack_f16(bf16_lo(raw[2 * ks + 1]) * inv, bf16_hi(raw[2 * ks + 1]) * inv);
+            if constexpr (Q_SMEM) {
+                if (warp == 0) qs[(ks * NT + nt) * 32 + lane] = make_uint2(q0, q1);
+            } else {
+                qf[nt][ks][0] = q0;
+                qf[nt][ks][1] = q1;
+            }
         }
         const float mine = __int_as_float(field << 23) * a.scale_log2e;      // of row g; the products' columns are rows 2 t, 2 t + 1
-        rq[nt][0] = __shfl_sync(0xffffffffu, mine, 8 * t);
-        rq[nt][1] = __shfl_sync(0xffffffffu, mine, 8 * t + 4);
+        rq[nt].x = __shfl_sync(0xffffffffu, mine, 8 * t);
+        rq[nt].y = __shfl_sync(0xffffffffu, mine, 8 * t + 4);
     }
 
+    if constexpr (Q_SMEM) __syncthreads();
+
     float o[D / 16][NT][4];
-    float m[NT][2], l[NT][2];
+    float2 m[NT], l[NT];                 // references and denominators of rows 2 t, 2 t + 1
+    bool first = true;                   // no key yet: the same for all rows, a key counts for all of them or for none
     int e0 = 0;                          // biased; 0: nothing met yet
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
-        m[nt][0] = m[nt][1] = -INFINITY;
-        l[nt][0] = l[nt][1] = 0.f;
+        m[nt] = l[nt] = make_float2(0.f, 0.f);
 #pragma unroll
         for (int i = 0; i < D / 16; ++i)
 #pragma unroll
@@ -194,126 +207,138 @@ __global__ void __launch_bounds__(RW * 32) kv8_attn_rows_kernel(const Kv8AttnArg
     for (int step = 0; warp + step * RW < steps; ++step) {
         const int s = warp + step * RW, key0 = key_lo + s * RSTEP;
         const uint32_t st = (step % RSTAGES) * L::STAGE;
-        uint32_t there = key_hi - key0 >= 32 ? ~0u : (1u << (key_hi - key0)) - 1u;      // the step's keys that count
-        if (a.key_drop) {
-            // keys of a split start at a multiple of 32
-            const int w = key0 >> 5;
-            if (w < a.drop_words) there &= ~__ldg(a.key_drop + (int64_t)b * a.drop_words + w);
-        }
-        int ek[2], ev[2];
-        bool blank[2];                       // a block that holds nothing has zero keys and values, whatever its codes
+        uint32_t there = key_hi - key0 >= RSTEP ? ~0u : (1u << (key_hi - key0)) - 1u;      // the step's keys that count
+        if (a.key_drop) there &= ~__ldg(a.key_drop + (int64_t)b * a.drop_words + (key0 >> 5));
+        int ek[MT], ev[MT];
+        bool blank[MT];                       // a block that holds nothing has zero keys and values, whatever its codes
 #pragma unroll
-        for (int mt = 0; mt < 2; ++mt) {
+        for (int mt = 0; mt < MT; ++mt) {
             ek[mt] = e_next[mt];
-            ev[mt] = e_next[2 + mt];
+            ev[mt] = e_next[MT + mt];
             blank[mt] = ev[mt] == 0;
             if (blank[mt]) ev[mt] = e0 ? e0 : 127;      // its scale is of no account
             if (ev[mt] > e0) {
                 const float grow = kv8_scale(127 + min(ev[mt] - e0, kFarApart));
                 e0 = ev[mt];
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt) { l[nt][0] *= grow; l[nt][1] *= grow; }
+                for (int nt = 0; nt < NT; ++nt) { l[nt].x *= grow; l[nt].y *= grow; }
             }
         }
         exponents(step + 1, e_next);
-        cp_async_wait<RSTAGES - 2>();
+        ring_wait<RSTAGES - 2>();
+        __syncwarp();                        // this step's stage is there for every lane, and every lane is done with the last one's
+        fetch(step + RSTAGES - 1);
         // ---- S^T = K Q^T, then y - M in place ----
-        float sv[2][NT][4];
+        float sv[MT][NT][4];
 #pragma unroll
-        for (int mt = 0; mt < 2; ++mt) {
+        for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) sv[mt][nt][j] = 0.f;
 #pragma unroll
-            for (int c = 0; c < L::KCH; ++c) {
-                uint32_t k0[4], k1[4];
-                lds<4>(ring + st + ((mt * 2 + 0) * L::KCH + c) * 512, k0);
-                lds<4>(ring + st + ((mt * 2 + 1) * L::KCH + c) * 512, k1);
+        for (int c = 0; c < L::KCH; ++c) {
+            uint32_t kw[MT][2][4];
 #pragma unroll
-                for (int w = 0; w < 4; ++w) {
-                    uint32_t fa[4];
-                    kv8_to_f16<FMT>(k0[w], fa[0], fa[2]);
-                    kv8_to_f16<FMT>(k1[w], fa[1], fa[3]);
+            for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) mma_f16_16816(sv[mt][nt], fa, qf[nt][c * 4 + w][0], qf[nt][c * 4 + w][1]);
+                for (int r = 0; r < 2; ++r) {
+                    lds<4>(ring + st + k_at(mt * 16 + r * 8 + g, c * 4 + t), kw[mt][r]);
+                    if (ek[mt] == 0) kw[mt][r][0] = kw[mt][r][1] = kw[mt][r][2] = kw[mt][r][3] = 0u;
+                }
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                uint32_t fa[MT][4];
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt) {
+                    kv8_to_f16<FMT>(kw[mt][0][w], fa[mt][0], fa[mt][2]);
+                    kv8_to_f16<FMT>(kw[mt][1][w], fa[mt][1], fa[mt][3]);
+                }
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                    uint2 q;
+                    if constexpr (Q_SMEM) q = qs[((c * 4 + w) * NT + nt) * 32 + lane];
+                    else q = make_uint2(qf[nt][c * 4 + w][0], qf[nt][c * 4 + w][1]);
+#pragma unroll
+                    for (int mt = 0; mt < MT; ++mt) mma_f16_16816(sv[mt][nt], fa[mt], q.x, q.y);
                 }
             }
         }
-        bool raise = false;
+        float top = -INFINITY;
 #pragma unroll
-        for (int mt = 0; mt < 2; ++mt) {
-            const float ks = kv8_scale(ek[mt]);
-            const float vy = (float)(max(ev[mt], e0 - kFarApart) - 127);
+        for (int mt = 0; mt < MT; ++mt) {
+            const float ks = kv8_scale(ek[mt]), vy = (float)(max(ev[mt], e0 - kFarApart) - 127);
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
+            for (int nt = 0; nt < NT; ++nt) {
+                const float2 fa = __fmul2_rn(rq[nt], make_float2(ks, ks)), fb = __fadd2_rn(make_float2(vy, vy), make_float2(-m[nt].x, -m[nt].y));
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const float off = vy - (m[nt][j & 1] == -INFINITY ? 0.f : m[nt][j & 1]);
-                    sv[mt][nt][j] = ek[mt] ? fmaf(sv[mt][nt][j], rq[nt][j & 1] * ks, off) : off;
+                for (int r = 0; r < 2; ++r) {
+                    const float2 y = __ffma2_rn(make_float2(sv[mt][nt][2 * r], sv[mt][nt][2 * r + 1]), fa, fb);
+                    sv[mt][nt][2 * r] = y.x;
+                    sv[mt][nt][2 * r + 1] = y.y;
                 }
+            }
         }
         if (there != ~0u) {
 #pragma unroll
-            for (int mt = 0; mt < 2; ++mt)
+            for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
                     if (!((there >> (mt * 16 + (j >> 1) * 8 + g)) & 1u))
 #pragma unroll
                         for (int nt = 0; nt < NT; ++nt) sv[mt][nt][j] = -INFINITY;
         }
-        float top[NT][2];
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
+        for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-            for (int r = 0; r < 2; ++r) {
-                top[nt][r] = fmaxf(fmaxf(sv[0][nt][r], sv[0][nt][r + 2]), fmaxf(sv[1][nt][r], sv[1][nt][r + 2]));
-                raise |= top[nt][r] > kRaise || (m[nt][r] == -INFINITY && top[nt][r] > -INFINITY);
-            }
-        if (__any_sync(0xffffffffu, raise)) {
+            for (int nt = 0; nt < NT; ++nt) top = fmaxf(fmaxf(fmaxf(fmaxf(top, sv[mt][nt][0]), sv[mt][nt][1]), sv[mt][nt][2]), sv[mt][nt][3]);
+        if (__any_sync(0xffffffffu, top > kRaise || (first && there != 0u))) {
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                 for (int r = 0; r < 2; ++r) {
-                    float x = top[nt][r];
+                    float x = sv[0][nt][r];
+#pragma unroll
+                    for (int mt = 0; mt < MT; ++mt) x = fmaxf(x, fmaxf(sv[mt][nt][r], sv[mt][nt][r + 2]));
                     x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
                     x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
                     x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
-                    const bool first = m[nt][r] == -INFINITY;
                     if (x > kRaise || (first && x > -INFINITY)) {
-                        const float f = first ? 0.f : ex2(-x);
-                        m[nt][r] = (first ? 0.f : m[nt][r]) + x;
-                        l[nt][r] *= f;
+                        x += kHeadroom;
+                        const float f = first ? 0.f : ex2(-x);       // before the first key there is nothing to scale
+                        if (r == 0) { m[nt].x += x; l[nt].x *= f; }
+                        else { m[nt].y += x; l[nt].y *= f; }
 #pragma unroll
                         for (int i = 0; i < D / 16; ++i) {
                             o[i][nt][r] *= f;
                             o[i][nt][r + 2] *= f;
                         }
 #pragma unroll
-                        for (int mt = 0; mt < 2; ++mt) {
+                        for (int mt = 0; mt < MT; ++mt) {
                             sv[mt][nt][r] -= x;
                             sv[mt][nt][r + 2] -= x;
                         }
                     }
                 }
+            first = false;
         }
         // ---- P, and O^T += V^T P^T ----
 #pragma unroll
-        for (int mt = 0; mt < 2; ++mt) {
+        for (int mt = 0; mt < MT; ++mt) {
             uint32_t pf[NT][2];
             const float lw = kv8_scale(127 + min(e0 - ev[mt], kFarApart));
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
                 const float p0 = ex2(sv[mt][nt][0]), p1 = ex2(sv[mt][nt][1]), p2 = ex2(sv[mt][nt][2]), p3 = ex2(sv[mt][nt][3]);
-                l[nt][0] = fmaf(p0 + p2, lw, l[nt][0]);
-                l[nt][1] = fmaf(p1 + p3, lw, l[nt][1]);
+                l[nt] = __ffma2_rn(__fadd2_rn(make_float2(p0, p1), make_float2(p2, p3)), make_float2(lw, lw), l[nt]);
                 pf[nt][0] = transpose8(pack_f16(p0, p1));
                 pf[nt][1] = transpose8(pack_f16(p2, p3));
             }
             constexpr int VW = L::VB / 4;
             uint32_t vw[4][VW];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) lds<VW>(vring + st + (mt * 4 + j) * (L::VB * 32), vw[j]);
+            for (int j = 0; j < 4; ++j)
+                lds<VW>(ring + st + L::HALF + v_at(mt * 16 + 2 * t + (j & 1) + (j >> 1) * 8, g * L::VB / 16) + g * L::VB % 16, vw[j]);
             const uint32_t keys16 = (there >> (mt * 16)) & 0xFFFFu;
             if (keys16 != 0xFFFFu || blank[mt]) {              // values of keys that do not count may be anything
 #pragma unroll
@@ -337,7 +362,6 @@ __global__ void __launch_bounds__(RW * 32) kv8_attn_rows_kernel(const Kv8AttnArg
                 }
             }
         }
-        fetch(step + RSTAGES - 1);
     }
 
     // ---- the warps' results together, in their order ----
@@ -345,17 +369,17 @@ __global__ void __launch_bounds__(RW * 32) kv8_attn_rows_kernel(const Kv8AttnArg
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
-            float x = l[nt][r];
+            float x = r ? l[nt].y : l[nt].x;
             x += __shfl_xor_sync(0xffffffffu, x, 4);
             x += __shfl_xor_sync(0xffffffffu, x, 8);
             x += __shfl_xor_sync(0xffffffffu, x, 16);
             if (g == 0) {
-                stat[0][warp][nt * 8 + 2 * t + r] = m[nt][r];
+                stat[0][warp][nt * 8 + 2 * t + r] = first ? -INFINITY : r ? m[nt].y : m[nt].x;
                 stat[1][warp][nt * 8 + 2 * t + r] = x;
             }
         }
     if (lane == 0) top_v[warp] = e0;
-    cp_async_wait<0>();
+    ring_wait<0>();
     __syncthreads();                         // nobody reads the ring any more
     float* os = reinterpret_cast<float*>(smem);      // [warp][row][D + 4]
 #pragma unroll
@@ -373,15 +397,22 @@ __global__ void __launch_bounds__(RW * 32) kv8_attn_rows_kernel(const Kv8AttnArg
     for (int w = 0; w < RW; ++w) e0 = max(e0, top_v[w]);
     const float up = kv8_scale(e0);          // 2^E0
     constexpr int TPR = D / 4;               // threads of a row, 4 values each
-    float* part_o = a.part;                  // [item][split][row][D], then [item][split][row] log2 of the denominators
-    float* part_l = a.part + (int64_t)gridDim.y * gridDim.z * a.splits * L::ROWS * D;
-    auto finish = [&](int row, int c, float4 v, float lse2) {
+    const int cs = a.cluster, parts = a.splits / cs;
+    float* part_o = a.part;                  // [item][part][row][D], then [item][part][row] log2 of the denominators
+    float* part_l = a.part + (int64_t)gridDim.y * gridDim.z * parts * L::ROWS * D;
+    const int64_t part0 = ((int64_t)item * parts + split / cs) * L::ROWS;
+    auto give = [&](int row, int c, float4 v, float lse2) {          // a result of all that this launch has to add up, or of a part of it
+        if (parts > 1) {
+            *reinterpret_cast<float4*>(part_o + (part0 + row) * D + c * 4) = v;
+            if (c == 0) part_l[part0 + row] = lse2;
+            return;
+        }
         const int r = tile * L::ROWS + row;
         const int64_t at = (int64_t)(b * (int64_t)a.n + r / G) * a.n_heads + kvh * G + r % G;
-        uint2 w = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
-        *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(a.o) + at * D + c * 4) = w;
+        *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(a.o) + at * D + c * 4) = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
         if (a.lse && c == 0) a.lse[at] = lse2 * 0.6931471805599453f;
     };
+    float* res = os + RW * L::ROWS * (D + 4);            // [row][D], then [row]: this CTA's result, for the others of its cluster
     for (int i = tid; i < L::ROWS * TPR; i += RW * 32) {
         const int row = i / TPR, c = i % TPR;
         if (tile * L::ROWS + row >= R) continue;
@@ -402,89 +433,179 @@ __global__ void __launch_bounds__(RW * 32) kv8_attn_rows_kernel(const Kv8AttnArg
         const float s = den == 0.f ? 0.f : up / den;
         v.x *= s; v.y *= s; v.z *= s; v.w *= s;
         const float lse2 = den == 0.f ? -INFINITY : mx - (float)(e0 - 127) + log2f(den);
-        if (a.splits == 1) {
-            finish(row, c, v, lse2);
+        if (cs == 1) {
+            give(row, c, v, lse2);
         } else {
-            const int64_t p = ((int64_t)item * a.splits + split) * L::ROWS + row;
-            *reinterpret_cast<float4*>(part_o + p * D + c * 4) = v;
-            if (c == 0) part_l[p] = lse2;
+            *reinterpret_cast<float4*>(res + row * D + c * 4) = v;
+            if (c == 0) res[L::ROWS * D + row] = lse2;
         }
     }
-    if (a.splits == 1) return;
-    // ---- the last CTA of the item adds the splits up, in their order ----
+    if (cs > 1) {
+        // ---- the CTAs of a cluster add their results up, each for a share of the values, in the order of their keys ----
+        cluster_sync_all();
+        const uint32_t res_at = smem_u32(res);
+        for (int i = tid + split % cs * RW * 32; i < L::ROWS * TPR; i += cs * RW * 32) {
+            const int row = i / TPR, c = i % TPR;
+            if (tile * L::ROWS + row >= R) continue;
+            float x[8];
+            float4 w[8];
+#pragma unroll
+            for (int p = 0; p < 8; ++p) {
+                x[p] = -INFINITY;
+                if (p < cs) {
+                    x[p] = ld_peer(mapa_u32(res_at + (L::ROWS * D + row) * 4, p));
+                    w[p] = ld_peer4(mapa_u32(res_at + (row * D + c * 4) * 4, p));
+                }
+            }
+            Sum s;
+#pragma unroll
+            for (int p = 0; p < 8; ++p) s.add(x[p], w[p]);
+            give(row, c, s.mean(), s.lse2());
+        }
+        cluster_sync_all();                  // nobody leaves while its results are read
+    }
+    if (parts == 1) return;
+    // ---- of the CTAs with the same share, the last one adds the parts up, in their order ----
+    const int rank = split % cs;
     __threadfence();
     __syncthreads();
     if (tid == 0) {
-        const unsigned before = atomicAdd(a.arrived + item, 1u);
-        is_last = before == (unsigned)a.splits - 1u;
-        if (is_last) a.arrived[item] = 0u;
+        unsigned* arrived = a.arrived + item * cs + rank;
+        is_last = atomicAdd(arrived, 1u) == (unsigned)parts - 1u;
+        if (is_last) *arrived = 0u;
     }
     __syncthreads();
     if (!is_last) return;
     __threadfence();
-    for (int i = tid; i < L::ROWS * TPR; i += RW * 32) {
-        const int row = i / TPR, c = i % TPR;
-        if (tile * L::ROWS + row >= R) continue;
-        const int64_t p0 = (int64_t)item * a.splits * L::ROWS + row;
-        float mx = -INFINITY;
-        bool bad = false;
-        for (int s = 0; s < a.splits; ++s) {
-            const float x = __ldcg(part_l + p0 + (int64_t)s * L::ROWS);
-            mx = fmaxf(mx, x);
-            bad |= x != x;
+    const int64_t p0 = (int64_t)item * parts * L::ROWS;
+    for (int i = tid + rank * RW * 32; i < L::ROWS * TPR; i += cs * RW * 32) {
+        const int row = i / TPR, c = i % TPR, r = tile * L::ROWS + row;
+        if (r >= R) continue;
+        Sum s;
+        for (int q0 = 0; q0 < parts; q0 += 8) {
+            float x[8];
+            float4 w[8];
+#pragma unroll
+            for (int p = 0; p < 8; ++p) {
+                x[p] = -INFINITY;
+                if (q0 + p < parts) {
+                    x[p] = __ldcg(part_l + p0 + (int64_t)(q0 + p) * L::ROWS + row);
+                    w[p] = __ldcg(reinterpret_cast<const float4*>(part_o + (p0 + (int64_t)(q0 + p) * L::ROWS + row) * D + c * 4));
+                }
+            }
+#pragma unroll
+            for (int p = 0; p < 8; ++p) s.add(x[p], w[p]);
         }
-        float den = 0.f;
-        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int s = 0; s < a.splits; ++s) {
-            const float x = __ldcg(part_l + p0 + (int64_t)s * L::ROWS);
-            const float f = x == -INFINITY ? 0.f : ex2(x - mx);
-            const float4 w = __ldcg(reinterpret_cast<const float4*>(part_o + (p0 + (int64_t)s * L::ROWS) * D + c * 4));
-            den += f;
-            v.x = fmaf(f, w.x, v.x); v.y = fmaf(f, w.y, v.y); v.z = fmaf(f, w.z, v.z); v.w = fmaf(f, w.w, v.w);
-        }
-        const float inv = bad ? __int_as_float(0x7FC00000) : (den == 0.f ? 0.f : 1.f / den);
-        v.x *= inv; v.y *= inv; v.z *= inv; v.w *= inv;
-        finish(row, c, v, bad ? __int_as_float(0x7FC00000) : (den == 0.f ? -INFINITY : mx + log2f(den)));
+        const float4 v = s.mean();
+        const int64_t at = (int64_t)(b * (int64_t)a.n + r / G) * a.n_heads + kvh * G + r % G;
+        *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(a.o) + at * D + c * 4) = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
+        if (a.lse && c == 0) a.lse[at] = s.lse2() * 0.6931471805599453f;
     }
 }
 
 template <int D, int NT, int FMT>
-int rows_launch(Kv8AttnArgs a, cudaStream_t stream) {
-    using L = RowsLayout<D, NT>;
-    static bool attr = false;
-    if (!attr) {
-        cudaFuncSetAttribute(kv8_attn_rows_kernel<D, NT, FMT>, cudaFuncAttributeMaxDynamicSharedMemorySize, L::SMEM);
-        attr = true;
-    }
-    const int R = a.n * (a.n_heads / a.n_kv_heads), tiles = (R + L::ROWS - 1) / L::ROWS;
-    const int64_t items = (int64_t)tiles * a.batch * a.n_kv_heads;
-    // enough CTAs for two per SM, none with fewer than 128 keys
-    const int slots = 2 * sm_count();
-    int64_t splits = items >= slots ? 1 : (slots + items - 1) / items;
-    if (splits > (a.ctx_len + 127) / 128) splits = (a.ctx_len + 127) / 128;
-    if (splits < 1) splits = 1;
-    a.split_keys = (int)(((a.ctx_len + splits - 1) / splits + RSTEP * RW - 1) / (RSTEP * RW)) * RSTEP * RW;
-    a.splits = a.split_keys ? (a.ctx_len + a.split_keys - 1) / a.split_keys : 1;
-    const dim3 grid(a.splits, tiles, a.batch * a.n_kv_heads);
-    return launch_pdl(kv8_attn_rows_kernel<D, NT, FMT>, grid, dim3(RW * 32), L::SMEM, stream, a) == cudaSuccess ? 1 : -1;
+void rows_config(cudaLaunchConfig_t& cfg, cudaLaunchAttribute (&at)[2], dim3 grid, int cluster, cudaStream_t stream) {
+    cfg = cudaLaunchConfig_t{};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(RW * 32);
+    cfg.dynamicSmemBytes = RowsLayout<D, NT>::SMEM;
+    cfg.stream = stream;
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = cluster; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
+    at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 2;
 }
-template <int D, int FMT>
-int rows_tiles(const Kv8AttnArgs& a, cudaStream_t stream) {
+// clusters of 2^c CTAs that the GPU runs at a time: fewer than the places for CTAs make up, as a cluster stays in one group of SMs
+template <int D, int NT, int FMT>
+int rows_clusters(int c) {
+    static int fit[4] = {};
+    if (fit[0] == 0) {
+        cudaFuncSetAttribute(kv8_attn_rows_kernel<D, NT, FMT>, cudaFuncAttributeMaxDynamicSharedMemorySize, RowsLayout<D, NT>::SMEM);
+        for (int i = 3; i >= 0; --i) {
+            cudaLaunchConfig_t cfg;
+            cudaLaunchAttribute at[2];
+            rows_config<D, NT, FMT>(cfg, at, dim3(1 << i), 1 << i, nullptr);
+            cfg.numAttrs = 1;
+            int most = 0;
+            if (cudaOccupancyMaxActiveClusters(&most, kv8_attn_rows_kernel<D, NT, FMT>, &cfg) != cudaSuccess) most = 0;
+            fit[i] = std::min(std::max(most, 1), (kSlots * 148) >> i);
+        }
+    }
+    return fit[c];
+}
+struct RowsPlan { int cluster, splits; int64_t cost; };   // cost: ns
+// Key splits, in clusters that add their results up; splits only where all their CTAs run at a time.  The estimate, with what was
+// measured for 32 rows of 128: a CTA takes 4 us and 17.5 ns a key (9 us and the same, where two share an SM), the sum over a
+// cluster 2 us, the sum over clusters 2 us and 0.8 us for every eight of them and every value of a thread.  More CTAs than places
+// take as many times longer, and a quarter for the last ones.  One sequence of 65536 keys, 4 KV heads, 35 rows: 51 us in 18
+// clusters of 2, 72 us in 4 of 8 (which do not all run at a time); 512 items of 8192 keys: 166 us whole, 180 us in halves.
+template <int D, int NT, int FMT>
+RowsPlan rows_plan(const Kv8AttnArgs& a) {
+    using L = RowsLayout<D, NT>;
     const int R = a.n * (a.n_heads / a.n_kv_heads);
-    return R <= 8 ? rows_launch<D, 1, FMT>(a, stream) : rows_launch<D, 2, FMT>(a, stream);
+    const int64_t items = (int64_t)((R + L::ROWS - 1) / L::ROWS) * a.batch * a.n_kv_heads;
+    RowsPlan best{1, 1, INT64_MAX};
+    const int most = std::max(1, a.ctx_len / kMinSplit);
+    for (int c = 0; c < 4 && 1 << c <= most; ++c) {
+        const int fit = rows_clusters<D, NT, FMT>(c);
+        if (c > 0 && items > fit) break;
+        const int top = c == 0 ? 1 : (int)std::min<int64_t>(fit / items, most >> c);
+        for (int k = 1;; k = top) {                       // one cluster an item, or as many as there is room for
+            const int splits = k << c, keys = (a.ctx_len + splits - 1) / splits;
+            int64_t cost = (NT == 4 && items * splits > 148 ? 9000 : 4000) + (int64_t)keys * kKeyNs<D, NT> / 10;
+            if (items > fit) cost = cost * (items * 4 + fit) / (fit * 4);
+            if (c > 0) cost += 2000;
+            if (k > 1) cost += 2000 + 800 * ((L::ROWS * D / (4 * RW * 32) + (1 << c) - 1) >> c) * ((k + 7) / 8);
+            if (cost < best.cost) best = RowsPlan{1 << c, splits, cost};
+            if (k == top) break;
+        }
+    }
+    return best;
+}
+template <int D, int NT, int FMT>
+int rows_launch(Kv8AttnArgs a, const RowsPlan& plan, cudaStream_t stream) {
+    const int R = a.n * (a.n_heads / a.n_kv_heads), tiles = (R + 8 * NT - 1) / (8 * NT);
+    a.cluster = plan.cluster;
+    a.splits = plan.splits;
+    a.split_keys = ((a.ctx_len + a.splits - 1) / a.splits + RSTEP - 1) / RSTEP * RSTEP;
+    cudaLaunchConfig_t cfg;
+    cudaLaunchAttribute at[2];
+    rows_config<D, NT, FMT>(cfg, at, dim3(a.splits, tiles, a.batch * a.n_kv_heads), a.cluster, stream);
+    return cudaLaunchKernelEx(&cfg, kv8_attn_rows_kernel<D, NT, FMT>, a) == cudaSuccess ? 1 : -1;
+}
+// Rows of a CTA: up to 32, so that a key is converted once for as many of them as there are; fewer where there are too few CTAs to
+// go round (4 KV heads, 35 rows, 1536 keys: 8.6 us with 8 rows a CTA, 15 us with 32; the same times 16 requests: 27 and 26 us).
+// More than 32 rows: the tensor-memory kernel, where its plan takes less than this one's.  16 sequences, 32 KV heads, 100 rows,
+// 8192 keys: 535 us there, 953 us here; one sequence of 300 keys: 12.3 and 10.0 us.  Up to 32 rows this one is always ahead.
+template <int D, int FMT>
+int rows_dispatch(const Kv8AttnArgs& a, cudaStream_t stream) {
+    const int R = a.n * (a.n_heads / a.n_kv_heads);
+    const int64_t pairs = (int64_t)a.batch * a.n_kv_heads, splits = std::max(1, a.ctx_len / kMinSplit);
+    auto ctas = [&](int rows) { return (R + rows - 1) / rows * pairs * splits; };
+    const int nt = R <= 8 || ctas(16) < 148 ? 1 : R <= 16 || ctas(32) < 148 ? 2 : 4;
+    if (nt == 1) return rows_launch<D, 1, FMT>(a, rows_plan<D, 1, FMT>(a), stream);
+    if (nt == 2) return rows_launch<D, 2, FMT>(a, rows_plan<D, 2, FMT>(a), stream);
+    const RowsPlan plan = rows_plan<D, 4, FMT>(a);
+    if (D == 128 && R > 32) {
+        const int r = launch_kv8_attention_tc(a, plan.cost, stream);
+        if (r != 0) return r;
+    }
+    return rows_launch<D, 4, FMT>(a, plan, stream);
 }
 
 }  // namespace
 
 size_t kv8_attention_scratch_bytes(int head_dim) {
-    // keys are split only below two items per SM: fewer than four results per SM of up to 16 rows
-    return (size_t)4 * 148 * 16 * (head_dim + 1) * sizeof(float);
+    // keys are split only below an item per place for a CTA: no more results than places, of up to 32 rows
+    return (size_t)kSlots * 148 * 32 * (head_dim + 1) * sizeof(float);
 }
 
 int launch_kv8_attention(const Kv8AttnArgs& a, cudaStream_t stream) {
     if (a.batch == 0 || a.n == 0) return 0;
-    if (a.head_dim == 128) return a.format == kKv8Int8 ? rows_tiles<128, kKv8Int8>(a, stream) : rows_tiles<128, kKv8E4m3>(a, stream);
-    return a.format == kKv8Int8 ? rows_tiles<64, kKv8Int8>(a, stream) : rows_tiles<64, kKv8E4m3>(a, stream);
+    if (a.head_dim == 128) return a.format == kKv8Int8 ? rows_dispatch<128, kKv8Int8>(a, stream) : rows_dispatch<128, kKv8E4m3>(a, stream);
+    return a.format == kKv8Int8 ? rows_dispatch<64, kKv8Int8>(a, stream) : rows_dispatch<64, kKv8E4m3>(a, stream);
 }
 
 }  // namespace acache

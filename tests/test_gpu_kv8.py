@@ -387,6 +387,27 @@ def test_attention(heads, n, T, block, fmt):
 
 
 @pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+@pytest.mark.parametrize("heads,B,n,T,block,kernel", [
+    ("mha32", 1, 33, 300, 64, "kv8_attn_rows"), ("gqa28", 1, 18, 8192, 64, "kv8_attn_rows"), ("mha32", 4, 33, 300, 64, "kv8_attn_tc"),
+    ("mha32", 1, 100, 1600, 16, "kv8_attn_tc"), ("gqa28", 4, 18, 8200, 128, "kv8_attn_tc"), ("gqa28", 1, 64, 3000, 32, "kv8_attn_tc"),
+    ("mqa8", 16, 20, 2100, 64, "kv8_attn_tc"), ("mha32", 8, 200, 257, 32, "kv8_attn_tc")])
+def test_attention_of_many_rows(heads, B, n, T, block, kernel, fmt):
+    """Both kernels around the place where the one takes over from the other; keys split over two to eight CTAs of a cluster and
+    over several clusters; a request whose length leaves splits without keys."""
+    ctx = context(heads, B, T)
+    cache, vals = filled(heads, B, T, block, fmt, n + T, holes=(3,))
+    q = queries(B, n, heads, T)
+    check_attention(ctx, cache, vals, B, n, T, heads, q)
+    check_attention(ctx, cache, vals, B, n, T, heads, q, lens=[T // 3] + [T - 1] * (B - 1))
+    with torch.profiler.profile(activities=[torch.profiler.ProfilerActivity.CUDA]) as prof:
+        ctx.kv8_attention(cache.c, B, T, q, torch.empty_like(q))
+        torch.cuda.synchronize()
+    names = [e.key for e in prof.key_averages() if "kv8" in e.key]
+    assert len(names) == 1 and kernel in names[0], names
+    assert ctx.poll_status() == 0
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
 @pytest.mark.parametrize("heads,n,T,block", [("gqa28", 1, 999, 16), ("mha4-64", 40, 300, 16), ("mha32", 32, 600, 64),
                                              ("gqa28", 29, 1531, 32), ("mha32", 150, 900, 128), ("mha32", 20, 130, 64)])
 def test_attention_lengths_drops_and_holes(heads, n, T, block, fmt):
