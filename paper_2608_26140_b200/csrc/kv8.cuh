@@ -62,6 +62,26 @@ __device__ __forceinline__ uint32_t kv8_round(float a, float b, float c, float d
         return w;
     }
 }
+// 4 bf16 values times a power of two; int8: multiplied (exactly, but for values too small to matter) and clamped in pairs
+template <int FMT>
+__device__ __forceinline__ uint32_t kv8_round_bf16(uint32_t ab, uint32_t cd, float pow2) {
+    if constexpr (FMT == kKv8Int8) {
+        auto pair = [](uint32_t x, uint32_t s) {
+            uint32_t y;
+            asm("{\n\t.reg .b32 t;\n\t"
+                "mul.rn.bf16x2 t, %1, %2;\n\t"
+                "min.bf16x2 t, t, %3;\n\t"
+                "max.bf16x2 %0, t, %4;\n\t}"
+                : "=r"(y) : "r"(x), "r"(s), "r"(0x42FE42FEu), "r"(0xC2FEC2FEu));          // 127, -127
+            return y;
+        };
+        auto r = [](float x) { return __float_as_uint(x + 12582912.f); };
+        const uint32_t half = __float_as_uint(pow2) >> 16, s = half | half << 16, y = pair(ab, s), z = pair(cd, s);
+        return __byte_perm(__byte_perm(r(bf16_lo(y)), r(bf16_hi(y)), 0x0040), __byte_perm(r(bf16_lo(z)), r(bf16_hi(z)), 0x0040), 0x5410);
+    } else {
+        return kv8_round<FMT>(bf16_lo(ab) * pow2, bf16_hi(ab) * pow2, bf16_lo(cd) * pow2, bf16_hi(cd) * pow2);
+    }
+}
 // The same for values that need care: not finite (int8: NaN is 0, an infinity the largest code; e4m3: both are NaN), or of
 // the block at the top of bf16's range, whose largest values would round past it (limit: the largest code to be used).
 template <int FMT>
@@ -72,6 +92,19 @@ __device__ __forceinline__ uint32_t kv8_round_careful(float a, float b, float c,
         return fminf(fmaxf(x, -limit), limit);
     };
     return kv8_round<FMT>(mend(a), mend(b), mend(c), mend(d));
+}
+
+// 32 bytes at a time: whole sectors of rows that lie apart.  whole: p is a multiple of 32 (callers guarantee 16)
+__device__ __forceinline__ bool on_sector(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 31u) == 0; }
+__device__ __forceinline__ void st_global32(void* p, const uint32_t (&v)[8], bool whole) {
+    if (!whole) {
+        static_cast<uint4*>(p)[0] = make_uint4(v[0], v[1], v[2], v[3]);
+        static_cast<uint4*>(p)[1] = make_uint4(v[4], v[5], v[6], v[7]);
+        return;
+    }
+    asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]),
+                 "r"(v[6]), "r"(v[7])
+                 : "memory");
 }
 
 // ---- what the attention kernels share ----------------------------------------------------

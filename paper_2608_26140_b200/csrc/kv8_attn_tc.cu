@@ -370,7 +370,7 @@ __global__ void __launch_bounds__(TT_THREADS, 1) kv8_attn_tc_kernel(const Kv8Att
                             for (int h = 0; h < 2; ++h) {
 #pragma unroll
                                 for (int k = 0; k < 8; ++k) u[k] = pack_bf16(v[h * 16 + 2 * k] * inv, v[h * 16 + 2 * k + 1] * inv);
-                                st_global32(out + h * 16, u);
+                                st_global32(out + h * 16, u, on_sector(a.o));
                             }
                         } else {
 #pragma unroll

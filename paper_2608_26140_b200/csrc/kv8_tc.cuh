@@ -195,11 +195,4 @@ __device__ __forceinline__ void rows_held(uint32_t empty8, uint32_t (&rows)[4]) 
     }
 }
 
-// 32 bytes at a time: whole sectors of rows that lie apart
-__device__ __forceinline__ void st_global32(void* p, const uint32_t (&v)[8]) {
-    asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]),
-                 "r"(v[6]), "r"(v[7])
-                 : "memory");
-}
-
 }  // namespace acache

@@ -664,6 +664,39 @@ def test_layer_step(shape, B, pre, L, post, gen, extra, ratio, block, fmt, flags
 # --------------------------------------------------------------------------
 # refusals
 # --------------------------------------------------------------------------
+@pytest.mark.parametrize("heads,n", [("gqa28", 1), ("mha4-64", 70), ("mha32", 150)])
+def test_tensors_that_begin_at_16_bytes(heads, n):
+    """Every tensor at an address that is a multiple of 16 bytes but not of 32: the same bits as at rounder addresses."""
+    B, T, block = 2, 640, 32
+    H, hkv, d = HEADS[heads]
+    ctx = context(heads, B, T)
+
+    def at16(t):
+        """a copy at an address of 16 mod 32"""
+        raw = torch.zeros(t.numel() * t.element_size() + 64, dtype=torch.uint8, device=DEV)
+        off = (16 - raw.data_ptr()) % 32
+        view = raw[off:off + t.numel() * t.element_size()].view(t.dtype).view(t.shape)
+        view.copy_(t)
+        assert view.data_ptr() % 32 == 16
+        return view
+
+    cache, _ = filled(heads, B, T, block, "int8", 3)
+    q = queries(B, n, heads, 4)
+    k, v = (torch.randn((B, 50, hkv, d), device=DEV).bfloat16() for _ in range(2))
+    results = []
+    for place in (torch.clone, at16):
+        kc, vc, ke, ve = (place(t) for t in cache.dev)
+        c = ab.Context.kv8(kc, vc, ke, ve, block, ab.KV8_FORMATS["int8"])
+        o, ko, vo = place(torch.zeros_like(q)), place(torch.zeros_like(k)), place(torch.zeros_like(v))
+        ctx.kv8_write(c, B, T, place(k), place(v), start=33)
+        ctx.kv8_read(c, B, T, ko, vo, start=30)
+        ctx.kv8_attention(c, B, T, place(q), o)
+        torch.cuda.synchronize()
+        results.append((kc, vc, ke, ve, ko, vo, o))
+    assert all(torch.equal(x, y) for x, y in zip(*results))
+    assert ctx.poll_status() == 0
+
+
 def test_refusals():
     heads, B, T = "gqa28", 2, 256
     H, hkv, d = HEADS[heads]
