@@ -39,6 +39,10 @@ static_assert(tt_smem<1>() >= kAloneBytes && tt_smem<2>() <= 227 * 1024);
 template <int FMT, int SETS>
 __global__ void __launch_bounds__(TT_THREADS, 1) kv8_attn_tc_kernel(const Kv8AttnArgs a) {
     constexpr int CW = SETS == 2 ? 4 : 8;                 // converter warps
+    // Parts of a row tile's S, each a product of its own.  Alone, a row tile leaves the tensor core idle while its softmax runs, and
+    // halves let the next S be made meanwhile (100 rows, 8192 keys, 512 pairs: 510 us, whole 535); two fill each other's gaps, and
+    // products of 64 keys, which read Q twice as often from shared memory, only cost (922 rows, 2560 keys: 829 us, whole 806).
+    constexpr int S_PARTS = SETS == 2 ? 1 : 2;
     constexpr int CT = CW * 32;
     extern __shared__ unsigned char smem_raw[];
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -49,8 +53,8 @@ __global__ void __launch_bounds__(TT_THREADS, 1) kv8_attn_tc_kernel(const Kv8Att
     const uint32_t bars = smem_u32(tail + kTables * sizeof(KeyTable));
     volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(tail + kTables * sizeof(KeyTable) + 232);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tail + kTables * sizeof(KeyTable) + 236);
-    // barriers: 0 q_full | 1,2 k_full | 3,4 k_empty | 5,6 v_full | 7,8 v_empty | 9 + t: s_full | 11 + 2 t + hb: p_full |
-    //           15 + 2 t + hb: pv_done (row tile t, key half hb) | 19 + j % 4: table of key tile j
+    // barriers: 0 q_full | 1,2 k_full | 3,4 k_empty | 5,6 v_full | 7,8 v_empty | 11 + 2 t + hb: p_full | 15 + 2 t + hb: pv_done |
+    //           19 + j % 4: table of key tile j | 23 + 2 t + part: s_full   (row tile t, key half hb)
     auto bar = [&](int i) { return bars + 8 * i; };
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int split = blockIdx.x, tile = blockIdx.y, b = blockIdx.z / a.n_kv_heads, kvh = blockIdx.z % a.n_kv_heads;
@@ -63,8 +67,8 @@ __global__ void __launch_bounds__(TT_THREADS, 1) kv8_attn_tc_kernel(const Kv8Att
         mbar_init(bar(0), warps_of(0) + (n_sets == 2 ? warps_of(1) : 0));
         for (int i = 1; i <= 2; ++i) { mbar_init(bar(i), CW); mbar_init(bar(4 + i), CW); mbar_init(bar(2 + i), 1); mbar_init(bar(6 + i), 1); }
         for (int t = 0; t < 2; ++t) {
-            mbar_init(bar(9 + t), 1);
             for (int hb = 0; hb < 2; ++hb) {
+                mbar_init(bar(23 + 2 * t + hb), 1);
                 mbar_init(bar(11 + 2 * t + hb), t < n_sets ? warps_of(t) : 1);
                 mbar_init(bar(15 + 2 * t + hb), 1);
             }
@@ -157,27 +161,33 @@ __global__ void __launch_bounds__(TT_THREADS, 1) kv8_attn_tc_kernel(const Kv8Att
         }
     } else if (warp == 12) {
         // ---------------- MMA issuer: the whole warp runs the loop, one lane issues ----------------
-        const uint32_t idesc_s = (1u << 4) | ((uint32_t)(128 >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);    // f16 x f16 -> fp32
-        const uint32_t idesc_o = idesc_s | (1u << 16);    // B = V is MN-major
-        auto wait = [&](int i, uint32_t parity) { return __all_sync(0xffffffffu, mbar_poll(bar(i), parity, abort_flag)); };
-        auto issue_s = [&](int t, int j) {
-            const uint32_t k = sK0 + (j & 1) * TT_TILE;
+        const uint32_t idesc = (1u << 4) | ((uint32_t)(128 >> 4) << 24);                 // f16 x f16 -> fp32, 128 rows
+        const uint32_t idesc_s = idesc | ((uint32_t)(128 / S_PARTS >> 3) << 17);         // keys of a part
+        const uint32_t idesc_o = idesc | ((uint32_t)(128 >> 3) << 17) | (1u << 16);      // 128 columns of V, which is MN-major
+        auto wait = [&](int i, uint32_t parity) { return __all_sync(0xffffffffu, tt_spin(bar(i), parity, abort_flag)); };
+        auto issue_s = [&](int t, int j, int part) {
+            const uint32_t k = sK0 + (j & 1) * TT_TILE + part * (64 * 128);
             if (!elect_lane()) return;
 #pragma unroll
             for (int ks = 0; ks < 8; ++ks) {
                 const uint64_t da = smem_desc_sw128(sQ + t * TT_TILE + (ks >> 2) * TT_PANEL) + (uint64_t)((ks & 3) * 2);
                 const uint64_t db = smem_desc_sw128(k + (ks >> 2) * TT_PANEL) + (uint64_t)((ks & 3) * 2);
-                tc_mma(tmem_base + t * 128, da, db, idesc_s, ks > 0 ? 1u : 0u);
+                tc_mma(tmem_base + t * 128 + part * 64, da, db, idesc_s, ks > 0 ? 1u : 0u);
             }
-            tc_commit(bar(9 + t));
+            tc_commit(bar(23 + 2 * t + part));
         };
         bool ok = n_tiles > 0 && wait(0, 0) && wait(1, 0);
         if (ok) {
             tc_fence_after();
-            for (int t = 0; t < n_sets; ++t) issue_s(t, 0);
+            for (int t = 0; t < n_sets; ++t)
+                for (int part = 0; part < S_PARTS; ++part) {
+                    issue_s(t, 0, part);
+                    __syncwarp();
+                }
             if (elect_lane()) tc_commit(bar(3));
             __syncwarp();
         }
+        // The next key tile's S goes out right behind the P V that reads the P in its columns: the products execute in order.
         for (int j = 0; j < n_tiles && ok; ++j) {
             const int s = j & 1;
             const bool more = j + 1 < n_tiles;
@@ -190,17 +200,15 @@ __global__ void __launch_bounds__(TT_THREADS, 1) kv8_attn_tc_kernel(const Kv8Att
                     tc_fence_after();
                     if (elect_lane()) {
 #pragma unroll
-                        for (int k4 = 0; k4 < 4; ++k4) {
-                            const int ks = hb * 4 + k4;
-                            tt_mma_ta(tmem_base + O_COL + t * 128, tmem_base + t * 128 + ks * 8, tt_desc_mn(v + ks * 2048), idesc_o,
-                                      (j > 0 || ks > 0) ? 1u : 0u);
-                        }
+                        for (int k4 = 0; k4 < 4; ++k4)
+                            tt_mma_ta(tmem_base + O_COL + t * 128, tmem_base + t * 128 + hb * 64 + k4 * 8, tt_desc_mn(v + (hb * 4 + k4) * 2048), idesc_o,
+                                      (j > 0 || hb > 0 || k4 > 0) ? 1u : 0u);
                         tc_commit(bar(15 + 2 * t + hb));
                     }
                     __syncwarp();
+                    if (more && hb + S_PARTS >= 2) issue_s(t, j + 1, S_PARTS == 2 ? hb : 0);
+                    __syncwarp();
                 }
-                if (ok && more) issue_s(t, j + 1);        // overwrites P: executes after the P V just issued
-                __syncwarp();
             }
             if (elect_lane()) {
                 tc_commit(bar(7 + s));
@@ -253,7 +261,9 @@ __global__ void __launch_bounds__(TT_THREADS, 1) kv8_attn_tc_kernel(const Kv8Att
                     if (!(ok = __all_sync(0xffffffffu, tt_spin(bar(19 + (j & (kTables - 1))), (j >> 2) & 1, abort_flag)))) break;
                     l *= tab.grow;
                     e0 = tab.e0;
-                    if (!(ok = __all_sync(0xffffffffu, tt_spin(bar(9 + t), j & 1, abort_flag)))) break;
+                }
+                if (hb < S_PARTS) {
+                    if (!(ok = __all_sync(0xffffffffu, tt_spin(bar(23 + 2 * t + hb), j & 1, abort_flag)))) break;
                     tc_fence_after();
                 }
                 const uint2 keep2 = *reinterpret_cast<const uint2*>(&tab.keep[2 * hb]);
@@ -322,7 +332,7 @@ __global__ void __launch_bounds__(TT_THREADS, 1) kv8_attn_tc_kernel(const Kv8Att
                             for (int e = 0; e < 32; ++e) sv[c][e] -= mx;
                     }
                 }
-                // P as packed f16: the half's 64 keys go to columns 32 hb .. of the S buffer, over S values that this thread has read
+                // P as packed f16 over the first 32 of the half's 64 columns of S, which this thread has read
                 uint32_t pk[32];
 #pragma unroll
                 for (int g = 0; g < 4; ++g) {
@@ -338,7 +348,7 @@ __global__ void __launch_bounds__(TT_THREADS, 1) kv8_attn_tc_kernel(const Kv8Att
                     }
                     l = fmaf((sa.x + sa.y) + (sb.x + sb.y), sc[g].z, l);
                 }
-                tt_st32(tS + hb * 32, pk);
+                tt_st32(tS + hb * 64, pk);
                 tt_wait_st();
                 tc_fence_before();
                 __syncwarp();
