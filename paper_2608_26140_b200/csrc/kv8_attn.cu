@@ -10,12 +10,15 @@
 // V's codes are f16 whatever their scales, which leaves p 11 bits (with bf16 operands, 8).  q is f16 too, each row over a
 // power of two of its own that brings its largest value to [1, 2).
 //
-// Bound by HBM on the codes.  A warp streams keys on its own: the bytes go from the cache to a ring in shared memory in
-// which every thread has its own slots (cp.async; a thread reads back what it asked for, so no barrier), from there to
-// registers, become matrix-instruction fragments there and are used for all the rows.  The order of d inside a product is
-// free, so a thread's 16 contiguous bytes of a key row serve as its fragment of four products:
+// A warp streams keys on its own, 32 a step: the bytes go from the cache to a ring of its own in shared memory (cp.async, whole
+// rows side by side; half rows stopped at 4.8 TB/s), swizzled so that the fragments' reads meet different banks, from there to
+// registers, become matrix-instruction fragments there and are used for all the rows.  The order of d inside a product is free,
+// so a thread's 16 contiguous bytes of a key row serve as its fragment of four products:
 //   S^T = K Q^T (keys x rows)   O^T += V^T P^T (d x rows): keys and d are the long sides of both products, so up to 8 rows cost
 //   one instruction, and P only has to be transposed in 8 x 8 blocks (movmatrix).
+// Up to 8 rows HBM bounds it: one token over 2 x 65537 keys of 32 heads (1074 MB) 171 us, 6.3 TB/s.  At 32 rows (16 x 2560 keys of
+// 32 heads, 344 MB, 98 us) HBM, the matrix instructions and the issue slots are each taken for about 40 % of the time: with 255
+// registers a thread there are two warps a scheduler to hide each other's waits.
 // The reference M moves only when a logit passes it by 2^15 (f16 ends at 2^16), found by a vote; then maxima are exchanged and O is scaled.
 #include <algorithm>
 #include <climits>
@@ -47,15 +50,21 @@ __device__ __forceinline__ void mma_f16_16816(float* c, const uint32_t* a, uint3
         : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
+__device__ __forceinline__ void mma_f16_16816_first(float* c, const uint32_t* a, uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};\n"
+        : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
+}
 __device__ __forceinline__ uint32_t transpose8(uint32_t v) {
     uint32_t r;
     asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
     return r;
 }
-template <int BYTES>
-__device__ __forceinline__ void cp_async(uint32_t dst, const void* src, bool on) {
-    if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;\n" ::"r"(dst), "l"(src), "r"(on ? 16 : 0) : "memory");
-    else asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;\n" ::"r"(dst), "l"(src), "r"(on ? 8 : 0) : "memory");
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool on) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;\n" ::"r"(dst), "l"(src), "r"(on ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;\n" ::"r"(dst), "l"(src) : "memory");
 }
 // the copies asked for are there but for the newest N groups; what is read from them stays behind this
 template <int N>
@@ -115,24 +124,39 @@ __global__ void __launch_bounds__(RW * 32, NT < 4 ? kSlots : 1) kv8_attn_rows_ke
     auto k_at = [](int row, int piece) { return row * D + ((D == 128 ? piece ^ ((row & 1) << 2) : piece ^ ((row >> 1) & 3)) << 4); };
     auto v_at = [](int row, int piece) { return row * D + ((D == 128 ? piece ^ (row & 6) : piece ^ ((row >> 1) & 3)) << 4); };
 
-    auto fetch = [&](int step) {         // this warp's `step`-th step into its ring
+    // a lane's piece of the first rows of a copy; the next ones are 32 / PIECES rows further, in the ring's values with the
+    // upper bit of the swizzle turned over
+    constexpr int PASS = 32 / PIECES, PASSES = RSTEP / PASS;
+    const int row0 = lane / PIECES, piece = lane % PIECES;
+    const uint32_t ring_at = smem_u32(ring), k_to = k_at(row0, piece), v_to = L::HALF + v_at(row0, piece), v_to_odd = L::HALF + v_at(row0 + PASS, piece);
+    auto fetch = [&](int step, int stage) {          // this warp's `step`-th step into its ring
         const int s = warp + step * RW;
         if (s < steps) {
             const int key0 = key_lo + s * RSTEP;
-            const uint32_t st = smem_u32(ring) + (step % RSTAGES) * L::STAGE;
+            const uint32_t st = ring_at + stage * L::STAGE;
+            if (key0 + RSTEP <= key_hi) {
+                const uint8_t* from = kb + (int64_t)(key0 + row0) * D + piece * 16;
+                const uint8_t* from_v = vb + (int64_t)(key0 + row0) * D + piece * 16;
 #pragma unroll
-            for (int i = 0; i < RSTEP * PIECES / 32; ++i) {
-                const int row = (i * 32 + lane) / PIECES, piece = lane % PIECES;
-                const bool on = key0 + row < key_hi;
-                const int64_t at = (int64_t)(on ? key0 + row : key_lo) * D + piece * 16;
-                cp_async<16>(st + k_at(row, piece), kb + at, on);
-                cp_async<16>(st + L::HALF + v_at(row, piece), vb + at, on);
+                for (int i = 0; i < PASSES; ++i) {
+                    cp_async16(st + k_to + i * PASS * D, from + i * PASS * D);
+                    cp_async16(i % 2 == 0 || PASS >= 8 ? st + v_to + i * PASS * D : st + v_to_odd + (i - 1) * PASS * D, from_v + i * PASS * D);
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < PASSES; ++i) {
+                    const int row = i * PASS + row0;
+                    const bool on = key0 + row < key_hi;
+                    const int64_t at = (int64_t)(on ? key0 + row : key_lo) * D + piece * 16;
+                    cp_async16(st + k_at(row, piece), kb + at, on);
+                    cp_async16(st + L::HALF + v_at(row, piece), vb + at, on);
+                }
             }
         }
         cp_async_commit();
     };
 #pragma unroll
-    for (int s = 0; s < RSTAGES - 1; ++s) fetch(s);
+    for (int s = 0; s < RSTAGES - 1; ++s) fetch(s, s);
 
     // exponent bytes of a step's two 16-key tiles: K, K, V, V (a block holds whole tiles)
     const int64_t exps_at = ((int64_t)(a.shared ? 0 : b) * a.n_kv_heads + kvh) * a.n_blocks;
@@ -204,17 +228,19 @@ __global__ void __launch_bounds__(RW * 32, NT < 4 ? kSlots : 1) kv8_attn_rows_ke
             for (int j = 0; j < 4; ++j) o[i][nt][j] = 0.f;
     }
 
+    int stage = 0;                       // step % RSTAGES
     for (int step = 0; warp + step * RW < steps; ++step) {
         const int s = warp + step * RW, key0 = key_lo + s * RSTEP;
-        const uint32_t st = (step % RSTAGES) * L::STAGE;
+        const uint32_t st = stage * L::STAGE;
         uint32_t there = key_hi - key0 >= RSTEP ? ~0u : (1u << (key_hi - key0)) - 1u;      // the step's keys that count
         if (a.key_drop) there &= ~__ldg(a.key_drop + (int64_t)b * a.drop_words + (key0 >> 5));
         int ek[MT], ev[MT];
-        bool blank[MT];                       // a block that holds nothing has zero keys and values, whatever its codes
+        bool blank[MT], no_keys = false;      // a block that holds nothing has zero keys and values, whatever its codes
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
             ek[mt] = e_next[mt];
             ev[mt] = e_next[MT + mt];
+            no_keys |= ek[mt] == 0;
             blank[mt] = ev[mt] == 0;
             if (blank[mt]) ev[mt] = e0 ? e0 : 127;      // its scale is of no account
             if (ev[mt] > e0) {
@@ -227,25 +253,25 @@ __global__ void __launch_bounds__(RW * 32, NT < 4 ? kSlots : 1) kv8_attn_rows_ke
         exponents(step + 1, e_next);
         ring_wait<RSTAGES - 2>();
         __syncwarp();                        // this step's stage is there for every lane, and every lane is done with the last one's
-        fetch(step + RSTAGES - 1);
+        fetch(step + RSTAGES - 1, stage == 0 ? RSTAGES - 1 : stage - 1);
+        stage = stage == RSTAGES - 1 ? 0 : stage + 1;
         // ---- S^T = K Q^T, then y - M in place ----
         float sv[MT][NT][4];
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) sv[mt][nt][j] = 0.f;
 #pragma unroll
         for (int c = 0; c < L::KCH; ++c) {
             uint32_t kw[MT][2][4];
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-                for (int r = 0; r < 2; ++r) {
-                    lds<4>(ring + st + k_at(mt * 16 + r * 8 + g, c * 4 + t), kw[mt][r]);
-                    if (ek[mt] == 0) kw[mt][r][0] = kw[mt][r][1] = kw[mt][r][2] = kw[mt][r][3] = 0u;
-                }
+                for (int r = 0; r < 2; ++r) lds<4>(ring + st + k_at(mt * 16 + r * 8 + g, c * 4 + t), kw[mt][r]);
+            if (no_keys) {
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                    for (int r = 0; r < 2; ++r)
+#pragma unroll
+                        for (int w = 0; w < 4; ++w) kw[mt][r][w] = ek[mt] ? kw[mt][r][w] : 0u;
+            }
 #pragma unroll
             for (int w = 0; w < 4; ++w) {
                 uint32_t fa[MT][4];
@@ -260,7 +286,10 @@ __global__ void __launch_bounds__(RW * 32, NT < 4 ? kSlots : 1) kv8_attn_rows_ke
                     if constexpr (Q_SMEM) q = qs[((c * 4 + w) * NT + nt) * 32 + lane];
                     else q = make_uint2(qf[nt][c * 4 + w][0], qf[nt][c * 4 + w][1]);
 #pragma unroll
-                    for (int mt = 0; mt < MT; ++mt) mma_f16_16816(sv[mt][nt], fa[mt], q.x, q.y);
+                    for (int mt = 0; mt < MT; ++mt) {
+                        if (c == 0 && w == 0) mma_f16_16816_first(sv[mt][nt], fa[mt], q.x, q.y);
+                        else mma_f16_16816(sv[mt][nt], fa[mt], q.x, q.y);
+                    }
                 }
             }
         }
