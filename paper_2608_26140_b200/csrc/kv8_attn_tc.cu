@@ -32,9 +32,56 @@ static_assert(kTables * sizeof(KeyTable) + 256 <= kResL && kResL + 256 * 4 <= TT
 template <int SETS>
 constexpr int tt_smem() { return (SETS + 4) * TT_TILE + TT_TAIL + TT_SLACK; }
 template <int SETS>
-constexpr bool tt_res_fits() { return SETS * 128 * 132 * 4 <= (SETS + 4) * TT_TILE && 128 * 132 * 4 <= (SETS + 2) * TT_TILE; }
+constexpr bool tt_res_fits() {           // the sums' weights behind the results; the first row tile's results off V
+    return SETS * 128 * (132 + 8) * 4 <= (SETS + 4) * TT_TILE && 128 * 132 * 4 <= (SETS + 2) * TT_TILE;
+}
 static_assert(tt_res_fits<1>() && tt_res_fits<2>());
 static_assert(tt_smem<1>() >= kAloneBytes && tt_smem<2>() <= 227 * 1024);
+
+// The CTAs of a cluster add their results up, each for a share of the rows, in the order of their keys.  A function of its own: what
+// it needs should not take registers from the loops before it.  (Its code runs once and comes from L2, so there is little of it.)
+template <int SETS>
+__device__ __noinline__ void tc_sum(unsigned char* base, unsigned char* tail, void* o, float* lse, int n, int n_heads, int G, int cs) {
+    const float* res = reinterpret_cast<const float*>(base);                                // [row][132]
+    const float* res_l = reinterpret_cast<const float*>(tail + kResL);
+    float* weight = reinterpret_cast<float*>(base + SETS * 128 * 132 * 4);                  // [row][8]: of a CTA's part in the sum
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, n_kv = n_heads / G, row0 = blockIdx.y * SETS * 128;
+    const int rows = min(n * G - row0, SETS * 128), rank = (int)cluster_ctarank();
+    const int mine = rows > rank ? (rows - rank + cs - 1) / cs : 0;                         // rows rank, rank + cs, ..
+    const int64_t first = (int64_t)(blockIdx.z / n_kv) * n * n_heads + blockIdx.z % n_kv * G;
+    cluster_sync_all();                                   // (one that gave up takes part as well: the call reports it)
+    for (int i = tid; i < mine * 8; i += TT_THREADS) {    // a whole group of eight lanes, or none of it
+        const int row = rank + (i >> 3) * cs, part = i & 7;
+        const float x = part < cs ? ld_peer(mapa_u32(smem_u32(res_l + row), part)) : -INFINITY;
+        const uint32_t eight = 0xFFu << (lane & 24);
+        float mx = x;
+#pragma unroll
+        for (int k = 4; k > 0; k >>= 1) mx = fmaxf(mx, __shfl_xor_sync(eight, mx, k));
+        const float f = x == -INFINITY ? 0.f : ex2(x - mx);                                 // (a NaN comes through)
+        float den = f;
+#pragma unroll
+        for (int k = 4; k > 0; k >>= 1) den += __shfl_xor_sync(eight, den, k);
+        weight[i] = den == 0.f ? 0.f : f / den;
+        const int r = row0 + row;
+        if (part == 0 && lse) lse[first + (int64_t)(r / G) * n_heads + r % G] = den == 0.f ? -INFINITY : (mx + log2f(den)) * 0.6931471805599453f;
+    }
+    __syncthreads();
+    for (int i = warp; i < mine; i += TT_THREADS / 32) {
+        const int row = rank + i * cs, r = row0 + row;
+        const uint32_t at = smem_u32(res + row * 132 + lane * 4);
+        float4 w[8], v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int p = 0; p < 8; ++p) w[p] = p < cs ? ld_peer4(mapa_u32(at, p)) : v;
+#pragma unroll
+        for (int p = 0; p < 8; ++p) {
+            const float f = weight[i * 8 + p];
+            v.x = fmaf(f, w[p].x, v.x); v.y = fmaf(f, w[p].y, v.y); v.z = fmaf(f, w[p].z, v.z); v.w = fmaf(f, w[p].w, v.w);
+        }
+        *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(o) + (first + (int64_t)(r / G) * n_heads + r % G) * 128 + lane * 4) =
+            make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
+    }
+    cluster_sync_all();                                   // nobody leaves while its results are read
+}
 
 template <int FMT, int SETS>
 __global__ void __launch_bounds__(TT_THREADS, 1) kv8_attn_tc_kernel(const Kv8AttnArgs a) {
@@ -413,31 +460,7 @@ __global__ void __launch_bounds__(TT_THREADS, 1) kv8_attn_tc_kernel(const Kv8Att
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(SETS * 256));
     }
     if (a.splits == 1) return;
-    // ---------------- the CTAs of a cluster add their results up, each for a share of the rows, in the order of their keys ----------------
-    cluster_sync_all();                                   // (one that gave up takes part as well: the call reports it)
-    const int rows = min(R - row0, SETS * 128), cs = a.splits;
-    const uint32_t res_at = smem_u32(res), res_l_at = smem_u32(res_l);
-    for (int n = (int)cluster_ctarank() + warp * cs; n < rows; n += cs * (TT_THREADS / 32)) {
-        float x[8];
-        float4 w[8];
-#pragma unroll
-        for (int p = 0; p < 8; ++p) {
-            x[p] = -INFINITY;
-            if (p < cs) {
-                x[p] = ld_peer(mapa_u32(res_l_at + n * 4, p));
-                w[p] = ld_peer4(mapa_u32(res_at + (n * 132 + lane * 4) * 4, p));
-            }
-        }
-        Sum s;
-#pragma unroll
-        for (int p = 0; p < 8; ++p) s.add(x[p], w[p]);
-        const float4 v = s.mean();
-        const int r = row0 + n;
-        const int64_t at = (int64_t)(b * (int64_t)a.n + r / G) * a.n_heads + kvh * G + r % G;
-        *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(a.o) + at * 128 + lane * 4) = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
-        if (a.lse && lane == 0) a.lse[at] = s.lse2() * 0.6931471805599453f;
-    }
-    cluster_sync_all();                                   // nobody leaves while its results are read
+    tc_sum<SETS>(base_ptr, tail, a.o, a.lse, a.n, a.n_heads, G, a.splits);
 }
 
 template <int FMT, int SETS>
