@@ -23,6 +23,7 @@ from paper_2608_26140_b200 import binding as ab
 from paper_2608_26140_b200 import workloads as wl
 
 from helpers import DEV, DeviceCase, assert_close_bf16
+from launched_kv8 import launched_kv8
 
 pytestmark = pytest.mark.gpu
 
@@ -386,11 +387,14 @@ def test_attention(heads, n, T, block, fmt):
     assert ctx.poll_status() == 0
 
 
-@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
-@pytest.mark.parametrize("heads,B,n,T,block,kernel", [
+MANY_ROWS = [
     ("mha32", 1, 33, 300, 64, "kv8_attn_rows"), ("gqa28", 1, 18, 8192, 64, "kv8_attn_rows"), ("mha32", 4, 33, 300, 64, "kv8_attn_tc"),
     ("mha32", 1, 100, 1600, 16, "kv8_attn_tc"), ("gqa28", 4, 18, 8200, 128, "kv8_attn_tc"), ("gqa28", 1, 64, 3000, 32, "kv8_attn_tc"),
-    ("mqa8", 16, 20, 2100, 64, "kv8_attn_tc"), ("mha32", 8, 200, 257, 32, "kv8_attn_tc")])
+    ("mqa8", 16, 20, 2100, 64, "kv8_attn_tc"), ("mha32", 8, 200, 257, 32, "kv8_attn_tc")]
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+@pytest.mark.parametrize("heads,B,n,T,block,kernel", MANY_ROWS)
 def test_attention_of_many_rows(heads, B, n, T, block, kernel, fmt):
     """Both kernels around the place where the one takes over from the other; keys split over two to eight CTAs of a cluster and
     over several clusters; a request whose length leaves splits without keys."""
@@ -399,12 +403,13 @@ def test_attention_of_many_rows(heads, B, n, T, block, kernel, fmt):
     q = queries(B, n, heads, T)
     check_attention(ctx, cache, vals, B, n, T, heads, q)
     check_attention(ctx, cache, vals, B, n, T, heads, q, lens=[T // 3] + [T - 1] * (B - 1))
-    with torch.profiler.profile(activities=[torch.profiler.ProfilerActivity.CUDA]) as prof:
-        ctx.kv8_attention(cache.c, B, T, q, torch.empty_like(q))
-        torch.cuda.synchronize()
-    names = [e.key for e in prof.key_averages() if "kv8" in e.key]
-    assert len(names) == 1 and kernel in names[0], names
     assert ctx.poll_status() == 0
+
+
+def test_which_kernel_takes_how_many_rows():
+    names = launched_kv8([(*HEADS[heads], B, n, T, block, "int8") for heads, B, n, T, block, _ in MANY_ROWS])
+    for case, name in zip(MANY_ROWS, names):
+        assert name.count("kernel") == 1 and case[-1] in name, (case, name)
 
 
 @pytest.mark.parametrize("fmt", ["e4m3", "int8"])
