@@ -23,7 +23,16 @@ constexpr int kTcSplits = 8;                              // a portable cluster
 // ns, measured: a key tile for one and for two row tiles, a CTA's start and end, the sum over a cluster
 constexpr int kTileNs1 = 2050, kTileNs2 = 2300, kCtaNs = 6000, kSumNs = 2000;
 
-constexpr int TT_THREADS = 416;                           // 12 warps of converters and softmax, one that issues
+// Warps: converters, from warp 8 on softmax, one that issues.  128 registers a thread allow four warps a scheduler.  Two row tiles: 7
+// converters and the issuing warp in front of 8 softmax warps (922 rows, 2560 keys, int8: 781 us; 3 converters 910, 4 and the issuing
+// one behind them 805).  One: 8, 4 and the issuing one behind them (100 rows, 8192 keys: 501 us; 7 converters 509, 11 511).
+template <int SETS>
+constexpr int kConverters = SETS == 2 ? 7 : 8;
+template <int SETS>
+constexpr int kIssuer = SETS == 2 ? 7 : 12;
+template <int SETS>
+constexpr int kThreads = SETS == 2 ? 512 : 416;
+constexpr int TT_SOFTMAX = 8;                             // the first softmax warp
 constexpr int TT_SLACK = 1024;
 constexpr int TT_TAIL = 2048;                             // tables, barriers; from kResL a float per row
 constexpr int kResL = 1024;
@@ -50,7 +59,7 @@ __device__ __noinline__ void tc_sum(unsigned char* base, unsigned char* tail, vo
     const int mine = rows > rank ? (rows - rank + cs - 1) / cs : 0;                         // rows rank, rank + cs, ..
     const int64_t first = (int64_t)(blockIdx.z / n_kv) * n * n_heads + blockIdx.z % n_kv * G;
     cluster_sync_all();                                   // (one that gave up takes part as well: the call reports it)
-    for (int i = tid; i < mine * 8; i += TT_THREADS) {    // a whole group of eight lanes, or none of it
+    for (int i = tid; i < mine * 8; i += kThreads<SETS>) {    // a whole group of eight lanes, or none of it
         const int row = rank + (i >> 3) * cs, part = i & 7;
         const float x = part < cs ? ld_peer(mapa_u32(smem_u32(res_l + row), part)) : -INFINITY;
         const uint32_t eight = 0xFFu << (lane & 24);
@@ -66,7 +75,7 @@ __device__ __noinline__ void tc_sum(unsigned char* base, unsigned char* tail, vo
         if (part == 0 && lse) lse[first + (int64_t)(r / G) * n_heads + r % G] = den == 0.f ? -INFINITY : (mx + log2f(den)) * 0.6931471805599453f;
     }
     __syncthreads();
-    for (int i = warp; i < mine; i += TT_THREADS / 32) {
+    for (int i = warp; i < mine; i += kThreads<SETS> / 32) {
         const int row = rank + i * cs, r = row0 + row;
         const uint32_t at = smem_u32(res + row * 132 + lane * 4);
         float4 w[8], v = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -84,11 +93,11 @@ __device__ __noinline__ void tc_sum(unsigned char* base, unsigned char* tail, vo
 }
 
 template <int FMT, int SETS>
-__global__ void __launch_bounds__(TT_THREADS, 1) kv8_attn_tc_kernel(const Kv8AttnArgs a) {
-    constexpr int CW = SETS == 2 ? 4 : 8;                 // converter warps
+__global__ void __launch_bounds__(kThreads<SETS>, 1) kv8_attn_tc_kernel(const Kv8AttnArgs a) {
+    constexpr int CW = kConverters<SETS>, ISSUER = kIssuer<SETS>;
     // Parts of a row tile's S, each a product of its own.  Alone, a row tile leaves the tensor core idle while its softmax runs, and
     // halves let the next S be made meanwhile (100 rows, 8192 keys, 512 pairs: 510 us, whole 535); two fill each other's gaps, and
-    // products of 64 keys, which read Q twice as often from shared memory, only cost (922 rows, 2560 keys: 829 us, whole 806).
+    // products of 64 keys, which read Q twice as often from shared memory, only cost (922 rows, 2560 keys: 829 us, whole 805).
     constexpr int S_PARTS = SETS == 2 ? 1 : 2;
     constexpr int CT = CW * 32;
     extern __shared__ unsigned char smem_raw[];
@@ -124,7 +133,7 @@ __global__ void __launch_bounds__(TT_THREADS, 1) kv8_attn_tc_kernel(const Kv8Att
         *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == 12) {
+    if (warp == ISSUER) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
                      ::"r"(smem_u32(const_cast<uint32_t*>(tmem_slot))), "r"(SETS * 256) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
@@ -206,7 +215,7 @@ __global__ void __launch_bounds__(TT_THREADS, 1) kv8_attn_tc_kernel(const Kv8Att
             if (lane == 0) mbar_arrive(bar(5 + s));
             if (j + 1 < n_tiles) vr.load(vb, key_lo + (j + 1) * 128, key_hi, tid);
         }
-    } else if (warp == 12) {
+    } else if (warp == ISSUER) {
         // ---------------- MMA issuer: the whole warp runs the loop, one lane issues ----------------
         const uint32_t idesc = (1u << 4) | ((uint32_t)(128 >> 4) << 24);                 // f16 x f16 -> fp32, 128 rows
         const uint32_t idesc_s = idesc | ((uint32_t)(128 / S_PARTS >> 3) << 17);         // keys of a part
@@ -263,9 +272,9 @@ __global__ void __launch_bounds__(TT_THREADS, 1) kv8_attn_tc_kernel(const Kv8Att
             }
             __syncwarp();
         }
-    } else if (warp >= CW && warp < CW + 4 * n_sets) {
+    } else if (warp >= TT_SOFTMAX && warp < TT_SOFTMAX + 4 * n_sets) {
         // ---------------- softmax: one thread per query row ----------------
-        const int t = (warp - CW) >> 2, q4 = warp & 3;    // the warp's TMEM lane quarter
+        const int t = (warp - TT_SOFTMAX) >> 2, q4 = warp & 3;    // the warp's TMEM lane quarter
         const int row = q4 * 32 + lane, r = row0 + t * 128 + row;
         const uint32_t lane_off = (uint32_t)(q4 * 32) << 16;
         const uint32_t tS = tmem_base + t * 128 + lane_off, tO = tmem_base + O_COL + t * 128 + lane_off;
@@ -455,7 +464,7 @@ __global__ void __launch_bounds__(TT_THREADS, 1) kv8_attn_tc_kernel(const Kv8Att
         }
         __syncthreads();
     }
-    if (warp == 12) {
+    if (warp == ISSUER) {
         tc_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(SETS * 256));
     }
@@ -467,7 +476,7 @@ template <int FMT, int SETS>
 void tc_config(cudaLaunchConfig_t& cfg, cudaLaunchAttribute (&at)[2], dim3 grid, cudaStream_t stream) {
     cfg = cudaLaunchConfig_t{};
     cfg.gridDim = grid;
-    cfg.blockDim = dim3(TT_THREADS);
+    cfg.blockDim = dim3(kThreads<SETS>);
     cfg.dynamicSmemBytes = tt_smem<SETS>();
     cfg.stream = stream;
     at[0].id = cudaLaunchAttributeClusterDimension;

@@ -149,13 +149,14 @@ __device__ __forceinline__ void write_table(KeyTable& t, uint32_t meta, int lane
 // 16-byte pieces of a [128 keys][128 codes] tile, piece i of a thread: row i CT / 8 + tid / 8, codes 16 (tid % 8) ..
 template <int CT>
 struct TilePieces {
-    static constexpr int CH = 1024 / CT;
+    static constexpr int CH = (1024 + CT - 1) / CT;
+    static __device__ __forceinline__ bool in_tile(int row) { return 1024 % CT == 0 || row < 128; }
     uint4 x[CH];
     __device__ __forceinline__ void load(const uint8_t* from, int key0, int key_hi, int tid) {
 #pragma unroll
         for (int i = 0; i < CH; ++i) {
-            const int key = key0 + i * (CT / 8) + (tid >> 3);
-            x[i] = key < key_hi ? ld_codes(from + (int64_t)key * 128 + (tid & 7) * 16) : make_uint4(0u, 0u, 0u, 0u);
+            const int row = i * (CT / 8) + (tid >> 3), key = key0 + row;
+            x[i] = key < key_hi && in_tile(row) ? ld_codes(from + (int64_t)key * 128 + (tid & 7) * 16) : make_uint4(0u, 0u, 0u, 0u);
         }
     }
     // as f16 into a 128-byte-swizzled tile; rows whose bit is not set become zeros
@@ -165,9 +166,11 @@ struct TilePieces {
 #pragma unroll
         for (int i = 0; i < CH; ++i) {
             const int row = i * (CT / 8) + (tid >> 3);
+            if (!in_tile(row)) break;
             uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w}, f[8];
             if (!all) {
-                const bool on = (rows[i * (CT / 8) >> 5] >> (row & 31)) & 1u;
+                const uint32_t lo = row & 32 ? rows[1] : rows[0], hi = row & 32 ? rows[3] : rows[2];
+                const bool on = ((row & 64 ? hi : lo) >> (row & 31)) & 1u;
 #pragma unroll
                 for (int k = 0; k < 4; ++k) w[k] = on ? w[k] : 0u;
             }
