@@ -20,8 +20,12 @@ namespace acache {
 namespace {
 
 constexpr int kTcSplits = 8;                              // a portable cluster
-// ns, measured: a key tile for one and for two row tiles, a CTA's start and end, the sum over a cluster
-constexpr int kTileNs1 = 2050, kTileNs2 = 2300, kCtaNs = 6000, kSumNs = 2000;
+// ns, measured, for one and for two row tiles: a key tile, the sum over a cluster; a CTA's start and end
+template <int SETS>
+constexpr int kTileNs = SETS == 2 ? 2300 : 2050;
+template <int SETS>
+constexpr int kSumNs = SETS == 2 ? 6000 : 2000;
+constexpr int kCtaNs = 6000;
 
 // Warps: converters, from warp 8 on softmax, one that issues.  128 registers a thread allow four warps a scheduler.  Two row tiles: 7
 // converters and the issuing warp in front of 8 softmax warps (922 rows, 2560 keys, int8: 781 us; 3 converters 910, 4 and the issuing
@@ -505,7 +509,8 @@ int tc_clusters(int n) {
     return fit[n];
 }
 struct TcPlan { int per, splits; int64_t cost; };         // key tiles of a split, splits, ns
-// The number of splits with which the rounds of CTAs take least.
+// The number of splits with which the rounds of CTAs take least.  1639 rows of 32 heads, 8288 keys (224 items): whole 317 us, in
+// thirds 325, in quarters 370; 100 rows, 8192 keys (32 items): whole 78 us, in quarters 42, in eighths (15 at a time) 75.
 template <int FMT, int SETS>
 TcPlan tc_plan(const Kv8AttnArgs& a) {
     const int R = a.n * (a.n_heads / a.n_kv_heads), tiles = (R + SETS * 128 - 1) / (SETS * 128);
@@ -514,7 +519,7 @@ TcPlan tc_plan(const Kv8AttnArgs& a) {
     TcPlan best{key_tiles, 1, INT64_MAX};
     for (int s = 1; s <= kTcSplits && s <= key_tiles; ++s) {
         const int per = (key_tiles + s - 1) / s, n = (key_tiles + per - 1) / per, fit = tc_clusters<FMT, SETS>(n);
-        const int64_t cost = (items + fit - 1) / fit * (per * (SETS == 2 ? kTileNs2 : kTileNs1) + kCtaNs + (n > 1 ? kSumNs : 0));
+        const int64_t cost = (items + fit - 1) / fit * (per * kTileNs<SETS> + kCtaNs + (n > 1 ? kSumNs<SETS> : 0));
         if (cost < best.cost) best = TcPlan{per, n, cost};
     }
     return best;
