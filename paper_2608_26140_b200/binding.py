@@ -193,8 +193,8 @@ def _ptr(t) -> Optional[int]:
 
 
 def _check_tensor(t, dtype, shape):
-    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
-        raise ValueError(f"a tensor {tuple(t.shape)} of {t.dtype} where contiguous {shape} of {dtype} is wanted")
+    if t.shape != shape or t.dtype is not dtype or not t.is_cuda or not t.is_contiguous():
+        raise ValueError(f"a tensor {tuple(t.shape)} of {t.dtype} on {t.device} where contiguous {tuple(shape)} of {dtype} on a GPU is wanted")
 
 
 def _stream() -> int:
@@ -212,6 +212,7 @@ class Context:
         self.lib = load_library()
         self.desc = ModelDesc(hidden, n_heads, n_kv_heads, head_dim, ffn, rms_eps, int(bool(qkv_bias)),
                               max_batch, max_ctx, max_affix, max_rows, max_masked, max_vocab, max_block)
+        self.heads = (n_heads, n_kv_heads, head_dim)
         h = C.c_void_p()
         st = self.lib.acache_create(C.byref(self.desc), C.byref(h))
         if st != OK:
@@ -357,61 +358,64 @@ class Context:
                                                int(x_is_compact), float(ratio), int(flags), _ptr(scores),
                                                _ptr(anchor_idx), _ptr(y), _stream()))
 
+    # A call of the three below takes 6-8 us, more than many of their kernels, most of it here: tensors are asked for each property once.
     def kv8_write(self, cache: KV8, batch, ctx_len, k_rows, v_rows, start=0, pos=None):
         """Rows [B, n, Hkv, d] (bf16; requests may lie further apart) to positions start .. or pos [B, n] (int32)."""
-        stride = self._check_rows(k_rows, batch, pos)
-        if self._check_rows(v_rows, batch, pos) != stride or v_rows.shape != k_rows.shape:
+        shape, stride = self._rows(k_rows, batch, pos)
+        if self._rows(v_rows, batch, None) != (shape, stride):
             raise ValueError("k_rows and v_rows differ in shape or stride")
-        self._check(self.lib.acache_kv8_write(self.h, C.byref(cache), batch, ctx_len, _ptr(k_rows), _ptr(v_rows), stride,
-                                              k_rows.shape[1], _ptr(pos), start, _stream()))
+        self._check(self.lib.acache_kv8_write(self.h, C.byref(cache), batch, ctx_len, k_rows.data_ptr(), v_rows.data_ptr(), stride,
+                                              shape[1], _ptr(pos), start, _stream()))
 
     def kv8_read(self, cache: KV8, batch, ctx_len, k_out, v_out, start=0, pos=None):
         """Rows at positions start .. or pos [B, n] into k_out, v_out [B, n, Hkv, d] (contiguous; either may be None)."""
-        n = None
-        for t in (k_out, v_out):
-            if t is not None:
-                self._check_rows(t, batch, pos)
-                if not t.is_contiguous() or n not in (None, t.shape[1]):
-                    raise ValueError("k_out and v_out are contiguous and of one length")
-                n = t.shape[1]
-        if n is None:
+        one = v_out if k_out is None else k_out
+        if one is None:
             raise AcacheError(ERR_INVALID_ARG, "neither k_out nor v_out is given")
-        self._check(self.lib.acache_kv8_read(self.h, C.byref(cache), batch, ctx_len, _ptr(k_out), _ptr(v_out), n, _ptr(pos),
-                                             start, _stream()))
+        shape, _ = self._rows(one, batch, pos)
+        if not one.is_contiguous():
+            raise ValueError("k_out and v_out are contiguous")
+        if one is not v_out and v_out is not None:
+            _check_tensor(v_out, one.dtype, shape)
+        self._check(self.lib.acache_kv8_read(self.h, C.byref(cache), batch, ctx_len, _ptr(k_out), _ptr(v_out), shape[1], _ptr(pos), start,
+                                             _stream()))
 
     def kv8_attention(self, cache: KV8, batch, ctx_len, q, o, lse=None, lens=None, key_drop=None):
         """q, o: bf16 [B, n, H, d]; lse: fp32 [B, n, H]; lens: int32 [B]; key_drop: int32 [B, ceil(ctx_len / 32)] (pack_key_drop)."""
         import torch
-        B, n, H, d = q.shape
-        if B != batch or H != self.desc.n_heads or d != self.desc.head_dim:
-            raise ValueError(f"q {tuple(q.shape)} is not [batch, n, H, d]")
-        _check_tensor(q, torch.bfloat16, (B, n, H, d))
-        _check_tensor(o, torch.bfloat16, (B, n, H, d))
+        shape = q.shape
+        B, n, H, d = shape
+        if B != batch or H != self.heads[0] or d != self.heads[2]:
+            raise ValueError(f"q {tuple(shape)} is not [batch, n, H, d]")
+        _check_tensor(q, torch.bfloat16, shape)
+        _check_tensor(o, torch.bfloat16, shape)
         if lse is not None:
-            _check_tensor(lse, torch.float32, (B, n, H))
+            _check_tensor(lse, torch.float32, shape[:3])
         if lens is not None:
             _check_tensor(lens, torch.int32, (B,))
         if key_drop is not None:
             _check_tensor(key_drop, torch.int32, (B, -(-ctx_len // 32)))
-        self._check(self.lib.acache_kv8_attention(self.h, C.byref(cache), batch, n, ctx_len, _ptr(q), _ptr(lens), _ptr(key_drop),
-                                                  _ptr(o), _ptr(lse), _stream()))
+        self._check(self.lib.acache_kv8_attention(self.h, C.byref(cache), batch, n, ctx_len, q.data_ptr(), _ptr(lens), _ptr(key_drop),
+                                                  o.data_ptr(), _ptr(lse), _stream()))
 
     def layer_step_kv8(self, w: LayerWeights, req: Request, cache: KV8, x, x_is_compact, ratio, flags, scores, anchor_idx, y):
         """The layer-step on an 8-bit cache."""
         self._check(self.lib.acache_layer_step_kv8(self.h, C.byref(w), C.byref(req), C.byref(cache), _ptr(x), int(x_is_compact),
                                                    float(ratio), int(flags), _ptr(scores), _ptr(anchor_idx), _ptr(y), _stream()))
 
-    def _check_rows(self, t, batch, pos) -> int:
-        """Elements between the requests of rows [B, n, Hkv, d]."""
+    def _rows(self, t, batch, pos):
+        """Shape of rows [B, n, Hkv, d], and elements between the requests."""
         import torch
-        B, n, hkv, d = t.shape
-        if t.dtype != torch.bfloat16 or (B, hkv, d) != (batch, self.desc.n_kv_heads, self.desc.head_dim):
-            raise ValueError(f"rows {tuple(t.shape)} of {t.dtype} are not bf16 [batch, n, Hkv, d]")
-        if n and t.stride()[1:] != (hkv * d, d, 1):
+        shape = t.shape
+        B, n, hkv, d = shape
+        if B != batch or hkv != self.heads[1] or d != self.heads[2] or t.dtype is not torch.bfloat16 or not t.is_cuda:
+            raise ValueError(f"rows {tuple(shape)} of {t.dtype} on {t.device} are not bf16 [batch, n, Hkv, d] on a GPU")
+        stride = t.stride()
+        if n and stride[1:] != (hkv * d, d, 1):
             raise ValueError("the rows of a request are contiguous")
         if pos is not None:
             _check_tensor(pos, torch.int32, (B, n))
-        return t.stride(0) if B > 1 else n * hkv * d
+        return shape, stride[0] if B > 1 else n * hkv * d
 
     def predict_commit(self, h, h_rows, block_rows, batch, n_blk, final_norm_g, w_lm, vocab, threshold, token,
                        confidence, commit):

@@ -539,12 +539,12 @@ void rows_config(cudaLaunchConfig_t& cfg, cudaLaunchAttribute (&at)[2], dim3 gri
     cfg.blockDim = dim3(RW * 32);
     cfg.dynamicSmemBytes = RowsLayout<D, NT>::SMEM;
     cfg.stream = stream;
-    at[0].id = cudaLaunchAttributeClusterDimension;
-    at[0].val.clusterDim.x = cluster; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
-    at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at[1].val.programmaticStreamSerializationAllowed = 1;
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = cluster; at[1].val.clusterDim.y = 1; at[1].val.clusterDim.z = 1;
     cfg.attrs = at;
-    cfg.numAttrs = 2;
+    cfg.numAttrs = cluster > 1 ? 2 : 1;
 }
 // clusters of 2^c CTAs that the GPU runs at a time: fewer than the places for CTAs make up, as a cluster stays in one group of SMs
 template <int D, int NT, int FMT>
@@ -556,6 +556,7 @@ int rows_clusters(int c) {
             cudaLaunchConfig_t cfg;
             cudaLaunchAttribute at[2];
             rows_config<D, NT, FMT>(cfg, at, dim3(1 << i), 1 << i, nullptr);
+            cfg.attrs = at + 1;                           // the cluster alone
             cfg.numAttrs = 1;
             int most = 0;
             if (cudaOccupancyMaxActiveClusters(&most, kv8_attn_rows_kernel<D, NT, FMT>, &cfg) != cudaSuccess) most = 0;

@@ -483,12 +483,12 @@ void tc_config(cudaLaunchConfig_t& cfg, cudaLaunchAttribute (&at)[2], dim3 grid,
     cfg.blockDim = dim3(kThreads<SETS>);
     cfg.dynamicSmemBytes = tt_smem<SETS>();
     cfg.stream = stream;
-    at[0].id = cudaLaunchAttributeClusterDimension;
-    at[0].val.clusterDim.x = grid.x; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
-    at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at[1].val.programmaticStreamSerializationAllowed = 1;
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = grid.x; at[1].val.clusterDim.y = 1; at[1].val.clusterDim.z = 1;
     cfg.attrs = at;
-    cfg.numAttrs = 2;
+    cfg.numAttrs = grid.x > 1 ? 2 : 1;
 }
 // clusters of n CTAs that the GPU runs at a time (fewer than SMs / n: a cluster stays in one group of SMs)
 template <int FMT, int SETS>
@@ -500,6 +500,7 @@ int tc_clusters(int n) {
             cudaLaunchConfig_t cfg;
             cudaLaunchAttribute at[2];
             tc_config<FMT, SETS>(cfg, at, dim3(s), nullptr);
+            cfg.attrs = at + 1;                           // the cluster alone
             cfg.numAttrs = 1;
             int most = 0;
             if (cudaOccupancyMaxActiveClusters(&most, kv8_attn_tc_kernel<FMT, SETS>, &cfg) != cudaSuccess) most = 0;

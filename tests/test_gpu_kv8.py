@@ -751,3 +751,21 @@ def test_refusals():
     with pytest.raises(ValueError):
         ab.Context.kv8(keep[0].transpose(1, 2), keep[1], keep[2], keep[3], 64, 0)
     assert ctx.launch_count() == launched and ctx.poll_status() == 0
+
+
+def test_tensors_of_the_host_are_refused():
+    heads, B, T, n = "gqa28", 1, 64, 2
+    H, hkv, d = HEADS[heads]
+    ctx = context(heads, B, T)
+    keep, c = ctx.new_kv8(B, T, 16, "e4m3")
+    launched = ctx.launch_count()
+    rows, q = torch.zeros((B, n, hkv, d), dtype=torch.bfloat16, device=DEV), torch.zeros((B, n, H, d), dtype=torch.bfloat16, device=DEV)
+    pos, lens = torch.zeros((B, n), dtype=torch.int32, device=DEV), torch.zeros((B,), dtype=torch.int32, device=DEV)
+    for call in (lambda: ctx.kv8_write(c, B, T, rows.cpu(), rows), lambda: ctx.kv8_write(c, B, T, rows, rows.cpu()),
+                 lambda: ctx.kv8_write(c, B, T, rows, rows, pos=pos.cpu()), lambda: ctx.kv8_read(c, B, T, rows, rows.cpu()),
+                 lambda: ctx.kv8_read(c, B, T, rows.cpu(), None), lambda: ctx.kv8_read(c, B, T, None, rows, pos=pos.cpu()),
+                 lambda: ctx.kv8_attention(c, B, T, q.cpu(), q), lambda: ctx.kv8_attention(c, B, T, q, q.cpu()),
+                 lambda: ctx.kv8_attention(c, B, T, q, q, lens=lens.cpu())):
+        with pytest.raises(ValueError):
+            call()
+    assert ctx.launch_count() == launched
