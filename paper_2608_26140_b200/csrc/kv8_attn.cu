@@ -39,7 +39,9 @@ constexpr int RW = 4;                    // warps of a CTA
 constexpr int MT = 2;                    // 16-key tiles of a warp's step
 constexpr int RSTEP = 16 * MT;
 constexpr int RSTAGES = 3;
-constexpr int kMinSplit = 256;           // keys
+// Fewest keys of a split.  With 8 rows a CTA one cluster takes 128: one row, 1664 keys 6.7 us in 8 splits, 8.3 in 4; 32 rows and sums over
+// clusters are worse off (32 rows, 1000 keys: 13.9 and 11.5 us).
+constexpr int kMinSplit = 256, kMinSplitNarrow = 128;
 constexpr int kSlots = 2;                // CTAs of an SM
 // tenths of a nanosecond that a key takes a CTA
 template <int D, int NT>
@@ -567,9 +569,9 @@ int rows_clusters(int c) {
 }
 struct RowsPlan { int cluster, splits; int64_t cost; };   // cost: ns
 // Key splits, in clusters that add their results up; splits only where all their CTAs run at a time.  The estimate, with what was
-// measured for 32 rows of 128: a CTA takes 4 us and 17.5 ns a key (9 us and the same, where two share an SM), the sum over a
-// cluster 2 us, the sum over clusters 2 us and 0.8 us for every eight of them and every value of a thread.  More CTAs than places
-// take as many times longer, and a quarter for the last ones.  One sequence of 65536 keys, 4 KV heads, 35 rows: 51 us in 18
+// measured for 32 rows of 128 (and for fewer): a CTA takes 4 us and 17.5 (13) ns a key, where two share an SM 9 (5.2) us and the same;
+// the sum over a cluster 5 (1.5) us, 1.5 us where two share an SM; the sum over clusters 2 us and 0.8 us for every eight of them and
+// every value of a thread.  More CTAs than places take as many times longer, and a quarter for the last ones.  One sequence of 65536 keys, 4 KV heads, 35 rows: 51 us in 18
 // clusters of 2, 72 us in 4 of 8 (which do not all run at a time); 512 items of 8192 keys: 166 us whole, 180 us in halves.
 template <int D, int NT, int FMT>
 RowsPlan rows_plan(const Kv8AttnArgs& a) {
@@ -577,16 +579,17 @@ RowsPlan rows_plan(const Kv8AttnArgs& a) {
     const int R = a.n * (a.n_heads / a.n_kv_heads);
     const int64_t items = (int64_t)((R + L::ROWS - 1) / L::ROWS) * a.batch * a.n_kv_heads;
     RowsPlan best{1, 1, INT64_MAX};
-    const int most = std::max(1, a.ctx_len / kMinSplit);
-    for (int c = 0; c < 4 && 1 << c <= most; ++c) {
+    const int most = a.ctx_len / kMinSplit, most_one = a.ctx_len / (NT == 1 ? kMinSplitNarrow : kMinSplit);
+    for (int c = 0; c < 4 && (c == 0 || 1 << c <= most_one); ++c) {
         const int fit = rows_clusters<D, NT, FMT>(c);
         if (c > 0 && items > fit) break;
-        const int top = c == 0 ? 1 : (int)std::min<int64_t>(fit / items, most >> c);
+        const int top = c == 0 ? 1 : std::max(1, (int)std::min<int64_t>(fit / items, most >> c));
         for (int k = 1;; k = top) {                       // one cluster an item, or as many as there is room for
             const int splits = k << c, keys = (a.ctx_len + splits - 1) / splits;
-            int64_t cost = (NT == 4 && items * splits > 148 ? 9000 : 4000) + (int64_t)keys * kKeyNs<D, NT> / 10;
+            const bool two = items * splits > 148;
+            int64_t cost = (!two ? 4000 : NT == 4 ? 9000 : 5200) + (int64_t)keys * kKeyNs<D, NT> / 10;
             if (items > fit) cost = cost * (items * 4 + fit) / (fit * 4);
-            if (c > 0) cost += 2000;
+            if (c > 0) cost += NT == 4 && !two ? 5000 : 1500;
             if (k > 1) cost += 2000 + 800 * ((L::ROWS * D / (4 * RW * 32) + (1 << c) - 1) >> c) * ((k + 7) / 8);
             if (cost < best.cost) best = RowsPlan{1 << c, splits, cost};
             if (k == top) break;
