@@ -571,8 +571,9 @@ struct RowsPlan { int cluster, splits; int64_t cost; };   // cost: ns
 // Key splits, in clusters that add their results up; splits only where all their CTAs run at a time.  The estimate, with what was
 // measured for 32 rows of 128 (and for fewer): a CTA takes 4 us and 17.5 (13) ns a key, where two share an SM 9 (5.2) us and the same;
 // the sum over a cluster 5 (1.5) us, 1.5 us where two share an SM; the sum over clusters 2 us and 0.8 us for every eight of them and
-// every value of a thread.  More CTAs than places take as many times longer, and a quarter for the last ones.  One sequence of 65536 keys, 4 KV heads, 35 rows: 51 us in 18
-// clusters of 2, 72 us in 4 of 8 (which do not all run at a time); 512 items of 8192 keys: 166 us whole, 180 us in halves.
+// every value of a thread.  More CTAs than places take as many times longer, and a quarter for the last ones.  One
+// sequence of 65536 keys, 4 KV heads, 35 rows (8 items): 49 us in 4 clusters of 8 each, 72 us in 9 of 4 (72, where 71 run at a time);
+// 512 items of 8192 keys: 166 us whole, 180 us in halves.
 template <int D, int NT, int FMT>
 RowsPlan rows_plan(const Kv8AttnArgs& a) {
     using L = RowsLayout<D, NT>;
@@ -609,15 +610,17 @@ int rows_launch(Kv8AttnArgs a, const RowsPlan& plan, cudaStream_t stream) {
     return cudaLaunchKernelEx(&cfg, kv8_attn_rows_kernel<D, NT, FMT>, a) == cudaSuccess ? 1 : -1;
 }
 // Rows of a CTA: up to 32, so that a key is converted once for as many of them as there are; fewer where there are too few CTAs to
-// go round (4 KV heads, 35 rows, 1536 keys: 8.6 us with 8 rows a CTA, 15 us with 32; the same times 16 requests: 27 and 26 us).
+// go round.  us with 8, 16 and 32 rows a CTA: 4 KV heads, 28 rows, 1536 keys 8.3, 10.3, 14.3; 16 times as many requests 20.8, 17.5,
+// 17.9, and 8192 keys 84, 56, 49; 32 KV heads, 1536 keys, 32 rows 12.8, 12.1, 15.6, 16 rows 9.8, 10.8.
 // More than 32 rows: the tensor-memory kernel, where its plan takes less than this one's.  16 sequences, 32 KV heads, 100 rows,
-// 8192 keys: 535 us there, 953 us here; one sequence of 300 keys: 12.3 and 10.0 us.  Up to 32 rows this one is always ahead.
+// 8192 keys: 501 us there, 953 us here; one sequence of 300 keys: 12.3 and 10.0 us.  Up to 32 rows this one is always ahead.
 template <int D, int FMT>
 int rows_dispatch(const Kv8AttnArgs& a, cudaStream_t stream) {
     const int R = a.n * (a.n_heads / a.n_kv_heads);
     const int64_t pairs = (int64_t)a.batch * a.n_kv_heads, splits = std::max(1, a.ctx_len / kMinSplit);
     auto ctas = [&](int rows) { return (R + rows - 1) / rows * pairs * splits; };
-    const int nt = R <= 8 || ctas(16) < 148 ? 1 : R <= 16 || ctas(32) < 148 ? 2 : 4;
+    const int few = R > 32 ? 148 : 222;                   // (of more than 32 rows, the tensor-memory kernel takes some of those between)
+    const int nt = R <= 8 || ctas(16) < few ? 1 : R <= 16 || ctas(32) < few ? 2 : 4;
     if (nt == 1) return rows_launch<D, 1, FMT>(a, rows_plan<D, 1, FMT>(a), stream);
     if (nt == 2) return rows_launch<D, 2, FMT>(a, rows_plan<D, 2, FMT>(a), stream);
     const RowsPlan plan = rows_plan<D, 4, FMT>(a);
