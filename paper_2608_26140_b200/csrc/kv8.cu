@@ -29,7 +29,7 @@ __global__ void __launch_bounds__(kWriteThreads, 4) kv8_write_kernel(const Kv8Wr
     constexpr int RPP = UT / CPR;                       // rows of a pass: a thread's pieces are RPP rows apart
     __shared__ int row_of[LIST ? BLOCK : 1];            // row that serves a position, or -1
     __shared__ int2 write[LIST ? BLOCK : 1];            // of the k-th row to write: the row, its position
-    __shared__ int warp_max[2][2][kWriteThreads / 32];
+    __shared__ __align__(8) int warp_max[2][2][kWriteThreads / 32];
     pdl_wait();
     pdl_launch_dependents();
     const int tid = threadIdx.x, b = blockIdx.z;
@@ -64,8 +64,8 @@ __global__ void __launch_bounds__(kWriteThreads, 4) kv8_write_kernel(const Kv8Wr
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const int i = i0 + j * kWriteThreads;
-                if (i < a.n && p[j] >= t0 && p[j] < t0 + here) atomicMax(&row_of[p[j] - t0], i);
-                bad |= p[j] < 0 || p[j] >= a.ctx_len;
+                if (i < a.n && (unsigned)(p[j] - t0) < (unsigned)here) atomicMax(&row_of[p[j] - t0], i);
+                bad |= (unsigned)p[j] >= (unsigned)a.ctx_len;
             }
         }
         if (bad && !a.by_row && blockIdx.x == 0 && blockIdx.y == 0) atomicOr(a.status, kFlagBadIndex);
@@ -98,11 +98,12 @@ __global__ void __launch_bounds__(kWriteThreads, 4) kv8_write_kernel(const Kv8Wr
         const uint32_t lo = w & 0x7F80u, hi = w & 0x7F800000u;
         return (lo == 0x7F80u ? 0u : lo) | (hi == 0x7F800000u ? 0u : hi);
     };
-    // The largest over the unit's threads, of exponent fields; returned: over all the threads that come together here.
-    // turn: which of two places, so that one barrier does.
+    // The largest over the unit's threads, of exponent fields; returned: whether one is 255 among all the threads that come together
+    // here.  turn: which of two places, so that one barrier does.
     int turn = 0;
     auto unit_max = [&](auto& m) {
         constexpr int N = sizeof(m) / sizeof(m[0]);
+        int top = 0;
 #pragma unroll
         for (int p = 0; p < N; ++p) {
             int f = (int)(max(m[p] & 0xFFFFu, m[p] >> 16) >> 7);
@@ -114,25 +115,23 @@ __global__ void __launch_bounds__(kWriteThreads, 4) kv8_write_kernel(const Kv8Wr
                 if (UT > 32 && (tid & 31) == 0) warp_max[turn][p][tid >> 5] = f;
             }
             m[p] = f;
+            top = max(top, f);
         }
-        int top = 0;
         if constexpr (UT > 32) {
-            __syncthreads();
+            const bool any = __syncthreads_or(top == 255);
 #pragma unroll
             for (int p = 0; p < N; ++p)
 #pragma unroll
-                for (int w = 0; w < kWriteThreads / 32; ++w) {
-                    const int f = warp_max[turn][p][w];
-                    if (w / (UT / 32) == u) m[p] = max((int)m[p], f);
-                    top = max(top, f);
+                for (int w = 0; w < UT / 32; w += 2) {
+                    const int2 f = *reinterpret_cast<const int2*>(&warp_max[turn][p][u * (UT / 32) + w]);
+                    m[p] = max((int)m[p], max(f.x, f.y));
                 }
             turn ^= 1;
+            return any;
         } else {
-#pragma unroll
-            for (int p = 0; p < N; ++p) top = max(top, (int)m[p]);
             if constexpr (UT < 32) top = max(top, __shfl_xor_sync(0xffffffffu, top, UT));
+            return top == 255;
         }
-        return top;
     };
     // The units of this CTA, N of them at a time: one, or K and V of a head.
     auto run = [&](auto n_units) {
@@ -142,7 +141,6 @@ __global__ void __launch_bounds__(kWriteThreads, 4) kv8_write_kernel(const Kv8Wr
         while (v0 < all) {
             const int v = v0 + u;
             const bool active = v < all;
-            const int n_here = active ? n_written : 0;
             auto is_v = [&](int p) { return N == 2 ? p == 1 : v >= a.n_kv_heads; };
             const int h = !active ? 0 : N == 2 || v < a.n_kv_heads ? v : v - a.n_kv_heads;
             const int64_t exps_at = ((int64_t)(a.shared ? 0 : b) * a.n_kv_heads + h) * a.n_blocks + blk;
@@ -153,13 +151,11 @@ __global__ void __launch_bounds__(kWriteThreads, 4) kv8_write_kernel(const Kv8Wr
 #pragma unroll
             for (int i = 0; i < SLOTS; ++i) {
                 if (LIST && i * RPP >= n_written) break;
-                const int k = i * RPP + k0;
-                const int64_t at = rows_at + write_at(k < n_here ? k : 0).x * row_elems;
+                // (threads past the last row take it again: it changes no maximum)
+                const int64_t at = rows_at + write_at(min(i * RPP + k0, n_written - 1)).x * row_elems;
 #pragma unroll
-                for (int p = 0; p < N; ++p) {
-                    x[p][i] = make_uint4(0u, 0u, 0u, 0u);
-                    if (k < n_here) x[p][i] = __ldg(reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(is_v(p) ? a.v_rows : a.k_rows) + at));
-                }
+                for (int p = 0; p < N; ++p)
+                    x[p][i] = __ldg(reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(is_v(p) ? a.v_rows : a.k_rows) + at));
             }
             uint32_t field[N];
 #pragma unroll
@@ -173,11 +169,11 @@ __global__ void __launch_bounds__(kWriteThreads, 4) kv8_write_kernel(const Kv8Wr
 #pragma unroll
                 for (int p = 0; p < N; ++p) field[p] = __vmaxu2(field[p], largest(x[p][i], magnitude));
             }
-            const int top = unit_max(field);
+            const bool any_odd = unit_max(field);
             bool odd[N];                                 // a unit has a value that is not finite: the largest of the others counts
 #pragma unroll
             for (int p = 0; p < N; ++p) odd[p] = field[p] == 255;
-            if (top == 255) {
+            if (any_odd) {
 #pragma unroll
                 for (int p = 0; p < N; ++p) {
                     if (odd[p] && ut == 0) atomicOr(a.status, kFlagNonFinite);
