@@ -18,7 +18,7 @@ namespace acache {
 // in the list (the last of two that name a position wins): n loads per CTA from L2, no map and no second launch; the rows found
 // are packed, so that passes over the registers that a block's few rows leave empty are skipped.
 // 16 requests of 2560 tokens, 32 heads of 128: all rows (1007 MB) 148 us, 6.8 TB/s; 922 rows each at positions of a list, int8
-// (364 MB) 91 us: there 70 % of the issue slots are taken (search, packing, the sum of short loops), not DRAM.
+// (364 MB) 88 us: there 70 % of the issue slots are taken (search, packing, short loops), not DRAM.
 constexpr int kWriteThreads = 256;
 
 template <int D, int BLOCK, int FMT, bool LIST>
@@ -243,7 +243,7 @@ __global__ void __launch_bounds__(kWriteThreads, 4) kv8_write_kernel(const Kv8Wr
         }
     };
     // K and V of a head together where both fit a thread's registers: twice the loads in flight, half the barriers and searches
-    // (the 922 rows above: 91 us; 157 us one by one)
+    // (the 922 rows above, when this was measured: 91 us; 157 us one by one)
     if (LIST && 2 * n_written <= BLOCK) run(std::integral_constant<int, 2>{});
     else run(std::integral_constant<int, 1>{});
 }
