@@ -9,6 +9,9 @@
 //   one issuing warp   S = Q K^T and O += P V by tcgen05.mma 128 x 128 x 16, P read from tensor memory, V MN-major
 //   softmax warps      one thread per query row, S in two halves of 64 keys: y - M, maximum, exp2, P as f16 over S's columns
 // Per 16 keys a table entry (the converters write it) gives the softmax both scales and the weight in l.
+// Bound by the chain product - maximum - exponentials - product of a row tile: 4300 cycles a key tile with two row tiles, of which the
+// tensor core is busy for 2170, the special-function units for 2050.  16 x 922 rows, 2560 keys, 32 heads: 781 us in int8, 763 in e4m3
+// (0.79 and 0.81 PFLOP/s); 1639 rows, 8288 keys: 317 us (0.70: 224 CTAs on 148 SMs).
 #include <algorithm>
 #include <climits>
 
