@@ -313,7 +313,7 @@ __global__ void __launch_bounds__(kThreads<SETS>, 1) kv8_attn_tc_kernel(const Kv
             __syncwarp();
             if (lane == 0 && n_tiles > 0) mbar_arrive(bar(0));
 
-            float m_use = -INFINITY, l = 0.f;
+            float m_use = -INFINITY, l = 0.f, top = -INFINITY;
             int e0 = 127;
             bool ok = true;
             for (int i = 0; i < 2 * n_tiles && ok; ++i) {
@@ -366,33 +366,23 @@ __global__ void __launch_bounds__(kThreads<SETS>, 1) kv8_attn_tc_kernel(const Kv
 #pragma unroll
                     for (int e = 0; e < 32; e += 2) m4[(e >> 1) & 3] = fmaxf(fmaxf(m4[(e >> 1) & 3], sv[c][e]), sv[c][e + 1]);
                 float mx = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
-                const bool raise = mx > kRaise || (first && mx > -INFINITY);
-                if (__any_sync(0xffffffffu, raise)) {
-                    mx += kHeadroom;
-                    const float f = raise ? (first ? 0.f : ex2(-mx)) : 1.f;
-                    if (i > 0) {
-                        // O may only be touched once the P V of half i - 1 (and with it every earlier one) has completed
-                        if (!(ok = __all_sync(0xffffffffu, mbar_wait(bar(15 + 2 * t + ((i - 1) & 1)), ((i - 1) >> 1) & 1, abort_flag)))) break;
-                        tc_fence_after();
-#pragma unroll 1
-                        for (int c = 0; c < 4; ++c) {
-                            float v[32];
-                            uint32_t u[32];
-                            tt_ld32(tO + c * 32, v);
-                            tt_wait_ld<32>(v);
-#pragma unroll
-                            for (int e = 0; e < 32; ++e) u[e] = __float_as_uint(v[e] * f);
-                            tt_st32(tO + c * 32, u);
-                        }
-                        tt_wait_st();
-                    }
-                    l *= f;
-                    if (raise) {
-                        m_use = m_ref + mx;
+                // The reference moves for the warp's rows together.  l and P take the new one at once; O, which waits for a product, once P is
+                // out (in front of it: 673 us for 16 x 922 rows with their own lengths where it is 639; without that price, but with small
+                // weights lost, 607: kv8.cuh).  top: the largest y - M met so far.
+                top = fmaxf(top, mx);
+                float f = 1.f;
+                const bool moves = __any_sync(0xffffffffu, mx > kRaise || (first && mx > -INFINITY));
+                if (moves) {
+                    if (top > kStart || (first && mx > -INFINITY)) {
+                        const float up = top - kStart;
+                        f = first ? 0.f : ex2(-up);
+                        m_use = m_ref + up;
+                        top = kStart;
+                        l *= f;
 #pragma unroll
                         for (int c = 0; c < 2; ++c)
 #pragma unroll
-                            for (int e = 0; e < 32; ++e) sv[c][e] -= mx;
+                            for (int e = 0; e < 32; ++e) sv[c][e] -= up;
                     }
                 }
                 // P as packed f16 over the first 32 of the half's 64 columns of S, which this thread has read
@@ -412,6 +402,26 @@ __global__ void __launch_bounds__(kThreads<SETS>, 1) kv8_attn_tc_kernel(const Kv
                     l = fmaf((sa.x + sa.y) + (sb.x + sb.y), sc[g].z, l);
                 }
                 tt_st32(tS + hb * 64, pk);
+                if (moves && i > 0) {
+                    // O may only be touched once the P V of half i - 1 (and with it every earlier one) has completed: by now it has
+                    if (!(ok = __all_sync(0xffffffffu, tt_spin(bar(15 + 2 * t + ((i - 1) & 1)), ((i - 1) >> 1) & 1, abort_flag)))) break;
+                    tc_fence_after();
+#pragma unroll 1
+                    for (int c = 0; c < 2; ++c) {
+                        float v[2][32];
+                        tt_ld32(tO + c * 64, v[0]);
+                        tt_ld32(tO + c * 64 + 32, v[1]);
+                        tt_wait_ld<32>(v[0]);
+                        tt_wait_ld<32>(v[1]);
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            uint32_t u[32];
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) u[e] = __float_as_uint(v[h][e] * f);
+                            tt_st32(tO + c * 64 + h * 32, u);
+                        }
+                    }
+                }
                 tt_wait_st();
                 tc_fence_before();
                 __syncwarp();
