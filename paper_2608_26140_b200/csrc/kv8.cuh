@@ -114,6 +114,13 @@ __device__ __forceinline__ void st_global32(void* p, const uint32_t (&v)[8], boo
 // The price is that references move: one 4 above the largest logit moved 0.04 to 0.14 times a warp, this one 2.3 to 3 times.
 constexpr float kRaise = 15.9f, kStart = 8.f;
 constexpr int kFarApart = 100;                       // most by which E0 is above an ev
+// A key's weight in the denominator, 2^(E0 - ev), times 2^-kWeightBias: 2^20 keys of the largest p and the largest weight come to 2^104
+// (without it 2^136, past fp32), one key of p = 2^8 and the smallest weight to 2^-24.
+constexpr int kWeightBias = 32;
+__device__ __forceinline__ float kv8_weight(int behind) { return kv8_scale(127 - kWeightBias + min(behind, kFarApart)); }
+// 2^(E0 - 127 - kWeightBias), exact down to the lowest exponent (2^-143, not a normal number): what sums over denominators are multiplied by.
+// By itself, after the division: 1 / l times it may be smaller than any number, or larger.
+__device__ __forceinline__ float kv8_unbias(int e0) { return kv8_scale(e0) * (1.f / 4294967296.f); }
 
 __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
     uint32_t r;

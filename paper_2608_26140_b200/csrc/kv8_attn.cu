@@ -5,7 +5,7 @@
 // with K_j = 2^(ek) k_j, V_j = 2^(ev) v_j, k_j and v_j the codes: whole numbers or e4m3 values, exact in f16.  The products
 // run on the codes; ek joins the factor that turns a product into x, ev the exponent:
 //   y_rj = x_rj + ev,   p_rj = 2^(y_rj - M)  (M: running reference of y),   O = sum p v,   l = sum p 2^(E0 - ev)
-// so that o = 2^E0 O / l with E0 the largest ev met so far (l follows it), and no code is ever multiplied by its scale.  The
+// (l over 2^32: kv8.cuh) so that o = 2^E0 O / l with E0 the largest ev met so far (l follows it), and no code is ever multiplied by its scale.  The
 // scales of one head's values may differ by 2^100, which is where the weights in l end.  p is f16:
 // V's codes are f16 whatever their scales, which leaves p 11 bits (with bf16 operands, 8).  q is f16 too, each row over a
 // power of two of its own that brings its largest value to [1, 2).
@@ -358,7 +358,7 @@ __global__ void __launch_bounds__(RW * 32, NT < 4 ? kSlots : 1) kv8_attn_rows_ke
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
             uint32_t pf[NT][2];
-            const float lw = kv8_scale(127 + min(e0 - ev[mt], kFarApart));
+            const float lw = kv8_weight(e0 - ev[mt]);
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
                 const float p0 = ex2(sv[mt][nt][0]), p1 = ex2(sv[mt][nt][1]), p2 = ex2(sv[mt][nt][2]), p3 = ex2(sv[mt][nt][3]);
@@ -427,7 +427,7 @@ __global__ void __launch_bounds__(RW * 32, NT < 4 ? kSlots : 1) kv8_attn_rows_ke
     const int item = blockIdx.z * gridDim.y + tile;
 #pragma unroll
     for (int w = 0; w < RW; ++w) e0 = max(e0, top_v[w]);
-    const float up = kv8_scale(e0);          // 2^E0
+    const float up = kv8_unbias(e0);
     constexpr int TPR = D / 4;               // threads of a row, 4 values each
     const int cs = a.cluster, parts = a.splits / cs;
     float* part_o = a.part;                  // [item][part][row][D], then [item][part][row] log2 of the denominators
@@ -462,9 +462,9 @@ __global__ void __launch_bounds__(RW * 32, NT < 4 ? kSlots : 1) kv8_attn_rows_ke
             den = fmaf(f, stat[1][w][row] * kv8_scale(127 + min(e0 - top_v[w], kFarApart)), den);
             v.x = fmaf(f, x.x, v.x); v.y = fmaf(f, x.y, v.y); v.z = fmaf(f, x.z, v.z); v.w = fmaf(f, x.w, v.w);
         }
-        const float s = den == 0.f ? 0.f : up / den;
-        v.x *= s; v.y *= s; v.z *= s; v.w *= s;
-        const float lse2 = den == 0.f ? -INFINITY : mx - (float)(e0 - 127) + log2f(den);
+        const float s = den == 0.f ? 0.f : 1.f / den;
+        v.x = v.x * s * up; v.y = v.y * s * up; v.z = v.z * s * up; v.w = v.w * s * up;
+        const float lse2 = den == 0.f ? -INFINITY : mx - (float)(e0 - 127 - kWeightBias) + log2f(den);
         if (cs == 1) {
             give(row, c, v, lse2);
         } else {

@@ -431,8 +431,8 @@ __global__ void __launch_bounds__(kThreads<SETS>, 1) kv8_attn_tc_kernel(const Kv
             if (ok && n_tiles > 0) ok = __all_sync(0xffffffffu, mbar_wait(bar(15 + 2 * t + 1), (n_tiles - 1) & 1, abort_flag));
             if (ok) {
                 tc_fence_after();
-                const float inv = l == 0.f ? 0.f : kv8_scale(e0) / l;
-                const float lse2 = l == 0.f ? -INFINITY : m_use - (float)(e0 - 127) + log2f(l);
+                const float inv = l == 0.f ? 0.f : 1.f / l, up = kv8_unbias(e0);
+                const float lse2 = l == 0.f ? -INFINITY : m_use - (float)(e0 - 127 - kWeightBias) + log2f(l);
                 const int64_t at = (int64_t)(b * (int64_t)a.n + r / G) * a.n_heads + kvh * G + r % G;
 #pragma unroll 1
                 for (int c = 0; c < 4; ++c) {
@@ -442,24 +442,22 @@ __global__ void __launch_bounds__(kThreads<SETS>, 1) kv8_attn_tc_kernel(const Kv
                         tt_wait_ld<32>(v);
                     }
                     if (r < R) {
-                        if (l == 0.f) {
 #pragma unroll
-                            for (int e = 0; e < 32; ++e) v[e] = 0.f;
-                        }
+                        for (int e = 0; e < 32; ++e) v[e] = l == 0.f ? 0.f : v[e] * inv * up;
                         if (a.splits == 1) {
                             uint32_t u[8];
                             __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.o) + at * 128 + c * 32;
 #pragma unroll
                             for (int h = 0; h < 2; ++h) {
 #pragma unroll
-                                for (int k = 0; k < 8; ++k) u[k] = pack_bf16(v[h * 16 + 2 * k] * inv, v[h * 16 + 2 * k + 1] * inv);
+                                for (int k = 0; k < 8; ++k) u[k] = pack_bf16(v[h * 16 + 2 * k], v[h * 16 + 2 * k + 1]);
                                 st_global32(out + h * 16, u, on_sector(a.o));
                             }
                         } else {
 #pragma unroll
                             for (int k4 = 0; k4 < 8; ++k4)
                                 *reinterpret_cast<float4*>(res + (t * 128 + row) * 132 + c * 32 + k4 * 4) =
-                                    make_float4(v[k4 * 4] * inv, v[k4 * 4 + 1] * inv, v[k4 * 4 + 2] * inv, v[k4 * 4 + 3] * inv);
+                                    make_float4(v[k4 * 4], v[k4 * 4 + 1], v[k4 * 4 + 2], v[k4 * 4 + 3]);
                         }
                     }
                     __syncwarp();

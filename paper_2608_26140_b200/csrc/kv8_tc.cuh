@@ -136,7 +136,7 @@ __device__ __forceinline__ void write_table(KeyTable& t, uint32_t meta, int lane
     if (top == 0) top = 127;                          // nothing but empty blocks so far: their scale is of no account
     if (lane < 8) {
         const int e = ev ? ev : top;
-        t.group[lane] = make_float4(kv8_scale((int)meta), (float)(max(e, top - kFarApart) - 127), kv8_scale(127 + min(top - e, kFarApart)), 0.f);
+        t.group[lane] = make_float4(kv8_scale((int)meta), (float)(max(e, top - kFarApart) - 127), kv8_weight(top - e), 0.f);
     }
     if (lane == 0) {
         t.grow = kv8_scale(127 + min(top - e0, kFarApart));

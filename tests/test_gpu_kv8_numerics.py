@@ -75,3 +75,35 @@ def test_logits_that_keep_rising(heads, B, n, T):
         keep, c, vals = held(ctx, heads, B, T, k * at, v, 64, "int8")
         check_attention(ctx, None, vals, B, n, T, heads, queries_along(heads, B, n, u), c=c)
     assert ctx.poll_status() == 0
+
+
+@pytest.mark.parametrize("first,others,c_first", [
+    (177, 77, -55), (177, 77, -67),              # the others' values 2^100 smaller, their weights 2^106 and 2^118 larger
+    (77, 177, 55), (16, 16, 42), (16, 116, 49), (247, 247, 42), (247, 147, -55)])
+@pytest.mark.parametrize("n,T", [(1, 65536), (32, 65536), (140, 24576)])
+def test_scales_of_values_at_the_ends_of_what_is_allowed(n, T, first, others, c_first):
+    """The first 128 keys (one step of every warp, one key tile) and all others, each kind with logits and a scale of its own: denominators run from the smallest to the largest
+    that there can be, results from 2^-104 to 2^127.  As many items as leave the keys whole."""
+    heads, B, block = "mha32", 9, 16
+    H, hkv, d = HEADS[heads]
+    ctx = ab.Context(128, H, hkv, d, 128, 1e-5, 0, B, T, 0, 1, 0, DEV)
+    g = torch.Generator(device=DEV).manual_seed(n)
+    u = torch.where(torch.rand((d,), generator=g, device=DEV) < 0.5, -1, 1)
+    c = torch.full((T,), 49, device=DEV)
+    c[:128] = c_first
+    k = (c[:, None] * u).to(torch.int8).view(torch.uint8).expand(B, hkv, T, d).contiguous()
+    v = torch.randint(64, 127, (1, hkv, T, d), generator=g, device=DEV, dtype=torch.uint8).expand(B, hkv, T, d).contiguous()
+    ke = torch.full((B, hkv, T // block), 123, dtype=torch.uint8, device=DEV)      # a logit is c / sqrt(2)
+    ve = torch.full((B, hkv, T // block), others, dtype=torch.uint8, device=DEV)
+    ve[:, :, :128 // block] = first
+    cache = ab.Context.kv8(k, v, ke, ve, block, ab.KV8_FORMATS["int8"])
+    q = u.expand(B, n, H, d).bfloat16().contiguous()
+    o, lse = torch.empty_like(q), torch.empty((B, n, H), dtype=torch.float32, device=DEV)
+    ctx.kv8_attention(cache, B, T, q, o, lse=lse)
+    for b, h in ((0, 0), (4, 17), (8, 31)):
+        K, V = (t[b, h].view(torch.int8).double() * torch.exp2(e[b, h].double() - 127).repeat_interleave(block)[:, None] for t, e in ((k, ke), (v, ve)))
+        ro, rl, A, X = ref_attention(q[b, :1, h:h + 1].double(), K[None], V[None], torch.ones(T, dtype=torch.bool, device=DEV))
+        assert float(X.max()) < 64
+        assert ((o[b, :, h].double() - ro[:, 0]).abs() <= 2.0 ** -8 * ro[:, 0].abs() + 2.0 ** -9 * A[:, 0]).all()
+        assert ((lse[b, :, h].double() - rl[:, 0]).abs() <= 2.0 ** -16 * X[:, 0] + 2.0 ** -18 * (1 + rl[:, 0].abs())).all()
+    assert ctx.poll_status() == 0
