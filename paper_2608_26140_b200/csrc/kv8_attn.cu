@@ -5,7 +5,7 @@
 // with K_j = 2^(ek) k_j, V_j = 2^(ev) v_j, k_j and v_j the codes: whole numbers or e4m3 values, exact in f16.  The products
 // run on the codes; ek joins the factor that turns a product into x, ev the exponent:
 //   y_rj = x_rj + ev,   p_rj = 2^(y_rj - M)  (M: running reference of y),   O = sum p v,   l = sum p 2^(E0 - ev)
-// (l over 2^32: kv8.cuh) so that o = 2^E0 O / l with E0 the largest ev met so far (l follows it), and no code is ever multiplied by its scale.  The
+// (l over 2^32: kv8.cuh) so that o = 2^E0 O / l with E0 the largest ev so far of values that count (l follows it), and no code is ever multiplied by its scale.  The
 // scales of one head's values may differ by 2^100, which is where the weights in l end.  p is f16:
 // V's codes are f16 whatever their scales, which leaves p 11 bits (with bf16 operands, 8).  q is f16 too, each row over a
 // power of two of its own that brings its largest value to [1, 2).
@@ -221,7 +221,7 @@ __global__ void __launch_bounds__(RW * 32, NT < 4 ? kSlots : 1) kv8_attn_rows_ke
     float o[D / 16][NT][4];
     float2 m[NT], l[NT];                 // references and denominators of rows 2 t, 2 t + 1
     bool first = true;                   // no key yet: the same for all rows, a key counts for all of them or for none
-    int e0 = 0;                          // biased; 0: nothing met yet
+    int e0 = 0;                          // E0, biased; 0: no value that counts met yet
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
         m[nt] = l[nt] = make_float2(0.f, 0.f);
@@ -239,20 +239,28 @@ __global__ void __launch_bounds__(RW * 32, NT < 4 ? kSlots : 1) kv8_attn_rows_ke
         if (a.key_drop) there &= ~__ldg(a.key_drop + (int64_t)b * a.drop_words + (key0 >> 5));
         int ek[MT], ev[MT];
         bool blank[MT], no_keys = false;      // a block that holds nothing has zero keys and values, whatever its codes
+        int most = e0;                        // (nor has a tile without a key that counts any values)
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
             ek[mt] = e_next[mt];
             ev[mt] = e_next[MT + mt];
             no_keys |= ek[mt] == 0;
-            blank[mt] = ev[mt] == 0;
-            if (blank[mt]) ev[mt] = e0 ? e0 : 127;      // its scale is of no account
-            if (ev[mt] > e0) {
-                const float grow = kv8_scale(127 + min(ev[mt] - e0, kFarApart));
-                e0 = ev[mt];
+            blank[mt] = ev[mt] == 0 || ((there >> (mt * 16)) & 0xFFFFu) == 0u;
+            most = blank[mt] ? most : max(most, ev[mt]);
+        }
+        if (most > e0) {
+            // so far nothing but tiles without values, under E0 = 127: they have this scale as well as any, and M moves along with it
+            const float grow = e0 ? kv8_scale(127 + min(most - e0, kFarApart)) : 1.f, along = e0 ? 0.f : (float)(most - 127);
+            e0 = most;
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt) { l[nt].x *= grow; l[nt].y *= grow; }
+            for (int nt = 0; nt < NT; ++nt) {
+                l[nt].x *= grow; l[nt].y *= grow;
+                m[nt].x += along; m[nt].y += along;
             }
         }
+        const int e_top = e0 ? e0 : 127;
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) ev[mt] = blank[mt] ? e_top : ev[mt];
         exponents(step + 1, e_next);
         ring_wait<RSTAGES - 2>();
         __syncwarp();                        // this step's stage is there for every lane, and every lane is done with the last one's
@@ -299,7 +307,7 @@ __global__ void __launch_bounds__(RW * 32, NT < 4 ? kSlots : 1) kv8_attn_rows_ke
         float top = -INFINITY;
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
-            const float ks = kv8_scale(ek[mt]), vy = (float)(max(ev[mt], e0 - kFarApart) - 127);
+            const float ks = kv8_scale(ek[mt]), vy = (float)(max(ev[mt], e_top - kFarApart) - 127);
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
                 const float2 fa = __fmul2_rn(rq[nt], make_float2(ks, ks)), fb = __fadd2_rn(make_float2(vy, vy), make_float2(-m[nt].x, -m[nt].y));
@@ -358,7 +366,7 @@ __global__ void __launch_bounds__(RW * 32, NT < 4 ? kSlots : 1) kv8_attn_rows_ke
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
             uint32_t pf[NT][2];
-            const float lw = kv8_weight(e0 - ev[mt]);
+            const float lw = kv8_weight(e_top - ev[mt]);
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
                 const float p0 = ex2(sv[mt][nt][0]), p1 = ex2(sv[mt][nt][1]), p2 = ex2(sv[mt][nt][2]), p3 = ex2(sv[mt][nt][3]);
@@ -427,7 +435,14 @@ __global__ void __launch_bounds__(RW * 32, NT < 4 ? kSlots : 1) kv8_attn_rows_ke
     const int item = blockIdx.z * gridDim.y + tile;
 #pragma unroll
     for (int w = 0; w < RW; ++w) e0 = max(e0, top_v[w]);
+    e0 = e0 ? e0 : 127;
     const float up = kv8_unbias(e0);
+    float along[RW], grow[RW];               // of a warp's reference and denominator, on the way to the CTA's E0 (as in the loop)
+#pragma unroll
+    for (int w = 0; w < RW; ++w) {
+        along[w] = top_v[w] ? 0.f : (float)(e0 - 127);
+        grow[w] = top_v[w] ? kv8_scale(127 + min(e0 - top_v[w], kFarApart)) : 1.f;
+    }
     constexpr int TPR = D / 4;               // threads of a row, 4 values each
     const int cs = a.cluster, parts = a.splits / cs;
     float* part_o = a.part;                  // [item][part][row][D], then [item][part][row] log2 of the denominators
@@ -450,16 +465,16 @@ __global__ void __launch_bounds__(RW * 32, NT < 4 ? kSlots : 1) kv8_attn_rows_ke
         if (tile * L::ROWS + row >= R) continue;
         float mx = -INFINITY;
 #pragma unroll
-        for (int w = 0; w < RW; ++w) mx = fmaxf(mx, stat[0][w][row]);
+        for (int w = 0; w < RW; ++w) mx = fmaxf(mx, stat[0][w][row] + along[w]);
         float den = 0.f;
         float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
         for (int w = 0; w < RW; ++w) {
-            const float mw = stat[0][w][row];
+            const float mw = stat[0][w][row] + along[w];
             // a NaN in the sums has to come through; a warp that met no key has sums of zero
             const float f = mw == -INFINITY ? 1.f : ex2(mw - mx);
             const float4 x = *reinterpret_cast<const float4*>(os + (w * L::ROWS + row) * (D + 4) + c * 4);
-            den = fmaf(f, stat[1][w][row] * kv8_scale(127 + min(e0 - top_v[w], kFarApart)), den);
+            den = fmaf(f, stat[1][w][row] * grow[w], den);
             v.x = fmaf(f, x.x, v.x); v.y = fmaf(f, x.y, v.y); v.z = fmaf(f, x.z, v.z); v.w = fmaf(f, x.w, v.w);
         }
         const float s = den == 0.f ? 0.f : 1.f / den;

@@ -323,6 +323,7 @@ __global__ void __launch_bounds__(kThreads<SETS>, 1) kv8_attn_tc_kernel(const Kv
                     // warp-uniform: the tensor-memory accesses below are collective
                     if (!(ok = __all_sync(0xffffffffu, tt_spin(bar(19 + (j & (kTables - 1))), (j >> 2) & 1, abort_flag)))) break;
                     l *= tab.grow;
+                    m_use += tab.along;
                     e0 = tab.e0;
                 }
                 if (hb < S_PARTS) {

@@ -13,9 +13,9 @@ constexpr int TT_PANEL = 128 * 64 * 2;
 struct KeyTable {                                         // of one 128-key tile
     float4 group[8];                                      // per 16 keys: scale of K, log2 of V's scale, weight in l, -
     uint32_t keep[4];                                     // keys that count
-    float grow;                                           // what l is multiplied by in front of this tile
+    float grow, along;                                    // in front of this tile: what l is multiplied by, what M goes up by
     int e0;
-    uint32_t pad[2];
+    uint32_t pad;
 };
 constexpr int kTables = 4;
 
@@ -126,21 +126,25 @@ struct TileMeta {
         return v;
     }
 };
-// A whole warp writes the table of a tile from its lanes' metas; e0: the largest ev so far (biased, 0: none), carried along.
+// A whole warp writes the table of a tile from its lanes' metas; e0: the largest ev so far of values that count (biased, 0: none), carried
+// along.  Groups that hold nothing, or without a key that counts, have no scale; as long as there is nothing else it is taken to be 127,
+// and M goes to the first real one with it.
 __device__ __forceinline__ void write_table(KeyTable& t, uint32_t meta, int lane, int& e0) {
-    const int ev = __shfl_sync(0xffffffffu, (int)meta, 8 + (lane & 7));
+    const uint32_t keys = __shfl_sync(0xffffffffu, meta, 16 + ((lane & 7) >> 1)) >> ((lane & 1) * 16);
+    const int held = __shfl_sync(0xffffffffu, (int)meta, 8 + (lane & 7)), ev = keys & 0xFFFFu ? held : 0;
     int top = ev;
 #pragma unroll
     for (int o = 4; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
     top = max(top, e0);
-    if (top == 0) top = 127;                          // nothing but empty blocks so far: their scale is of no account
+    const int e_top = top ? top : 127;
     if (lane < 8) {
-        const int e = ev ? ev : top;
-        t.group[lane] = make_float4(kv8_scale((int)meta), (float)(max(e, top - kFarApart) - 127), kv8_weight(top - e), 0.f);
+        const int e = ev ? ev : e_top;
+        t.group[lane] = make_float4(kv8_scale((int)meta), (float)(max(e, e_top - kFarApart) - 127), kv8_weight(e_top - e), 0.f);
     }
     if (lane == 0) {
-        t.grow = kv8_scale(127 + min(top - e0, kFarApart));
-        t.e0 = top;
+        t.grow = e0 ? kv8_scale(127 + min(top - e0, kFarApart)) : 1.f;
+        t.along = e0 ? 0.f : (float)(e_top - 127);
+        t.e0 = e_top;
     }
     if (lane >= 16 && lane < 20) t.keep[lane - 16] = meta;
     e0 = top;

@@ -8,7 +8,7 @@ import torch
 from paper_2608_26140_b200 import binding as ab
 
 from helpers import DEV
-from test_gpu_kv8 import HEADS, check_attention, context, queries, ref_attention
+from test_gpu_kv8 import HEADS, check_attention, context, filled, queries, ref_attention
 
 pytestmark = pytest.mark.gpu
 
@@ -106,4 +106,48 @@ def test_scales_of_values_at_the_ends_of_what_is_allowed(n, T, first, others, c_
         assert float(X.max()) < 64
         assert ((o[b, :, h].double() - ro[:, 0]).abs() <= 2.0 ** -8 * ro[:, 0].abs() + 2.0 ** -9 * A[:, 0]).all()
         assert ((lse[b, :, h].double() - rl[:, 0]).abs() <= 2.0 ** -16 * X[:, 0] + 2.0 ** -18 * (1 + rl[:, 0].abs())).all()
+    assert ctx.poll_status() == 0
+
+
+PLACES = [("mha32", 1, 4096, 64), ("mha32", 1, 300, 16), ("mha32", 32, 1000, 64), ("gqa28", 29, 1531, 32), ("mha32", 140, 1500, 128),
+          ("mha4-64", 40, 700, 16)]
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+@pytest.mark.parametrize("heads,n,T,block", PLACES)
+def test_exponents_of_places_that_do_not_count(heads, n, T, block, fmt):
+    """Blocks none of whose keys exists, and blocks past a request's length, with exponents of any kind: of no account."""
+    B = 4
+    ctx = context(heads, B, T)
+    cache, vals = filled(heads, B, T, block, fmt, n + T)
+    blocks = -(-T // block)
+    g = torch.Generator(device=DEV).manual_seed(3)
+    gone = torch.rand((B, blocks), generator=g, device=DEV) < 0.3
+    gone[0, 0], gone[1, :blocks // 2], gone[2, -1], gone[3] = True, True, True, True
+    gone[3, blocks // 3] = False
+    drop = (torch.rand((B, T), generator=g, device=DEV) < 0.2) | gone.repeat_interleave(block, 1)[:, :T]
+    lens = [T, T, T // 2 + 3, T]
+    past = torch.arange(blocks, device=DEV)[None] * block >= torch.tensor(lens, device=DEV)[:, None]
+    odd = torch.tensor([247, 16, 255, 1, 254, 0], dtype=torch.uint8, device=DEV)
+    for e in cache.dev[2:]:
+        e[:, :, :blocks] = torch.where((gone | past)[:, None], odd[torch.randint(0, 6, (B, e.shape[1], blocks), generator=g, device=DEV)], e[:, :, :blocks])
+    q = queries(B, n, heads, 5)
+    check_attention(ctx, cache, vals, B, n, T, heads, q, lens=lens, drop=drop)
+    assert ctx.poll_status() == 0
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+@pytest.mark.parametrize("heads,n,T,block", PLACES)
+def test_blocks_that_hold_nothing_have_no_scale(heads, n, T, block, fmt):
+    """Empty blocks in front, behind and between; the values of the others, up to 2^-95, lie near the lowest exponent."""
+    B = 2
+    ctx = context(heads, B, T)
+    blocks = -(-T // block)
+    holes = [i for i in range(blocks) if i < blocks // 3 or i % 5 == 4]
+    cache, vals = filled(heads, B, T, block, fmt, n + T, holes=holes)
+    e = cache.dev[3]
+    e.copy_(torch.where(e > 0, e - 100, e))
+    assert int(e[e > 0].min()) >= 16
+    vals[1] *= 2.0 ** -100
+    check_attention(ctx, cache, vals, B, n, T, heads, queries(B, n, heads, 5))
     assert ctx.poll_status() == 0
