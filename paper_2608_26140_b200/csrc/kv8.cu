@@ -272,7 +272,7 @@ void write_blocks(const Kv8WriteArgs& a, unsigned blocks, cudaStream_t stream) {
 void launch_kv8_write(Kv8WriteArgs a, cudaStream_t stream) {
     unsigned blocks;
     if (a.pos) {
-        const int all = (a.ctx_len + a.block - 1) / a.block;
+        const int all = a.ctx_len > 0 ? (a.ctx_len + a.block - 1) / a.block : 1;      // (none: one CTA says that no row has a place)
         a.first_block = 0;
         a.by_row = a.n < all;
         blocks = a.by_row ? a.n : all;
