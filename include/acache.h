@@ -122,6 +122,7 @@ typedef struct {
 /* formats of the codes of an 8-bit cache */
 #define ACACHE_KV8_E4M3 0   /* floating point, 4 exponent and 3 mantissa bits, no infinities */
 #define ACACHE_KV8_INT8 1   /* whole numbers -127 .. 127                                     */
+#define ACACHE_KV8_MAX_ROWS 2097120 /* most query rows of one request per KV head, n_rows H / Hkv, of an attention over one */
 
 /* One layer's KV cache held in 8 bits (the paper has no counterpart; half the memory of acache_kv and half the bytes of every
  * pass over it).  DEVICE codes [B, Hkv, ctx_capacity, d], a (request, head)'s tokens side by side, K after the rotary
@@ -129,7 +130,7 @@ typedef struct {
  * the exponent byte e stands for c * 2^(e - 127), which is exact in bf16.  e = 0: the block holds nothing and reads as
  * zero; a new cache is one whose exponent bytes are 0.
  * batch_stride: codes between two requests (normally Hkv * ctx_capacity * d; a multiple of 16); exponents of the requests follow
- * each other.  0: one cache shared by the batch, for the calls that only read it. */
+ * each other.  0: one cache shared by the batch, for the calls that only read it.  Calls take up to 65535 / Hkv requests. */
 typedef struct {
     void    *k, *v;
     uint8_t *k_exp, *v_exp;
@@ -353,8 +354,8 @@ acache_status acache_kv8_read(acache_ctx *ctx, const acache_kv8 *kv, int32_t bat
  * (DEVICE uint32 [B, ceil(ctx_len / 32)]; NULL: all).  Where there is none, o = 0 and lse = -inf.  What the cache holds in
  * places that do not count is of no account, NaN included.  A length outside [0, ctx_len] raises ACACHE_FLAG_BAD_INDEX and is
  * taken as the nearer end.
- *   q, o: DEVICE bf16 [B, n_rows, H, d], n_rows from one (a single token) to many; lse: DEVICE fp32 [B, n_rows, H], natural
- *   logarithm, may be NULL (with it, results over several caches can be put together).
+ *   q, o: DEVICE bf16 [B, n_rows, H, d], n_rows from one (a single token) to ACACHE_KV8_MAX_ROWS Hkv / H; lse: DEVICE fp32
+ *   [B, n_rows, H], natural logarithm, may be NULL (with it, results over several caches can be put together).
  * Logits, softmax and sums in fp32.  Codes enter the products exactly, probabilities and queries rounded to 11 bits or, where that is
  * coarser, to 2^-33 of the row's largest probability and 2^-25 of the query's largest element.  The scales of
  * one head's values may differ by a factor of 2^100. */

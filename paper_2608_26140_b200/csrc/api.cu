@@ -137,6 +137,9 @@ acache_status check_kv8(acache_ctx* c, const acache_kv8* kv, int32_t batch, int3
     return ACACHE_OK;
 }
 
+// rows of one request that share a KV head: the attention's row tiles are a dimension of its grid
+bool kv8_rows_fit(const acache_ctx* c, int64_t n_rows) { return n_rows * (c->d.n_heads / c->d.n_kv_heads) <= ACACHE_KV8_MAX_ROWS; }
+
 int log2_of(int block) { return block == 16 ? 4 : block == 32 ? 5 : block == 64 ? 6 : 7; }
 
 // rows k_rows / v_rows [B, n, Hkv, d] at positions pos (or start ..) of the cache
@@ -181,7 +184,7 @@ acache_status run_kv8_attention(acache_ctx* c, const acache_kv8* kv, int32_t bat
     a.part = wsp<float>(c, c->o_gemm);           // the projections' partial tiles: no projection runs beside an attention
     a.arrived = wsp<unsigned int>(c, c->o_arrived);
     a.status = wsp<uint32_t>(c, c->o_status);
-    if (a.shared && !lens && !key_drop) {        // one cache and one set of keys: the batch's rows are rows of one request
+    if (a.shared && !lens && !key_drop && kv8_rows_fit(c, (int64_t)n * batch)) {   // one cache and one set of keys: the batch's rows are rows of one request
         a.n *= a.batch;
         a.batch = 1;
     }
@@ -659,6 +662,8 @@ acache_status layer_step_impl(acache_ctx* ctx, const acache_layer_weights* w, co
     acache_status s = check_request(ctx, req, kv, k, true, to_slots);
     if (s != ACACHE_OK) return s;
     if (kv8 && (s = check_kv8(ctx, kv8, req->batch, req->ctx_len, true)) != ACACHE_OK) return s;
+    if (kv8 && !kv8_rows_fit(ctx, (int64_t)k + req->n_extra))
+        return fail(ctx, ACACHE_ERR_UNSUPPORTED_SHAPE, "%d rows of a request are more than %d per KV head", k + req->n_extra, ACACHE_KV8_MAX_ROWS);
     const bool do_score = flags & ACACHE_F_SCORE, do_select = flags & ACACHE_F_SELECT;
     const bool do_recompute = !(flags & ACACHE_F_NO_RECOMPUTE);
     if ((s = check_weights(ctx, w, !do_recompute)) != ACACHE_OK) return s;
@@ -843,8 +848,7 @@ acache_status acache_kv8_attention(acache_ctx* ctx, const acache_kv8* kv, int32_
     if (s != ACACHE_OK) return s;
     if (n_rows < 0) return fail(ctx, ACACHE_ERR_INVALID_ARG, "n_rows %d is negative", n_rows);
     if (batch == 0 || n_rows == 0) return ACACHE_OK;
-    if ((int64_t)batch * n_rows * (ctx->d.n_heads / ctx->d.n_kv_heads) > (1 << 19))
-        return fail(ctx, ACACHE_ERR_UNSUPPORTED_SHAPE, "more than 2^19 query rows per KV head");
+    if (!kv8_rows_fit(ctx, n_rows)) return fail(ctx, ACACHE_ERR_UNSUPPORTED_SHAPE, "%d rows of a request are more than %d per KV head", n_rows, ACACHE_KV8_MAX_ROWS);
     if (!q || !o || !aligned16(q) || !aligned16(o)) return fail(ctx, ACACHE_ERR_INVALID_ARG, "q / o NULL or misaligned");
     return run_kv8_attention(ctx, kv, batch, n_rows, ctx_len, q, o, lse, lens, key_drop, stream);
 }
