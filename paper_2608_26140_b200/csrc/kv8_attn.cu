@@ -22,11 +22,13 @@
 // The reference M moves only when a logit passes it by 2^15.9 (f16 ends at 2^16), found by a vote; then maxima are exchanged and O is scaled.
 // It starts 2^8 below the first keys' largest (kv8.cuh); 2^4 above it, 32 rows took 98.8 us where they take 101.8, and lost small weights.
 #include <algorithm>
+#include <array>
 #include <climits>
 
 #include "kernels.h"
 #include "kv8.cuh"
 #include "launch.h"
+#include "per_device.h"
 #include "tc_ptx.cuh"
 
 namespace acache {
@@ -564,11 +566,14 @@ void rows_config(cudaLaunchConfig_t& cfg, cudaLaunchAttribute (&at)[2], dim3 gri
     cfg.attrs = at;
     cfg.numAttrs = cluster > 1 ? 2 : 1;
 }
-// clusters of 2^c CTAs that the GPU runs at a time: fewer than the places for CTAs make up, as a cluster stays in one group of SMs
+// [c]: clusters of 2^c CTAs that the current device runs at a time: fewer than the places for CTAs make up, as a cluster stays in one
+// group of SMs
 template <int D, int NT, int FMT>
-int rows_clusters(int c) {
-    static int fit[4] = {};
-    if (fit[0] == 0) {
+std::array<int, 4> rows_clusters() {
+    static PerDevice<std::array<int, 4>> fits;
+    int device = 0;
+    cudaGetDevice(&device);
+    return fits.of(device, [](std::array<int, 4>& fit) {
         cudaFuncSetAttribute(kv8_attn_rows_kernel<D, NT, FMT>, cudaFuncAttributeMaxDynamicSharedMemorySize, RowsLayout<D, NT>::SMEM);
         for (int i = 3; i >= 0; --i) {
             cudaLaunchConfig_t cfg;
@@ -580,8 +585,7 @@ int rows_clusters(int c) {
             if (cudaOccupancyMaxActiveClusters(&most, kv8_attn_rows_kernel<D, NT, FMT>, &cfg) != cudaSuccess) most = 0;
             fit[i] = std::min(std::max(most, 1), (kSlots * 148) >> i);
         }
-    }
-    return fit[c];
+    });
 }
 struct RowsPlan { int cluster, splits; int64_t cost; };   // cost: ns
 // Key splits, in clusters that add their results up; splits only where all their CTAs run at a time.  The estimate, with what was
@@ -597,8 +601,9 @@ RowsPlan rows_plan(const Kv8AttnArgs& a) {
     const int64_t items = (int64_t)((R + L::ROWS - 1) / L::ROWS) * a.batch * a.n_kv_heads;
     RowsPlan best{1, 1, INT64_MAX};
     const int most = a.ctx_len / kMinSplit, most_one = a.ctx_len / (NT == 1 ? kMinSplitNarrow : kMinSplit);
+    const std::array<int, 4> fits = rows_clusters<D, NT, FMT>();
     for (int c = 0; c < 4 && (c == 0 || 1 << c <= most_one); ++c) {
-        const int fit = rows_clusters<D, NT, FMT>(c);
+        const int fit = fits[c];
         if (c > 0 && items > fit) break;
         const int top = c == 0 ? 1 : std::max(1, (int)std::min<int64_t>(fit / items, most >> c));
         for (int k = 1;; k = top) {                       // one cluster an item, or as many as there is room for

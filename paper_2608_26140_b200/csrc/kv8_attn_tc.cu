@@ -13,10 +13,12 @@
 // tensor core is busy for 2170, the special-function units for 2050.  16 x 922 rows, 2560 keys, 32 heads: 781 us in int8, 763 in e4m3
 // (0.79 and 0.81 PFLOP/s); 1639 rows, 8288 keys: 317 us (0.70: 224 CTAs on 148 SMs).
 #include <algorithm>
+#include <array>
 #include <climits>
 
 #include "kv8_tc.cuh"
 #include "launch.h"
+#include "per_device.h"
 
 namespace acache {
 
@@ -502,11 +504,13 @@ void tc_config(cudaLaunchConfig_t& cfg, cudaLaunchAttribute (&at)[2], dim3 grid,
     cfg.attrs = at;
     cfg.numAttrs = grid.x > 1 ? 2 : 1;
 }
-// clusters of n CTAs that the GPU runs at a time (fewer than SMs / n: a cluster stays in one group of SMs)
+// [n]: clusters of n CTAs that the current device runs at a time (fewer than SMs / n: a cluster stays in one group of SMs)
 template <int FMT, int SETS>
-int tc_clusters(int n) {
-    static int fit[kTcSplits + 1] = {};
-    if (fit[1] == 0) {
+std::array<int, kTcSplits + 1> tc_clusters() {
+    static PerDevice<std::array<int, kTcSplits + 1>> fits;
+    int device = 0;
+    cudaGetDevice(&device);
+    return fits.of(device, [](std::array<int, kTcSplits + 1>& fit) {
         cudaFuncSetAttribute(kv8_attn_tc_kernel<FMT, SETS>, cudaFuncAttributeMaxDynamicSharedMemorySize, tt_smem<SETS>());
         for (int s = kTcSplits; s >= 1; --s) {
             cudaLaunchConfig_t cfg;
@@ -518,8 +522,7 @@ int tc_clusters(int n) {
             if (cudaOccupancyMaxActiveClusters(&most, kv8_attn_tc_kernel<FMT, SETS>, &cfg) != cudaSuccess) most = 0;
             fit[s] = std::max(most, 1);
         }
-    }
-    return fit[n];
+    });
 }
 struct TcPlan { int per, splits; int64_t cost; };         // key tiles of a split, splits, ns
 // The number of splits with which the rounds of CTAs take least.  1639 rows of 32 heads, 8288 keys (224 items): whole 317 us, in
@@ -529,9 +532,10 @@ TcPlan tc_plan(const Kv8AttnArgs& a) {
     const int R = a.n * (a.n_heads / a.n_kv_heads), tiles = (R + SETS * 128 - 1) / (SETS * 128);
     const int64_t items = (int64_t)tiles * a.batch * a.n_kv_heads;
     const int key_tiles = std::max(1, (a.ctx_len + 127) / 128);
+    const std::array<int, kTcSplits + 1> fits = tc_clusters<FMT, SETS>();
     TcPlan best{key_tiles, 1, INT64_MAX};
     for (int s = 1; s <= kTcSplits && s <= key_tiles; ++s) {
-        const int per = (key_tiles + s - 1) / s, n = (key_tiles + per - 1) / per, fit = tc_clusters<FMT, SETS>(n);
+        const int per = (key_tiles + s - 1) / s, n = (key_tiles + per - 1) / per, fit = fits[n];
         const int64_t cost = (items + fit - 1) / fit * (per * kTileNs<SETS> + kCtaNs + (n > 1 ? kSumNs<SETS> : 0));
         if (cost < best.cost) best = TcPlan{per, n, cost};
     }
