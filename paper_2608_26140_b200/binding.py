@@ -52,6 +52,7 @@ class KV(C.Structure):
 class KV8(C.Structure):
     _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_exp", C.c_void_p), ("v_exp", C.c_void_p), ("batch_stride", C.c_int64),
                 ("ctx_capacity", C.c_int32), ("block", C.c_int32), ("format", C.c_int32)]
+    made_of = None      # of the tensors that Context.kv8 made it over: requests (shared: any number), KV heads, head dimension, all on a GPU
 
 
 class Request(C.Structure):
@@ -265,15 +266,20 @@ class Context:
     def kv8(codes_k, codes_v, exp_k, exp_v, block, fmt, shared=False) -> KV8:
         """8-bit cache over one-byte codes [B, Hkv, capacity, d] and exponent bytes [B, Hkv, capacity / block]; fmt: a value of
         KV8_FORMATS.  Requests may lie further apart than their codes take.  shared: one request's cache for every request."""
-        _, hkv, cap, d = codes_k.shape
+        requests, hkv, cap, d = codes_k.shape
         for c, e in ((codes_k, exp_k), (codes_v, exp_v)):
             if c.element_size() != 1 or e.element_size() != 1:
                 raise ValueError("codes and exponents are bytes")
             if c.shape != codes_k.shape or tuple(e.shape) != (c.shape[0], hkv, cap // block):
                 raise ValueError(f"codes {tuple(c.shape)} and exponents {tuple(e.shape)} do not go together with blocks of {block}")
-            if c.stride()[1:] != (cap * d, d, 1) or not e.is_contiguous() or c.stride(0) != codes_k.stride(0):
+            if c.stride()[1:] != (cap * d, d, 1) or not e.is_contiguous() or (requests > 1 and c.stride(0) != codes_k.stride(0)):
                 raise ValueError("the codes of a request and all exponents are contiguous")
-        return KV8(_ptr(codes_k), _ptr(codes_v), _ptr(exp_k), _ptr(exp_v), 0 if shared else codes_k.stride(0), cap, block, fmt)
+        stride = codes_k.stride(0) if requests > 1 else hkv * cap * d
+        if stride == 0 and not shared:
+            raise ValueError("the codes of all requests lie in one place: shared=True is for that")
+        c = KV8(_ptr(codes_k), _ptr(codes_v), _ptr(exp_k), _ptr(exp_v), 0 if shared else stride, cap, block, fmt)
+        c.made_of = (float("inf") if shared else requests, hkv, d, all(t.is_cuda for t in (codes_k, codes_v, exp_k, exp_v)))
+        return c
 
     def new_kv8(self, batch, ctx_capacity, block=64, fmt="e4m3"):
         """An empty 8-bit cache for this context's shape: (tensors to keep alive: codes k, v, exponents k, v; the KV8)."""
@@ -361,6 +367,7 @@ class Context:
     # A call of the three below takes 6-8 us, more than many of their kernels, most of it here: tensors are asked for each property once.
     def kv8_write(self, cache: KV8, batch, ctx_len, k_rows, v_rows, start=0, pos=None):
         """Rows [B, n, Hkv, d] (bf16; requests may lie further apart) to positions start .. or pos [B, n] (int32)."""
+        self._cache_fits(cache, batch)
         shape, stride = self._rows(k_rows, batch, pos)
         if self._rows(v_rows, batch, None) != (shape, stride):
             raise ValueError("k_rows and v_rows differ in shape or stride")
@@ -369,6 +376,7 @@ class Context:
 
     def kv8_read(self, cache: KV8, batch, ctx_len, k_out, v_out, start=0, pos=None):
         """Rows at positions start .. or pos [B, n] into k_out, v_out [B, n, Hkv, d] (contiguous; either may be None)."""
+        self._cache_fits(cache, batch)
         one = v_out if k_out is None else k_out
         if one is None:
             raise AcacheError(ERR_INVALID_ARG, "neither k_out nor v_out is given")
@@ -383,6 +391,7 @@ class Context:
     def kv8_attention(self, cache: KV8, batch, ctx_len, q, o, lse=None, lens=None, key_drop=None):
         """q, o: bf16 [B, n, H, d]; lse: fp32 [B, n, H]; lens: int32 [B]; key_drop: int32 [B, ceil(ctx_len / 32)] (pack_key_drop)."""
         import torch
+        self._cache_fits(cache, batch)
         shape = q.shape
         B, n, H, d = shape
         if B != batch or H != self.heads[0] or d != self.heads[2]:
@@ -400,8 +409,16 @@ class Context:
 
     def layer_step_kv8(self, w: LayerWeights, req: Request, cache: KV8, x, x_is_compact, ratio, flags, scores, anchor_idx, y):
         """The layer-step on an 8-bit cache."""
+        self._cache_fits(cache, req.batch)
         self._check(self.lib.acache_layer_step_kv8(self.h, C.byref(w), C.byref(req), C.byref(cache), _ptr(x), int(x_is_compact),
                                                    float(ratio), int(flags), _ptr(scores), _ptr(anchor_idx), _ptr(y), _stream()))
+
+    def _cache_fits(self, cache, batch):
+        """What a call would read or write past the cache's tensors for (a KV8 filled in by hand is the caller's affair)."""
+        m = cache.made_of
+        if m is not None and (m[0] < batch or m[1:] != (self.heads[1], self.heads[2], True)):
+            raise ValueError(f"a cache of {m[0]} requests, {m[1]} KV heads of {m[2]}, {'not ' if not m[3] else ''}all on a GPU, "
+                             f"for {batch} requests and {self.heads[1]} KV heads of {self.heads[2]}")
 
     def _rows(self, t, batch, pos):
         """Shape of rows [B, n, Hkv, d], and elements between the requests."""
