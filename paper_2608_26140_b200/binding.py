@@ -198,6 +198,11 @@ def _check_tensor(t, dtype, shape):
         raise ValueError(f"a tensor {tuple(t.shape)} of {t.dtype} on {t.device} where contiguous {tuple(shape)} of {dtype} on a GPU is wanted")
 
 
+def _dense(t, strides):
+    """All dimensions but the first as in a contiguous tensor; the stride of a dimension of one element says nothing."""
+    return t.numel() == 0 or all(n == 1 or have == want for n, have, want in zip(t.shape[1:], t.stride()[1:], strides))
+
+
 def _stream() -> int:
     """The current stream of the current device (torch.cuda.current_stream() builds an object around it: 3.3 us a call, this 0.2)."""
     import torch
@@ -272,7 +277,7 @@ class Context:
                 raise ValueError("codes and exponents are bytes")
             if c.shape != codes_k.shape or tuple(e.shape) != (c.shape[0], hkv, cap // block):
                 raise ValueError(f"codes {tuple(c.shape)} and exponents {tuple(e.shape)} do not go together with blocks of {block}")
-            if c.stride()[1:] != (cap * d, d, 1) or not e.is_contiguous() or (requests > 1 and c.stride(0) != codes_k.stride(0)):
+            if not _dense(c, (cap * d, d, 1)) or not e.is_contiguous() or (requests > 1 and c.stride(0) != codes_k.stride(0)):
                 raise ValueError("the codes of a request and all exponents are contiguous")
         stride = codes_k.stride(0) if requests > 1 else hkv * cap * d
         if stride == 0 and not shared:
@@ -428,7 +433,7 @@ class Context:
         if B != batch or hkv != self.heads[1] or d != self.heads[2] or t.dtype is not torch.bfloat16 or not t.is_cuda:
             raise ValueError(f"rows {tuple(shape)} of {t.dtype} on {t.device} are not bf16 [batch, n, Hkv, d] on a GPU")
         stride = t.stride()
-        if n and stride[1:] != (hkv * d, d, 1):
+        if stride[1:] != (hkv * d, d, 1) and not _dense(t, (hkv * d, d, 1)):
             raise ValueError("the rows of a request are contiguous")
         if pos is not None:
             _check_tensor(pos, torch.int32, (B, n))

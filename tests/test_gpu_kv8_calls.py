@@ -62,3 +62,48 @@ def test_the_most_rows_of_one_request():
     with pytest.raises(ab.AcacheError) as e:
         ctx.kv8_attention(cache.c, 1, T, q, o)
     assert e.value.status == ab.ERR_UNSUPPORTED_SHAPE and ctx.launch_count() == launched
+
+
+def test_single_rows_and_single_heads_have_no_stride_of_their_own():
+    """One token's K and V inside a joint Q/K/V buffer; rows and codes of one KV head whose head dimension was moved: all are contiguous
+    where there is more than one of something."""
+    heads, B, T, block = "gqa28", 3, 40, 16
+    H, hkv, d = HEADS[heads]
+    ctx = context(heads, B, 48)
+    qkv = torch.randn((B, 1, H + 2 * hkv, d), device=DEV).bfloat16()
+    k, v = qkv[:, :, H:H + hkv], qkv[:, :, H + hkv:]
+    results = []
+    for rows in ((k, v), (k.clone(memory_format=torch.contiguous_format), v.clone(memory_format=torch.contiguous_format))):
+        keep, c = ctx.new_kv8(B, 48, block, "int8")
+        ctx.kv8_write(c, B, T, *rows, start=17)
+        results.append(keep)
+    assert all(torch.equal(a, b) for a, b in zip(*results)) and int(results[0][2].max()) > 0
+
+    heads, n = "mqa8", 5
+    H, hkv, d = HEADS[heads]
+    ctx = context(heads, B, 48)
+    rows = torch.randn((B, 1, n, d), device=DEV).bfloat16().transpose(1, 2)
+    results = []
+    for r, moved in ((rows, True), (rows.clone(memory_format=torch.contiguous_format), False)):
+        t = [torch.zeros((B, 48, 1, d), dtype=torch.uint8, device=DEV).transpose(1, 2) if moved else torch.zeros((B, 1, 48, d), dtype=torch.uint8, device=DEV) for _ in range(2)]
+        t += [torch.zeros((B, 1, 3), dtype=torch.uint8, device=DEV) for _ in range(2)]
+        c = ab.Context.kv8(*t, block, 0)
+        assert c.batch_stride == 48 * d
+        ctx.kv8_write(c, B, T, r, r, start=3)
+        results.append(t)
+    assert all(torch.equal(a, b) for a, b in zip(*results)) and int(results[0][2].max()) > 0
+    assert ctx.poll_status() == 0
+
+
+def test_rows_that_do_lie_apart_are_refused():
+    heads, B, T = "gqa28", 2, 40
+    H, hkv, d = HEADS[heads]
+    ctx = context(heads, B, 48)
+    keep, c = ctx.new_kv8(B, 48, 16, "int8")
+    for rows in (torch.zeros((B, 4, 2 * hkv, d), dtype=torch.bfloat16, device=DEV)[:, :, :hkv], torch.zeros((B, 1, hkv, 2 * d), dtype=torch.bfloat16, device=DEV)[..., :d],
+                 torch.zeros((B, 1, hkv, d, 2), dtype=torch.bfloat16, device=DEV)[..., 0]):
+        with pytest.raises(ValueError):
+            ctx.kv8_write(c, B, T, rows, rows)
+    codes, exps = torch.zeros((B, hkv, 96, d), dtype=torch.uint8, device=DEV)[:, :, :48], torch.zeros((B, hkv, 3), dtype=torch.uint8, device=DEV)
+    with pytest.raises(ValueError):
+        ab.Context.kv8(codes, codes, exps, exps, 16, 0)
