@@ -700,18 +700,6 @@ acache_status layer_step_impl(acache_ctx* ctx, const acache_layer_weights* w, co
     auto score_now = [&]() -> acache_status {
         if (do_score && !score_in_attention && req->batch > 0 && req->affix_len > 0) {
             void* qmask = wsp<void>(ctx, ctx->o_qmask);
-            acache_kv read_back{};
-            const acache_kv* keys = kv;
-            if (kv8) {
-                // the keys that the scores (and with the full normaliser, their softmax) are about, as bf16 in their places
-                const bool all = flags & ACACHE_F_SCORE_NORM_FULL;
-                const int kvd = d.n_kv_heads * d.head_dim, first = all ? 0 : req->affix_start;
-                char* at = wsp<char>(ctx, ctx->o_xstage);
-                read_back = acache_kv{at, at, (int64_t)req->ctx_len * kvd, req->ctx_len};
-                run_kv8_read(ctx, kv8, req->batch, req->ctx_len, at + (size_t)first * kvd * 2, nullptr, read_back.batch_stride,
-                             all ? req->ctx_len : req->affix_len, nullptr, first, stream);
-                keys = &read_back;
-            }
             mark(ctx, ACACHE_STAGE_MASK_Q, stream);
             if (req->n_masked > 0) {
                 int32_t* mpos = wsp<int32_t>(ctx, ctx->o_mrow_pos);
@@ -749,6 +737,18 @@ acache_status layer_step_impl(acache_ctx* ctx, const acache_layer_weights* w, co
                 ctx->launches += nl; }
             }
             mark(ctx, ACACHE_STAGE_SCORE, stream);
+            acache_kv read_back{};
+            const acache_kv* keys = kv;
+            if (kv8) {
+                // the keys that the scores (and with the full normaliser, their softmax) are about, as bf16 in their places
+                const bool all = flags & ACACHE_F_SCORE_NORM_FULL;
+                const int kvd = d.n_kv_heads * d.head_dim, first = all ? 0 : req->affix_start;
+                char* at = wsp<char>(ctx, ctx->o_xstage);
+                read_back = acache_kv{at, at, (int64_t)req->ctx_len * kvd, req->ctx_len};
+                run_kv8_read(ctx, kv8, req->batch, req->ctx_len, at + (size_t)first * kvd * 2, nullptr, read_back.batch_stride,
+                             all ? req->ctx_len : req->affix_len, nullptr, first, stream);
+                keys = &read_back;
+            }
             // with a selection to follow, the ordered sum over heads is folded into the selection kernel
             // (only while one CTA per request can read all heads' partial sums quickly: at L = 8192 the separate,
             // grid-wide head sum takes 4 us where the folded one took 28)

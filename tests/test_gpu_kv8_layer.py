@@ -142,3 +142,27 @@ def test_nothing_to_do():
     s.run(c, ab.F_SCORE | ab.F_SELECT | ab.F_NO_RECOMPUTE, scores, anchors, 0.25, req=unmasked)
     assert (scores == 0).all() and torch.equal(anchors, torch.arange(K, dtype=torch.int32, device=DEV).expand(2, K))
     assert all(torch.equal(p, q) for p, q in zip(keep, was)) and s.ctx.poll_status() == 0
+
+
+def test_stage_times_hold_the_keys_that_are_read_back():
+    """Scores on many keys: the stages' times add up to the call's."""
+    shape = wl.LayerShape(512, 32, 32, 128, 512, 1e-5, False, 5e5, "wide-heads")
+    B, T = 4, 8192
+    s = Step(shape, wl.make_layout(1, 0, T - 40, 8, 32, 32, "masked"), 64, "int8")
+    ctx = ab.Context.for_shape(shape, B, T, T - 40, 32, 32, DEV)
+    keep, c = ctx.new_kv8(B, T, 64, "int8")
+    keep[2].fill_(120)
+    x = s.dc.x.expand(B, T, 512).contiguous()
+    pos = s.dc.masked.expand(B, 32).contiguous()
+    req = ab.Context.request(B, T, 0, T - 40, pos, pos, s.dc.cos, s.dc.sin)
+    scores = torch.zeros((B, T - 40), dtype=torch.float32, device=DEV)
+    shares = []
+    ctx.stage_timing(True)
+    for i in range(12):
+        a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        a.record()
+        ctx.layer_step_kv8(s.dc.lw, req, c, x, 0, 0.0, ab.F_SCORE | ab.F_SCORE_NORM_FULL | ab.F_NO_RECOMPUTE, scores, None, None)
+        b.record()
+        shares.append(sum(ctx.read_stage_times().values()) / a.elapsed_time(b))
+    assert ctx.poll_status() == 0
+    assert np.median(shares[2:]) > 0.8, shares
