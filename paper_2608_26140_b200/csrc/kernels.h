@@ -207,11 +207,11 @@ size_t attention_scratch_bytes(int head_dim);   // bytes for part_o followed by 
 int launch_attention(const AttnArgs& a, cudaStream_t stream);
 
 // ---- kv8.cu: the cache held in 8 bits (kv8.cuh: what a code stands for) -------------------
-// codes [B, Hkv, capacity, d], exponent bytes [B, Hkv, n_blocks]; batch_stride in codes, 0 with `shared`
+// codes [B, Hkv, capacity, d], exponent bytes [B, Hkv, n_blocks]; batch_stride in codes, 0 with `shared` (of calls that only read)
 struct Kv8WriteArgs {
     uint8_t *k, *v, *k_exp, *v_exp;
     int64_t batch_stride;
-    int shared, capacity, n_blocks, block, format;
+    int capacity, n_blocks, block, format;
     int batch, n_kv_heads, head_dim, ctx_len;
     const void *k_rows, *v_rows;    // bf16 [B, n, Hkv, d], requests rows_batch_stride elements apart
     int64_t rows_batch_stride;

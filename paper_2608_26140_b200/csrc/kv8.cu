@@ -143,7 +143,7 @@ __global__ void __launch_bounds__(kWriteThreads, 4) kv8_write_kernel(const Kv8Wr
             const bool active = v < all;
             auto is_v = [&](int p) { return N == 2 ? p == 1 : v >= a.n_kv_heads; };
             const int h = !active ? 0 : N == 2 || v < a.n_kv_heads ? v : v - a.n_kv_heads;
-            const int64_t exps_at = ((int64_t)(a.shared ? 0 : b) * a.n_kv_heads + h) * a.n_blocks + blk;
+            const int64_t exps_at = ((int64_t)b * a.n_kv_heads + h) * a.n_blocks + blk;
             const int64_t rows_at = (int64_t)b * a.rows_batch_stride + h * D + piece;
             const int64_t codes_at = (int64_t)b * a.batch_stride + ((int64_t)h * a.capacity + t0) * D + piece;
             uint4 x[N][SLOTS];
