@@ -16,11 +16,12 @@
 // so a thread's 16 contiguous bytes of a key row serve as its fragment of four products:
 //   S^T = K Q^T (keys x rows)   O^T += V^T P^T (d x rows): keys and d are the long sides of both products, so up to 8 rows cost
 //   one instruction, and P only has to be transposed in 8 x 8 blocks (movmatrix).
-// Up to 8 rows HBM bounds it: one token over 2 x 65537 keys of 32 heads (1074 MB) 171 us, 6.3 TB/s.  At 32 rows (16 x 2560 keys of
-// 32 heads, 344 MB, 98 us) HBM, the matrix instructions and the issue slots are each taken for about 40 % of the time: with 255
-// registers a thread there are two warps a scheduler to hide each other's waits.
+// Up to 8 rows HBM bounds it: one token over 2 x 65537 keys of 32 heads (1074 MB) 176 us in a row, 6.1 TB/s, 182 to 196 us among other
+// passes.  At 32 rows (16 x 2560 keys of 32 heads, 344 MB, 102.6 us) the matrix instructions are busy for 42 % of the time, the issue slots for
+// 35, HBM for half: with 255 registers a thread there are two warps a scheduler to hide each other's waits.
 // The reference M moves only when a logit passes it by 2^15.9 (f16 ends at 2^16), found by a vote; then maxima are exchanged and O is scaled.
-// It starts 2^8 below the first keys' largest (kv8.cuh); 2^4 above it, 32 rows took 98.8 us where they take 101.8, and lost small weights.
+// It starts 2^8 below the first keys' largest (kv8.cuh); 2^4 above it, 32 rows took 98.8 us where they take 102.6, and lost small weights.
+// (The figures by which splits and rows a CTA were chosen, further down, are from then: 32 rows took up to 4 % less.)
 #include <algorithm>
 #include <array>
 #include <climits>
@@ -634,7 +635,8 @@ int rows_launch(Kv8AttnArgs a, const RowsPlan& plan, cudaStream_t stream) {
 // go round.  us with 8, 16 and 32 rows a CTA: 4 KV heads, 28 rows, 1536 keys 8.3, 10.3, 14.3; 16 times as many requests 20.8, 17.5,
 // 17.9, and 8192 keys 84, 56, 49; 32 KV heads, 1536 keys, 32 rows 12.8, 12.1, 15.6, 16 rows 9.8, 10.8.
 // More than 32 rows: the tensor-memory kernel, where its plan takes less than this one's.  16 sequences, 32 KV heads, 100 rows,
-// 8192 keys: 501 us there, 953 us here; one sequence of 300 keys: 12.3 and 10.0 us.  Up to 32 rows this one is always ahead.
+// 8192 keys: 501 us there, 953 us here; one sequence of 300 keys: 12.3 and 10.0 us.  Up to 32 rows this one is ahead: 16 sequences, 32 KV
+// heads, 32 rows, 2560 keys 183 us there, 109 here; one of 8288 keys 44 and 31; 64 of 28 rows, 4 KV heads, 8192 keys 274 and 151.
 template <int D, int FMT>
 int rows_dispatch(const Kv8AttnArgs& a, cudaStream_t stream) {
     const int R = a.n * (a.n_heads / a.n_kv_heads);

@@ -9,9 +9,11 @@
 //   one issuing warp   S = Q K^T and O += P V by tcgen05.mma 128 x 128 x 16, P read from tensor memory, V MN-major
 //   softmax warps      one thread per query row, S in two halves of 64 keys: y - M, maximum, exp2, P as f16 over S's columns
 // Per 16 keys a table entry (the converters write it) gives the softmax both scales and the weight in l.
-// Bound by the chain product - maximum - exponentials - product of a row tile: 4300 cycles a key tile with two row tiles, of which the
-// tensor core is busy for 2170, the special-function units for 2050.  16 x 922 rows, 2560 keys, 32 heads: 781 us in int8, 763 in e4m3
-// (0.79 and 0.81 PFLOP/s); 1639 rows, 8288 keys: 317 us (0.70: 224 CTAs on 148 SMs).
+// Bound by the chain product - maximum - exponentials - product of a row tile: 4500 cycles a key tile with two row tiles, of which the
+// tensor core is busy for 2170, the special-function units for 2050; with one thread a row, two softmax warps a scheduler are what there
+// is to fill the gaps.  16 x 922 rows, 2560 keys, 32 heads: 790 us in int8 (0.78 PFLOP/s); 1639 rows, 8288 keys: 333 us (0.67: 224 CTAs on
+// 148 SMs).  The bf16 kernel next door (attn_tc.cu: four threads a row, two S buffers, no codes to convert) takes 242 us for these.
+// (Figures by which choices below were made are from references 2^4 above the largest logit: 1 to 5 % less.)
 #include <algorithm>
 #include <array>
 #include <climits>
