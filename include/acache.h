@@ -356,9 +356,9 @@ acache_status acache_kv8_read(acache_ctx *ctx, const acache_kv8 *kv, int32_t bat
  * taken as the nearer end.
  *   q, o: DEVICE bf16 [B, n_rows, H, d], n_rows from one (a single token) to ACACHE_KV8_MAX_ROWS Hkv / H; lse: DEVICE fp32
  *   [B, n_rows, H], natural logarithm, may be NULL (with it, results over several caches can be put together).
- * Logits, softmax and sums in fp32.  Codes enter the products exactly, probabilities and queries rounded to 11 bits or, where that is
- * coarser, to 2^-33 of the row's largest probability and 2^-25 of the query's largest element.  The scales of
- * one head's values may differ by a factor of 2^100. */
+ * Logits, softmax and sums in fp32.  Codes enter the products exactly.  A probability times the scale of its value is rounded to 11
+ * bits or, where that is coarser, to 2^-33 of the row's largest such product, an element of a query to 11 bits or 2^-25 of the query's
+ * largest.  The scales of one head's values may differ by a factor of 2^100. */
 acache_status acache_kv8_attention(acache_ctx *ctx, const acache_kv8 *kv, int32_t batch, int32_t n_rows, int32_t ctx_len,
                                    const void *q, const int32_t *lens, const uint32_t *key_drop, void *o, float *lse,
                                    acache_stream_t stream);

@@ -111,6 +111,7 @@ __device__ __forceinline__ void st_global32(void* p, const uint32_t (&v)[8], boo
 // log2 units.  p is f16, normal from 2^-14 to 2^16: a new reference lies kStart below the largest logit, whose p is then 2^kStart, and moves
 // when one passes it by kRaise.  So the largest p of a row is between 2^8 and 2^16, keys 2^-22 below it keep 11 bits and what is lost of any
 // other is at most 2^-33 of the largest: thousands of keys 16 nats below a first one that says little still give their sum to 2^-10.
+// (Logits here are y, which hold the scales of the values: p is what softmax and scale make together.)
 // The price is that references move: one 4 above the largest logit moved 0.04 to 0.14 times a warp, this one 2.3 to 3 times.
 constexpr float kRaise = 15.9f, kStart = 8.f;
 constexpr int kFarApart = 100;                       // most by which E0 is above an ev

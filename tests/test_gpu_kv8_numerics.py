@@ -151,3 +151,28 @@ def test_blocks_that_hold_nothing_have_no_scale(heads, n, T, block, fmt):
     vals[1] *= 2.0 ** -100
     check_attention(ctx, cache, vals, B, n, T, heads, queries(B, n, heads, 5))
     assert ctx.poll_status() == 0
+
+
+@pytest.mark.parametrize("heads,n,T,block", PLACES)
+def test_sharp_logits_over_scales_far_apart_to_the_bound_that_is_stated(heads, n, T, block):
+    """Queries along one key, value blocks 2^30 and more apart: the key that softmax prefers may be small beside another's p times scale.
+    To the usual bound come 2^-33 of the row's largest product of a probability and a scale, for every code of a column."""
+    B = 2
+    H, hkv, d = HEADS[heads]
+    ctx = context(heads, B, T)
+    cache, vals = filled(heads, B, T, block, "int8", n + T, v_spread=8.0)
+    for at, nats in ((T // 2, 9.0), (T - 1, 25.0)):
+        k = vals[0][:, :, at].repeat_interleave(H // hkv, 1)
+        q = (k / (k ** 2).sum(-1, keepdim=True) * nats * math.sqrt(d))[:, None].expand(B, n, H, d).bfloat16().contiguous()
+        o = torch.empty_like(q)
+        ctx.kv8_attention(cache.c, B, T, q, o)
+        for b in range(B):
+            ro, _, A, X = ref_attention(q[b].double(), vals[0][b], vals[1][b], torch.ones(T, dtype=torch.bool, device=DEV))
+            assert float(X.max()) < 64
+            scale = torch.exp2(cache.dev[3][b].double() - 127).repeat_interleave(block, 1)[:, :T]
+            codes = (vals[1][b].abs() / scale[..., None]).sum(1)
+            for h in range(H):
+                p = torch.softmax(q[b, :, h].double() @ vals[0][b, h // (H // hkv)].T / math.sqrt(d), 1)
+                lost = 2.0 ** -33 * (p * scale[h // (H // hkv)]).amax(1)[:, None] * codes[h // (H // hkv)]
+                assert ((o[b, :, h].double() - ro[:, h]).abs() <= 2.0 ** -8 * ro[:, h].abs() + 2.0 ** -9 * A[:, h] + lost).all()
+    assert ctx.poll_status() == 0
