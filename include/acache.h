@@ -140,6 +140,26 @@ typedef struct {
     int32_t  format;                /* ACACHE_KV8_E4M3 or ACACHE_KV8_INT8 */
 } acache_kv8;
 
+/* One layer's KV cache in pages (the paper keeps its cache so, Section 4.1; with pages of one token the table is its read-slot map).  DEVICE
+ * bf16 pools [n_pages, Hkv, page, d], page_stride elements between two pages (at least Hkv * page * d, a multiple of 8), K after the
+ * rotary embedding; table: DEVICE int32 [B, table_stride], request b's tokens t page .. t page + page - 1 lie in page table[b, t].  Requests may name
+ * the same pages (a shared affix) as far as they only read them.  Entries behind a request's last token are not looked at. */
+typedef struct {
+    void          *k, *v;
+    int64_t        page_stride;
+    int32_t        n_pages;
+    int32_t        page;            /* tokens of a page: a power of two, 1 .. 1024 */
+    const int32_t *table;
+    int32_t        table_stride;    /* entries of a request */
+} acache_paged_kv;
+
+/* DEVICE bf16 rows [B, n, heads, d]: row i of request b at element b * batch_stride + i * row_stride (multiples of 8), its heads side by side.
+ * The rows may be columns of wider ones (a fused projection's). */
+typedef struct {
+    const void *p;
+    int64_t     batch_stride, row_stride;
+} acache_rows;
+
 /* The request batch: every request shares the layout (ctx_len, affix span, m, e). */
 typedef struct {
     int32_t batch, ctx_len;
@@ -370,6 +390,34 @@ acache_status acache_kv8_attention(acache_ctx *ctx, const acache_kv8 *kv, int32_
 acache_status acache_layer_step_kv8(acache_ctx *ctx, const acache_layer_weights *w, const acache_request *req, acache_kv8 *kv,
                                     const void *x, int x_is_compact, double ratio, uint32_t flags, float *scores,
                                     int32_t *anchor_idx, void *y, acache_stream_t stream);
+
+/* Appends rows to a cache in pages, the rotary embedding applied on the way.  Row i of request b is token lens[b] + i (lens: DEVICE int32 [B],
+ * the tokens that each request has), or token pos[b, i] (DEVICE int32 [B, n_rows]); one of lens and pos is NULL.
+ *   K: (k_j, k_{j + d/2}) -> (k_j cos - k_{j + d/2} sin, k_{j + d/2} cos + k_j sin) with row t of the tables for token t, in fp32, rounded once
+ *   V: as it is.   Q: turned as K, to q_out DEVICE bf16 [B, n_rows, H, d] (the rows q themselves, or memory that they do not touch)
+ * counts (DEVICE int32 [B], NULL: n_rows each): rows of each request; nothing is done for the rows behind them, in q_out neither.
+ * rope_cos, rope_sin: DEVICE fp32 [>= ctx_len, d/2], both NULL: K and Q are as they are.  q, q_out: both NULL without queries.
+ * A row whose token lies outside [0, ctx_len), or whose page is none of the pool's, raises ACACHE_FLAG_BAD_INDEX and is skipped (its query
+ * too); so does a count outside [0, n_rows], which is taken as the nearer end.  Of two rows of one token in pos the last is written.  A page
+ * that is written to has to be named by one request only, once.  ctx_len: at most table_stride * page, and 2^30; batch: at most 65535.
+ * The descriptor's max_ctx and max_rows are no limit here and in acache_paged_attention. */
+acache_status acache_paged_append(acache_ctx *ctx, acache_paged_kv *kv, int32_t batch, int32_t ctx_len, const acache_rows *k,
+                                  const acache_rows *v, const acache_rows *q, void *q_out, int32_t n_rows, const int32_t *lens,
+                                  const int32_t *pos, const int32_t *counts, const float *rope_cos, const float *rope_sin,
+                                  acache_stream_t stream);
+
+/* Bidirectional attention of few rows (new tokens, the block being decoded) over a cache in pages:
+ *   o[b, i, h] = sum_j softmax_j(q[b, i, h] . K[b, j, kv(h)] / sqrt(d)) V[b, j, kv(h)],   lse[b, i, h] = log sum_j exp(...)
+ * over the positions j < lens[b] (DEVICE int32 [B]; NULL: ctx_len) that exist: bit j % 32 of key_drop[b, j / 32] is clear
+ * (DEVICE uint32 [B, ceil(ctx_len / 32)]; NULL: all).  Where there is none, o = 0 and lse = -inf.  What the pages hold in
+ * places that do not count is of no account, NaN included.  A length outside [0, ctx_len] raises ACACHE_FLAG_BAD_INDEX and is
+ * taken as the nearer end; so does a page that is none of the pool's, whose keys do not exist.
+ *   q, o: DEVICE bf16 [B, n_rows, H, d], any number of rows (every 32 rows of a KV head, n_rows H / Hkv, read the keys once); lse: DEVICE fp32
+ *   [B, n_rows, H], natural logarithm, may be NULL (with it, results over several caches can be put together).
+ * Logits, softmax and sums in fp32; a probability is rounded to bf16 where it meets its value. */
+acache_status acache_paged_attention(acache_ctx *ctx, const acache_paged_kv *kv, int32_t batch, int32_t n_rows, int32_t ctx_len,
+                                     const void *q, const int32_t *lens, const uint32_t *key_drop, void *o, float *lse,
+                                     acache_stream_t stream);
 
 /* Predict-then-commit on the current block (Section 3.1, Eq. 2-3, with the confidence-threshold
  * commit rule the paper's set-up uses, threshold 0.9 in Section 5):

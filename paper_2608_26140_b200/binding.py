@@ -27,7 +27,8 @@ EXPORTS = ["acache_create", "acache_workspace_bytes", "acache_set_workspace", "a
            "acache_commit_update", "acache_generate_block", "acache_denoise_step_shared", "acache_recompute_rows_shared",
            "acache_decode_step_shared", "acache_generate_block_shared", "acache_layer_step_shared",
            "acache_host_x_in_place", "acache_score_kv_deviation", "acache_debug_expire_next_wait",
-           "acache_kv8_write", "acache_kv8_read", "acache_kv8_attention", "acache_layer_step_kv8"]
+           "acache_kv8_write", "acache_kv8_read", "acache_kv8_attention", "acache_layer_step_kv8",
+           "acache_paged_append", "acache_paged_attention"]
 
 STAGES = ["mask_q", "score", "topk", "gather_norm", "qkv", "attention", "oproj", "mlp_norm", "gate_up", "down"]
 
@@ -53,6 +54,16 @@ class KV8(C.Structure):
     _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_exp", C.c_void_p), ("v_exp", C.c_void_p), ("batch_stride", C.c_int64),
                 ("ctx_capacity", C.c_int32), ("block", C.c_int32), ("format", C.c_int32)]
     made_of = None      # of the tensors that Context.kv8 made it over: requests (shared: any number), KV heads, head dimension, all on a GPU
+
+
+class PagedKV(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("page_stride", C.c_int64), ("n_pages", C.c_int32), ("page", C.c_int32),
+                ("table", C.c_void_p), ("table_stride", C.c_int32)]
+    made_of = None      # of the tensors that Context.paged_kv made it over: requests, KV heads, head dimension, all on a GPU
+
+
+class Rows(C.Structure):
+    _fields_ = [("p", C.c_void_p), ("batch_stride", C.c_int64), ("row_stride", C.c_int64)]
 
 
 class Request(C.Structure):
@@ -163,6 +174,11 @@ def load_library(path: Optional[str] = None) -> C.CDLL:
     lib.acache_layer_step_kv8.argtypes = [vp, C.POINTER(LayerWeights), C.POINTER(Request), C.POINTER(KV8), vp, C.c_int,
                                           C.c_double, u32, vp, vp, vp, vp]
     lib.acache_layer_step_kv8.restype = C.c_int
+    rows = C.POINTER(Rows)
+    lib.acache_paged_append.argtypes = [vp, C.POINTER(PagedKV), i32, i32, rows, rows, rows, vp, i32, vp, vp, vp, vp, vp, vp]
+    lib.acache_paged_append.restype = C.c_int
+    lib.acache_paged_attention.argtypes = [vp, C.POINTER(PagedKV), i32, i32, i32, vp, vp, vp, vp, vp, vp]
+    lib.acache_paged_attention.restype = C.c_int
     lib.acache_stage_timing.argtypes = [vp, C.c_int]
     lib.acache_stage_timing.restype = C.c_int
     lib.acache_read_stage_times.argtypes = [vp, C.POINTER(C.c_float)]
@@ -295,6 +311,22 @@ class Context:
         t += [torch.zeros((batch, hkv, cap // block), dtype=torch.uint8, device=self.device) for _ in range(2)]
         return t, self.kv8(*t, block, KV8_FORMATS[fmt])
 
+    def paged_kv(self, k_pages, v_pages, table) -> PagedKV:
+        """Cache in pages over bf16 pools [n_pages, Hkv, page, d] and a table int32 [B, entries]: the pages of each request in order.  Pages may
+        lie further apart than they take."""
+        import torch
+        n_pages, hkv, page, d = k_pages.shape
+        for p in (k_pages, v_pages):
+            if p.dtype is not torch.bfloat16 or p.shape != k_pages.shape or not _dense(p, (page * d, d, 1)) or (n_pages > 1 and p.stride(0) != k_pages.stride(0)):
+                raise ValueError(f"pools {tuple(k_pages.shape)} and {tuple(v_pages.shape)} are not bf16 [n_pages, Hkv, page, d] of one layout, a page contiguous")
+        if table.dtype is not torch.int32 or table.dim() != 2 or not table.is_contiguous():
+            raise ValueError("the table is a contiguous int32 [B, entries]")
+        if (hkv, d) != self.heads[1:]:
+            raise ValueError(f"pages of {hkv} KV heads of {d} for a context of {self.heads[1]} of {self.heads[2]}")
+        c = PagedKV(_ptr(k_pages), _ptr(v_pages), k_pages.stride(0) if n_pages > 1 else hkv * page * d, n_pages, page, _ptr(table), table.shape[1])
+        c.made_of = (table.shape[0], hkv, d, all(t.is_cuda for t in (k_pages, v_pages, table)))
+        return c
+
     @staticmethod
     def pack_key_drop(drop):
         """Boolean [B, T] (True: the position does not exist as a key) as the bit mask of kv8_attention, int32 [B, ceil(T / 32)]."""
@@ -417,6 +449,63 @@ class Context:
         self._cache_fits(cache, req.batch)
         self._check(self.lib.acache_layer_step_kv8(self.h, C.byref(w), C.byref(req), C.byref(cache), _ptr(x), int(x_is_compact),
                                                    float(ratio), int(flags), _ptr(scores), _ptr(anchor_idx), _ptr(y), _stream()))
+
+    def paged_append(self, cache: PagedKV, ctx_len, k, v, lens=None, pos=None, counts=None, rope=None, q=None, q_out=None):
+        """Rows k, v [B, n, Hkv, d] (bf16; rows and requests may lie apart) as tokens lens[b] .. or pos [B, n] (int32), turned by rope = (cos, sin)
+        [>= ctx_len, d / 2] (fp32) on the way; counts [B]: rows of each request; q [B, n, H, d] turned likewise to q_out."""
+        import torch
+        B, n = k.shape[0], k.shape[1]
+        self._cache_fits(cache, B)
+        if v.shape != k.shape:
+            raise ValueError(f"k {tuple(k.shape)} and v {tuple(v.shape)} differ in shape")
+        at_k, at_v = self._rows_at(k, B, n, self.heads[1]), self._rows_at(v, B, n, self.heads[1])
+        at_q = None if q is None else self._rows_at(q, B, n, self.heads[0])
+        if (q is None) != (q_out is None):
+            raise ValueError("q and q_out go together")
+        if q_out is not None:
+            _check_tensor(q_out, torch.bfloat16, q.shape)
+        for t, shape in ((lens, (B,)), (counts, (B,)), (pos, (B, n))):
+            if t is not None:
+                _check_tensor(t, torch.int32, shape)
+        cos = sin = None
+        if rope is not None:
+            cos, sin = rope
+            for t in rope:
+                _check_tensor(t, torch.float32, (t.shape[0], self.heads[2] // 2))
+                if t.shape[0] < ctx_len:
+                    raise ValueError(f"a rope table of {t.shape[0]} rows for a context of {ctx_len}")
+        self._check(self.lib.acache_paged_append(self.h, C.byref(cache), B, ctx_len, at_k, at_v, at_q, _ptr(q_out), n, _ptr(lens), _ptr(pos),
+                                                 _ptr(counts), _ptr(cos), _ptr(sin), _stream()))
+
+    def paged_attention(self, cache: PagedKV, ctx_len, q, o, lse=None, lens=None, key_drop=None):
+        """q, o: bf16 [B, n, H, d]; lse: fp32 [B, n, H]; lens: int32 [B]; key_drop: int32 [B, ceil(ctx_len / 32)] (pack_key_drop)."""
+        import torch
+        shape = q.shape
+        B, n, H, d = shape
+        self._cache_fits(cache, B)
+        if H != self.heads[0] or d != self.heads[2]:
+            raise ValueError(f"q {tuple(shape)} is not [B, n, H, d]")
+        _check_tensor(q, torch.bfloat16, shape)
+        _check_tensor(o, torch.bfloat16, shape)
+        if lse is not None:
+            _check_tensor(lse, torch.float32, shape[:3])
+        if lens is not None:
+            _check_tensor(lens, torch.int32, (B,))
+        if key_drop is not None:
+            _check_tensor(key_drop, torch.int32, (B, -(-ctx_len // 32)))
+        self._check(self.lib.acache_paged_attention(self.h, C.byref(cache), B, n, ctx_len, q.data_ptr(), _ptr(lens), _ptr(key_drop),
+                                                    o.data_ptr(), _ptr(lse), _stream()))
+
+    def _rows_at(self, t, B, n, heads):
+        """Where rows [B, n, heads, d] lie; the heads of a row side by side."""
+        import torch
+        d = self.heads[2]
+        if t.shape != (B, n, heads, d) or t.dtype is not torch.bfloat16 or not t.is_cuda:
+            raise ValueError(f"rows {tuple(t.shape)} of {t.dtype} on {t.device} are not bf16 [B, n, {heads}, {d}] on a GPU")
+        batch, row, head, one = t.stride()
+        if (head != d and heads > 1) or one != 1:
+            raise ValueError("the heads of a row lie side by side")
+        return C.byref(Rows(t.data_ptr(), batch if B > 1 else 0, row if n > 1 else heads * d))
 
     def _cache_fits(self, cache, batch):
         """What a call would read or write past the cache's tensors for (a KV8 filled in by hand is the caller's affair)."""

@@ -194,6 +194,55 @@ acache_status run_kv8_attention(acache_ctx* c, const acache_kv8* kv, int32_t bat
     return check_cuda(c, "8-bit attention");
 }
 
+// The cache in pages of a call.
+acache_status check_paged(acache_ctx* c, const acache_paged_kv* kv, int32_t batch, int32_t ctx_len) {
+    const acache_model_desc& d = c->d;
+    if (!c->ws) return fail(c, ACACHE_ERR_WORKSPACE, "workspace not set");
+    if (!kv) return fail(c, ACACHE_ERR_INVALID_ARG, "paged kv is NULL");
+    if (batch < 0 || batch > d.max_batch) return fail(c, ACACHE_ERR_INVALID_ARG, "batch %d outside [0, %d]", batch, d.max_batch);
+    if (batch > 65535) return fail(c, ACACHE_ERR_UNSUPPORTED_SHAPE, "batch %d above 65535", batch);
+    if (!kv->k || !kv->v || !aligned16(kv->k) || !aligned16(kv->v) || !kv->table)
+        return fail(c, ACACHE_ERR_INVALID_ARG, "page pool or table NULL, or the pool misaligned");
+    if (kv->page <= 0 || kv->page > 1024 || (kv->page & (kv->page - 1)))
+        return fail(c, ACACHE_ERR_UNSUPPORTED_SHAPE, "pages of %d tokens: not a power of two up to 1024", kv->page);
+    if (kv->n_pages <= 0 || kv->table_stride < 0) return fail(c, ACACHE_ERR_INVALID_ARG, "n_pages %d / table_stride %d out of range", kv->n_pages, kv->table_stride);
+    if (kv->page_stride < (int64_t)d.n_kv_heads * kv->page * d.head_dim || (kv->page_stride & 7))
+        return fail(c, ACACHE_ERR_INVALID_ARG, "page_stride smaller than a page or not a multiple of 8");
+    if (ctx_len < 0 || ctx_len > (1 << 30) || ctx_len > (int64_t)kv->table_stride * kv->page)
+        return fail(c, ACACHE_ERR_INVALID_ARG, "ctx_len %d outside what %d pages of %d tokens hold", ctx_len, kv->table_stride, kv->page);
+    return ACACHE_OK;
+}
+
+Pages pages_of(const acache_paged_kv* kv) {
+    int log2_page = 0;
+    while ((1 << log2_page) < kv->page) ++log2_page;
+    return Pages{kv->table, kv->table_stride, kv->n_pages, log2_page, kv->page_stride};
+}
+
+// rows of `heads` heads that lie apart as r says
+bool rows_ok(const acache_ctx* c, const acache_rows* r, int heads, int32_t batch, int32_t n) {
+    return r->p && aligned16(r->p) && (r->batch_stride & 7) == 0 && (r->row_stride & 7) == 0 && (batch <= 1 || r->batch_stride >= 0) &&
+           (n <= 1 || r->row_stride >= (int64_t)heads * c->d.head_dim);
+}
+
+acache_status run_paged_attention(acache_ctx* c, const acache_paged_kv* kv, int32_t batch, int32_t n, int32_t ctx_len, const void* q, void* o,
+                                  float* lse, const int32_t* lens, const uint32_t* key_drop, cudaStream_t st) {
+    const acache_model_desc& d = c->d;
+    PagedAttnArgs a{};
+    a.pages = pages_of(kv);
+    a.k = kv->k; a.v = kv->v; a.q = q; a.o = o; a.lse = lse;
+    a.batch = batch; a.n = n; a.ctx_len = ctx_len; a.n_heads = d.n_heads; a.n_kv_heads = d.n_kv_heads; a.head_dim = d.head_dim;
+    a.lens = lens; a.key_drop = key_drop; a.drop_words = (ctx_len + 31) / 32;
+    a.scale_log2e = 1.4426950408889634f / sqrtf((float)d.head_dim);
+    a.part = wsp<float>(c, c->o_gemm);           // the projections' partial tiles: no projection runs beside an attention
+    a.arrived = wsp<unsigned int>(c, c->o_arrived);
+    a.status = wsp<uint32_t>(c, c->o_status);
+    const int nl = launch_paged_attention(a, st);
+    if (nl < 0) return check_cuda(c, "paged attention") == ACACHE_OK ? fail(c, ACACHE_ERR_CUDA, "paged attention launch failed") : ACACHE_ERR_CUDA;
+    c->launches += nl;
+    return check_cuda(c, "paged attention");
+}
+
 // Q for the masked rows, then Eq. 4-5.
 acache_status run_score(acache_ctx* c, const acache_request* r, const void* q_mask, const acache_kv* kv,
                         float* scores, int accumulate, int norm_full, int defer_head_sum, cudaStream_t st, int early_k = 0) {
@@ -475,6 +524,7 @@ acache_status acache_create(const acache_model_desc* desc, acache_ctx** out) {
         pb = std::max(pb, gemm_partial_bytes(nri, d.ffn, d.hidden, false));
         pb = std::max(pb, gemm_partial_bytes(nmi, d.hidden, qd, false));
         pb = std::max(pb, kv8_attention_scratch_bytes(d.head_dim));
+        pb = std::max(pb, paged_attention_scratch_bytes(d.head_dim));
         c->o_gemm = take(cur, pb);
     }
     c->o_attn = take(cur, attention_scratch_bytes(d.head_dim));
@@ -851,6 +901,51 @@ acache_status acache_kv8_attention(acache_ctx* ctx, const acache_kv8* kv, int32_
     if (!kv8_rows_fit(ctx, n_rows)) return fail(ctx, ACACHE_ERR_UNSUPPORTED_SHAPE, "%d rows of a request are more than %d per KV head", n_rows, ACACHE_KV8_MAX_ROWS);
     if (!q || !o || !aligned16(q) || !aligned16(o)) return fail(ctx, ACACHE_ERR_INVALID_ARG, "q / o NULL or misaligned");
     return run_kv8_attention(ctx, kv, batch, n_rows, ctx_len, q, o, lse, lens, key_drop, stream);
+}
+
+acache_status acache_paged_append(acache_ctx* ctx, acache_paged_kv* kv, int32_t batch, int32_t ctx_len, const acache_rows* k,
+                                  const acache_rows* v, const acache_rows* q, void* q_out, int32_t n_rows, const int32_t* lens,
+                                  const int32_t* pos, const int32_t* counts, const float* rope_cos, const float* rope_sin,
+                                  acache_stream_t stream) {
+    if (!ctx) return ACACHE_ERR_INVALID_ARG;
+    acache_status s = check_paged(ctx, kv, batch, ctx_len);
+    if (s != ACACHE_OK) return s;
+    const acache_model_desc& d = ctx->d;
+    if (n_rows < 0) return fail(ctx, ACACHE_ERR_INVALID_ARG, "n_rows %d is negative", n_rows);
+    if (batch == 0 || n_rows == 0) return ACACHE_OK;
+    if ((lens != nullptr) == (pos != nullptr)) return fail(ctx, ACACHE_ERR_INVALID_ARG, "one of lens and pos is wanted");
+    if ((q != nullptr) != (q_out != nullptr)) return fail(ctx, ACACHE_ERR_INVALID_ARG, "q and q_out go together");
+    if ((rope_cos != nullptr) != (rope_sin != nullptr) || !aligned16(rope_cos) || !aligned16(rope_sin))
+        return fail(ctx, ACACHE_ERR_INVALID_ARG, "one rope table without the other, or misaligned");
+    if (!k || !v || !rows_ok(ctx, k, d.n_kv_heads, batch, n_rows) || !rows_ok(ctx, v, d.n_kv_heads, batch, n_rows) ||
+        (q && (!rows_ok(ctx, q, d.n_heads, batch, n_rows) || !aligned16(q_out))))
+        return fail(ctx, ACACHE_ERR_INVALID_ARG, "rows NULL or misaligned, or strides that are no multiples of 8 or let rows overlap");
+    PagedAppendArgs a{};
+    a.pages = pages_of(kv);
+    a.k = kv->k; a.v = kv->v;
+    a.k_rows = Rows{k->p, k->batch_stride, k->row_stride};
+    a.v_rows = Rows{v->p, v->batch_stride, v->row_stride};
+    if (q) a.q_rows = Rows{q->p, q->batch_stride, q->row_stride};
+    a.q_out = q_out;
+    a.batch = batch; a.n = n_rows; a.ctx_len = ctx_len; a.n_heads = d.n_heads; a.n_kv_heads = d.n_kv_heads; a.head_dim = d.head_dim;
+    a.lens = lens; a.pos = pos; a.counts = counts; a.rope_cos = rope_cos; a.rope_sin = rope_sin;
+    a.status = wsp<uint32_t>(ctx, ctx->o_status);
+    const int nl = launch_paged_append(a, stream);
+    if (nl < 0) return check_cuda(ctx, "paged append") == ACACHE_OK ? fail(ctx, ACACHE_ERR_CUDA, "paged append launch failed") : ACACHE_ERR_CUDA;
+    ctx->launches += nl;
+    return check_cuda(ctx, "paged append");
+}
+
+acache_status acache_paged_attention(acache_ctx* ctx, const acache_paged_kv* kv, int32_t batch, int32_t n_rows, int32_t ctx_len, const void* q,
+                                     const int32_t* lens, const uint32_t* key_drop, void* o, float* lse, acache_stream_t stream) {
+    if (!ctx) return ACACHE_ERR_INVALID_ARG;
+    acache_status s = check_paged(ctx, kv, batch, ctx_len);
+    if (s != ACACHE_OK) return s;
+    if (n_rows < 0 || (int64_t)n_rows * (ctx->d.n_heads / ctx->d.n_kv_heads) > (1 << 30))
+        return fail(ctx, ACACHE_ERR_INVALID_ARG, "n_rows %d is negative or too large", n_rows);
+    if (batch == 0 || n_rows == 0) return ACACHE_OK;
+    if (!q || !o || !aligned16(q) || !aligned16(o)) return fail(ctx, ACACHE_ERR_INVALID_ARG, "q / o NULL or misaligned");
+    return run_paged_attention(ctx, kv, batch, n_rows, ctx_len, q, o, lse, lens, key_drop, stream);
 }
 
 acache_status acache_predict_commit(acache_ctx* ctx, const void* h, int32_t h_rows, const int32_t* block_rows,

@@ -260,4 +260,46 @@ constexpr int kKv8Counters = 4096;
 size_t kv8_attention_scratch_bytes(int head_dim);
 int launch_kv8_attention(const Kv8AttnArgs& a, cudaStream_t stream);     // kernels launched, or -1
 
+// ---- paged.cu: the cache in pages ---------------------------------------------------------
+// pool [n_pages, Hkv, 1 << log2_page, d], pages page_stride elements apart; table [B, table_stride]: each request's pages in order
+struct Pages {
+    const int32_t* table;
+    int table_stride, n_pages, log2_page;
+    int64_t page_stride;
+};
+struct Rows {                       // bf16 [B, n, heads, d], the heads of a row side by side
+    const void* p;
+    int64_t batch_stride, row_stride;   // elements
+};
+struct PagedAppendArgs {
+    Pages pages;
+    void *k, *v;
+    Rows k_rows, v_rows, q_rows;    // q_rows.p null: no queries
+    void* q_out;                    // [B, n, H, d]
+    int batch, n, ctx_len, n_heads, n_kv_heads, head_dim;
+    const int32_t *lens, *pos, *counts;    // of pos [B, n] and lens [B] one is null; counts [B] or null: rows of each request
+    const float *rope_cos, *rope_sin;      // [>= ctx_len, d / 2], or null: keys and queries as they are
+    uint32_t* status;
+};
+int launch_paged_append(const PagedAppendArgs& a, cudaStream_t stream);     // kernels launched, or -1
+
+// ---- paged_attn.cu ------------------------------------------------------------------------
+struct PagedAttnArgs {
+    Pages pages;
+    const void *k, *v;
+    const void* q;                  // bf16 [B, n, H, d]
+    void* o;                        // bf16 [B, n, H, d]
+    float* lse;                     // fp32 [B, n, H] or null
+    int batch, n, ctx_len, n_heads, n_kv_heads, head_dim;
+    const int32_t* lens;            // [B] or null: keys of each request
+    const uint32_t* key_drop;       // [B, drop_words] or null: bit t = position t does not exist as a key
+    int drop_words;
+    float scale_log2e;              // log2(e) / sqrt(d)
+    float* part;                    // scratch of paged_attention_scratch_bytes()
+    unsigned int* arrived;          // kKv8Counters words that are zero between launches
+    uint32_t* status;
+};
+size_t paged_attention_scratch_bytes(int head_dim);
+int launch_paged_attention(const PagedAttnArgs& a, cudaStream_t stream);    // kernels launched, or -1
+
 }  // namespace acache

@@ -1,0 +1,452 @@
+// Attention of few query rows over a cache in pages.
+//
+//   o_r = sum_j p_rj V_j / sum_j p_rj,   p_rj = 2^(x_rj - M_r),   x_rj = log2(e) / sqrt(d) q_r K_j
+//
+// in one pass over the keys, M_r a running reference.  Keys and values are the long sides of both products,
+//   S^T = K Q^T (keys x rows),   O^T += V^T P^T (d x rows),
+// so that up to 8 rows (the query heads of a KV head, times the tokens) cost one matrix instruction for every 16 keys and 16 d; P only has
+// to be transposed in 8 x 8 blocks (movmatrix).  P is rounded to bf16, as V is: 2^-8 of each probability at most; its sum is not.
+//
+// The work of all requests, KV heads and row tiles is one line of units of 64 keys, cut into equal pieces, one a CTA, whatever
+// the requests' lengths (they are known on the device only).  A CTA that does not have all keys of an item leaves a partial result
+// and the last one to arrive adds the parts up, in their order.
+// A warp streams 16 keys a step through a ring of its own in shared memory (cp.async, whole rows side by side, the page's number asked for a
+// step ahead), swizzled so that ldmatrix meets different banks.  Keys that do not count are not read: their places are zero.
+#include <algorithm>
+
+#include "kernels.h"
+#include "kv8.cuh"
+#include "launch.h"
+#include "per_device.h"
+
+namespace acache {
+namespace {
+
+constexpr int PW = 4;                    // warps of a CTA
+constexpr int PSTEP = 16;                // keys of a warp's step
+constexpr int PSTAGES = 3;
+constexpr int kUnit = PW * PSTEP;        // keys of a unit of work
+constexpr int kMinUnits = 2;             // fewest units that are worth a CTA
+constexpr int kPlaces = 2 * 148;         // CTAs that run at a time
+constexpr float kPagedRaise = 8.f;       // M moves when a logit passes it by this (log2): P and sums stay within 2^8 of what they are with M the largest
+
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t v) {
+    uint32_t r;
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+    return r;
+}
+__device__ __forceinline__ void cp_async16_or_zero(uint32_t dst, const void* src, bool on) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;\n" ::"r"(dst), "l"(src), "r"(on ? 16 : 0) : "memory");
+}
+template <int N>
+__device__ __forceinline__ void ring_wait() { asm volatile("cp.async.wait_group %0;\n" ::"n"(N) : "memory"); }
+
+template <int D, int NT>
+struct PagedLayout {
+    static constexpr int ROWS = 8 * NT;
+    static constexpr int HALF = PSTEP * D * 2;               // bytes of a stage's keys, then its values
+    static constexpr int STAGE = 2 * HALF;
+    static constexpr int RING = PW * PSTAGES * STAGE;
+    static constexpr int MERGE = PW * ROWS * (D + 4) * 4;    // the warps' results, in the ring's place
+    static constexpr int QS = (D / 16) * NT * 32 * 8;        // the queries as fragments
+    static constexpr int SMEM = (RING > MERGE ? RING : MERGE) + QS;
+};
+
+// Units of a request's items (row tile and KV head): one for an empty request too, which has outputs like any other.
+__device__ __forceinline__ int units_of(int len) { return max(1, (len + kUnit - 1) / kUnit); }
+
+template <int D, int NT>
+__global__ void __launch_bounds__(PW * 32, 2) paged_attn_kernel(const PagedAttnArgs a) {
+    using L = PagedLayout<D, NT>;
+    extern __shared__ __align__(128) unsigned char smem[];
+    __shared__ float stat[2][PW][8 * NT];                    // references, denominators
+    __shared__ uint32_t there_of[PW][PSTAGES];               // a stage's keys that count
+    __shared__ long long sums[PW];
+    __shared__ long long at_request[2];                      // (request, first unit of it) that this CTA begins with
+    __shared__ int is_last;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
+    pdl_wait();
+    pdl_launch_dependents();
+    const int hkv = a.n_kv_heads, G = a.n_heads / hkv, R = a.n * G, tiles = (R + L::ROWS - 1) / L::ROWS, per_request = hkv * tiles;
+    uint2* qs = reinterpret_cast<uint2*>(smem + L::SMEM - L::QS);
+
+    // ---- this CTA's share of the units ----
+    auto len_of = [&](int b) { return a.lens ? min(max(a.lens[b], 0), a.ctx_len) : a.ctx_len; };
+    int64_t total, mine_lo, mine_hi;
+    int ctas;                                                // that have work
+    auto share = [&](int64_t units) {
+        total = units;
+        ctas = (int)min((int64_t)gridDim.x, max((int64_t)1, units / kMinUnits));
+        mine_lo = units * blockIdx.x / ctas;
+        mine_hi = units * (blockIdx.x + 1) / ctas;
+    };
+    int b;
+    int64_t b_lo;                                            // first unit of request b
+    if (!a.lens) {
+        const int64_t u = (int64_t)units_of(a.ctx_len) * per_request;
+        share(u * a.batch);
+        if ((int)blockIdx.x >= ctas) return;
+        b = (int)(mine_lo / u);
+        b_lo = u * b;
+    } else {
+        // the threads count the units of equal runs of requests; the one whose run holds the first unit of the share finds its request
+        const int run = (a.batch + PW * 32 - 1) / (PW * 32), r0 = min(tid * run, a.batch), r1 = min(r0 + run, a.batch);
+        int64_t sum = 0;
+        for (int r = r0; r < r1; ++r) {
+            const int len = a.lens[r];
+            if (blockIdx.x == 0 && (len < 0 || len > a.ctx_len)) atomicOr(a.status, kFlagBadIndex);
+            sum += (int64_t)units_of(len_of(r)) * per_request;
+        }
+        int64_t upto = sum;
+#pragma unroll
+        for (int off = 1; off < 32; off <<= 1) {
+            const int64_t v = __shfl_up_sync(0xffffffffu, upto, off);
+            if (lane >= off) upto += v;
+        }
+        if (lane == 31) sums[warp] = upto;
+        __syncthreads();
+        int64_t all = 0;
+#pragma unroll
+        for (int w = 0; w < PW; ++w) {
+            if (w == warp) upto += all;
+            all += sums[w];
+        }
+        share(all);
+        if ((int)blockIdx.x >= ctas) return;
+        int64_t lo = upto - sum;
+        if (lo <= mine_lo && mine_lo < upto) {
+            int r = r0;
+            for (; r < r1 - 1; ++r) {
+                const int64_t u = (int64_t)units_of(len_of(r)) * per_request;
+                if (mine_lo < lo + u) break;
+                lo += u;
+            }
+            at_request[0] = r;
+            at_request[1] = lo;
+        }
+        __syncthreads();
+        b = (int)at_request[0];
+        b_lo = at_request[1];
+    }
+    if (mine_hi <= mine_lo) return;
+
+    const int page_mask = (1 << a.pages.log2_page) - 1;
+    const bool whole = a.pages.log2_page >= 4;               // a step's keys lie in one page
+    const __nv_bfloat16 *kp = static_cast<const __nv_bfloat16*>(a.k), *vp = static_cast<const __nv_bfloat16*>(a.v);
+    constexpr int PIECES = D / 8;                            // 16-byte pieces of a row
+    constexpr int PASS = 32 / PIECES, PASSES = PSTEP / PASS;
+    const int row0 = lane / PIECES, piece = lane % PIECES;
+    const uint32_t ring = smem_u32(smem) + warp * (PSTAGES * L::STAGE);
+    const uint32_t put = ring + row0 * D * 2 + ((piece ^ row0) << 4);        // of the pass i: the row i PASS further, swizzled by its number
+    const int mrow = lane & 7, mj = lane >> 3;               // ldmatrix: this lane's row of the matrix mj
+    const uint32_t k_get = ((mj & 1) * 8 + mrow) * D * 2 + (((mj >> 1) ^ mrow) << 4);
+    const uint32_t v_get = L::HALF + ((mj >> 1) * 8 + mrow) * D * 2 + (((mj & 1) ^ mrow) << 4);
+
+    int64_t unit = mine_lo;
+    while (unit < mine_hi) {
+        // ---- the item and this CTA's keys of it ----
+        int len = len_of(b), units = units_of(len);
+        while (unit >= b_lo + (int64_t)units * per_request) {
+            b_lo += (int64_t)units * per_request;
+            ++b;
+            len = len_of(b);
+            units = units_of(len);
+        }
+        const int item = (int)((unit - b_lo) / units), tile = item % tiles, kvh = item / tiles;
+        const int64_t item_lo = b_lo + (int64_t)item * units, item_hi = item_lo + units;
+        const int64_t seg_hi = min(item_hi, mine_hi);
+        const int key_lo = (int)(unit - item_lo) * kUnit, key_hi = min(len, (int)(seg_hi - item_lo) * kUnit);
+        const int steps = max(0, (key_hi - key_lo + PSTEP - 1) / PSTEP), my_steps = (steps - warp + PW - 1) / PW;
+        const int32_t* table = a.pages.table + (int64_t)b * a.pages.table_stride;
+
+        // ---- queries as fragments, the rows dealt out to the warps ----
+        __syncthreads();                                     // nobody reads the last item's any more
+        for (int f = warp; f < (D / 16) * NT; f += PW) {
+            const int ks = f / NT, r = tile * L::ROWS + (f % NT) * 8 + g;
+            uint2 q = make_uint2(0u, 0u);
+            if (r < R) {
+                const uint32_t* from = reinterpret_cast<const uint32_t*>(static_cast<const __nv_bfloat16*>(a.q) +
+                                                                         ((int64_t)(b * (int64_t)a.n + r / G) * a.n_heads + kvh * G + r % G) * D + ks * 16);
+                q = make_uint2(__ldg(from + t), __ldg(from + t + 4));
+            }
+            qs[f * 32 + lane] = q;
+        }
+
+        // ---- the ring ----
+        int entry = 0;                                       // page of this lane's key of the next step to be fetched
+        uint32_t drop = 0u;
+        auto look_up = [&](int s) {
+            if (s >= my_steps) return;
+            const int key0 = key_lo + (warp + s * PW) * PSTEP, key = key0 + (whole ? 0 : lane & 15);
+            entry = key < key_hi ? __ldg(table + (key >> a.pages.log2_page)) : 0;
+            drop = a.key_drop ? __ldg(a.key_drop + (int64_t)b * a.drop_words + (key0 >> 5)) >> (key0 & 16) : 0u;
+        };
+        auto fetch = [&](int s, int stage) {
+            if (s < my_steps) {
+                const int key0 = key_lo + (warp + s * PW) * PSTEP, left = key_hi - key0;
+                const bool good = entry >= 0 && entry < a.pages.n_pages;
+                uint32_t there = (left >= PSTEP ? 0xFFFFu : (1u << left) - 1u) & ~drop;
+                const uint32_t known = __ballot_sync(0xffffffffu, good);
+                if (known != 0xffffffffu) {                  // keys in pages that are none do not count
+                    if ((there & ~known) != 0u && lane == 0) atomicOr(a.status, kFlagBadIndex);
+                    there &= known;
+                }
+                if (lane == 0) there_of[warp][stage] = there;
+                const int64_t off = (good ? entry * a.pages.page_stride : 0) +
+                                    (((int64_t)kvh << a.pages.log2_page) + ((key0 + (whole ? 0 : lane & 15)) & page_mask)) * D;
+                const uint32_t to = put + stage * L::STAGE;
+#pragma unroll
+                for (int i = 0; i < PASSES; ++i) {
+                    const int row = i * PASS + row0;
+                    const int64_t at = (whole ? off + row * D : __shfl_sync(0xffffffffu, off, row)) + piece * 8;
+                    const bool on = (there >> row) & 1u;
+                    const uint32_t dst = (to + i * PASS * D * 2) ^ (((i * PASS) & 7) << 4);
+                    cp_async16_or_zero(dst, kp + at, on);
+                    cp_async16_or_zero(dst + L::HALF, vp + at, on);
+                }
+            }
+            cp_async_commit();
+        };
+        look_up(0);
+#pragma unroll
+        for (int s = 0; s < PSTAGES - 1; ++s) {
+            fetch(s, s);
+            look_up(s + 1);
+        }
+        __syncthreads();                                     // the queries are there
+
+        constexpr bool Q_REGS = NT * D <= 256;
+        uint2 qf[Q_REGS ? D / 16 : 1][Q_REGS ? NT : 1];
+        if constexpr (Q_REGS) {
+#pragma unroll
+            for (int ks = 0; ks < D / 16; ++ks)
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) qf[ks][nt] = qs[(ks * NT + nt) * 32 + lane];
+        }
+        float o[D / 16][NT][4];
+        float m[NT][2], l[NT][2];                            // references, denominators of rows 2 t, 2 t + 1
+        unsigned unset = (1u << (2 * NT)) - 1u;              // rows without a reference yet (no key, or none with a logit above -inf)
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            m[nt][0] = m[nt][1] = l[nt][0] = l[nt][1] = 0.f;
+#pragma unroll
+            for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) o[i][nt][j] = 0.f;
+        }
+        int stage = 0;                                       // step % PSTAGES
+        for (int s = 0; s < my_steps; ++s) {
+            const uint32_t st = ring + stage * L::STAGE;
+            ring_wait<PSTAGES - 2>();
+            __syncwarp();                                    // this step's stage is there for every lane, and every lane is done with the last one's
+            const uint32_t there = there_of[warp][stage];
+            fetch(s + PSTAGES - 1, stage == 0 ? PSTAGES - 1 : stage - 1);
+            look_up(s + PSTAGES);
+            stage = stage == PSTAGES - 1 ? 0 : stage + 1;
+            if (there == 0u) continue;
+            // ---- S^T = K Q^T ----
+            float sv[NT][4];
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) sv[nt][0] = sv[nt][1] = sv[nt][2] = sv[nt][3] = 0.f;
+#pragma unroll
+            for (int ks = 0; ks < D / 16; ++ks) {
+                uint32_t fa[4];
+                ldmatrix_x4(fa[0], fa[1], fa[2], fa[3], st + (k_get ^ (ks << 5)));
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                    uint2 q;
+                    if constexpr (Q_REGS) q = qf[ks][nt];
+                    else q = qs[(ks * NT + nt) * 32 + lane];
+                    mma_bf16_16816(sv[nt], fa, q.x, q.y);
+                }
+            }
+            float top = -INFINITY;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    sv[nt][j] = fmaf(sv[nt][j], a.scale_log2e, -m[nt][j & 1]);
+                    if (there != 0xFFFFu && !((there >> ((j >> 1) * 8 + g)) & 1u)) sv[nt][j] = -INFINITY;
+                    top = fmaxf(top, sv[nt][j]);
+                }
+            if (__any_sync(0xffffffffu, top > kPagedRaise || unset != 0u)) {
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int r = 0; r < 2; ++r) {
+                        float x = fmaxf(sv[nt][r], sv[nt][r + 2]);
+                        x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
+                        x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
+                        x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
+                        const unsigned bit = 1u << (2 * nt + r);
+                        if (x > 0.f || ((unset & bit) && x > -INFINITY)) {
+                            const float f = unset & bit ? 0.f : ex2(-x);
+                            unset &= ~bit;
+                            m[nt][r] += x;
+                            l[nt][r] *= f;
+#pragma unroll
+                            for (int i = 0; i < D / 16; ++i) {
+                                o[i][nt][r] *= f;
+                                o[i][nt][r + 2] *= f;
+                            }
+                            sv[nt][r] -= x;
+                            sv[nt][r + 2] -= x;
+                        }
+                    }
+            }
+            // ---- P, and O^T += V^T P^T ----
+            uint32_t pf[NT][2];
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                const float p0 = ex2(sv[nt][0]), p1 = ex2(sv[nt][1]), p2 = ex2(sv[nt][2]), p3 = ex2(sv[nt][3]);
+                l[nt][0] += p0 + p2;
+                l[nt][1] += p1 + p3;
+                pf[nt][0] = transpose8x8(pack_bf16(p0, p1));
+                pf[nt][1] = transpose8x8(pack_bf16(p2, p3));
+            }
+#pragma unroll
+            for (int i = 0; i < D / 16; ++i) {
+                uint32_t fa[4];
+                ldmatrix_x4_trans(fa[0], fa[1], fa[2], fa[3], st + (v_get ^ (i << 5)));
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) mma_bf16_16816(o[i][nt], fa, pf[nt][0], pf[nt][1]);
+            }
+        }
+
+        // ---- the warps' results together, in their order ----
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+                float x = l[nt][r];
+                x += __shfl_xor_sync(0xffffffffu, x, 4);
+                x += __shfl_xor_sync(0xffffffffu, x, 8);
+                x += __shfl_xor_sync(0xffffffffu, x, 16);
+                if (g == 0) {
+                    stat[0][warp][nt * 8 + 2 * t + r] = (unset >> (2 * nt + r)) & 1u ? -INFINITY : m[nt][r];
+                    stat[1][warp][nt * 8 + 2 * t + r] = x;
+                }
+            }
+        ring_wait<0>();
+        __syncthreads();                                     // nobody reads the ring any more
+        float* os = reinterpret_cast<float*>(smem);          // [warp][row][D + 4]
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    os[(warp * L::ROWS + nt * 8 + 2 * t + (j & 1)) * (D + 4) + i * 16 + (j >> 1) * 8 + g] = o[i][nt][j];
+        __syncthreads();
+        const bool all_of_it = unit == item_lo && seg_hi == item_hi;
+        constexpr int TPR = D / 4;                           // threads of a row, 4 values each
+        auto give = [&](int row, int c, const float4& v, float lse2) {
+            const int r = tile * L::ROWS + row;
+            const int64_t at = (int64_t)(b * (int64_t)a.n + r / G) * a.n_heads + kvh * G + r % G;
+            *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(a.o) + at * D + c * 4) = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
+            if (a.lse && c == 0) a.lse[at] = lse2 * 0.6931471805599453f;
+        };
+        // parts: [2 CTA + (whether the item began with it)][row][D], then [..][row] log2 of the denominators
+        float* part_o = a.part;
+        float* part_l = a.part + (int64_t)2 * gridDim.x * L::ROWS * D;
+        const int64_t my_part = (int64_t)(2 * blockIdx.x + (unit == item_lo)) * L::ROWS;
+        for (int i = tid; i < L::ROWS * TPR; i += PW * 32) {
+            const int row = i / TPR, c = i % TPR;
+            if (tile * L::ROWS + row >= R) break;
+            float mx = -INFINITY;
+#pragma unroll
+            for (int w = 0; w < PW; ++w) mx = fmaxf(mx, stat[0][w][row]);
+            float den = 0.f;
+            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int w = 0; w < PW; ++w) {
+                const float mw = stat[0][w][row];
+                if (mw == -INFINITY) continue;               // a warp that met no key
+                const float f = ex2(mw - mx);
+                const float4 x = *reinterpret_cast<const float4*>(os + (w * L::ROWS + row) * (D + 4) + c * 4);
+                den = fmaf(f, stat[1][w][row], den);
+                v.x = fmaf(f, x.x, v.x); v.y = fmaf(f, x.y, v.y); v.z = fmaf(f, x.z, v.z); v.w = fmaf(f, x.w, v.w);
+            }
+            const float inv = den == 0.f ? 0.f : 1.f / den;
+            v.x *= inv; v.y *= inv; v.z *= inv; v.w *= inv;
+            const float lse2 = den == 0.f ? -INFINITY : mx + log2f(den);
+            if (all_of_it) {
+                give(row, c, v, lse2);
+            } else {
+                *reinterpret_cast<float4*>(part_o + (my_part + row) * D + c * 4) = v;
+                if (c == 0) part_l[my_part + row] = lse2;
+            }
+        }
+        if (!all_of_it) {
+            // ---- the last of the item's CTAs adds the parts up, in their order ----
+            const int c0 = (int)(((item_lo + 1) * ctas - 1) / total), c1 = (int)((item_hi * ctas - 1) / total);
+            __threadfence();
+            __syncthreads();
+            if (tid == 0) {
+                unsigned* arrived = a.arrived + c0;          // an item that goes on past a CTA is the last one that begins there
+                is_last = atomicAdd(arrived, 1u) == (unsigned)(c1 - c0);
+                if (is_last) *arrived = 0u;
+            }
+            __syncthreads();
+            if (is_last) {
+                __threadfence();
+                for (int i = tid; i < L::ROWS * TPR; i += PW * 32) {
+                    const int row = i / TPR, c = i % TPR;
+                    if (tile * L::ROWS + row >= R) break;
+                    Sum sum;
+                    for (int q0 = c0; q0 <= c1; q0 += 8) {
+                        float x[8];
+                        float4 w[8];
+#pragma unroll
+                        for (int p = 0; p < 8; ++p) {
+                            x[p] = -INFINITY;
+                            if (q0 + p <= c1) {
+                                const int64_t at = (int64_t)(2 * (q0 + p) + (q0 + p == c0)) * L::ROWS + row;
+                                x[p] = __ldcg(part_l + at);
+                                w[p] = __ldcg(reinterpret_cast<const float4*>(part_o + at * D + c * 4));
+                            }
+                        }
+#pragma unroll
+                        for (int p = 0; p < 8; ++p) sum.add(x[p], w[p]);
+                    }
+                    give(row, c, sum.mean(), sum.lse2());
+                }
+            }
+        }
+        unit = seg_hi;
+    }
+}
+
+template <int D, int NT>
+int paged_launch(const PagedAttnArgs& a, cudaStream_t stream) {
+    using L = PagedLayout<D, NT>;
+    static PerDevice<bool> ready;
+    int device = 0;
+    cudaGetDevice(&device);
+    if (!ready.of(device, [](bool& ok) {
+            ok = cudaFuncSetAttribute(paged_attn_kernel<D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, L::SMEM) == cudaSuccess;
+        }))
+        return -1;
+    const int R = a.n * (a.n_heads / a.n_kv_heads), tiles = (R + L::ROWS - 1) / L::ROWS;
+    const int64_t units = (int64_t)std::max(1, (a.ctx_len + kUnit - 1) / kUnit) * tiles * a.batch * a.n_kv_heads;
+    const int ctas = (int)std::min<int64_t>(kPlaces, std::max<int64_t>(1, units / kMinUnits));
+    return launch_pdl(paged_attn_kernel<D, NT>, dim3(ctas), dim3(PW * 32), L::SMEM, stream, a) == cudaSuccess ? 1 : -1;
+}
+template <int D>
+int paged_dispatch(const PagedAttnArgs& a, cudaStream_t stream) {
+    const int R = a.n * (a.n_heads / a.n_kv_heads);
+    if (R <= 8) return paged_launch<D, 1>(a, stream);
+    if (R <= 16) return paged_launch<D, 2>(a, stream);
+    return paged_launch<D, 4>(a, stream);
+}
+
+}  // namespace
+
+size_t paged_attention_scratch_bytes(int head_dim) { return (size_t)2 * kPlaces * 32 * (head_dim + 1) * sizeof(float); }
+
+int launch_paged_attention(const PagedAttnArgs& a, cudaStream_t stream) {
+    if (a.batch == 0 || a.n == 0) return 0;
+    return a.head_dim == 128 ? paged_dispatch<128>(a, stream) : paged_dispatch<64>(a, stream);
+}
+
+}  // namespace acache
