@@ -67,7 +67,7 @@ typedef enum {
 /* bits of the device status word returned by acache_poll_status */
 #define ACACHE_FLAG_BAD_INDEX   0x1u  /* an anchor / masked / extra index was out of range; row skipped */
 #define ACACHE_FLAG_WAIT_EXPIRED 0x2u /* a bounded wait inside a kernel gave up                          */
-#define ACACHE_FLAG_NONFINITE   0x4u  /* a row written to an 8-bit cache held an infinity or a NaN       */
+#define ACACHE_FLAG_NONFINITE   0x4u  /* a row written to an 8-bit cache held an infinity or a NaN, or logits to be sampled a NaN */
 
 /* flags of acache_layer_step */
 #define ACACHE_F_SCORE            0x1u /* form Q for the masked rows from x and run the scoring (Eq. 4-5) */
@@ -159,6 +159,20 @@ typedef struct {
     const void *p;
     int64_t     batch_stride, row_stride;
 } acache_rows;
+
+/* element types of logits */
+#define ACACHE_BF16 0
+#define ACACHE_F32  1
+
+/* How tokens are drawn: DEVICE arrays of one setting for every rows_per_setting rows (row r: element r / rows_per_setting; 1, or the rows of a
+ * request), each NULL where it is not asked for. */
+typedef struct {
+    const float   *temperature;     /* T; 0 (below, or NaN): the largest logit.  NULL: 1                              */
+    const float   *top_p;           /* 1 and more, or NaN: off                                                        */
+    const float   *min_p;           /* 0 and less, or NaN: off; above 1: 1                                            */
+    const int32_t *top_k;           /* 0 and less: off                                                                */
+    int32_t        rows_per_setting;
+} acache_sampling;
 
 /* The request batch: every request shares the layout (ctx_len, affix span, m, e). */
 typedef struct {
@@ -419,6 +433,30 @@ acache_status acache_paged_attention(acache_ctx *ctx, const acache_paged_kv *kv,
                                      const void *q, const int32_t *lens, const uint32_t *key_drop, void *o, float *lse,
                                      acache_stream_t stream);
 
+/* acache_layer_step(flags = 0, no scoring, no selection) on a cache in pages: the rows R = A u E of every request go through the layer, their fresh K/V are
+ * written to their places in the request's pages, and their attention is acache_paged_attention over its first lens[b] tokens (DEVICE int32 [B];
+ * NULL: ctx_len) as they then are.  Pages that hold rows of R belong to one request; all others may be shared.  A decode pass: k = 0,
+ * extra_rows = the new tokens' positions, lens = the tokens with them.  anchor_idx: DEVICE int32 [B, k], relative to affix_start; x, x_is_compact, y
+ * as acache_recompute_anchors. */
+acache_status acache_recompute_paged(acache_ctx *ctx, const acache_layer_weights *w, const acache_request *req, acache_paged_kv *kv,
+                                     const void *x, int x_is_compact, const int32_t *anchor_idx, int32_t k, const int32_t *lens,
+                                     void *y, acache_stream_t stream);
+
+/* Draws a token from each row of logits by a given random number:
+ *   w_i = exp((l_i - max l) / T).  In the order of falling l, equal ones by their index, a prefix is kept: the first top_k; of their weight,
+ *   the fewest that make up the share top_p (one at least); those with w_i >= min_p; whichever is shortest.
+ *   token = the first of them whose running sum of w is above u S, S the sum over all that are kept
+ *   prob = w_token / S,   confidence = softmax(l)[token] (T = 1, all tokens: as in acache_predict_commit)
+ * Sums are exact sums of weights rounded to 2^-46 (2^-45 above 65536 tokens, 2^-44 above 131072): a token whose weight is less than half of
+ * that against the largest is never drawn, and results do not depend on any order.  u in [0, 1), DEVICE fp32 [rows]; outside, the nearer end.
+ *   logits: DEVICE bf16 or fp32 (type ACACHE_BF16, ACACHE_F32), rows row_stride elements apart, aligned to an element; vocab: up to 262144.
+ *   token: DEVICE int32 [rows]; prob, confidence: DEVICE fp32 [rows], may be NULL.
+ * Infinite logits weigh what their limit does (+inf: all of it, in equal parts).  NaN counts as -inf and raises ACACHE_FLAG_NONFINITE.  A row
+ * without any logit above -inf has the token -1, prob and confidence 0. */
+acache_status acache_sample_tokens(acache_ctx *ctx, const void *logits, int32_t type, int32_t rows, int32_t vocab, int64_t row_stride,
+                                   const acache_sampling *how, const float *u, int32_t *token, float *prob, float *confidence,
+                                   acache_stream_t stream);
+
 /* Predict-then-commit on the current block (Section 3.1, Eq. 2-3, with the confidence-threshold
  * commit rule the paper's set-up uses, threshold 0.9 in Section 5):
  *   z = W_lm (RMSNorm(h_i) g);  token_i = argmax_v z_v;  conf_i = softmax(z)[token_i]
@@ -433,6 +471,14 @@ acache_status acache_predict_commit(acache_ctx *ctx, const void *h, int32_t h_ro
                                     int32_t batch, int32_t n_blk, const void *final_norm_g, const void *w_lm,
                                     int32_t vocab, float threshold, int32_t *token, float *confidence,
                                     int32_t *commit, acache_stream_t stream);
+
+/* acache_predict_commit with tokens drawn from the logits (acache_sample_tokens) instead of the arg max; the commit rule is the same, on the drawn
+ * token's confidence.  logits: DEVICE fp32 [B * n_blk, vocab] out (the LM head's sums, not rounded further); how: a setting per row, or with
+ * rows_per_setting = n_blk per request; u: DEVICE fp32 [B, n_blk].  With T = 0 token and commit are acache_predict_commit's. */
+acache_status acache_predict_sample(acache_ctx *ctx, const void *h, int32_t h_rows, const int32_t *block_rows, int32_t batch, int32_t n_blk,
+                                    const void *final_norm_g, const void *w_lm, int32_t vocab, float *logits, const acache_sampling *how,
+                                    const float *u, float threshold, int32_t *token, float *confidence, int32_t *commit,
+                                    acache_stream_t stream);
 
 /* One denoising step's model pass for a batch of requests (the "recompute forward" of Section 4.3
  * followed by Eq. 2-3): the rows R = A u E of every request go through n_layers layers, each layer

@@ -28,7 +28,7 @@ EXPORTS = ["acache_create", "acache_workspace_bytes", "acache_set_workspace", "a
            "acache_decode_step_shared", "acache_generate_block_shared", "acache_layer_step_shared",
            "acache_host_x_in_place", "acache_score_kv_deviation", "acache_debug_expire_next_wait",
            "acache_kv8_write", "acache_kv8_read", "acache_kv8_attention", "acache_layer_step_kv8",
-           "acache_paged_append", "acache_paged_attention"]
+           "acache_paged_append", "acache_paged_attention", "acache_recompute_paged", "acache_sample_tokens", "acache_predict_sample"]
 
 STAGES = ["mask_q", "score", "topk", "gather_norm", "qkv", "attention", "oproj", "mlp_norm", "gate_up", "down"]
 
@@ -64,6 +64,10 @@ class PagedKV(C.Structure):
 
 class Rows(C.Structure):
     _fields_ = [("p", C.c_void_p), ("batch_stride", C.c_int64), ("row_stride", C.c_int64)]
+
+
+class Sampling(C.Structure):
+    _fields_ = [("temperature", C.c_void_p), ("top_p", C.c_void_p), ("min_p", C.c_void_p), ("top_k", C.c_void_p), ("rows_per_setting", C.c_int32)]
 
 
 class Request(C.Structure):
@@ -179,6 +183,12 @@ def load_library(path: Optional[str] = None) -> C.CDLL:
     lib.acache_paged_append.restype = C.c_int
     lib.acache_paged_attention.argtypes = [vp, C.POINTER(PagedKV), i32, i32, i32, vp, vp, vp, vp, vp, vp]
     lib.acache_paged_attention.restype = C.c_int
+    lib.acache_recompute_paged.argtypes = [vp, C.POINTER(LayerWeights), C.POINTER(Request), C.POINTER(PagedKV), vp, C.c_int, vp, i32, vp, vp, vp]
+    lib.acache_recompute_paged.restype = C.c_int
+    lib.acache_sample_tokens.argtypes = [vp, vp, i32, i32, i32, i64, C.POINTER(Sampling), vp, vp, vp, vp, vp]
+    lib.acache_sample_tokens.restype = C.c_int
+    lib.acache_predict_sample.argtypes = [vp, vp, i32, vp, i32, i32, vp, vp, i32, vp, C.POINTER(Sampling), vp, C.c_float, vp, vp, vp, vp]
+    lib.acache_predict_sample.restype = C.c_int
     lib.acache_stage_timing.argtypes = [vp, C.c_int]
     lib.acache_stage_timing.restype = C.c_int
     lib.acache_read_stage_times.argtypes = [vp, C.POINTER(C.c_float)]
@@ -495,6 +505,52 @@ class Context:
             _check_tensor(key_drop, torch.int32, (B, -(-ctx_len // 32)))
         self._check(self.lib.acache_paged_attention(self.h, C.byref(cache), B, n, ctx_len, q.data_ptr(), _ptr(lens), _ptr(key_drop),
                                                     o.data_ptr(), _ptr(lse), _stream()))
+
+    def recompute_paged(self, w: LayerWeights, req: Request, cache: PagedKV, x, x_is_compact, anchor_idx, k, y, lens=None):
+        """The rows of R through the layer, over a cache in pages; lens: int32 [B], the tokens of each request with them."""
+        import torch
+        self._cache_fits(cache, req.batch)
+        if lens is not None:
+            _check_tensor(lens, torch.int32, (req.batch,))
+        self._check(self.lib.acache_recompute_paged(self.h, C.byref(w), C.byref(req), C.byref(cache), _ptr(x), int(x_is_compact), _ptr(anchor_idx), k,
+                                                    _ptr(lens), _ptr(y), _stream()))
+
+    def sample_tokens(self, logits, u, token, prob=None, confidence=None, temperature=None, top_k=None, top_p=None, min_p=None, rows_per_setting=1):
+        """logits: bf16 or fp32 [rows, vocab] (rows may lie apart); u: fp32 [rows]; token: int32 [rows]; prob, confidence: fp32 [rows]; temperature,
+        top_p, min_p (fp32) and top_k (int32): one for every rows_per_setting rows."""
+        import torch
+        rows, vocab = logits.shape
+        if logits.dtype not in (torch.bfloat16, torch.float32) or not logits.is_cuda or (vocab > 1 and logits.stride(1) != 1):
+            raise ValueError(f"logits of {logits.dtype} on {logits.device}, strides {logits.stride()}: bf16 or fp32 rows on a GPU are wanted")
+        _check_tensor(token, torch.int32, (rows,))
+        for t in (prob, confidence):
+            if t is not None:
+                _check_tensor(t, torch.float32, (rows,))
+        how = self._sampling(rows, u, temperature, top_k, top_p, min_p, rows_per_setting)
+        self._check(self.lib.acache_sample_tokens(self.h, logits.data_ptr(), 0 if logits.dtype is torch.bfloat16 else 1, rows, vocab,
+                                                  logits.stride(0) if rows > 1 else vocab, how, u.data_ptr(), token.data_ptr(), _ptr(prob),
+                                                  _ptr(confidence), _stream()))
+
+    def predict_sample(self, h, h_rows, block_rows, batch, n_blk, final_norm_g, w_lm, vocab, logits, u, threshold, token, confidence, commit,
+                       temperature=None, top_k=None, top_p=None, min_p=None, rows_per_setting=1):
+        """predict_commit with drawn tokens; logits: fp32 [batch * n_blk, vocab] out; u: fp32 [batch, n_blk]; settings as sample_tokens."""
+        import torch
+        rows = batch * n_blk
+        _check_tensor(logits, torch.float32, (rows, vocab))
+        how = self._sampling(rows, u.view(-1), temperature, top_k, top_p, min_p, rows_per_setting)
+        self._check(self.lib.acache_predict_sample(self.h, _ptr(h), h_rows, _ptr(block_rows), batch, n_blk, _ptr(final_norm_g), _ptr(w_lm), vocab,
+                                                   _ptr(logits), how, _ptr(u), float(threshold), _ptr(token), _ptr(confidence), _ptr(commit),
+                                                   _stream()))
+
+    @staticmethod
+    def _sampling(rows, u, temperature, top_k, top_p, min_p, rows_per_setting):
+        import torch
+        _check_tensor(u, torch.float32, (rows,))
+        per = (-(-rows // max(rows_per_setting, 1)),)
+        for t, dtype in ((temperature, torch.float32), (top_p, torch.float32), (min_p, torch.float32), (top_k, torch.int32)):
+            if t is not None:
+                _check_tensor(t, dtype, per)
+        return C.byref(Sampling(_ptr(temperature), _ptr(top_p), _ptr(min_p), _ptr(top_k), rows_per_setting))
 
     def _rows_at(self, t, B, n, heads):
         """Where rows [B, n, heads, d] lie; the heads of a row side by side."""

@@ -243,6 +243,29 @@ acache_status run_paged_attention(acache_ctx* c, const acache_paged_kv* kv, int3
     return check_cuda(c, "paged attention");
 }
 
+acache_status check_sampling(acache_ctx* c, int64_t rows, int32_t vocab, const acache_sampling* how, const float* u) {
+    if (!c->ws) return fail(c, ACACHE_ERR_WORKSPACE, "workspace not set");
+    if (!how) return fail(c, ACACHE_ERR_INVALID_ARG, "sampling is NULL");
+    if (rows < 0 || vocab <= 0) return fail(c, ACACHE_ERR_INVALID_ARG, "rows %lld / vocab %d out of range", (long long)rows, vocab);
+    if (vocab > kSampleMaxVocab || rows > (1 << 24)) return fail(c, ACACHE_ERR_UNSUPPORTED_SHAPE, "vocab %d above %d, or more than 2^24 rows", vocab, kSampleMaxVocab);
+    if (how->rows_per_setting <= 0) return fail(c, ACACHE_ERR_INVALID_ARG, "rows_per_setting %d is not positive", how->rows_per_setting);
+    if (rows > 0 && !u) return fail(c, ACACHE_ERR_INVALID_ARG, "u is NULL");
+    return ACACHE_OK;
+}
+
+acache_status run_sample(acache_ctx* c, const void* logits, int32_t type, int32_t rows, int32_t vocab, int64_t row_stride, const acache_sampling* how,
+                         const float* u, int32_t* token, float* prob, float* confidence, cudaStream_t st) {
+    SampleArgs a{};
+    a.logits = logits; a.bf16 = type == ACACHE_BF16; a.rows = rows; a.vocab = vocab; a.row_stride = row_stride;
+    a.temperature = how->temperature; a.top_p = how->top_p; a.min_p = how->min_p; a.top_k = how->top_k; a.rows_per_setting = how->rows_per_setting;
+    a.u = u; a.token = token; a.prob = prob; a.confidence = confidence;
+    a.status = wsp<uint32_t>(c, c->o_status);
+    const int nl = launch_sample(a, st);
+    if (nl < 0) return check_cuda(c, "sampling") == ACACHE_OK ? fail(c, ACACHE_ERR_CUDA, "sampling launch failed") : ACACHE_ERR_CUDA;
+    c->launches += nl;
+    return check_cuda(c, "sampling");
+}
+
 // Q for the masked rows, then Eq. 4-5.
 acache_status run_score(acache_ctx* c, const acache_request* r, const void* q_mask, const acache_kv* kv,
                         float* scores, int accumulate, int norm_full, int defer_head_sum, cudaStream_t st, int early_k = 0) {
@@ -298,7 +321,7 @@ acache_status run_recompute(acache_ctx* c, const acache_layer_weights* w, const 
                             const PrivateRows* priv = nullptr, MapReuse maps = MapReuse{false}, bool drop_non_anchor = false,
                             const FusedScore* fs = nullptr,
                             const std::function<acache_status()>& after_qkv = std::function<acache_status()>(),
-                            const acache_kv8* kv8 = nullptr) {
+                            const acache_kv8* kv8 = nullptr, const acache_paged_kv* paged = nullptr, const int32_t* lens = nullptr) {
     const acache_model_desc& d = c->d;
     const int rows = k + r->n_extra, n = r->batch * rows;
     if (n == 0) {
@@ -350,13 +373,25 @@ acache_status run_recompute(acache_ctx* c, const acache_layer_weights* w, const 
     c->launches += nl; }
 
     if (kv8) run_kv8_write(c, kv8, r->batch, r->ctx_len, k_new, v_new, (int64_t)rows * kvd, rows, row_pos, 0, st);
+    if (paged) {                // the projection has turned them already
+        PagedAppendArgs pa{};
+        pa.pages = pages_of(paged);
+        pa.k = paged->k; pa.v = paged->v;
+        pa.k_rows = Rows{k_new, (int64_t)rows * kvd, kvd};
+        pa.v_rows = Rows{v_new, (int64_t)rows * kvd, kvd};
+        pa.batch = r->batch; pa.n = rows; pa.ctx_len = r->ctx_len; pa.n_heads = d.n_heads; pa.n_kv_heads = d.n_kv_heads; pa.head_dim = d.head_dim;
+        pa.pos = row_pos; pa.status = status;
+        const int nl = launch_paged_append(pa, st);
+        if (nl < 0) return check_cuda(c, "paged append") == ACACHE_OK ? fail(c, ACACHE_ERR_CUDA, "paged append launch failed") : ACACHE_ERR_CUDA;
+        c->launches += nl;
+    }
     if (after_qkv) {            // work of the caller that wants the fresh K/V in place but precedes the attention
         const acache_status sq = after_qkv();
         if (sq != ACACHE_OK) return sq;
     }
     mark(c, ACACHE_STAGE_ATTENTION, st);
     AttnArgs at{};
-    if (!kv8) {
+    if (!kv8 && !paged) {
     at.q = q; at.cache_k = kv->k; at.cache_v = kv->v; at.kv_batch_stride = kv->batch_stride;
     if (!fuse_scatter) {
         // the rows that serve their positions from k_new / v_new: the rows recomputed now, or the whole private
@@ -391,6 +426,9 @@ acache_status run_recompute(acache_ctx* c, const acache_layer_weights* w, const 
     }
     if (kv8) {
         const acache_status sa = run_kv8_attention(c, kv8, r->batch, rows, r->ctx_len, q, o, nullptr, nullptr, at.key_drop, st);
+        if (sa != ACACHE_OK) return sa;
+    } else if (paged) {
+        const acache_status sa = run_paged_attention(c, paged, r->batch, rows, r->ctx_len, q, o, nullptr, lens, nullptr, st);
         if (sa != ACACHE_OK) return sa;
     } else {
     at.batch = r->batch; at.n = rows; at.ctx_len = r->ctx_len;
@@ -948,11 +986,43 @@ acache_status acache_paged_attention(acache_ctx* ctx, const acache_paged_kv* kv,
     return run_paged_attention(ctx, kv, batch, n_rows, ctx_len, q, o, lse, lens, key_drop, stream);
 }
 
-acache_status acache_predict_commit(acache_ctx* ctx, const void* h, int32_t h_rows, const int32_t* block_rows,
-                                    int32_t batch, int32_t n_blk, const void* final_norm_g, const void* w_lm,
-                                    int32_t vocab, float threshold, int32_t* token, float* confidence,
-                                    int32_t* commit, acache_stream_t stream) {
+acache_status acache_recompute_paged(acache_ctx* ctx, const acache_layer_weights* w, const acache_request* req, acache_paged_kv* kv,
+                                     const void* x, int x_is_compact, const int32_t* anchor_idx, int32_t k, const int32_t* lens, void* y,
+                                     acache_stream_t stream) {
     if (!ctx) return ACACHE_ERR_INVALID_ARG;
+    acache_status s = check_request(ctx, req, nullptr, k, true);
+    if (s != ACACHE_OK) return s;
+    if ((s = check_paged(ctx, kv, req->batch, req->ctx_len)) != ACACHE_OK) return s;
+    if ((s = check_weights(ctx, w, false)) != ACACHE_OK) return s;
+    if (req->batch * (k + req->n_extra) == 0) return ACACHE_OK;
+    if (!x || !y || !aligned16(x) || !aligned16(y)) return fail(ctx, ACACHE_ERR_INVALID_ARG, "x / y NULL or misaligned");
+    if (k > 0 && !anchor_idx) return fail(ctx, ACACHE_ERR_INVALID_ARG, "anchor_idx is NULL");
+    return run_recompute(ctx, w, req, nullptr, false, x, x_is_compact, anchor_idx, k, wsp<void>(ctx, ctx->o_knew), wsp<void>(ctx, ctx->o_vnew), y,
+                         stream, nullptr, MapReuse{false}, false, nullptr, std::function<acache_status()>(), nullptr, kv, lens);
+}
+
+acache_status acache_sample_tokens(acache_ctx* ctx, const void* logits, int32_t type, int32_t rows, int32_t vocab, int64_t row_stride,
+                                   const acache_sampling* how, const float* u, int32_t* token, float* prob, float* confidence,
+                                   acache_stream_t stream) {
+    if (!ctx) return ACACHE_ERR_INVALID_ARG;
+    acache_status s = check_sampling(ctx, rows, vocab, how, u);
+    if (s != ACACHE_OK) return s;
+    if (type != ACACHE_BF16 && type != ACACHE_F32) return fail(ctx, ACACHE_ERR_INVALID_ARG, "type %d is neither bf16 nor fp32", type);
+    if (rows == 0) return ACACHE_OK;
+    if (!logits || (reinterpret_cast<uintptr_t>(logits) & (type == ACACHE_BF16 ? 1 : 3)) || !token)
+        return fail(ctx, ACACHE_ERR_INVALID_ARG, "logits / token NULL, or logits between two elements");
+    if (rows > 1 && row_stride < vocab) return fail(ctx, ACACHE_ERR_INVALID_ARG, "row_stride %lld smaller than a row of %d", (long long)row_stride, vocab);
+    return run_sample(ctx, logits, type, rows, vocab, row_stride, how, u, token, prob, confidence, stream);
+}
+
+}  // extern "C"
+
+namespace {
+// Predict-then-commit: the LM head on rows block_rows of h, then the arg max of each row (how null) or a token drawn from its logits,
+// which are kept in `logits` (fp32 [B n_blk, vocab]).
+acache_status predict_impl(acache_ctx* ctx, const void* h, int32_t h_rows, const int32_t* block_rows, int32_t batch, int32_t n_blk,
+                           const void* final_norm_g, const void* w_lm, int32_t vocab, float* logits, const acache_sampling* how,
+                           const float* u, float threshold, int32_t* token, float* confidence, int32_t* commit, cudaStream_t stream) {
     if (!ctx->ws) return fail(ctx, ACACHE_ERR_WORKSPACE, "workspace not set");
     const acache_model_desc& d = ctx->d;
     if (batch < 0 || n_blk < 0 || h_rows <= 0 || vocab <= 0) return fail(ctx, ACACHE_ERR_INVALID_ARG, "negative size");
@@ -960,9 +1030,13 @@ acache_status acache_predict_commit(acache_ctx* ctx, const void* h, int32_t h_ro
         return fail(ctx, ACACHE_ERR_INVALID_ARG, "batch * n_blk = %lld / vocab = %d exceed the context's limits (%lld, %d)",
                     (long long)batch * n_blk, vocab, (long long)d.max_batch * d.max_block, d.max_vocab);
     if (vocab % 128) return fail(ctx, ACACHE_ERR_UNSUPPORTED_SHAPE, "vocab %d is not a multiple of 128", vocab);
+    if (how) {
+        const acache_status s = check_sampling(ctx, batch * n_blk, vocab, how, u);
+        if (s != ACACHE_OK) return s;
+    }
     if (batch * n_blk == 0) return ACACHE_OK;
     if (!h || !block_rows || !final_norm_g || !w_lm || !token || !confidence || !commit || !aligned16(h) ||
-        !aligned16(final_norm_g) || !aligned16(w_lm))
+        !aligned16(final_norm_g) || !aligned16(w_lm) || (how && (!logits || !aligned16(logits))))
         return fail(ctx, ACACHE_ERR_INVALID_ARG, "NULL or misaligned pointer");
     GemmArgs g{};
     g.a = wsp<void>(ctx, ctx->o_lxn); g.M = batch * n_blk; g.K = d.hidden;
@@ -971,15 +1045,44 @@ acache_status acache_predict_commit(acache_ctx* ctx, const void* h, int32_t h_ro
     g.prep.enabled = 3; g.prep.x = h; g.prep.x_is_compact = 1; g.prep.compact_idx = block_rows; g.prep.compact_rows = h_rows;
     g.prep.k = 0; g.prep.e = n_blk; g.prep.gain = final_norm_g; g.prep.eps = d.rms_eps;
     g.logit_stats = wsp<float4>(ctx, ctx->o_lstats);
+    g.logits = how ? logits : nullptr;
     g.partial = wsp<float>(ctx, ctx->o_gemm); g.status = wsp<uint32_t>(ctx, ctx->o_status);
     g.grid_bar = wsp<unsigned int>(ctx, ctx->o_gridbar);
     int nl = launch_gemm(g, stream);
     if (nl < 0) return check_cuda(ctx, "LM head") == ACACHE_OK ? fail(ctx, ACACHE_ERR_CUDA, "LM head launch failed") : ACACHE_ERR_CUDA;
     ctx->launches += nl;
-    nl = launch_predict_commit(g, batch, n_blk, threshold, token, confidence, commit, stream);
+    if (how) {
+        const acache_status s = run_sample(ctx, logits, ACACHE_F32, batch * n_blk, vocab, vocab, how, u, token, nullptr, confidence, stream);
+        if (s != ACACHE_OK) return s;
+        nl = launch_commit(confidence, batch, n_blk, threshold, commit, stream);
+    } else {
+        nl = launch_predict_commit(g, batch, n_blk, threshold, token, confidence, commit, stream);
+    }
     if (nl < 0) return check_cuda(ctx, "predict/commit") == ACACHE_OK ? fail(ctx, ACACHE_ERR_CUDA, "predict/commit launch failed") : ACACHE_ERR_CUDA;
     ctx->launches += nl;
     return check_cuda(ctx, "predict_commit");
+}
+}  // namespace
+
+extern "C" {
+
+acache_status acache_predict_commit(acache_ctx* ctx, const void* h, int32_t h_rows, const int32_t* block_rows,
+                                    int32_t batch, int32_t n_blk, const void* final_norm_g, const void* w_lm,
+                                    int32_t vocab, float threshold, int32_t* token, float* confidence,
+                                    int32_t* commit, acache_stream_t stream) {
+    if (!ctx) return ACACHE_ERR_INVALID_ARG;
+    return predict_impl(ctx, h, h_rows, block_rows, batch, n_blk, final_norm_g, w_lm, vocab, nullptr, nullptr, nullptr, threshold, token,
+                        confidence, commit, stream);
+}
+
+acache_status acache_predict_sample(acache_ctx* ctx, const void* h, int32_t h_rows, const int32_t* block_rows, int32_t batch, int32_t n_blk,
+                                    const void* final_norm_g, const void* w_lm, int32_t vocab, float* logits, const acache_sampling* how,
+                                    const float* u, float threshold, int32_t* token, float* confidence, int32_t* commit,
+                                    acache_stream_t stream) {
+    if (!ctx) return ACACHE_ERR_INVALID_ARG;
+    if (!how) return fail(ctx, ACACHE_ERR_INVALID_ARG, "sampling is NULL");
+    return predict_impl(ctx, h, h_rows, block_rows, batch, n_blk, final_norm_g, w_lm, vocab, logits, how, u, threshold, token, confidence,
+                        commit, stream);
 }
 
 acache_status acache_denoise_step(acache_ctx* ctx, int32_t n_layers, const acache_layer_weights* layers,

@@ -145,6 +145,14 @@ __device__ __forceinline__ float4* logit_entry(const GemmArgs& g, int nt, int en
     return g.logit_stats + ((int64_t)nt * 16 + entry) * g.M + row;
 }
 
+// The logits themselves, for who samples from them.
+template <int W>
+__device__ __forceinline__ void store_logits(const GemmArgs& g, int row, int col, const float (&v)[W]) {
+    float4* to = reinterpret_cast<float4*>(g.logits + (int64_t)row * g.n[0] + col);
+#pragma unroll
+    for (int i = 0; i < W / 4; ++i) to[i] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+}
+
 // Softmax statistics of W logits starting at vocabulary index col: running (max, sum exp(z - max),
 // arg max with the lowest index on ties).
 template <int W>
@@ -261,6 +269,7 @@ __device__ __forceinline__ void finish_item(const GemmArgs& g, const TcPlan& p, 
         float m = -INFINITY, sm = 0.f;
         int arg = 0;
         logit_stats_update<16>(lo, nt * TC_BN + item * 16, m, sm, arg);
+        if (g.logits) store_logits<16>(g, grow, nt * TC_BN + item * 16, lo);
         *logit_entry(g, nt, item, grow) = make_float4(m, sm, __int_as_float(arg), 16.f);
     } else if (g.epilogue == kEpiSwiGLU) {
         out_swiglu<16>(g, grow, nt * 128 + item * 16, lo, hi);
@@ -328,6 +337,7 @@ __device__ __forceinline__ void half_epilogue(const GemmArgs& g, const TcPlan& p
             float v[32];
             tc_ld32(taddr + hf * 128 + c * 32, v);
             logit_stats_update<32>(v, nt * TC_BN + hf * 128 + c * 32, m, sm, arg);
+            if (g.logits && valid) store_logits<32>(g, grow, nt * TC_BN + hf * 128 + c * 32, v);
         }
         if (valid) *logit_entry(g, nt, hf, grow) = make_float4(m, sm, __int_as_float(arg), (float)n_halves);
     } else if (g.epilogue == kEpiSwiGLU) {
@@ -1222,10 +1232,13 @@ int launch_predict_commit(const GemmArgs& g, int batch, int n_blk, float thresho
     if (g.M == 0) return 0;
     const GemmLaunch gl = plan_gemm(g);
     if (launch_pdl(logit_reduce_kernel, dim3(g.M), dim3(LR_THREADS), 0, stream, g, gl.p, gl.split, token, confidence) != cudaSuccess) return -1;
-    if (launch_pdl(commit_kernel, dim3(batch), dim3(32), 0, stream, (const float*)confidence, n_blk, threshold, commit) !=
-        cudaSuccess)
-        return -1;
-    return 2;
+    const int nl = launch_commit(confidence, batch, n_blk, threshold, commit, stream);
+    return nl < 0 ? -1 : 1 + nl;
+}
+
+int launch_commit(const float* confidence, int batch, int n_blk, float threshold, int32_t* commit, cudaStream_t stream) {
+    if (batch == 0 || n_blk == 0) return 0;
+    return launch_pdl(commit_kernel, dim3(batch), dim3(32), 0, stream, confidence, n_blk, threshold, commit) == cudaSuccess ? 1 : -1;
 }
 
 }  // namespace acache

@@ -154,6 +154,7 @@ struct GemmArgs {
     // --- kEpiSwiGLU / kEpiResidual output ---
     void* c;                  // bf16 [M, Nout]
     // --- kEpiLogits ---
+    float* logits;            // fp32 [M, n[0]] or null: the logits as well
     float4* logit_stats;      // [n_tiles, 16, M] of (max, sum exp(z - max), argmax as int bits, entries of the tile)
     // --- row work fused in front of the contraction ---
     RowPrep prep;             // writes the A rows (a) before the contraction
@@ -172,6 +173,8 @@ int launch_gemm(const GemmArgs& g, cudaStream_t stream);      // kernels launche
 // commit[b, i] = conf > threshold, and if no row of request b qualifies, its most confident row.
 int launch_predict_commit(const GemmArgs& g, int batch, int n_blk, float threshold, int32_t* token, float* confidence,
                           int32_t* commit, cudaStream_t stream);
+// The commit rule alone; kernels launched, or -1.
+int launch_commit(const float* confidence, int batch, int n_blk, float threshold, int32_t* commit, cudaStream_t stream);
 
 // ---- attn.cu ----------------------------------------------------------------------------
 struct AttnArgs {
@@ -301,5 +304,23 @@ struct PagedAttnArgs {
 };
 size_t paged_attention_scratch_bytes(int head_dim);
 int launch_paged_attention(const PagedAttnArgs& a, cudaStream_t stream);    // kernels launched, or -1
+
+// ---- sample.cu ----------------------------------------------------------------------------
+constexpr int kSampleMaxVocab = 1 << 18;
+struct SampleArgs {
+    const void* logits;             // [rows, vocab] bf16 or fp32, rows row_stride elements apart
+    int bf16, rows, vocab;
+    int64_t row_stride;
+    const float *temperature, *top_p, *min_p;    // [rows / rows_per_setting, rounded up] or null
+    const int32_t* top_k;
+    int rows_per_setting;
+    const float* u;                 // [rows]
+    int32_t* token;
+    float *prob, *confidence;       // or null
+    uint32_t* status;
+    int shift;                      // a weight is a whole number of 2^-shift
+    int cluster, chunk;             // set by the launcher: CTAs of a row, logits of each
+};
+int launch_sample(const SampleArgs& a, cudaStream_t stream);                // kernels launched, or -1
 
 }  // namespace acache
