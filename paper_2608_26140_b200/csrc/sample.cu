@@ -4,13 +4,16 @@
 //   make up top_p of their weight, those with w_i >= min_p, whatever is least; the token is the first of them whose running sum
 //   passes u times the sum S of all that are kept.
 //
-// Nothing is sorted.  A weight is a whole number of 2^-shift (46 bits behind the point for up to 2^16 tokens, one less for every doubling), so that sums are exact and do not
-// depend on their order; what is below half of that is never drawn.  Each of the three searches (the k-th token, the one
-// at which top_p is reached, the one that is drawn) goes over a histogram of counts and weights, whose bins part the logits evenly from the largest
-// to the smallest that counts, then over the tokens of one bin: by comparing them all with one another, where
-// they are few, else by another histogram of their keys.  Searches end at a value; among the tokens that have it the index decides.
-// The row lies in the shared memory of a cluster of CTAs, read once; what a CTA finds out is read by the others from there.  Every CTA takes
-// every decision by itself, so that a search costs one barrier of the cluster, and a histogram two.
+// A weight is a whole number of 2^-shift (46 bits behind the point for up to 2^16 tokens, one less for every doubling), so that sums are exact and do not
+// depend on their order; what is below half of that is never drawn.  The row lies in the shared memory of a cluster of CTAs, read once; what a CTA
+// finds out is read by the others from there, and every CTA takes every decision by itself, so that a step of a search costs one barrier
+// of the cluster.  The logits are counted by bins that part them evenly from the largest to the smallest whose weight counts.
+//  - With a top_k of up to kTop (and room in the list) the tokens of the bins that hold the first top_k go into a list; one CTA sorts it, adds up their weights
+//    and decides.  No other weight is formed.
+//  - Else the bins have weights too (32-bit atomics on the two halves of a sum: adding 64 bits at once took five times as long).  Each of the searches (the
+//    k-th token, the one at which top_p is reached, the one that is drawn) goes to a bin, then over the tokens of that bin: by comparing
+//    them all with one another, where they are few, else by another histogram of their keys.  A search ends at a value; among the tokens that have
+//    it the index decides.
 #include <algorithm>
 
 #include "kernels.h"
@@ -26,7 +29,9 @@ using u64 = unsigned long long;
 constexpr int kThreads = 512, kWarps = kThreads / 32;
 constexpr int kBins = 2048;
 constexpr int kFew = 512;                // tokens of a bin that are compared with one another
+constexpr int kTop = 1024, kList = 2048; // largest top_k that is sorted; room for the tokens of its bins
 constexpr int kMaxCluster = 8;
+constexpr int kSteps = 32, kCopies = 16; // a table of 2^(-j / 32), a copy for every lane of half a warp: no two in one bank
 
 __device__ __forceinline__ uint32_t order_key(float f) {     // larger float, larger key; 0 and -0 are one
     uint32_t u = __float_as_uint(f);
@@ -62,6 +67,7 @@ struct Share {                           // what the others read
 };
 struct alignas(16) Scratch {
     Share share;
+    double power[kSteps][kCopies];
     float f[2][kWarps];
     double d[kWarps];
     u64 m[2][kWarps];
@@ -72,35 +78,54 @@ struct alignas(16) Scratch {
     Found found;
     int list_n;
     uint32_t list_lo, list_hi;
+    u64 reached[2];
 };
 struct Entry {
     u64 weight;
     uint32_t key, pad;
 };
+struct Hist {                            // this CTA's counts and weights; a weight in two halves
+    uint32_t count[kBins], lo[kBins], hi[kBins];
+};
+union Work {                             // one after the other
+    Hist hist;
+    u64 top[kList];                      // key and index of the tokens of the first bins, a word each
+    struct {
+        uint32_t key[2][kFew];           // of a bin's tokens, two in turn
+        Entry merged[kFew];              // the cluster's
+    } few;
+};
 
 template <class T>
 struct SampleSmem {
+    static constexpr size_t kSorted = 2 * kList * sizeof(u64);               // the sorted list and its running sums, in the row's place
     static size_t bytes(int chunk, int cluster) {
-        return sizeof(Scratch) + kBins * 12 + 2 * (kBins / cluster) * sizeof(Totals) + 3 * kFew * sizeof(Entry) + (chunk + 16) * sizeof(T) + 64;
+        return sizeof(Work) + sizeof(Scratch) + 2 * (kBins / cluster) * sizeof(Totals) +
+               std::max(kSorted, (chunk + 32) * sizeof(T));
     }
 };
 
 template <class T>
-__global__ void __launch_bounds__(kThreads) sample_kernel(const SampleArgs a) {
+__global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a) {
     extern __shared__ __align__(16) unsigned char smem[];
     const int cluster = a.cluster, row = blockIdx.x / cluster, rank = blockIdx.x % cluster;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int slice = kBins / cluster;
-    u64* hist_mass = reinterpret_cast<u64*>(smem);
-    Entry* lists = reinterpret_cast<Entry*>(hist_mass + kBins);              // [2][kFew], then the cluster's
-    Entry* merged = lists + 2 * kFew;
-    Totals* totals = reinterpret_cast<Totals*>(merged + kFew);               // [2][slice]
-    Scratch& s = *reinterpret_cast<Scratch*>(totals + 2 * slice);
-    uint32_t* hist_count = reinterpret_cast<uint32_t*>(&s + 1);
-    T* held = reinterpret_cast<T*>(hist_count + kBins);
+    Work& work = *reinterpret_cast<Work*>(smem);
+    Hist& hist = work.hist;
+    Scratch& s = *reinterpret_cast<Scratch*>(&work + 1);
+    Totals* totals = reinterpret_cast<Totals*>(&s + 1);                      // [2][slice]
+    T* held = reinterpret_cast<T*>(totals + 2 * slice);
     Share& share = s.share;
 
-    for (int i = tid; i < kBins; i += kThreads) { hist_mass[i] = 0ull; hist_count[i] = 0u; }
+    auto clear = [&] {
+        __syncthreads();
+        for (int i = tid; i < kBins; i += kThreads) hist.count[i] = hist.lo[i] = hist.hi[i] = 0u;
+        __syncthreads();
+    };
+    clear();
+    static_assert(kThreads == kSteps * kCopies, "a thread makes one");
+    s.power[tid / kCopies][tid % kCopies] = exp2(-(double)(tid / kCopies) / kSteps);
     pdl_wait();
     pdl_launch_dependents();
 
@@ -109,6 +134,7 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(const SampleArgs a) {
     const T* from = static_cast<const T*>(a.logits) + (int64_t)row * a.row_stride + e0;
     constexpr int VEC = 16 / sizeof(T);
     const int shift = (int)(reinterpret_cast<uintptr_t>(from) % 16 / sizeof(T));     // held[shift + i]: whole pieces of 16 bytes in both places
+    const int pieces = (shift + n + VEC - 1) / VEC;          // the first and the last filled up with -inf
     T* mine = held + shift;
     float top = -INFINITY, low = INFINITY;
     bool nan = false;
@@ -120,10 +146,20 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(const SampleArgs a) {
     };
     auto to_f = [](T v) -> float { if constexpr (sizeof(T) == 2) return __bfloat162float(v); else return v; };
     auto from_f = [](float v) -> T { if constexpr (sizeof(T) == 2) return __float2bfloat16(v); else return v; };
+    auto unpack = [](const uint4& v, float (&x)[VEC]) {
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            if constexpr (sizeof(T) == 2) { x[2 * k] = bf16_lo(w[k]); x[2 * k + 1] = bf16_hi(w[k]); }
+            else x[k] = __uint_as_float(w[k]);
+        }
+    };
     {
-        const int lead = min(n, (VEC - shift) % VEC), body = (n - lead) / VEC;
+        const int lead = min(n, (VEC - shift) % VEC), body = (n - lead) / VEC, tail = lead + body * VEC;
         for (int i = tid; i < lead; i += kThreads) mine[i] = from_f(take(to_f(from[i])));
-        for (int i = lead + body * VEC + tid; i < n; i += kThreads) mine[i] = from_f(take(to_f(from[i])));
+        for (int i = tail + tid; i < n; i += kThreads) mine[i] = from_f(take(to_f(from[i])));
+        if (tid < shift) held[tid] = from_f(-INFINITY);
+        if (shift + n + tid < pieces * VEC) mine[n + tid] = from_f(-INFINITY);
         constexpr int AHEAD = 4;
         for (int i0 = tid; i0 < body; i0 += AHEAD * kThreads) {
             uint4 v[AHEAD];
@@ -133,15 +169,29 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(const SampleArgs a) {
 #pragma unroll
             for (int j = 0; j < AHEAD; ++j) {
                 if (i0 + j * kThreads >= body) break;
-                T* x = reinterpret_cast<T*>(&v[j]);
+                float x[VEC];
+                unpack(v[j], x);
+                bool odd = false;
 #pragma unroll
-                for (int k = 0; k < VEC; ++k) x[k] = from_f(take(to_f(x[k])));
+                for (int k = 0; k < VEC; ++k) { odd |= x[k] != x[k]; x[k] = take(x[k]); }
+                if (odd) {
+                    T* w = reinterpret_cast<T*>(&v[j]);
+#pragma unroll
+                    for (int k = 0; k < VEC; ++k) w[k] = from_f(x[k]);
+                }
                 *(reinterpret_cast<uint4*>(mine + lead) + i0 + j * kThreads) = v[j];
             }
         }
     }
     if (nan) atomicOr(a.status, kFlagNonFinite);
-    auto logit = [&](int i) { return to_f(mine[i]); };
+    // each piece of 16 bytes to f(logits, index of the first)
+    auto each = [&](auto&& f) {
+        for (int i = tid; i < pieces; i += kThreads) {
+            float x[VEC];
+            unpack(reinterpret_cast<const uint4*>(held)[i], x);
+            f(x, i * VEC - shift);
+        }
+    };
 #pragma unroll
     for (int off = 16; off; off >>= 1) {
         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
@@ -185,53 +235,72 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(const SampleArgs a) {
     const int top_k = a.top_k ? a.top_k[at] : 0;
     const double unit = (double)(1ull << a.shift);
     const double rate = 1.4426950408889634074 / (double)temperature;         // log2 of a weight per logit
+    const u64 least = (u64)ceil((double)min_p * unit);
     // half of the distance from the largest, which may be infinite (the whole of it would pass fp32's range between finite logits)
     const float half_top = 0.5f * top;
     auto behind = [&](float l) { return l == top ? 0.f : fmaf(-0.5f, l, half_top); };
+    // 2^-y in units, for y up to shift + 1: y = j / 32 + r, the table's 2^(-j / 32) times 2^-r by its series, of which |r ln 2|^7 / 5040 < 2^-58 is left
+    // out; the last addition rounds to whole units
     auto weight = [&](float l) -> u64 {
         const double y = l == top ? 0.0 : ((double)top - (double)l) * rate;
-        return __double2ull_rn(exp2(-y) * unit);
+        constexpr double kRound = 1.5 * 140737488355328.0;                   // 1.5 * 2^47: what is added to it is rounded to 1 / 32
+        constexpr double kLn2 = 0.69314718055994530942;
+        const double t = y + kRound, r = (y - (t - kRound)) * -kLn2;
+        const int j = __double2loint(t);
+        const double at = s.power[j & (kSteps - 1)][lane & (kCopies - 1)];
+        const double scaled = __hiloint2double(__double2hiint(at) + ((a.shift - (j >> 5)) << 20), __double2loint(at));
+        double p = fma(r, 1.0 / 720, 1.0 / 120);
+        p = fma(r, p, 1.0 / 24);
+        p = fma(r, p, 1.0 / 6);
+        p = fma(r, p, 0.5);
+        p = fma(r, p, 1.0);
+        p = fma(r, p, 1.0);
+        return (u64)__double_as_longlong(fma(scaled, p, 4503599627370496.0)) & 0xFFFFFFFFFFFFFull;
     };
     // logits that count: their weight is not below half of the unit
     const float reach = fminf(fminf(behind(low), (float)(0.5 * (a.shift + 1.0) / rate)), 3.4028234663852886e38f);
-    const float bins_per = (float)kBins / reach;             // (infinite where all are equal: they are in bin 0, as 0 times it is NaN and that a 0)
-    auto bin_of = [&](float d) { return min((int)(d * bins_per), kBins - 1); };
+    const float bins_per = (float)(kBins - 1) / reach;       // (infinite where all are equal)
+    auto bin_of = [&](float d) { return d > 0.f ? (int)(__float_as_uint(fmaf(fminf(d, reach), bins_per, 8388608.f)) & (kBins - 1)) : 0; };      // to the nearest
 
-    // ---- weights and counts by bins; the sum for the confidence; what min_p leaves ----
-    const u64 least = (u64)ceil((double)min_p * unit);
-    double conf = 0.0;
+    // ---- counts and weights by bins; the sum for the confidence; what min_p leaves ----
+    float conf = 0.f;
     u64 mass_min_p = 0ull;
-    {
-        float c = 0.f;
-        for (int i = tid; i < n; i += kThreads) {
-            const float l = logit(i), d = behind(l);
-            c += exp2f(d * -2.8853900817779268f);
-            if (!greedy && d <= reach) {
-                const u64 w = weight(l);
-                const int bin = bin_of(d);
-                atomicAdd(&hist_mass[bin], w);
-                atomicAdd(&hist_count[bin], 1u);
-                if (w >= least) mass_min_p += w;
-            }
-        }
-        conf = c;
-    }
+    auto add_weight = [&](int bin, u64 w) {
+        const uint32_t w_lo = (uint32_t)w, was = atomicAdd(&hist.lo[bin], w_lo), w_hi = (uint32_t)(w >> 32) + (was + w_lo < was);
+        if (w_hi) atomicAdd(&hist.hi[bin], w_hi);
+    };
+    auto add_conf = [&](const float (&x)[VEC]) {
 #pragma unroll
-    for (int off = 16; off; off >>= 1) {
-        conf += __shfl_xor_sync(0xffffffffu, conf, off);
-        mass_min_p += __shfl_xor_sync(0xffffffffu, mass_min_p, off);
-    }
-    if (lane == 0) { s.d[warp] = conf; s.m[0][warp] = mass_min_p; }
-    __syncthreads();
-    if (tid == 0) {
-        double x = 0.0;
-        u64 y = 0ull;
-        for (int w = 0; w < kWarps; ++w) { x += s.d[w]; y += s.m[0][w]; }
-        share.confidence = x;
-        share.mass_min_p = y;
-    }
+        for (int k = 0; k < VEC; ++k) {
+            float e;
+            asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(behind(x[k]) * -2.8853900817779268f));
+            conf += e;
+        }
+    };
+    auto count_all = [&] {
+        each([&](const float (&x)[VEC], int) {
+#pragma unroll
+            for (int k = 0; k < VEC; ++k) {
+                const float d = behind(x[k]);
+                if (d <= reach) atomicAdd(&hist.count[bin_of(d)], 1u);
+            }
+        });
+    };
+    auto weigh_all = [&] {
+        each([&](const float (&x)[VEC], int) {
+#pragma unroll
+            for (int k = 0; k < VEC; ++k) {
+                const float d = behind(x[k]);
+                if (d <= reach) {
+                    const u64 w = weight(x[k]);
+                    add_weight(bin_of(d), w);
+                    if (w >= least) mass_min_p += w;
+                }
+            }
+        });
+    };
 
-    // sums over the cluster of this CTA's bins; the histogram is clear afterwards
+    // sums over the cluster of this CTA's bins
     auto add_up = [&](int level) {
         cluster_sync_all();
         u64 m = 0ull;
@@ -239,8 +308,9 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(const SampleArgs a) {
         for (int i = tid; i < slice; i += kThreads) {
             Totals t{0ull, 0u};
             for (int r = 0; r < cluster; ++r) {
-                t.mass += *of_peer(hist_mass + rank * slice + i, r);
-                t.count += *of_peer(hist_count + rank * slice + i, r);
+                const Hist* h = of_peer(&hist, r);
+                t.mass += (u64)h->hi[rank * slice + i] << 32 | h->lo[rank * slice + i];
+                t.count += h->count[rank * slice + i];
             }
             totals[level * slice + i] = t;
             m += t.mass;
@@ -259,10 +329,10 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(const SampleArgs a) {
             share.slice[level] = t;
         }
         cluster_sync_all();
-        for (int i = tid; i < kBins; i += kThreads) { hist_mass[i] = 0ull; hist_count[i] = 0u; }
     };
 
-    // the first bin at which the running count (or weight) comes to `target`, from s.bin_count, s.bin_mass on: s.bin, and what is before it
+    // the first bin at which the running count (or weight) comes to `target`, from s.bin_count, s.bin_mass on: s.bin, and what is before it.
+    // Returns the count up to the bin's end.
     auto locate = [&](int level, bool by_count, u64 target) {
         uint32_t count = s.bin_count;
         u64 mass = s.bin_mass;
@@ -303,39 +373,48 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(const SampleArgs a) {
                 s.bin = owner * slice + i;
                 s.bin_count = count;
                 s.bin_mass = mass;
+                s.list_n = (int)(count + t.count);
             }
             count += t.count;
             mass += t.mass;
         }
+        __syncthreads();
+        return s.list_n;
+    };
+    auto from_the_first = [&] {
+        __syncthreads();
+        if (tid == 0) { s.bin_count = 0u; s.bin_mass = 0ull; }
         __syncthreads();
     };
 
     // the value at which the running count (or weight) comes to `target`
     int turn = 0;
     auto find = [&](bool by_count, u64 target) -> Found {
-        __syncthreads();
-        if (tid == 0) { s.bin_count = 0u; s.bin_mass = 0ull; }
-        __syncthreads();
+        from_the_first();
         locate(0, by_count, target);
         uint32_t lo = 0u, hi = 0xffffffffu;                  // keys of the bin, once it is one of keys
         bool keys = false;
         for (;;) {
             // the bin's tokens, in a list of this CTA's
+            __syncthreads();
             if (tid == 0) { s.list_n = 0; s.list_lo = 0xffffffffu; s.list_hi = 0u; }
             __syncthreads();
-            Entry* list = lists + turn * kFew;
+            uint32_t* list = work.few.key[turn];
             const int bin = s.bin;
             uint32_t k_lo = 0xffffffffu, k_hi = 0u;
-            for (int i = tid; i < n; i += kThreads) {
-                const float l = logit(i), d = behind(l);
-                const uint32_t key = order_key(l);
-                if (d <= reach && (keys ? key >= lo && key <= hi : bin_of(d) == bin)) {
-                    k_lo = min(k_lo, key);
-                    k_hi = max(k_hi, key);
-                    const int slot = atomicAdd(&s.list_n, 1);
-                    if (slot < kFew) { list[slot].key = key; list[slot].weight = weight(l); }
+            each([&](const float (&x)[VEC], int) {
+#pragma unroll
+                for (int k = 0; k < VEC; ++k) {
+                    const float d = behind(x[k]);
+                    const uint32_t key = order_key(x[k]);
+                    if (d <= reach && (keys ? key >= lo && key <= hi : bin_of(d) == bin)) {
+                        k_lo = min(k_lo, key);
+                        k_hi = max(k_hi, key);
+                        const int slot = atomicAdd(&s.list_n, 1);
+                        if (slot < kFew) list[slot] = key;
+                    }
                 }
-            }
+            });
             k_lo = __reduce_min_sync(0xffffffffu, k_lo);
             k_hi = __reduce_max_sync(0xffffffffu, k_hi);
             if (lane == 0 && k_lo <= k_hi) { atomicMin(&s.list_lo, k_lo); atomicMax(&s.list_hi, k_hi); }
@@ -358,10 +437,14 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(const SampleArgs a) {
                 return Found{lo, (uint32_t)all, count, weight(value_of(lo)), mass};
             }
             if (all <= kFew) {
+                Entry* merged = work.few.merged;
                 int first = 0;
                 for (int r = 0; r < cluster; ++r) {
                     const int m = of_peer(&share, r)->n[turn];
-                    for (int i = tid; i < m; i += kThreads) merged[first + i] = *of_peer(list + i, r);
+                    for (int i = tid; i < m; i += kThreads) {
+                        const uint32_t key = *of_peer(list + i, r);
+                        merged[first + i] = Entry{weight(value_of(key)), key, 0u};
+                    }
                     first += m;
                 }
                 turn ^= 1;
@@ -390,16 +473,19 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(const SampleArgs a) {
             }
             // too many: a histogram of their keys, the largest first
             turn ^= 1;
+            clear();
             const uint32_t width = hi - lo;
             const int by = max(0, 21 - __clz(width));        // at most 2048 bins
-            for (int i = tid; i < n; i += kThreads) {
-                const float l = logit(i);
-                const uint32_t key = order_key(l);
-                if (behind(l) <= reach && key >= lo && key <= hi) {
-                    atomicAdd(&hist_mass[(hi - key) >> by], weight(l));
-                    atomicAdd(&hist_count[(hi - key) >> by], 1u);
+            each([&](const float (&x)[VEC], int) {
+#pragma unroll
+                for (int k = 0; k < VEC; ++k) {
+                    const uint32_t key = order_key(x[k]);
+                    if (behind(x[k]) <= reach && key >= lo && key <= hi) {
+                        add_weight((hi - key) >> by, weight(x[k]));
+                        atomicAdd(&hist.count[(hi - key) >> by], 1u);
+                    }
                 }
-            }
+            });
             add_up(1);
             locate(1, by_count, target);
             const uint32_t b_lo = (uint32_t)s.bin << by, b_hi = b_lo + ((1u << by) - 1u);
@@ -409,11 +495,152 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(const SampleArgs a) {
             keys = true;
         }
     };
+    // sum of a value over the CTA, in thread 0
+    auto cta_sum = [&](auto v, auto* at_warp) {
+#pragma unroll
+        for (int off = 16; off; off >>= 1) v += __shfl_xor_sync(0xffffffffu, v, off);
+        if (lane == 0) at_warp[warp] = v;
+        __syncthreads();
+        v = 0;
+        if (tid == 0)
+            for (int w = 0; w < kWarps; ++w) v += at_warp[w];
+        return v;
+    };
+    // what is kept of a sum by top_p
+    auto enough_of = [&](u64 sum) { return min(max((u64)ceil((double)fmaxf(top_p, 0.f) * (double)sum), 1ull), sum); };
+    auto drawn_of = [&](u64 kept) {
+        const float u = a.u[row];
+        return u > 0.f ? min((u64)((double)fminf(u, 1.f) * (double)kept), kept - 1ull) : 0ull;
+    };
+    auto give = [&](int token, float l, double prob, double total) {
+        a.token[row] = token;
+        if (a.prob) a.prob[row] = (float)prob;
+        if (a.confidence) a.confidence[row] = (float)((l == top ? 1.0 : exp((double)l - (double)top)) / total);
+    };
+
+    if (a.confidence) {
+        each([&](const float (&x)[VEC], int) { add_conf(x); });
+        const double c = cta_sum((double)conf, s.d);
+        if (tid == 0) share.confidence = c;
+    }
+    auto total_of = [&] {
+        double total = 0.0;
+        if (a.confidence)
+            for (int r = 0; r < cluster; ++r) total += of_peer(&share, r)->confidence;
+        return total;
+    };
+
+    // ---- a small top_k: its tokens in a list ----
+    if (!greedy && top_k > 0 && top_k <= kTop) {
+        count_all();
+        add_up(0);
+        uint32_t count = 0u;
+        for (int r = 0; r < cluster; ++r) count += of_peer(&share, r)->slice[0].count;
+        const u64 k = min((u64)top_k, (u64)count);
+        from_the_first();
+        const int all = locate(0, true, k);
+        if (all <= kList) {
+            const int bin = s.bin;
+            __syncthreads();
+            if (tid == 0) s.list_n = 0;
+            __syncthreads();
+            each([&](const float (&x)[VEC], int i0) {
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) {
+                    const float d = behind(x[j]);
+                    if (d <= reach && bin_of(d) <= bin)
+                        work.top[atomicAdd(&s.list_n, 1)] = (u64)order_key(x[j]) << 32 | ~(uint32_t)(e0 + i0 + j);
+                }
+            });
+            __syncthreads();
+            if (tid == 0) share.n[0] = s.list_n;
+            cluster_sync_all();
+            if (rank == 0) {
+                u64* sorted = reinterpret_cast<u64*>(held);
+                u64* upto = sorted + kList;
+                int first = 0;
+                for (int r = 0; r < cluster; ++r) {
+                    const int m = of_peer(&share, r)->n[0];
+                    const u64* of = of_peer(work.top, r);
+                    for (int i = tid; i < m; i += kThreads) sorted[first + i] = of[i];
+                    first += m;
+                }
+                int room = 2;
+                while (room < all) room *= 2;
+                for (int i = all + tid; i < room; i += kThreads) sorted[i] = 0ull;
+                for (int size = 2; size <= room; size *= 2)
+                    for (int step = size / 2; step; step /= 2) {
+                        __syncthreads();
+                        for (int i = tid; i < room / 2; i += kThreads) {
+                            const int x = 2 * i - (i & (step - 1)), y = x + step;
+                            const u64 u = sorted[x], v = sorted[y];
+                            if ((u < v) == ((x & size) == 0)) { sorted[x] = v; sorted[y] = u; }      // the largest first
+                        }
+                    }
+                __syncthreads();
+                // running sums of the weights, four tokens a thread
+                constexpr int PER = kList / kThreads;
+                u64 w[PER], sum = 0ull;
+#pragma unroll
+                for (int j = 0; j < PER; ++j) {
+                    const int i = tid * PER + j;
+                    w[j] = (u64)i < k ? weight(value_of((uint32_t)(sorted[i] >> 32))) : 0ull;
+                    sum += w[j];
+                }
+                u64 run = sum;
+#pragma unroll
+                for (int off = 1; off < 32; off <<= 1) {
+                    const u64 x = __shfl_up_sync(0xffffffffu, run, off);
+                    if (lane >= off) run += x;
+                }
+                if (lane == 31) s.m[0][warp] = run;
+                __syncthreads();
+                run -= sum;
+                u64 kept = 0ull;
+                for (int v = 0; v < kWarps; ++v) {
+                    if (v < warp) run += s.m[0][v];
+                    kept += s.m[0][v];
+                }
+                // the sum at the first token where it comes to `target`; [1]: at the last one that min_p leaves
+                const u64 enough = top_p < 1.f ? enough_of(kept) : kept;
+                if (tid == 0) s.reached[1] = kept;
+                __syncthreads();
+                u64 r0 = run;
+#pragma unroll
+                for (int j = 0; j < PER; ++j) {
+                    const u64 r1 = r0 + w[j];
+                    if (r0 < enough && enough <= r1) s.reached[0] = r1;
+                    if (r0 < r1 && w[j] < least) atomicMin(&s.reached[1], r0);
+                    r0 = r1;
+                }
+                __syncthreads();
+                kept = min(s.reached[0], s.reached[1]);
+                const u64 target = drawn_of(kept) + 1ull;
+                r0 = run;
+#pragma unroll
+                for (int j = 0; j < PER; ++j) {
+                    const u64 r1 = r0 + w[j];
+                    if (r0 < target && target <= r1) {
+                        const u64 word = sorted[tid * PER + j];
+                        give((int)~(uint32_t)word, value_of((uint32_t)(word >> 32)), (double)w[j] / (double)kept, total_of());
+                    }
+                    r0 = r1;
+                }
+            }
+            cluster_sync_all();                              // nobody leaves while its shared memory is read
+            return;
+        }
+        clear();
+    }
 
     uint32_t token_key = order_key(top);
     u64 token_at = 0ull;                                     // which of the tokens of that value
     double prob = 1.0;
     if (!greedy) {
+        if (top_k > 0) count_all();
+        weigh_all();
+        const u64 left_here = cta_sum(mass_min_p, s.m[1]);
+        if (tid == 0) share.mass_min_p = left_here;
         add_up(0);
         u64 sum = 0ull, left = 0ull;
         uint32_t count = 0u;
@@ -429,23 +656,23 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(const SampleArgs a) {
         }
         u64 kept = sum;
         if (top_p < 1.f) {
-            const u64 enough = min(max((u64)ceil((double)fmaxf(top_p, 0.f) * (double)sum), 1ull), sum);
+            const u64 enough = enough_of(sum);
             const Found f = find(false, enough);
             kept = f.mass + (enough - f.mass + f.weight - 1ull) / f.weight * f.weight;
         }
         if (least > 0ull) kept = min(kept, left);
-        const float u = a.u[row];
-        const u64 share_of = u > 0.f ? min((u64)((double)fminf(u, 1.f) * (double)kept), kept - 1ull) : 0ull;
-        const Found f = find(false, share_of + 1ull);
+        const u64 drawn = drawn_of(kept);
+        const Found f = find(false, drawn + 1ull);
         token_key = f.key;
-        token_at = min((share_of - f.mass) / f.weight, (u64)(f.equal - 1u));
+        token_at = min((drawn - f.mass) / f.weight, (u64)(f.equal - 1u));
         prob = (double)f.weight / (double)kept;
     }
 
     // ---- among the tokens of the value, the one with that many before it ----
     const int seg = (n + kThreads - 1) / kThreads * 32, j0 = min(warp * seg, n), j1 = min(j0 + seg, n);
+    auto has_it = [&](int i) { return order_key(to_f(mine[i])) == token_key; };
     uint32_t equal = 0u;
-    for (int i = j0 + lane; i < j1; i += 32) equal += order_key(logit(i)) == token_key;
+    for (int i = j0 + lane; i < j1; i += 32) equal += has_it(i);
     equal = __reduce_add_sync(0xffffffffu, equal);
     __syncthreads();
     if (lane == 0) s.c[warp] = equal;
@@ -457,23 +684,13 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(const SampleArgs a) {
     }
     cluster_sync_all();
     u64 before = 0ull;
-    double total = 0.0;
-    for (int r = 0; r < cluster; ++r) {
-        const Share* p = of_peer(&share, r);
-        if (r < rank) before += p->equal;
-        total += p->confidence;
-    }
+    for (int r = 0; r < rank; ++r) before += of_peer(&share, r)->equal;
     for (int w = 0; w < warp; ++w) before += s.c[w];
     if (before <= token_at && token_at < before + equal) {   // one warp of the cluster
         for (int i = j0; i < j1; i += 32) {
-            const bool eq = i + lane < j1 && order_key(logit(i + lane)) == token_key;
+            const bool eq = i + lane < j1 && has_it(i + lane);
             const uint32_t eqs = __ballot_sync(0xffffffffu, eq);
-            if (eq && before + __popc(eqs & ((1u << lane) - 1u)) == token_at) {
-                const float l = value_of(token_key);
-                a.token[row] = e0 + i + lane;
-                if (a.prob) a.prob[row] = (float)prob;
-                if (a.confidence) a.confidence[row] = (float)((l == top ? 1.0 : exp((double)l - (double)top)) / total);
-            }
+            if (eq && before + __popc(eqs & ((1u << lane) - 1u)) == token_at) give(e0 + i + lane, value_of(token_key), prob, total_of());
             before += __popc(eqs);
         }
     }
