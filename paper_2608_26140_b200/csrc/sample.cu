@@ -15,6 +15,7 @@
 //    them all with one another, where they are few, else by another histogram of their keys.  A search ends at a value; among the tokens that have
 //    it the index decides.
 #include <algorithm>
+#include <type_traits>
 
 #include "kernels.h"
 #include "launch.h"
@@ -31,7 +32,7 @@ constexpr int kBins = 2048;
 constexpr int kFew = 512;                // tokens of a bin that are compared with one another
 constexpr int kTop = 1024, kList = 2048; // largest top_k that is sorted; room for the tokens of its bins
 constexpr int kMaxCluster = 8;
-constexpr int kSteps = 32, kCopies = 16; // a table of 2^(-j / 32), a copy for every lane of half a warp: no two in one bank
+constexpr int kSteps = 64, kCopies = 16; // a table of 2^(-j / 64), a copy for every lane of half a warp: no two in one bank
 
 __device__ __forceinline__ uint32_t order_key(float f) {     // larger float, larger key; 0 and -0 are one
     uint32_t u = __float_as_uint(f);
@@ -51,7 +52,7 @@ struct Totals {                          // of the bins that a CTA adds up for i
     u64 mass;
     uint32_t count;
 };
-struct Found {                           // where a search ended: a value, how many have it, and what comes before them
+struct Found {                           // where a search ended: a value, how many have it, its weight, and what comes before it
     uint32_t key, equal;
     uint32_t count;
     u64 weight, mass;
@@ -75,14 +76,10 @@ struct alignas(16) Scratch {
     int bin;
     uint32_t bin_count;
     u64 bin_mass;
-    Found found;
+    Totals slices[2][kMaxCluster];       // every CTA's, as read from them
     int list_n;
     uint32_t list_lo, list_hi;
     u64 reached[2];
-};
-struct Entry {
-    u64 weight;
-    uint32_t key, pad;
 };
 struct Hist {                            // this CTA's counts and weights; a weight in two halves
     uint32_t count[kBins], lo[kBins], hi[kBins];
@@ -92,13 +89,14 @@ union Work {                             // one after the other
     u64 top[kList];                      // key and index of the tokens of the first bins, a word each
     struct {
         uint32_t key[2][kFew];           // of a bin's tokens, two in turn
-        Entry merged[kFew];              // the cluster's
+        uint32_t merged[kFew];           // the cluster's
+        u64 upto[kFew];                  // sums of their weights, the largest first
     } few;
 };
 
 template <class T>
 struct SampleSmem {
-    static constexpr size_t kSorted = 2 * kList * sizeof(u64);               // the sorted list and its running sums, in the row's place
+    static constexpr size_t kSorted = kList * sizeof(u64);                   // the sorted list, in the row's place
     static size_t bytes(int chunk, int cluster) {
         return sizeof(Work) + sizeof(Scratch) + 2 * (kBins / cluster) * sizeof(Totals) +
                std::max(kSorted, (chunk + 32) * sizeof(T));
@@ -124,8 +122,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
         __syncthreads();
     };
     clear();
-    static_assert(kThreads == kSteps * kCopies, "a thread makes one");
-    s.power[tid / kCopies][tid % kCopies] = exp2(-(double)(tid / kCopies) / kSteps);
+    for (int i = tid; i < kSteps * kCopies; i += kThreads) s.power[i / kCopies][i % kCopies] = exp2(-(double)(i / kCopies) / kSteps);
     pdl_wait();
     pdl_launch_dependents();
 
@@ -210,11 +207,17 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
         if (lane == 0) { share.top = top; share.low = low; }
     }
     cluster_sync_all();
-    top = share.top; low = share.low;
-    for (int r = 0; r < cluster; ++r) {
-        const Share* p = of_peer(&share, r);
-        top = fmaxf(top, p->top);
-        low = fminf(low, p->low);
+    {
+        const Share* p = of_peer(&share, min(lane, cluster - 1));            // a lane for every CTA
+        top = p->top;
+        low = p->low;
+#pragma unroll
+        for (int off = kMaxCluster / 2; off; off >>= 1) {
+            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
+            low = fminf(low, __shfl_xor_sync(0xffffffffu, low, off));
+        }
+        top = __shfl_sync(0xffffffffu, top, 0);
+        low = __shfl_sync(0xffffffffu, low, 0);
     }
     if (top == -INFINITY) {                                  // nothing to draw
         if (rank == 0 && tid == 0) {
@@ -239,21 +242,20 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
     // half of the distance from the largest, which may be infinite (the whole of it would pass fp32's range between finite logits)
     const float half_top = 0.5f * top;
     auto behind = [&](float l) { return l == top ? 0.f : fmaf(-0.5f, l, half_top); };
-    // 2^-y in units, for y up to shift + 1: y = j / 32 + r, the table's 2^(-j / 32) times 2^-r by its series, of which |r ln 2|^7 / 5040 < 2^-58 is left
+    // 2^-y in units, for y up to shift + 1: y = j / 64 + r, the table's 2^(-j / 64) times 2^-r by its series, of which |r ln 2|^6 / 720 < 2^-54 is left
     // out; the last addition rounds to whole units
     auto weight = [&](float l) -> u64 {
         const double y = l == top ? 0.0 : ((double)top - (double)l) * rate;
-        constexpr double kRound = 1.5 * 140737488355328.0;                   // 1.5 * 2^47: what is added to it is rounded to 1 / 32
-        constexpr double kLn2 = 0.69314718055994530942;
-        const double t = y + kRound, r = (y - (t - kRound)) * -kLn2;
+        constexpr double kRound = 1.5 * 70368744177664.0;                    // 1.5 * 2^46: what is added to it is rounded to 1 / 64
+        constexpr double kLn2 = -0.69314718055994530942;
+        const double t = y + kRound, r = y - (t - kRound);
         const int j = __double2loint(t);
         const double at = s.power[j & (kSteps - 1)][lane & (kCopies - 1)];
-        const double scaled = __hiloint2double(__double2hiint(at) + ((a.shift - (j >> 5)) << 20), __double2loint(at));
-        double p = fma(r, 1.0 / 720, 1.0 / 120);
-        p = fma(r, p, 1.0 / 24);
-        p = fma(r, p, 1.0 / 6);
-        p = fma(r, p, 0.5);
-        p = fma(r, p, 1.0);
+        const double scaled = __hiloint2double(__double2hiint(at) + ((a.shift - (j >> 6)) << 20), __double2loint(at));
+        double p = fma(r, kLn2 * kLn2 * kLn2 * kLn2 * kLn2 / 120, kLn2 * kLn2 * kLn2 * kLn2 / 24);
+        p = fma(r, p, kLn2 * kLn2 * kLn2 / 6);
+        p = fma(r, p, kLn2 * kLn2 / 2);
+        p = fma(r, p, kLn2);
         p = fma(r, p, 1.0);
         return (u64)__double_as_longlong(fma(scaled, p, 4503599627370496.0)) & 0xFFFFFFFFFFFFFull;
     };
@@ -269,66 +271,79 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
         const uint32_t w_lo = (uint32_t)w, was = atomicAdd(&hist.lo[bin], w_lo), w_hi = (uint32_t)(w >> 32) + (was + w_lo < was);
         if (w_hi) atomicAdd(&hist.hi[bin], w_hi);
     };
-    auto add_conf = [&](const float (&x)[VEC]) {
-#pragma unroll
-        for (int k = 0; k < VEC; ++k) {
-            float e;
-            asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(behind(x[k]) * -2.8853900817779268f));
-            conf += e;
-        }
-    };
-    auto count_all = [&] {
+    // one pass over the logits, for what is asked for
+    auto pass = [&](auto with_conf, auto with_count, auto with_weight) {
         each([&](const float (&x)[VEC], int) {
 #pragma unroll
             for (int k = 0; k < VEC; ++k) {
                 const float d = behind(x[k]);
-                if (d <= reach) atomicAdd(&hist.count[bin_of(d)], 1u);
-            }
-        });
-    };
-    auto weigh_all = [&] {
-        each([&](const float (&x)[VEC], int) {
-#pragma unroll
-            for (int k = 0; k < VEC; ++k) {
-                const float d = behind(x[k]);
-                if (d <= reach) {
-                    const u64 w = weight(x[k]);
-                    add_weight(bin_of(d), w);
-                    if (w >= least) mass_min_p += w;
+                if constexpr (with_conf.value) {
+                    float e;
+                    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(d * -2.8853900817779268f));
+                    conf += e;
+                }
+                if ((with_count.value || with_weight.value) && d <= reach) {
+                    const int bin = bin_of(d);
+                    if constexpr (with_count.value) atomicAdd(&hist.count[bin], 1u);
+                    if constexpr (with_weight.value) {
+                        const u64 w = weight(x[k]);
+                        add_weight(bin, w);
+                        if (w >= least) mass_min_p += w;
+                    }
                 }
             }
         });
     };
+    using Yes = std::true_type;
+    using No = std::false_type;
+    // sum of a value over the CTA, in every thread of warp 0
+    auto cta_sum = [&](auto v, auto* at_warp) {
+#pragma unroll
+        for (int off = 16; off; off >>= 1) v += __shfl_xor_sync(0xffffffffu, v, off);
+        if (lane == 0) at_warp[warp] = v;
+        __syncthreads();
+        if (warp == 0) {
+            v = at_warp[lane % kWarps];
+#pragma unroll
+            for (int off = kWarps / 2; off; off >>= 1) v += __shfl_xor_sync(0xffffffffu, v, off);
+        }
+        return v;
+    };
 
     // sums over the cluster of this CTA's bins
-    auto add_up = [&](int level) {
+    auto add_up = [&](int level, bool counts, bool weights) {
         cluster_sync_all();
         u64 m = 0ull;
         uint32_t c = 0u;
         for (int i = tid; i < slice; i += kThreads) {
             Totals t{0ull, 0u};
-            for (int r = 0; r < cluster; ++r) {
+            uint32_t n_of[kMaxCluster], lo_of[kMaxCluster], hi_of[kMaxCluster];
+#pragma unroll
+            for (int r = 0; r < kMaxCluster; ++r) {          // (all asked for before the first is used)
+                n_of[r] = lo_of[r] = hi_of[r] = 0u;
+                if (r >= cluster) continue;
                 const Hist* h = of_peer(&hist, r);
-                t.mass += (u64)h->hi[rank * slice + i] << 32 | h->lo[rank * slice + i];
-                t.count += h->count[rank * slice + i];
+                if (counts) n_of[r] = h->count[rank * slice + i];
+                if (weights) {
+                    lo_of[r] = h->lo[rank * slice + i];
+                    hi_of[r] = h->hi[rank * slice + i];
+                }
+            }
+#pragma unroll
+            for (int r = 0; r < kMaxCluster; ++r) {
+                t.mass += (u64)hi_of[r] << 32 | lo_of[r];
+                t.count += n_of[r];
             }
             totals[level * slice + i] = t;
             m += t.mass;
             c += t.count;
         }
-#pragma unroll
-        for (int off = 16; off; off >>= 1) {
-            m += __shfl_xor_sync(0xffffffffu, m, off);
-            c += __shfl_xor_sync(0xffffffffu, c, off);
-        }
-        if (lane == 0) { s.m[0][warp] = m; s.c[warp] = c; }
-        __syncthreads();
-        if (tid == 0) {
-            Totals t{0ull, 0u};
-            for (int w = 0; w < kWarps; ++w) { t.mass += s.m[0][w]; t.count += s.c[w]; }
-            share.slice[level] = t;
-        }
+        m = cta_sum(m, s.m[0]);
+        c = cta_sum(c, s.c);
+        if (tid == 0) share.slice[level] = Totals{m, c};
         cluster_sync_all();
+        if (tid < cluster) s.slices[level][tid] = of_peer(&share, tid)->slice[level];
+        __syncthreads();
     };
 
     // the first bin at which the running count (or weight) comes to `target`, from s.bin_count, s.bin_mass on: s.bin, and what is before it.
@@ -338,7 +353,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
         u64 mass = s.bin_mass;
         int owner = 0;
         for (; owner < cluster - 1; ++owner) {
-            const Totals t = of_peer(&share, owner)->slice[level];
+            const Totals t = s.slices[level][owner];
             if ((by_count ? (u64)(count + t.count) : mass + t.mass) >= target) break;
             count += t.count;
             mass += t.mass;
@@ -387,6 +402,38 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
         __syncthreads();
     };
 
+    // lists of the CTAs one after the other; here: length of the list of the CTA that a lane stands for
+    auto merge = [&](int here, auto&& of, auto* to) {
+        int first = here;
+#pragma unroll
+        for (int off = 1; off < kMaxCluster; off <<= 1) {
+            const int x = __shfl_up_sync(0xffffffffu, first, off);
+            if (lane >= off) first += x;
+        }
+        first -= here;
+        for (int r = warp % cluster; r < cluster; r += kWarps) {             // (as many warps for each)
+            const int m = __shfl_sync(0xffffffffu, here, r), f = __shfl_sync(0xffffffffu, first, r);
+            const auto* list = of(r);
+            for (int i = warp / cluster * 32 + lane; i < m; i += kWarps / cluster * 32) to[f + i] = list[i];
+        }
+        __syncthreads();
+    };
+    // sum of a value over the threads up to this one
+    auto running = [&](u64 v) {
+#pragma unroll
+        for (int off = 1; off < 32; off <<= 1) {
+            const u64 x = __shfl_up_sync(0xffffffffu, v, off);
+            if (lane >= off) v += x;
+        }
+        __syncthreads();
+        if (lane == 31) s.m[0][warp] = v;
+        __syncthreads();
+        u64 before = lane < warp ? s.m[0][lane] : 0ull;      // (fewer warps than lanes)
+#pragma unroll
+        for (int off = kWarps / 2; off; off >>= 1) before += __shfl_xor_sync(0xffffffffu, before, off);
+        return v + __shfl_sync(0xffffffffu, before, 0);
+    };
+
     // the value at which the running count (or weight) comes to `target`
     int turn = 0;
     auto find = [&](bool by_count, u64 target) -> Found {
@@ -421,15 +468,12 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
             __syncthreads();
             if (tid == 0) { share.n[turn] = s.list_n; share.key_lo[turn] = s.list_lo; share.key_hi[turn] = s.list_hi; }
             cluster_sync_all();
-            int all = 0;
-            lo = 0xffffffffu;
-            hi = 0u;
-            for (int r = 0; r < cluster; ++r) {
-                const Share* p = of_peer(&share, r);
-                all += p->n[turn];
-                lo = min(lo, p->key_lo[turn]);
-                hi = max(hi, p->key_hi[turn]);
-            }
+            // a lane for every CTA
+            const Share* p = of_peer(&share, min(lane, cluster - 1));
+            const int here = lane < cluster ? p->n[turn] : 0;
+            lo = __reduce_min_sync(0xffffffffu, p->key_lo[turn]);
+            hi = __reduce_max_sync(0xffffffffu, p->key_hi[turn]);
+            const int all = __reduce_add_sync(0xffffffffu, here);
             const uint32_t count = s.bin_count;
             const u64 mass = s.bin_mass;
             if (lo == hi) {                                  // one value
@@ -437,39 +481,38 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
                 return Found{lo, (uint32_t)all, count, weight(value_of(lo)), mass};
             }
             if (all <= kFew) {
-                Entry* merged = work.few.merged;
-                int first = 0;
-                for (int r = 0; r < cluster; ++r) {
-                    const int m = of_peer(&share, r)->n[turn];
-                    for (int i = tid; i < m; i += kThreads) {
-                        const uint32_t key = *of_peer(list + i, r);
-                        merged[first + i] = Entry{weight(value_of(key)), key, 0u};
-                    }
-                    first += m;
-                }
+                uint32_t* merged = work.few.merged;
+                merge(here, [&](int r) { return of_peer(list, r); }, merged);
                 turn ^= 1;
-                __syncthreads();
-                for (int i = warp; i < all; i += kWarps) {
-                    const uint32_t key = merged[i].key;
-                    const u64 w = merged[i].weight;
-                    u64 m = 0ull;
-                    uint32_t c = 0u, e = 0u;
-                    for (int j = lane; j < all; j += 32) {
-                        const uint32_t k = merged[j].key;
-                        if (k > key) { m += merged[j].weight; ++c; }
-                        e += k == key;
+                // sorted, a key a thread
+                static_assert(kFew == kThreads, "a thread has a key");
+                uint32_t key = tid < all ? merged[tid] : 0u;
+                int room = 32;
+                while (room < all) room *= 2;
+                for (int size = 2; size <= room; size *= 2)
+                    for (int step = size / 2; step; step /= 2) {
+                        uint32_t other;
+                        if (step >= 32) {
+                            __syncthreads();
+                            merged[tid] = key;
+                            __syncthreads();
+                            other = merged[tid ^ step];
+                        } else {
+                            other = __shfl_xor_sync(0xffffffffu, key, step);
+                        }
+                        const bool larger = ((tid & size) == 0) == ((tid & step) == 0);      // the largest first
+                        key = larger ? max(key, other) : min(key, other);
                     }
-#pragma unroll
-                    for (int off = 16; off; off >>= 1) m += __shfl_xor_sync(0xffffffffu, m, off);
-                    c = __reduce_add_sync(0xffffffffu, c);
-                    e = __reduce_add_sync(0xffffffffu, e);
-                    m += mass;
-                    c += count;
-                    const u64 before = by_count ? (u64)c : m, upto = by_count ? (u64)(c + e) : m + w * e;
-                    if (lane == 0 && before < target && target <= upto) s.found = Found{key, e, c, w, m};
-                }
+                const u64 w = tid < all ? weight(value_of(key)) : 0ull;
+                const u64 run = running(w) + mass;           // with this key
+                const u64 before = by_count ? (u64)(count + tid) : run - w, upto = by_count ? (u64)(count + tid + 1) : run;
                 __syncthreads();
-                return s.found;
+                work.few.upto[tid] = run;
+                if (tid < all && before < target && target <= upto) s.list_lo = key;
+                __syncthreads();
+                const uint32_t found = s.list_lo;
+                const int larger = __syncthreads_count(tid < all && key > found), equal = __syncthreads_count(tid < all && key == found);
+                return Found{found, (uint32_t)equal, count + larger, weight(value_of(found)), larger ? work.few.upto[larger - 1] : mass};
             }
             // too many: a histogram of their keys, the largest first
             turn ^= 1;
@@ -486,7 +529,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
                     }
                 }
             });
-            add_up(1);
+            add_up(1, true, true);
             locate(1, by_count, target);
             const uint32_t b_lo = (uint32_t)s.bin << by, b_hi = b_lo + ((1u << by) - 1u);
             const uint32_t top_key = hi;
@@ -494,17 +537,6 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
             lo = max(lo, top_key - min(b_hi, width));
             keys = true;
         }
-    };
-    // sum of a value over the CTA, in thread 0
-    auto cta_sum = [&](auto v, auto* at_warp) {
-#pragma unroll
-        for (int off = 16; off; off >>= 1) v += __shfl_xor_sync(0xffffffffu, v, off);
-        if (lane == 0) at_warp[warp] = v;
-        __syncthreads();
-        v = 0;
-        if (tid == 0)
-            for (int w = 0; w < kWarps; ++w) v += at_warp[w];
-        return v;
     };
     // what is kept of a sum by top_p
     auto enough_of = [&](u64 sum) { return min(max((u64)ceil((double)fmaxf(top_p, 0.f) * (double)sum), 1ull), sum); };
@@ -518,24 +550,27 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
         if (a.confidence) a.confidence[row] = (float)((l == top ? 1.0 : exp((double)l - (double)top)) / total);
     };
 
-    if (a.confidence) {
-        each([&](const float (&x)[VEC], int) { add_conf(x); });
+    auto share_conf = [&] {
         const double c = cta_sum((double)conf, s.d);
         if (tid == 0) share.confidence = c;
-    }
+    };
     auto total_of = [&] {
         double total = 0.0;
-        if (a.confidence)
-            for (int r = 0; r < cluster; ++r) total += of_peer(&share, r)->confidence;
+        for (int r = 0; r < cluster; ++r) total += of_peer(&share, r)->confidence;
         return total;
     };
 
     // ---- a small top_k: its tokens in a list ----
     if (!greedy && top_k > 0 && top_k <= kTop) {
-        count_all();
-        add_up(0);
+        if (a.confidence) {
+            pass(Yes(), Yes(), No());
+            share_conf();
+        } else {
+            pass(No(), Yes(), No());
+        }
+        add_up(0, true, false);
         uint32_t count = 0u;
-        for (int r = 0; r < cluster; ++r) count += of_peer(&share, r)->slice[0].count;
+        for (int r = 0; r < cluster; ++r) count += s.slices[0][r].count;
         const u64 k = min((u64)top_k, (u64)count);
         from_the_first();
         const int all = locate(0, true, k);
@@ -557,14 +592,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
             cluster_sync_all();
             if (rank == 0) {
                 u64* sorted = reinterpret_cast<u64*>(held);
-                u64* upto = sorted + kList;
-                int first = 0;
-                for (int r = 0; r < cluster; ++r) {
-                    const int m = of_peer(&share, r)->n[0];
-                    const u64* of = of_peer(work.top, r);
-                    for (int i = tid; i < m; i += kThreads) sorted[first + i] = of[i];
-                    first += m;
-                }
+                merge(lane < cluster ? of_peer(&share, min(lane, cluster - 1))->n[0] : 0, [&](int r) { return of_peer(work.top, r); }, sorted);
                 int room = 2;
                 while (room < all) room *= 2;
                 for (int i = all + tid; i < room; i += kThreads) sorted[i] = 0ull;
@@ -587,20 +615,9 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
                     w[j] = (u64)i < k ? weight(value_of((uint32_t)(sorted[i] >> 32))) : 0ull;
                     sum += w[j];
                 }
-                u64 run = sum;
-#pragma unroll
-                for (int off = 1; off < 32; off <<= 1) {
-                    const u64 x = __shfl_up_sync(0xffffffffu, run, off);
-                    if (lane >= off) run += x;
-                }
-                if (lane == 31) s.m[0][warp] = run;
-                __syncthreads();
-                run -= sum;
+                const u64 run = running(sum) - sum;
                 u64 kept = 0ull;
-                for (int v = 0; v < kWarps; ++v) {
-                    if (v < warp) run += s.m[0][v];
-                    kept += s.m[0][v];
-                }
+                for (int v = 0; v < kWarps; ++v) kept += s.m[0][v];
                 // the sum at the first token where it comes to `target`; [1]: at the last one that min_p leaves
                 const u64 enough = top_p < 1.f ? enough_of(kept) : kept;
                 if (tid == 0) s.reached[1] = kept;
@@ -622,7 +639,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
                     const u64 r1 = r0 + w[j];
                     if (r0 < target && target <= r1) {
                         const u64 word = sorted[tid * PER + j];
-                        give((int)~(uint32_t)word, value_of((uint32_t)(word >> 32)), (double)w[j] / (double)kept, total_of());
+                        give((int)~(uint32_t)word, value_of((uint32_t)(word >> 32)), (double)w[j] / (double)kept, a.confidence ? total_of() : 1.0);
                     }
                     r0 = r1;
                 }
@@ -635,21 +652,29 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
 
     uint32_t token_key = order_key(top);
     u64 token_at = 0ull;                                     // which of the tokens of that value
+    uint32_t equal_all = 0u;                                 // how many there are, where that is known
     double prob = 1.0;
     if (!greedy) {
-        if (top_k > 0) count_all();
-        weigh_all();
+        const bool counts = top_k > 0, had_conf = counts && top_k <= kTop;   // (a list that was too long)
+        if (counts) {
+            if (a.confidence && !had_conf) pass(Yes(), Yes(), Yes());
+            else pass(No(), Yes(), Yes());
+        } else {
+            if (a.confidence) pass(Yes(), No(), Yes());
+            else pass(No(), No(), Yes());
+        }
+        if (a.confidence && !had_conf) share_conf();
         const u64 left_here = cta_sum(mass_min_p, s.m[1]);
         if (tid == 0) share.mass_min_p = left_here;
-        add_up(0);
+        add_up(0, counts, true);
         u64 sum = 0ull, left = 0ull;
         uint32_t count = 0u;
         for (int r = 0; r < cluster; ++r) {
-            const Share* p = of_peer(&share, r);
-            sum += p->slice[0].mass;
-            count += p->slice[0].count;
-            left += p->mass_min_p;
+            sum += s.slices[0][r].mass;
+            count += s.slices[0][r].count;
         }
+        if (least > 0ull)
+            for (int r = 0; r < cluster; ++r) left += of_peer(&share, r)->mass_min_p;
         if (top_k > 0 && (uint32_t)top_k < count) {
             const Found f = find(true, (u64)top_k);
             sum = f.mass + f.weight * ((u64)top_k - f.count);
@@ -664,8 +689,21 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
         const u64 drawn = drawn_of(kept);
         const Found f = find(false, drawn + 1ull);
         token_key = f.key;
+        equal_all = f.equal;
         token_at = min((drawn - f.mass) / f.weight, (u64)(f.equal - 1u));
         prob = (double)f.weight / (double)kept;
+    } else if (a.confidence) {
+        pass(Yes(), No(), No());
+        share_conf();
+    }
+    if (equal_all == 1u) {
+        each([&](const float (&x)[VEC], int i0) {
+#pragma unroll
+            for (int j = 0; j < VEC; ++j)
+                if (x[j] == value_of(token_key)) give(e0 + i0 + j, x[j], prob, a.confidence ? total_of() : 1.0);
+        });
+        cluster_sync_all();                                  // nobody leaves while its shared memory is read
+        return;
     }
 
     // ---- among the tokens of the value, the one with that many before it ----
@@ -690,7 +728,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
         for (int i = j0; i < j1; i += 32) {
             const bool eq = i + lane < j1 && has_it(i + lane);
             const uint32_t eqs = __ballot_sync(0xffffffffu, eq);
-            if (eq && before + __popc(eqs & ((1u << lane) - 1u)) == token_at) give(e0 + i + lane, value_of(token_key), prob, total_of());
+            if (eq && before + __popc(eqs & ((1u << lane) - 1u)) == token_at) give(e0 + i + lane, value_of(token_key), prob, a.confidence ? total_of() : 1.0);
             before += __popc(eqs);
         }
     }
