@@ -30,7 +30,8 @@ using u64 = unsigned long long;
 constexpr int kThreads = 512, kWarps = kThreads / 32;
 constexpr int kBins = 2048;
 constexpr int kFew = 512;                // tokens of a bin that are compared with one another
-constexpr int kTop = 1024, kList = 2048; // largest top_k that is sorted; room for the tokens of its bins
+constexpr int kTop = 1024, kList = 2048; // largest top_k whose tokens are sorted; room for them and those that come with them
+constexpr int kQuick = 128;              // largest top_k that the largest logits of the threads settle
 constexpr int kMaxCluster = 8;
 constexpr int kSteps = 64, kCopies = 16; // a table of 2^(-j / 64), a copy for every lane of half a warp: no two in one bank
 
@@ -58,7 +59,7 @@ struct Found {                           // where a search ended: a value, how m
     u64 weight, mass;
 };
 struct Share {                           // what the others read
-    float top, low;
+    float top, low, bound;
     double confidence;
     u64 mass_min_p;
     Totals slice[2];                     // sums over this CTA's bins; [1]: of a histogram of keys
@@ -74,8 +75,7 @@ struct alignas(16) Scratch {
     u64 m[2][kWarps];
     uint32_t c[kWarps];
     int bin;
-    uint32_t bin_count;
-    u64 bin_mass;
+    Totals before, upto;
     Totals slices[2][kMaxCluster];       // every CTA's, as read from them
     int list_n;
     uint32_t list_lo, list_hi;
@@ -121,10 +121,18 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
         for (int i = tid; i < kBins; i += kThreads) hist.count[i] = hist.lo[i] = hist.hi[i] = 0u;
         __syncthreads();
     };
-    clear();
     for (int i = tid; i < kSteps * kCopies; i += kThreads) s.power[i / kCopies][i % kCopies] = exp2(-(double)(i / kCopies) / kSteps);
     pdl_wait();
     pdl_launch_dependents();
+
+    // ---- the row's settings ----
+    const int at = row / a.rows_per_setting;
+    const float temperature = a.temperature ? a.temperature[at] : 1.f;
+    const bool greedy = !(temperature > 0.f);
+    const float top_p = a.top_p ? a.top_p[at] : 1.f;
+    const float min_p = a.min_p && a.min_p[at] > 0.f ? fminf(a.min_p[at], 1.f) : 0.f;
+    const int top_k = a.top_k ? a.top_k[at] : 0;
+    const bool sampled = !greedy && top_k > 0, quick = sampled && top_k <= kQuick;
 
     // ---- this CTA's part of the row into shared memory; largest and smallest finite logit ----
     const int e0 = min(rank * a.chunk, a.vocab), n = min(a.chunk, a.vocab - e0);
@@ -189,6 +197,30 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
             f(x, i * VEC - shift);
         }
     };
+    // a value a thread, the largest to the first thread; room: threads that have one (a power of two, 32 and more)
+    auto sorted = [&](auto v, int room, auto* exchange) {
+        for (int size = 2; size <= room; size *= 2)
+            for (int step = size / 2; step; step /= 2) {
+                decltype(v) other;
+                if (step >= 32) {
+                    __syncthreads();
+                    exchange[tid] = v;
+                    __syncthreads();
+                    other = exchange[tid ^ step];
+                } else {
+                    other = __shfl_xor_sync(0xffffffffu, v, step);
+                }
+                const bool larger = ((tid & size) == 0) == ((tid & step) == 0);
+                v = larger ? max(v, other) : min(v, other);
+            }
+        return v;
+    };
+    // A bound that top_k tokens reach at least: the largest logits of that many threads.  (Of 31 logits a thread, those of 50 threads of 512: about 53
+    // tokens of this CTA are as large.)
+    if (quick) {
+        const uint32_t key = sorted(order_key(top), kThreads, work.few.merged);
+        if (tid == top_k - 1) share.bound = value_of(key);
+    }
 #pragma unroll
     for (int off = 16; off; off >>= 1) {
         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
@@ -197,27 +229,32 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
     if (lane == 0) { s.f[0][warp] = top; s.f[1][warp] = low; }
     __syncthreads();
     if (warp == 0) {
-        top = lane < kWarps ? s.f[0][lane] : -INFINITY;
-        low = lane < kWarps ? s.f[1][lane] : INFINITY;
+        top = s.f[0][lane % kWarps];
+        low = s.f[1][lane % kWarps];
 #pragma unroll
-        for (int off = 16; off; off >>= 1) {
+        for (int off = kWarps / 2; off; off >>= 1) {
             top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
             low = fminf(low, __shfl_xor_sync(0xffffffffu, low, off));
         }
         if (lane == 0) { share.top = top; share.low = low; }
     }
+    if (!quick) clear();
     cluster_sync_all();
+    float bound = -INFINITY;
     {
         const Share* p = of_peer(&share, min(lane, cluster - 1));            // a lane for every CTA
         top = p->top;
         low = p->low;
+        if (quick) bound = p->bound;
 #pragma unroll
         for (int off = kMaxCluster / 2; off; off >>= 1) {
             top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
             low = fminf(low, __shfl_xor_sync(0xffffffffu, low, off));
+            bound = fmaxf(bound, __shfl_xor_sync(0xffffffffu, bound, off));
         }
         top = __shfl_sync(0xffffffffu, top, 0);
         low = __shfl_sync(0xffffffffu, low, 0);
+        bound = __shfl_sync(0xffffffffu, bound, 0);
     }
     if (top == -INFINITY) {                                  // nothing to draw
         if (rank == 0 && tid == 0) {
@@ -229,13 +266,6 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
         return;
     }
 
-    // ---- the row's settings ----
-    const int at = row / a.rows_per_setting;
-    const float temperature = a.temperature ? a.temperature[at] : 1.f;
-    const bool greedy = !(temperature > 0.f);
-    const float top_p = a.top_p ? a.top_p[at] : 1.f;
-    const float min_p = a.min_p && a.min_p[at] > 0.f ? fminf(a.min_p[at], 1.f) : 0.f;
-    const int top_k = a.top_k ? a.top_k[at] : 0;
     const double unit = (double)(1ull << a.shift);
     const double rate = 1.4426950408889634074 / (double)temperature;         // log2 of a weight per logit
     const u64 least = (u64)ceil((double)min_p * unit);
@@ -271,17 +301,18 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
         const uint32_t w_lo = (uint32_t)w, was = atomicAdd(&hist.lo[bin], w_lo), w_hi = (uint32_t)(w >> 32) + (was + w_lo < was);
         if (w_hi) atomicAdd(&hist.hi[bin], w_hi);
     };
+    auto add_conf = [&](float d) {
+        float e;
+        asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(d * -2.8853900817779268f));
+        conf += e;
+    };
     // one pass over the logits, for what is asked for
     auto pass = [&](auto with_conf, auto with_count, auto with_weight) {
         each([&](const float (&x)[VEC], int) {
 #pragma unroll
             for (int k = 0; k < VEC; ++k) {
                 const float d = behind(x[k]);
-                if constexpr (with_conf.value) {
-                    float e;
-                    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(d * -2.8853900817779268f));
-                    conf += e;
-                }
+                if constexpr (with_conf.value) add_conf(d);
                 if ((with_count.value || with_weight.value) && d <= reach) {
                     const int bin = bin_of(d);
                     if constexpr (with_count.value) atomicAdd(&hist.count[bin], 1u);
@@ -310,114 +341,6 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
         return v;
     };
 
-    // sums over the cluster of this CTA's bins
-    auto add_up = [&](int level, bool counts, bool weights) {
-        cluster_sync_all();
-        u64 m = 0ull;
-        uint32_t c = 0u;
-        for (int i = tid; i < slice; i += kThreads) {
-            Totals t{0ull, 0u};
-            uint32_t n_of[kMaxCluster], lo_of[kMaxCluster], hi_of[kMaxCluster];
-#pragma unroll
-            for (int r = 0; r < kMaxCluster; ++r) {          // (all asked for before the first is used)
-                n_of[r] = lo_of[r] = hi_of[r] = 0u;
-                if (r >= cluster) continue;
-                const Hist* h = of_peer(&hist, r);
-                if (counts) n_of[r] = h->count[rank * slice + i];
-                if (weights) {
-                    lo_of[r] = h->lo[rank * slice + i];
-                    hi_of[r] = h->hi[rank * slice + i];
-                }
-            }
-#pragma unroll
-            for (int r = 0; r < kMaxCluster; ++r) {
-                t.mass += (u64)hi_of[r] << 32 | lo_of[r];
-                t.count += n_of[r];
-            }
-            totals[level * slice + i] = t;
-            m += t.mass;
-            c += t.count;
-        }
-        m = cta_sum(m, s.m[0]);
-        c = cta_sum(c, s.c);
-        if (tid == 0) share.slice[level] = Totals{m, c};
-        cluster_sync_all();
-        if (tid < cluster) s.slices[level][tid] = of_peer(&share, tid)->slice[level];
-        __syncthreads();
-    };
-
-    // the first bin at which the running count (or weight) comes to `target`, from s.bin_count, s.bin_mass on: s.bin, and what is before it.
-    // Returns the count up to the bin's end.
-    auto locate = [&](int level, bool by_count, u64 target) {
-        uint32_t count = s.bin_count;
-        u64 mass = s.bin_mass;
-        int owner = 0;
-        for (; owner < cluster - 1; ++owner) {
-            const Totals t = s.slices[level][owner];
-            if ((by_count ? (u64)(count + t.count) : mass + t.mass) >= target) break;
-            count += t.count;
-            mass += t.mass;
-        }
-        const int per = (slice + kThreads - 1) / kThreads, i0 = tid * per;
-        const Totals* from_owner = of_peer(totals + level * slice, owner);
-        u64 m = 0ull;
-        uint32_t c = 0u;
-        for (int i = i0; i < min(i0 + per, slice); ++i) {
-            const Totals t = from_owner[i];
-            m += t.mass;
-            c += t.count;
-        }
-        u64 m_to = m;
-        uint32_t c_to = c;
-#pragma unroll
-        for (int off = 1; off < 32; off <<= 1) {
-            const u64 x = __shfl_up_sync(0xffffffffu, m_to, off);
-            const uint32_t y = __shfl_up_sync(0xffffffffu, c_to, off);
-            if (lane >= off) { m_to += x; c_to += y; }
-        }
-        if (lane == 31) { s.m[0][warp] = m_to; s.c[warp] = c_to; }
-        __syncthreads();                                     // (also: everyone has read where the search begins)
-        for (int w = 0; w < warp; ++w) { mass += s.m[0][w]; count += s.c[w]; }
-        mass += m_to - m;
-        count += c_to - c;
-        const bool last = i0 < slice && i0 + per >= slice;   // (whatever the target, some bin is found)
-        for (int i = i0; i < min(i0 + per, slice); ++i) {
-            const Totals t = from_owner[i];
-            const u64 before = by_count ? (u64)count : mass, upto = by_count ? (u64)(count + t.count) : mass + t.mass;
-            if (before < target && (target <= upto || (last && i == slice - 1))) {
-                s.bin = owner * slice + i;
-                s.bin_count = count;
-                s.bin_mass = mass;
-                s.list_n = (int)(count + t.count);
-            }
-            count += t.count;
-            mass += t.mass;
-        }
-        __syncthreads();
-        return s.list_n;
-    };
-    auto from_the_first = [&] {
-        __syncthreads();
-        if (tid == 0) { s.bin_count = 0u; s.bin_mass = 0ull; }
-        __syncthreads();
-    };
-
-    // lists of the CTAs one after the other; here: length of the list of the CTA that a lane stands for
-    auto merge = [&](int here, auto&& of, auto* to) {
-        int first = here;
-#pragma unroll
-        for (int off = 1; off < kMaxCluster; off <<= 1) {
-            const int x = __shfl_up_sync(0xffffffffu, first, off);
-            if (lane >= off) first += x;
-        }
-        first -= here;
-        for (int r = warp % cluster; r < cluster; r += kWarps) {             // (as many warps for each)
-            const int m = __shfl_sync(0xffffffffu, here, r), f = __shfl_sync(0xffffffffu, first, r);
-            const auto* list = of(r);
-            for (int i = warp / cluster * 32 + lane; i < m; i += kWarps / cluster * 32) to[f + i] = list[i];
-        }
-        __syncthreads();
-    };
     // sum of a value over the threads up to this one
     auto running = [&](u64 v) {
 #pragma unroll
@@ -434,20 +357,110 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
         return v + __shfl_sync(0xffffffffu, before, 0);
     };
 
+    // running sums over the cluster of this CTA's bins; s.slices: every CTA's whole sum
+    auto add_up = [&](int level, bool counts, bool weights) {
+        cluster_sync_all();
+        constexpr int PER = kBins / kThreads;                // of a cluster of one; else a bin a thread at most
+        const int per = (slice + kThreads - 1) / kThreads, i0 = tid * per;
+        u64 m[PER];
+        uint32_t c[PER];
+#pragma unroll
+        for (int j = 0; j < PER; ++j) {
+            m[j] = 0ull;
+            c[j] = 0u;
+            if (j >= per || i0 + j >= slice) continue;
+            uint32_t n_of[kMaxCluster], lo_of[kMaxCluster], hi_of[kMaxCluster];
+#pragma unroll
+            for (int r = 0; r < kMaxCluster; ++r) {          // (all asked for before the first is used)
+                n_of[r] = lo_of[r] = hi_of[r] = 0u;
+                if (r >= cluster) continue;
+                const Hist* h = of_peer(&hist, r);
+                if (counts) n_of[r] = h->count[rank * slice + i0 + j];
+                if (weights) {
+                    lo_of[r] = h->lo[rank * slice + i0 + j];
+                    hi_of[r] = h->hi[rank * slice + i0 + j];
+                }
+            }
+#pragma unroll
+            for (int r = 0; r < kMaxCluster; ++r) {
+                m[j] += (u64)hi_of[r] << 32 | lo_of[r];
+                c[j] += n_of[r];
+            }
+        }
+#pragma unroll
+        for (int j = 1; j < PER; ++j) {
+            m[j] += m[j - 1];
+            c[j] += c[j - 1];
+        }
+        const u64 before_m = weights ? running(m[PER - 1]) - m[PER - 1] : 0ull;
+        const uint32_t before_c = counts ? (uint32_t)running((u64)c[PER - 1]) - c[PER - 1] : 0u;
+#pragma unroll
+        for (int j = 0; j < PER; ++j)
+            if (j < per && i0 + j < slice) totals[level * slice + i0 + j] = Totals{before_m + m[j], before_c + c[j]};
+        if (tid == kThreads - 1) share.slice[level] = Totals{before_m + m[PER - 1], before_c + c[PER - 1]};
+        cluster_sync_all();
+        if (tid < cluster) s.slices[level][tid] = of_peer(&share, tid)->slice[level];
+        __syncthreads();
+    };
+
+    // the first bin at which the running count (or weight), `before` the first one, comes to `target`; upto: with that bin
+    struct Place {
+        int bin;
+        Totals before, upto;
+    };
+    auto locate = [&](int level, bool by_count, u64 target, Totals before) -> Place {
+        int owner = 0;
+        for (; owner < cluster - 1; ++owner) {
+            const Totals t = s.slices[level][owner];
+            if ((by_count ? (u64)(before.count + t.count) : before.mass + t.mass) >= target) break;
+            before.count += t.count;
+            before.mass += t.mass;
+        }
+        const Totals* of = of_peer(totals + level * slice, owner);
+        for (int i = tid; i < slice; i += kThreads) {
+            Totals t0 = i > 0 ? of[i - 1] : Totals{0ull, 0u}, t1 = of[i];
+            t0 = Totals{before.mass + t0.mass, before.count + t0.count};
+            t1 = Totals{before.mass + t1.mass, before.count + t1.count};
+            const u64 from_here = by_count ? (u64)t0.count : t0.mass, to_here = by_count ? (u64)t1.count : t1.mass;
+            if (from_here < target && (target <= to_here || i == slice - 1)) {      // (whatever the target, some bin is found)
+                s.bin = owner * slice + i;
+                s.before = t0;
+                s.upto = t1;
+            }
+        }
+        __syncthreads();
+        const Place p{s.bin, s.before, s.upto};
+        __syncthreads();                                     // everyone has it
+        return p;
+    };
+    // lists of the CTAs one after the other; here: length of the list of the CTA that a lane stands for
+    auto merge = [&](int here, auto&& of, auto* to) {
+        int first = here;
+#pragma unroll
+        for (int off = 1; off < kMaxCluster; off <<= 1) {
+            const int x = __shfl_up_sync(0xffffffffu, first, off);
+            if (lane >= off) first += x;
+        }
+        first -= here;
+        for (int r = warp % cluster; r < cluster; r += kWarps) {             // (as many warps for each)
+            const int m = __shfl_sync(0xffffffffu, here, r), f = __shfl_sync(0xffffffffu, first, r);
+            const auto* list = of(r);
+            for (int i = warp / cluster * 32 + lane; i < m; i += kWarps / cluster * 32) to[f + i] = list[i];
+        }
+        __syncthreads();
+    };
     // the value at which the running count (or weight) comes to `target`
     int turn = 0;
     auto find = [&](bool by_count, u64 target) -> Found {
-        from_the_first();
-        locate(0, by_count, target);
+        Place at_bin = locate(0, by_count, target, Totals{0ull, 0u});
         uint32_t lo = 0u, hi = 0xffffffffu;                  // keys of the bin, once it is one of keys
         bool keys = false;
         for (;;) {
             // the bin's tokens, in a list of this CTA's
-            __syncthreads();
             if (tid == 0) { s.list_n = 0; s.list_lo = 0xffffffffu; s.list_hi = 0u; }
             __syncthreads();
             uint32_t* list = work.few.key[turn];
-            const int bin = s.bin;
+            const int bin = at_bin.bin;
             uint32_t k_lo = 0xffffffffu, k_hi = 0u;
             each([&](const float (&x)[VEC], int) {
 #pragma unroll
@@ -474,8 +487,8 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
             lo = __reduce_min_sync(0xffffffffu, p->key_lo[turn]);
             hi = __reduce_max_sync(0xffffffffu, p->key_hi[turn]);
             const int all = __reduce_add_sync(0xffffffffu, here);
-            const uint32_t count = s.bin_count;
-            const u64 mass = s.bin_mass;
+            const uint32_t count = at_bin.before.count;
+            const u64 mass = at_bin.before.mass;
             if (lo == hi) {                                  // one value
                 turn ^= 1;
                 return Found{lo, (uint32_t)all, count, weight(value_of(lo)), mass};
@@ -484,25 +497,10 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
                 uint32_t* merged = work.few.merged;
                 merge(here, [&](int r) { return of_peer(list, r); }, merged);
                 turn ^= 1;
-                // sorted, a key a thread
                 static_assert(kFew == kThreads, "a thread has a key");
-                uint32_t key = tid < all ? merged[tid] : 0u;
                 int room = 32;
                 while (room < all) room *= 2;
-                for (int size = 2; size <= room; size *= 2)
-                    for (int step = size / 2; step; step /= 2) {
-                        uint32_t other;
-                        if (step >= 32) {
-                            __syncthreads();
-                            merged[tid] = key;
-                            __syncthreads();
-                            other = merged[tid ^ step];
-                        } else {
-                            other = __shfl_xor_sync(0xffffffffu, key, step);
-                        }
-                        const bool larger = ((tid & size) == 0) == ((tid & step) == 0);      // the largest first
-                        key = larger ? max(key, other) : min(key, other);
-                    }
+                const uint32_t key = sorted(tid < all ? merged[tid] : 0u, room, merged);
                 const u64 w = tid < all ? weight(value_of(key)) : 0ull;
                 const u64 run = running(w) + mass;           // with this key
                 const u64 before = by_count ? (u64)(count + tid) : run - w, upto = by_count ? (u64)(count + tid + 1) : run;
@@ -530,8 +528,8 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
                 }
             });
             add_up(1, true, true);
-            locate(1, by_count, target);
-            const uint32_t b_lo = (uint32_t)s.bin << by, b_hi = b_lo + ((1u << by) - 1u);
+            at_bin = locate(1, by_count, target, at_bin.before);
+            const uint32_t b_lo = (uint32_t)at_bin.bin << by, b_hi = b_lo + ((1u << by) - 1u);
             const uint32_t top_key = hi;
             hi = top_key - b_lo;
             lo = max(lo, top_key - min(b_hi, width));
@@ -554,108 +552,145 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
         const double c = cta_sum((double)conf, s.d);
         if (tid == 0) share.confidence = c;
     };
-    auto total_of = [&] {
-        double total = 0.0;
-        for (int r = 0; r < cluster; ++r) total += of_peer(&share, r)->confidence;
-        return total;
+    // a sum over the cluster, in every thread: v a lane's part, a lane for every CTA
+    auto cluster_sum = [&](auto v) {
+        if (lane >= cluster) v = 0;
+#pragma unroll
+        for (int off = kMaxCluster / 2; off; off >>= 1) v += __shfl_xor_sync(0xffffffffu, v, off);
+        return __shfl_sync(0xffffffffu, v, 0);
     };
+    auto total_of = [&] { return a.confidence ? cluster_sum(of_peer(&share, min(lane, cluster - 1))->confidence) : 1.0; };
 
     // ---- a small top_k: its tokens in a list ----
-    if (!greedy && top_k > 0 && top_k <= kTop) {
-        if (a.confidence) {
-            pass(Yes(), Yes(), No());
-            share_conf();
-        } else {
-            pass(No(), Yes(), No());
+    bool had_conf = false;
+    for (int attempt = quick ? 0 : 1; sampled && top_k <= kTop && attempt < 2; ++attempt) {
+        int bin = -1;
+        if (attempt == 1) {
+            // by the counts of the bins
+            if (quick) clear();                              // (too many tokens at the bound: as many as reach it are equal)
+            if (a.confidence && !had_conf) {
+                pass(Yes(), Yes(), No());
+                share_conf();
+                had_conf = true;
+            } else {
+                pass(No(), Yes(), No());
+            }
+            add_up(0, true, false);
+            uint32_t count = 0u;
+            for (int r = 0; r < cluster; ++r) count += s.slices[0][r].count;
+            const Place p = locate(0, true, min((u64)top_k, (u64)count), Totals{0ull, 0u});
+            if (p.upto.count > kList) break;
+            bin = p.bin;
         }
-        add_up(0, true, false);
-        uint32_t count = 0u;
-        for (int r = 0; r < cluster; ++r) count += s.slices[0][r].count;
-        const u64 k = min((u64)top_k, (u64)count);
-        from_the_first();
-        const int all = locate(0, true, k);
-        if (all <= kList) {
-            const int bin = s.bin;
-            __syncthreads();
-            if (tid == 0) s.list_n = 0;
-            __syncthreads();
-            each([&](const float (&x)[VEC], int i0) {
+        if (tid == 0) s.list_n = 0;
+        __syncthreads();
+        auto put = [&](float l, int i) {
+            const int slot = atomicAdd(&s.list_n, 1);
+            if (slot < kList) work.top[slot] = (u64)order_key(l) << 32 | ~(uint32_t)(e0 + i);
+        };
+        each([&](const float (&x)[VEC], int i0) {
 #pragma unroll
-                for (int j = 0; j < VEC; ++j) {
-                    const float d = behind(x[j]);
-                    if (d <= reach && bin_of(d) <= bin)
-                        work.top[atomicAdd(&s.list_n, 1)] = (u64)order_key(x[j]) << 32 | ~(uint32_t)(e0 + i0 + j);
-                }
-            });
-            __syncthreads();
-            if (tid == 0) share.n[0] = s.list_n;
-            cluster_sync_all();
-            if (rank == 0) {
-                u64* sorted = reinterpret_cast<u64*>(held);
-                merge(lane < cluster ? of_peer(&share, min(lane, cluster - 1))->n[0] : 0, [&](int r) { return of_peer(work.top, r); }, sorted);
-                int room = 2;
-                while (room < all) room *= 2;
-                for (int i = all + tid; i < room; i += kThreads) sorted[i] = 0ull;
-                for (int size = 2; size <= room; size *= 2)
-                    for (int step = size / 2; step; step /= 2) {
-                        __syncthreads();
-                        for (int i = tid; i < room / 2; i += kThreads) {
-                            const int x = 2 * i - (i & (step - 1)), y = x + step;
-                            const u64 u = sorted[x], v = sorted[y];
-                            if ((u < v) == ((x & size) == 0)) { sorted[x] = v; sorted[y] = u; }      // the largest first
-                        }
-                    }
-                __syncthreads();
-                // running sums of the weights, four tokens a thread
-                constexpr int PER = kList / kThreads;
-                u64 w[PER], sum = 0ull;
-#pragma unroll
-                for (int j = 0; j < PER; ++j) {
-                    const int i = tid * PER + j;
-                    w[j] = (u64)i < k ? weight(value_of((uint32_t)(sorted[i] >> 32))) : 0ull;
-                    sum += w[j];
-                }
-                const u64 run = running(sum) - sum;
-                u64 kept = 0ull;
-                for (int v = 0; v < kWarps; ++v) kept += s.m[0][v];
-                // the sum at the first token where it comes to `target`; [1]: at the last one that min_p leaves
-                const u64 enough = top_p < 1.f ? enough_of(kept) : kept;
-                if (tid == 0) s.reached[1] = kept;
-                __syncthreads();
-                u64 r0 = run;
-#pragma unroll
-                for (int j = 0; j < PER; ++j) {
-                    const u64 r1 = r0 + w[j];
-                    if (r0 < enough && enough <= r1) s.reached[0] = r1;
-                    if (r0 < r1 && w[j] < least) atomicMin(&s.reached[1], r0);
-                    r0 = r1;
-                }
-                __syncthreads();
-                kept = min(s.reached[0], s.reached[1]);
-                const u64 target = drawn_of(kept) + 1ull;
-                r0 = run;
-#pragma unroll
-                for (int j = 0; j < PER; ++j) {
-                    const u64 r1 = r0 + w[j];
-                    if (r0 < target && target <= r1) {
-                        const u64 word = sorted[tid * PER + j];
-                        give((int)~(uint32_t)word, value_of((uint32_t)(word >> 32)), (double)w[j] / (double)kept, a.confidence ? total_of() : 1.0);
-                    }
-                    r0 = r1;
+            for (int j = 0; j < VEC; ++j) {
+                const float d = behind(x[j]);
+                if (attempt == 0) {
+                    if (a.confidence) add_conf(d);
+                    if (x[j] >= bound && x[j] > -INFINITY) put(x[j], i0 + j);
+                } else if (d <= reach && bin_of(d) <= bin) {
+                    put(x[j], i0 + j);
                 }
             }
-            cluster_sync_all();                              // nobody leaves while its shared memory is read
-            return;
+        });
+        if (a.confidence && !had_conf) share_conf();
+        had_conf = true;
+        __syncthreads();
+        if (tid == 0) share.n[0] = s.list_n;
+        cluster_sync_all();
+        const int here = lane < cluster ? of_peer(&share, min(lane, cluster - 1))->n[0] : 0;
+        const int all = __reduce_add_sync(0xffffffffu, here);
+        if (all > kList) {
+            cluster_sync_all();                              // the lengths have been read
+            continue;
         }
-        clear();
+        u64* list = reinterpret_cast<u64*>(held);
+        double total = 1.0;
+        if (rank == 0) {
+            merge(here, [&](int r) { return of_peer(work.top, r); }, list);
+            total = total_of();
+        }
+        cluster_sync_all();                                  // nobody leaves while its shared memory is read
+        if (rank != 0) return;
+        u64 w[kList / kThreads], word[kList / kThreads];
+        constexpr int PER = kList / kThreads;
+        int per = 1;
+        if (all <= kThreads) {
+            int room = 32;
+            while (room < all) room *= 2;
+            word[0] = sorted(tid < all ? list[tid] : 0ull, room, work.top);
+        } else {
+            int room = kThreads;
+            while (room < all) room *= 2;
+            per = room / kThreads;
+            for (int i = all + tid; i < room; i += kThreads) list[i] = 0ull;
+            for (int size = 2; size <= room; size *= 2)
+                for (int step = size / 2; step; step /= 2) {
+                    __syncthreads();
+                    for (int i = tid; i < room / 2; i += kThreads) {
+                        const int x = 2 * i - (i & (step - 1)), y = x + step;
+                        const u64 u = list[x], v = list[y];
+                        if ((u < v) == ((x & size) == 0)) { list[x] = v; list[y] = u; }      // the largest first
+                    }
+                }
+            __syncthreads();
+#pragma unroll
+            for (int j = 0; j < PER; ++j)
+                if (j < per) word[j] = list[tid * per + j];
+        }
+        // running sums of the weights of the first top_k
+        u64 sum = 0ull;
+#pragma unroll
+        for (int j = 0; j < PER; ++j) {
+            w[j] = 0ull;
+            if (j < per && tid * per + j < min(top_k, all)) {
+                const float l = value_of((uint32_t)(word[j] >> 32));
+                if (behind(l) <= reach) w[j] = weight(l);
+            }
+            sum += w[j];
+        }
+        const u64 run = running(sum) - sum;
+        u64 kept = 0ull;
+        for (int v = 0; v < kWarps; ++v) kept += s.m[0][v];
+        // the sum at the first token where it comes to what top_p keeps; [1]: before the first that min_p does not leave
+        const u64 enough = top_p < 1.f ? enough_of(kept) : kept;
+        if (tid == 0) s.reached[1] = kept;
+        __syncthreads();
+        u64 r0 = run;
+#pragma unroll
+        for (int j = 0; j < PER; ++j) {
+            const u64 r1 = r0 + w[j];
+            if (r0 < enough && enough <= r1) s.reached[0] = r1;
+            if (r0 < r1 && w[j] < least) atomicMin(&s.reached[1], r0);
+            r0 = r1;
+        }
+        __syncthreads();
+        kept = min(s.reached[0], s.reached[1]);
+        const u64 target = drawn_of(kept) + 1ull;
+        r0 = run;
+#pragma unroll
+        for (int j = 0; j < PER; ++j) {
+            const u64 r1 = r0 + w[j];
+            if (r0 < target && target <= r1) give((int)~(uint32_t)word[j], value_of((uint32_t)(word[j] >> 32)), (double)w[j] / (double)kept, total);
+            r0 = r1;
+        }
+        return;
     }
+    if (sampled && top_k <= kTop) clear();                   // the list was too long
 
     uint32_t token_key = order_key(top);
     u64 token_at = 0ull;                                     // which of the tokens of that value
     uint32_t equal_all = 0u;                                 // how many there are, where that is known
-    double prob = 1.0;
+    double prob = 1.0, total = 1.0;
     if (!greedy) {
-        const bool counts = top_k > 0, had_conf = counts && top_k <= kTop;   // (a list that was too long)
+        const bool counts = top_k > 0;
         if (counts) {
             if (a.confidence && !had_conf) pass(Yes(), Yes(), Yes());
             else pass(No(), Yes(), Yes());
@@ -673,8 +708,8 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
             sum += s.slices[0][r].mass;
             count += s.slices[0][r].count;
         }
-        if (least > 0ull)
-            for (int r = 0; r < cluster; ++r) left += of_peer(&share, r)->mass_min_p;
+        if (least > 0ull) left = cluster_sum(of_peer(&share, min(lane, cluster - 1))->mass_min_p);
+        total = total_of();
         if (top_k > 0 && (uint32_t)top_k < count) {
             const Found f = find(true, (u64)top_k);
             sum = f.mass + f.weight * ((u64)top_k - f.count);
@@ -700,7 +735,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
         each([&](const float (&x)[VEC], int i0) {
 #pragma unroll
             for (int j = 0; j < VEC; ++j)
-                if (x[j] == value_of(token_key)) give(e0 + i0 + j, x[j], prob, a.confidence ? total_of() : 1.0);
+                if (x[j] == value_of(token_key)) give(e0 + i0 + j, x[j], prob, total);
         });
         cluster_sync_all();                                  // nobody leaves while its shared memory is read
         return;
@@ -721,14 +756,14 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
         share.equal = all;
     }
     cluster_sync_all();
-    u64 before = 0ull;
-    for (int r = 0; r < rank; ++r) before += of_peer(&share, r)->equal;
+    if (greedy) total = total_of();
+    u64 before = cluster_sum(lane < rank ? (u64)of_peer(&share, min(lane, cluster - 1))->equal : 0ull);
     for (int w = 0; w < warp; ++w) before += s.c[w];
     if (before <= token_at && token_at < before + equal) {   // one warp of the cluster
         for (int i = j0; i < j1; i += 32) {
             const bool eq = i + lane < j1 && has_it(i + lane);
             const uint32_t eqs = __ballot_sync(0xffffffffu, eq);
-            if (eq && before + __popc(eqs & ((1u << lane) - 1u)) == token_at) give(e0 + i + lane, value_of(token_key), prob, a.confidence ? total_of() : 1.0);
+            if (eq && before + __popc(eqs & ((1u << lane) - 1u)) == token_at) give(e0 + i + lane, value_of(token_key), prob, total);
             before += __popc(eqs);
         }
     }
