@@ -6,7 +6,7 @@
 //
 // A weight is a whole number of 2^-shift (46 bits behind the point for up to 2^16 tokens, one less for every doubling), so that sums are exact and do not
 // depend on their order; what is below half of that is never drawn.  The row lies in the shared memory of a cluster of CTAs, read once; what a CTA
-// finds out is read by the others from there, and every CTA takes every decision by itself, so that a step of a search costs one barrier
+// finds out it writes to the others, and every CTA takes every decision by itself, so that a step of a search costs one or two barriers
 // of the cluster.  The logits are counted by bins that part them evenly from the largest to the smallest whose weight counts.
 //  - With a top_k of up to kTop (and room in the list) the tokens of the bins that hold the first top_k go into a list; one CTA sorts it, adds up their weights
 //    and decides.  No other weight is formed.
@@ -31,7 +31,6 @@ constexpr int kThreads = 512, kWarps = kThreads / 32;
 constexpr int kBins = 2048;
 constexpr int kFew = 512;                // tokens of a bin that are compared with one another
 constexpr int kTop = 1024, kList = 2048; // largest top_k whose tokens are sorted; room for them and those that come with them
-constexpr int kQuick = 128;              // largest top_k that the largest logits of the threads settle
 constexpr int kMaxCluster = 8;
 constexpr int kSteps = 64, kCopies = 16; // a table of 2^(-j / 64), a copy for every lane of half a warp: no two in one bank
 
@@ -42,41 +41,45 @@ __device__ __forceinline__ uint32_t order_key(float f) {     // larger float, la
 }
 __device__ __forceinline__ float value_of(uint32_t key) { return __uint_as_float((key & 0x80000000u) ? key & 0x7FFFFFFFu : ~key); }
 
+// the same place in another CTA of the cluster
 template <class T>
-__device__ __forceinline__ const T* of_peer(const T* p, int rank) {
+__device__ __forceinline__ T* of_peer(T* p, int rank) {
     u64 out;
     asm("mapa.u64 %0, %1, %2;" : "=l"(out) : "l"(reinterpret_cast<u64>(p)), "r"(rank));
-    return reinterpret_cast<const T*>(out);
+    return reinterpret_cast<T*>(out);
 }
 
-struct Totals {                          // of the bins that a CTA adds up for its cluster
+struct Totals {
     u64 mass;
     uint32_t count;
+};
+struct Place {                           // a bin, what is before it, and with it
+    Totals before, upto;
+    int bin;
 };
 struct Found {                           // where a search ended: a value, how many have it, its weight, and what comes before it
     uint32_t key, equal;
     uint32_t count;
     u64 weight, mass;
 };
-struct Share {                           // what the others read
-    float top, low, bound;
-    double confidence;
-    u64 mass_min_p;
-    Totals slice[2];                     // sums over this CTA's bins; [1]: of a histogram of keys
-    int n[2];                            // list of a bin's tokens (two in turn)
-    uint32_t key_lo[2], key_hi[2];
-    uint32_t equal;
+// What the CTAs of a cluster tell one another, each in the others' memory before a barrier: reading there takes a thousand clocks.
+struct Inbox {
+    float top[kMaxCluster], low[kMaxCluster], bound[kMaxCluster], bound_each[kMaxCluster];
+    double confidence[kMaxCluster];
+    u64 mass_min_p[kMaxCluster];
+    Totals slice[2][kMaxCluster];        // of each CTA's share of the bins; [1]: of a histogram of keys
+    Place place;
+    int n[2][kMaxCluster];               // lengths of lists (two in turn)
+    uint32_t key_lo[2][kMaxCluster], key_hi[2][kMaxCluster];
+    uint32_t equal[kMaxCluster];
 };
 struct alignas(16) Scratch {
-    Share share;
+    Inbox box;
     double power[kSteps][kCopies];
     float f[2][kWarps];
     double d[kWarps];
     u64 m[2][kWarps];
     uint32_t c[kWarps];
-    int bin;
-    Totals before, upto;
-    Totals slices[2][kMaxCluster];       // every CTA's, as read from them
     int list_n;
     uint32_t list_lo, list_hi;
     u64 reached[2];
@@ -86,10 +89,11 @@ struct Hist {                            // this CTA's counts and weights; a wei
 };
 union Work {                             // one after the other
     Hist hist;
-    u64 top[kList];                      // key and index of the tokens of the first bins, a word each
+    u64 top[kList];                      // key and index of the tokens of the first bins, a word each: every CTA's in the first one's memory
     struct {
-        uint32_t key[2][kFew];           // of a bin's tokens, two in turn
-        uint32_t merged[kFew];           // the cluster's
+        uint32_t own[kFew];              // keys of a bin's tokens
+        uint32_t key[2][2 * kFew];       // every CTA's, two in turn
+        uint32_t merged[kFew];           // one after the other
         u64 upto[kFew];                  // sums of their weights, the largest first
     } few;
 };
@@ -114,13 +118,14 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
     Scratch& s = *reinterpret_cast<Scratch*>(&work + 1);
     Totals* totals = reinterpret_cast<Totals*>(&s + 1);                      // [2][slice]
     T* held = reinterpret_cast<T*>(totals + 2 * slice);
-    Share& share = s.share;
+    Inbox& box = s.box;
 
     auto clear = [&] {
         __syncthreads();
         for (int i = tid; i < kBins; i += kThreads) hist.count[i] = hist.lo[i] = hist.hi[i] = 0u;
         __syncthreads();
     };
+    cluster_arrive_relaxed();                                // waited for before the first word to another CTA: it has begun
     for (int i = tid; i < kSteps * kCopies; i += kThreads) s.power[i / kCopies][i % kCopies] = exp2(-(double)(i / kCopies) / kSteps);
     pdl_wait();
     pdl_launch_dependents();
@@ -132,7 +137,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
     const float top_p = a.top_p ? a.top_p[at] : 1.f;
     const float min_p = a.min_p && a.min_p[at] > 0.f ? fminf(a.min_p[at], 1.f) : 0.f;
     const int top_k = a.top_k ? a.top_k[at] : 0;
-    const bool sampled = !greedy && top_k > 0, quick = sampled && top_k <= kQuick;
+    const bool sampled = !greedy && top_k > 0, quick = sampled && top_k <= kTop && (top_k + cluster - 1) / cluster <= kThreads;
 
     // ---- this CTA's part of the row into shared memory; largest and smallest finite logit ----
     const int e0 = min(rank * a.chunk, a.vocab), n = min(a.chunk, a.vocab - e0);
@@ -215,11 +220,19 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
             }
         return v;
     };
-    // A bound that top_k tokens reach at least: the largest logits of that many threads.  (Of 31 logits a thread, those of 50 threads of 512: about 53
-    // tokens of this CTA are as large.)
+    cluster_wait();
+    // A bound that top_k tokens reach at least: the largest logits of that many threads.  Two bounds hold: top_k of one CTA's threads, and a share of top_k in every CTA's.  (Of 31 logits a thread, those of 50 threads of 512: about 53
+    // tokens of a CTA are as large; those of 7 threads in each of 8 CTAs, the least of them: 80 of the row.)
     if (quick) {
         const uint32_t key = sorted(order_key(top), kThreads, work.few.merged);
-        if (tid == top_k - 1) share.bound = value_of(key);
+        if (tid == top_k - 1) s.f[0][0] = value_of(key);
+        if (tid == (top_k + cluster - 1) / cluster - 1) s.f[0][1] = value_of(key);
+        __syncthreads();
+        if (tid < cluster) {
+            of_peer(&box, tid)->bound[rank] = top_k <= kThreads ? s.f[0][0] : -INFINITY;
+            of_peer(&box, tid)->bound_each[rank] = s.f[0][1];
+        }
+        __syncthreads();
     }
 #pragma unroll
     for (int off = 16; off; off >>= 1) {
@@ -236,25 +249,26 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
             top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
             low = fminf(low, __shfl_xor_sync(0xffffffffu, low, off));
         }
-        if (lane == 0) { share.top = top; share.low = low; }
+        if (lane < cluster) {
+            Inbox* of = of_peer(&box, lane);
+            of->top[rank] = top;
+            of->low[rank] = low;
+        }
     }
     if (!quick) clear();
     cluster_sync_all();
     float bound = -INFINITY;
     {
-        const Share* p = of_peer(&share, min(lane, cluster - 1));            // a lane for every CTA
-        top = p->top;
-        low = p->low;
-        if (quick) bound = p->bound;
-#pragma unroll
-        for (int off = kMaxCluster / 2; off; off >>= 1) {
-            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
-            low = fminf(low, __shfl_xor_sync(0xffffffffu, low, off));
-            bound = fmaxf(bound, __shfl_xor_sync(0xffffffffu, bound, off));
+        float each_of = INFINITY;
+        for (int r = 0; r < cluster; ++r) {
+            top = r ? fmaxf(top, box.top[r]) : box.top[0];
+            low = r ? fminf(low, box.low[r]) : box.low[0];
+            if (quick) {
+                bound = fmaxf(bound, box.bound[r]);
+                each_of = fminf(each_of, box.bound_each[r]);
+            }
         }
-        top = __shfl_sync(0xffffffffu, top, 0);
-        low = __shfl_sync(0xffffffffu, low, 0);
-        bound = __shfl_sync(0xffffffffu, bound, 0);
+        if (quick) bound = fmaxf(bound, each_of);
     }
     if (top == -INFINITY) {                                  // nothing to draw
         if (rank == 0 && tid == 0) {
@@ -262,7 +276,6 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
             if (a.prob) a.prob[row] = 0.f;
             if (a.confidence) a.confidence[row] = 0.f;
         }
-        cluster_sync_all();                                  // nobody leaves while its shared memory is read
         return;
     }
 
@@ -306,20 +319,36 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
         asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(d * -2.8853900817779268f));
         conf += e;
     };
-    // one pass over the logits, for what is asked for
+    // one pass over the logits, for what is asked for; four at a time, without a branch until their weights are there
     auto pass = [&](auto with_conf, auto with_count, auto with_weight) {
         each([&](const float (&x)[VEC], int) {
 #pragma unroll
-            for (int k = 0; k < VEC; ++k) {
-                const float d = behind(x[k]);
-                if constexpr (with_conf.value) add_conf(d);
-                if ((with_count.value || with_weight.value) && d <= reach) {
-                    const int bin = bin_of(d);
-                    if constexpr (with_count.value) atomicAdd(&hist.count[bin], 1u);
+            for (int k0 = 0; k0 < VEC; k0 += 4) {
+                int bin[4];
+                u64 w[4];
+                uint32_t was[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const float d = behind(x[k0 + k]);
+                    if constexpr (with_conf.value) add_conf(d);
+                    bin[k] = d <= reach ? bin_of(d) : -1;
+                    if constexpr (with_weight.value) w[k] = weight(bin[k] >= 0 ? x[k0 + k] : top);
+                }
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    if constexpr (with_count.value)
+                        if (bin[k] >= 0) atomicAdd(&hist.count[bin[k]], 1u);
                     if constexpr (with_weight.value) {
-                        const u64 w = weight(x[k]);
-                        add_weight(bin, w);
-                        if (w >= least) mass_min_p += w;
+                        was[k] = 0u;
+                        if (bin[k] >= 0) was[k] = atomicAdd(&hist.lo[bin[k]], (uint32_t)w[k]);
+                    }
+                }
+                if constexpr (with_weight.value) {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const uint32_t hi = (uint32_t)(w[k] >> 32) + (was[k] + (uint32_t)w[k] < was[k]);
+                        if (bin[k] >= 0 && hi) atomicAdd(&hist.hi[bin[k]], hi);
+                        if (bin[k] >= 0 && w[k] >= least) mass_min_p += w[k];
                     }
                 }
             }
@@ -357,97 +386,67 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
         return v + __shfl_sync(0xffffffffu, before, 0);
     };
 
-    // running sums over the cluster of this CTA's bins; s.slices: every CTA's whole sum
+    // running sums over the cluster of this CTA's bins; box.slice: every CTA's whole sum
     auto add_up = [&](int level, bool counts, bool weights) {
         cluster_sync_all();
-        constexpr int PER = kBins / kThreads;                // of a cluster of one; else a bin a thread at most
-        const int per = (slice + kThreads - 1) / kThreads, i0 = tid * per;
-        u64 m[PER];
-        uint32_t c[PER];
-#pragma unroll
-        for (int j = 0; j < PER; ++j) {
-            m[j] = 0ull;
-            c[j] = 0u;
-            if (j >= per || i0 + j >= slice) continue;
-            uint32_t n_of[kMaxCluster], lo_of[kMaxCluster], hi_of[kMaxCluster];
-#pragma unroll
-            for (int r = 0; r < kMaxCluster; ++r) {          // (all asked for before the first is used)
-                n_of[r] = lo_of[r] = hi_of[r] = 0u;
-                if (r >= cluster) continue;
-                const Hist* h = of_peer(&hist, r);
-                if (counts) n_of[r] = h->count[rank * slice + i0 + j];
-                if (weights) {
-                    lo_of[r] = h->lo[rank * slice + i0 + j];
-                    hi_of[r] = h->hi[rank * slice + i0 + j];
-                }
-            }
-#pragma unroll
-            for (int r = 0; r < kMaxCluster; ++r) {
-                m[j] += (u64)hi_of[r] << 32 | lo_of[r];
-                c[j] += n_of[r];
-            }
+        // a thread four bins of one CTA: the CTAs side by side
+        const int peer = tid & (cluster - 1), i0 = tid / cluster * 4;
+        static_assert(kBins == 4 * kThreads, "all bins of all CTAs at once");
+        const Hist* h = of_peer(&hist, peer);
+        uint4 n4 = make_uint4(0u, 0u, 0u, 0u), lo4 = n4, hi4 = n4;
+        if (counts) n4 = *reinterpret_cast<const uint4*>(h->count + rank * slice + i0);
+        if (weights) {
+            lo4 = *reinterpret_cast<const uint4*>(h->lo + rank * slice + i0);
+            hi4 = *reinterpret_cast<const uint4*>(h->hi + rank * slice + i0);
         }
+        u64 m[4] = {(u64)hi4.x << 32 | lo4.x, (u64)hi4.y << 32 | lo4.y, (u64)hi4.z << 32 | lo4.z, (u64)hi4.w << 32 | lo4.w};
+        uint32_t c[4] = {n4.x, n4.y, n4.z, n4.w};
+        for (int off = 1; off < cluster; off <<= 1)
 #pragma unroll
-        for (int j = 1; j < PER; ++j) {
+            for (int j = 0; j < 4; ++j) {
+                if (weights) m[j] += __shfl_xor_sync(0xffffffffu, m[j], off);
+                if (counts) c[j] += __shfl_xor_sync(0xffffffffu, c[j], off);
+            }
+#pragma unroll
+        for (int j = 1; j < 4; ++j) {
             m[j] += m[j - 1];
             c[j] += c[j - 1];
         }
-        const u64 before_m = weights ? running(m[PER - 1]) - m[PER - 1] : 0ull;
-        const uint32_t before_c = counts ? (uint32_t)running((u64)c[PER - 1]) - c[PER - 1] : 0u;
+        const u64 run_m = weights ? running(peer == 0 ? m[3] : 0ull) : 0ull;
+        const uint32_t run_c = counts ? (uint32_t)running(peer == 0 ? (u64)c[3] : 0ull) : 0u;
+        if (peer == 0) {
 #pragma unroll
-        for (int j = 0; j < PER; ++j)
-            if (j < per && i0 + j < slice) totals[level * slice + i0 + j] = Totals{before_m + m[j], before_c + c[j]};
-        if (tid == kThreads - 1) share.slice[level] = Totals{before_m + m[PER - 1], before_c + c[PER - 1]};
+            for (int j = 0; j < 4; ++j) totals[level * slice + i0 + j] = Totals{run_m - m[3] + m[j], run_c - c[3] + c[j]};
+        }
+        if (warp == kWarps - 1) {
+            const Totals all{__shfl_sync(0xffffffffu, run_m, 31), __shfl_sync(0xffffffffu, run_c, 31)};
+            if (lane < cluster) of_peer(&box, lane)->slice[level][rank] = all;
+        }
         cluster_sync_all();
-        if (tid < cluster) s.slices[level][tid] = of_peer(&share, tid)->slice[level];
-        __syncthreads();
     };
 
-    // the first bin at which the running count (or weight), `before` the first one, comes to `target`; upto: with that bin
-    struct Place {
-        int bin;
-        Totals before, upto;
-    };
+    // the first bin at which the running count (or weight), `before` the first one, comes to `target`: the CTA that has it tells the others
     auto locate = [&](int level, bool by_count, u64 target, Totals before) -> Place {
         int owner = 0;
         for (; owner < cluster - 1; ++owner) {
-            const Totals t = s.slices[level][owner];
+            const Totals t = box.slice[level][owner];
             if ((by_count ? (u64)(before.count + t.count) : before.mass + t.mass) >= target) break;
             before.count += t.count;
             before.mass += t.mass;
         }
-        const Totals* of = of_peer(totals + level * slice, owner);
-        for (int i = tid; i < slice; i += kThreads) {
-            Totals t0 = i > 0 ? of[i - 1] : Totals{0ull, 0u}, t1 = of[i];
-            t0 = Totals{before.mass + t0.mass, before.count + t0.count};
-            t1 = Totals{before.mass + t1.mass, before.count + t1.count};
-            const u64 from_here = by_count ? (u64)t0.count : t0.mass, to_here = by_count ? (u64)t1.count : t1.mass;
-            if (from_here < target && (target <= to_here || i == slice - 1)) {      // (whatever the target, some bin is found)
-                s.bin = owner * slice + i;
-                s.before = t0;
-                s.upto = t1;
+        if (rank == owner) {
+            const Totals* of = totals + level * slice;
+            for (int i = tid; i < slice; i += kThreads) {
+                Totals t0 = i > 0 ? of[i - 1] : Totals{0ull, 0u}, t1 = of[i];
+                t0 = Totals{before.mass + t0.mass, before.count + t0.count};
+                t1 = Totals{before.mass + t1.mass, before.count + t1.count};
+                const u64 from_here = by_count ? (u64)t0.count : t0.mass, to_here = by_count ? (u64)t1.count : t1.mass;
+                if (from_here < target && (target <= to_here || i == slice - 1))         // (whatever the target, some bin is found)
+                    for (int r = 0; r < cluster; ++r) of_peer(&box, r)->place = Place{t0, t1, owner * slice + i};
             }
         }
-        __syncthreads();
-        const Place p{s.bin, s.before, s.upto};
-        __syncthreads();                                     // everyone has it
-        return p;
-    };
-    // lists of the CTAs one after the other; here: length of the list of the CTA that a lane stands for
-    auto merge = [&](int here, auto&& of, auto* to) {
-        int first = here;
-#pragma unroll
-        for (int off = 1; off < kMaxCluster; off <<= 1) {
-            const int x = __shfl_up_sync(0xffffffffu, first, off);
-            if (lane >= off) first += x;
-        }
-        first -= here;
-        for (int r = warp % cluster; r < cluster; r += kWarps) {             // (as many warps for each)
-            const int m = __shfl_sync(0xffffffffu, here, r), f = __shfl_sync(0xffffffffu, first, r);
-            const auto* list = of(r);
-            for (int i = warp / cluster * 32 + lane; i < m; i += kWarps / cluster * 32) to[f + i] = list[i];
-        }
-        __syncthreads();
+        cluster_sync_all();
+        return box.place;
     };
     // the value at which the running count (or weight) comes to `target`
     int turn = 0;
@@ -459,7 +458,6 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
             // the bin's tokens, in a list of this CTA's
             if (tid == 0) { s.list_n = 0; s.list_lo = 0xffffffffu; s.list_hi = 0u; }
             __syncthreads();
-            uint32_t* list = work.few.key[turn];
             const int bin = at_bin.bin;
             uint32_t k_lo = 0xffffffffu, k_hi = 0u;
             each([&](const float (&x)[VEC], int) {
@@ -471,7 +469,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
                         k_lo = min(k_lo, key);
                         k_hi = max(k_hi, key);
                         const int slot = atomicAdd(&s.list_n, 1);
-                        if (slot < kFew) list[slot] = key;
+                        if (slot < kFew) work.few.own[slot] = key;
                     }
                 }
             });
@@ -479,28 +477,48 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
             k_hi = __reduce_max_sync(0xffffffffu, k_hi);
             if (lane == 0 && k_lo <= k_hi) { atomicMin(&s.list_lo, k_lo); atomicMax(&s.list_hi, k_hi); }
             __syncthreads();
-            if (tid == 0) { share.n[turn] = s.list_n; share.key_lo[turn] = s.list_lo; share.key_hi[turn] = s.list_hi; }
+            // to everyone: as many warps for each
+            const int room_of = cluster == 1 ? kFew : 2 * kFew / cluster, mine_n = s.list_n;
+            {
+                const int peer = warp % cluster;
+                uint32_t* to = of_peer(work.few.key[turn] + rank * room_of, peer);
+                for (int i = warp / cluster * 32 + lane; i < min(mine_n, room_of); i += kWarps / cluster * 32) to[i] = work.few.own[i];
+                if (warp < cluster && lane == 0) {
+                    Inbox* of = of_peer(&box, peer);
+                    of->n[turn][rank] = mine_n;
+                    of->key_lo[turn][rank] = s.list_lo;
+                    of->key_hi[turn][rank] = s.list_hi;
+                }
+            }
             cluster_sync_all();
-            // a lane for every CTA
-            const Share* p = of_peer(&share, min(lane, cluster - 1));
-            const int here = lane < cluster ? p->n[turn] : 0;
-            lo = __reduce_min_sync(0xffffffffu, p->key_lo[turn]);
-            hi = __reduce_max_sync(0xffffffffu, p->key_hi[turn]);
-            const int all = __reduce_add_sync(0xffffffffu, here);
+            lo = 0xffffffffu;
+            hi = 0u;
+            int all = 0, longest = 0;
+            for (int r = 0; r < cluster; ++r) {
+                all += box.n[turn][r];
+                longest = max(longest, box.n[turn][r]);
+                lo = min(lo, box.key_lo[turn][r]);
+                hi = max(hi, box.key_hi[turn][r]);
+            }
             const uint32_t count = at_bin.before.count;
             const u64 mass = at_bin.before.mass;
             if (lo == hi) {                                  // one value
                 turn ^= 1;
                 return Found{lo, (uint32_t)all, count, weight(value_of(lo)), mass};
             }
-            if (all <= kFew) {
+            if (all <= kFew && longest <= room_of) {
                 uint32_t* merged = work.few.merged;
-                merge(here, [&](int r) { return of_peer(list, r); }, merged);
+                const int r_of = warp % cluster;
+                int first = 0;
+                for (int r = 0; r < r_of; ++r) first += box.n[turn][r];
+                for (int i = warp / cluster * 32 + lane; i < box.n[turn][r_of]; i += kWarps / cluster * 32)
+                    merged[first + i] = work.few.key[turn][r_of * room_of + i];
+                __syncthreads();
                 turn ^= 1;
                 static_assert(kFew == kThreads, "a thread has a key");
                 int room = 32;
                 while (room < all) room *= 2;
-                const uint32_t key = sorted(tid < all ? merged[tid] : 0u, room, merged);
+                const uint32_t key = sorted(tid < all ? merged[tid] : 0u, room, work.few.own);
                 const u64 w = tid < all ? weight(value_of(key)) : 0ull;
                 const u64 run = running(w) + mass;           // with this key
                 const u64 before = by_count ? (u64)(count + tid) : run - w, upto = by_count ? (u64)(count + tid + 1) : run;
@@ -550,16 +568,15 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
 
     auto share_conf = [&] {
         const double c = cta_sum((double)conf, s.d);
-        if (tid == 0) share.confidence = c;
+        if (tid < cluster) of_peer(&box, tid)->confidence[rank] = c;
     };
-    // a sum over the cluster, in every thread: v a lane's part, a lane for every CTA
-    auto cluster_sum = [&](auto v) {
-        if (lane >= cluster) v = 0;
-#pragma unroll
-        for (int off = kMaxCluster / 2; off; off >>= 1) v += __shfl_xor_sync(0xffffffffu, v, off);
-        return __shfl_sync(0xffffffffu, v, 0);
+    auto cluster_sum = [&](const auto (&v)[kMaxCluster], int n) {
+        auto sum = v[0];
+        sum = 0;
+        for (int r = 0; r < n; ++r) sum += v[r];
+        return sum;
     };
-    auto total_of = [&] { return a.confidence ? cluster_sum(of_peer(&share, min(lane, cluster - 1))->confidence) : 1.0; };
+    auto total_of = [&] { return a.confidence ? cluster_sum(box.confidence, cluster) : 1.0; };
 
     // ---- a small top_k: its tokens in a list ----
     bool had_conf = false;
@@ -567,7 +584,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
         int bin = -1;
         if (attempt == 1) {
             // by the counts of the bins
-            if (quick) clear();                              // (too many tokens at the bound: as many as reach it are equal)
+            if (quick) clear();                              // (too many tokens reach the bound)
             if (a.confidence && !had_conf) {
                 pass(Yes(), Yes(), No());
                 share_conf();
@@ -577,16 +594,18 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
             }
             add_up(0, true, false);
             uint32_t count = 0u;
-            for (int r = 0; r < cluster; ++r) count += s.slices[0][r].count;
+            for (int r = 0; r < cluster; ++r) count += box.slice[0][r].count;
             const Place p = locate(0, true, min((u64)top_k, (u64)count), Totals{0ull, 0u});
             if (p.upto.count > kList) break;
             bin = p.bin;
         }
         if (tid == 0) s.list_n = 0;
         __syncthreads();
+        const int room_of = kList / cluster;
+        u64* to = of_peer(work.top + rank * room_of, 0);
         auto put = [&](float l, int i) {
             const int slot = atomicAdd(&s.list_n, 1);
-            if (slot < kList) work.top[slot] = (u64)order_key(l) << 32 | ~(uint32_t)(e0 + i);
+            if (slot < room_of) to[slot] = (u64)order_key(l) << 32 | ~(uint32_t)(e0 + i);
         };
         each([&](const float (&x)[VEC], int i0) {
 #pragma unroll
@@ -603,22 +622,24 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
         if (a.confidence && !had_conf) share_conf();
         had_conf = true;
         __syncthreads();
-        if (tid == 0) share.n[0] = s.list_n;
+        if (tid < cluster) of_peer(&box, tid)->n[attempt][rank] = s.list_n;
         cluster_sync_all();
-        const int here = lane < cluster ? of_peer(&share, min(lane, cluster - 1))->n[0] : 0;
-        const int all = __reduce_add_sync(0xffffffffu, here);
-        if (all > kList) {
-            cluster_sync_all();                              // the lengths have been read
-            continue;
+        int all = 0, longest = 0;
+        for (int r = 0; r < cluster; ++r) {
+            all += box.n[attempt][r];
+            longest = max(longest, box.n[attempt][r]);
         }
+        if (longest > room_of) continue;
+        if (rank != 0) return;                               // nobody writes to its memory, or reads there, any more
+        const double total = total_of();
         u64* list = reinterpret_cast<u64*>(held);
-        double total = 1.0;
-        if (rank == 0) {
-            merge(here, [&](int r) { return of_peer(work.top, r); }, list);
-            total = total_of();
+        {
+            const int r_of = warp % cluster;
+            int first = 0;
+            for (int r = 0; r < r_of; ++r) first += box.n[attempt][r];
+            for (int i = warp / cluster * 32 + lane; i < box.n[attempt][r_of]; i += kWarps / cluster * 32) list[first + i] = work.top[r_of * room_of + i];
         }
-        cluster_sync_all();                                  // nobody leaves while its shared memory is read
-        if (rank != 0) return;
+        __syncthreads();
         u64 w[kList / kThreads], word[kList / kThreads];
         constexpr int PER = kList / kThreads;
         int per = 1;
@@ -700,15 +721,14 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
         }
         if (a.confidence && !had_conf) share_conf();
         const u64 left_here = cta_sum(mass_min_p, s.m[1]);
-        if (tid == 0) share.mass_min_p = left_here;
+        if (tid < cluster) of_peer(&box, tid)->mass_min_p[rank] = left_here;
         add_up(0, counts, true);
-        u64 sum = 0ull, left = 0ull;
+        u64 sum = 0ull;
         uint32_t count = 0u;
         for (int r = 0; r < cluster; ++r) {
-            sum += s.slices[0][r].mass;
-            count += s.slices[0][r].count;
+            sum += box.slice[0][r].mass;
+            count += box.slice[0][r].count;
         }
-        if (least > 0ull) left = cluster_sum(of_peer(&share, min(lane, cluster - 1))->mass_min_p);
         total = total_of();
         if (top_k > 0 && (uint32_t)top_k < count) {
             const Found f = find(true, (u64)top_k);
@@ -720,7 +740,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
             const Found f = find(false, enough);
             kept = f.mass + (enough - f.mass + f.weight - 1ull) / f.weight * f.weight;
         }
-        if (least > 0ull) kept = min(kept, left);
+        if (least > 0ull) kept = min(kept, cluster_sum(box.mass_min_p, cluster));
         const u64 drawn = drawn_of(kept);
         const Found f = find(false, drawn + 1ull);
         token_key = f.key;
@@ -737,7 +757,6 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
             for (int j = 0; j < VEC; ++j)
                 if (x[j] == value_of(token_key)) give(e0 + i0 + j, x[j], prob, total);
         });
-        cluster_sync_all();                                  // nobody leaves while its shared memory is read
         return;
     }
 
@@ -750,14 +769,14 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
     __syncthreads();
     if (lane == 0) s.c[warp] = equal;
     __syncthreads();
-    if (tid == 0) {
+    if (tid < cluster) {
         uint32_t all = 0u;
         for (int w = 0; w < kWarps; ++w) all += s.c[w];
-        share.equal = all;
+        of_peer(&box, tid)->equal[rank] = all;
     }
     cluster_sync_all();
     if (greedy) total = total_of();
-    u64 before = cluster_sum(lane < rank ? (u64)of_peer(&share, min(lane, cluster - 1))->equal : 0ull);
+    u64 before = cluster_sum(box.equal, rank);
     for (int w = 0; w < warp; ++w) before += s.c[w];
     if (before <= token_at && token_at < before + equal) {   // one warp of the cluster
         for (int i = j0; i < j1; i += 32) {
@@ -767,7 +786,6 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
             before += __popc(eqs);
         }
     }
-    cluster_sync_all();                                      // nobody leaves while its shared memory is read
 }
 
 template <class T>
