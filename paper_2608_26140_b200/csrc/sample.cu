@@ -204,7 +204,10 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
     };
     // a value a thread, the largest to the first thread; room: threads that have one (a power of two, 32 and more)
     auto sorted = [&](auto v, int room, auto* exchange) {
-        for (int size = 2; size <= room; size *= 2)
+#pragma unroll
+        for (int size = 2; size <= kThreads; size *= 2) {
+            if (size > room) break;
+#pragma unroll
             for (int step = size / 2; step; step /= 2) {
                 decltype(v) other;
                 if (step >= 32) {
@@ -216,8 +219,9 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
                     other = __shfl_xor_sync(0xffffffffu, v, step);
                 }
                 const bool larger = ((tid & size) == 0) == ((tid & step) == 0);
-                v = larger ? max(v, other) : min(v, other);
+                v = (v > other) == larger ? v : other;
             }
+        }
         return v;
     };
     cluster_wait();
@@ -441,7 +445,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
                 t0 = Totals{before.mass + t0.mass, before.count + t0.count};
                 t1 = Totals{before.mass + t1.mass, before.count + t1.count};
                 const u64 from_here = by_count ? (u64)t0.count : t0.mass, to_here = by_count ? (u64)t1.count : t1.mass;
-                if (from_here < target && (target <= to_here || i == slice - 1))         // (whatever the target, some bin is found)
+                if ((from_here < target || i == 0) && (target <= to_here || i == slice - 1))     // (whatever the target, some bin is found)
                     for (int r = 0; r < cluster; ++r) of_peer(&box, r)->place = Place{t0, t1, owner * slice + i};
             }
         }
@@ -454,7 +458,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
         Place at_bin = locate(0, by_count, target, Totals{0ull, 0u});
         uint32_t lo = 0u, hi = 0xffffffffu;                  // keys of the bin, once it is one of keys
         bool keys = false;
-        for (;;) {
+        for (int level = 0;; ++level) {                      // (a histogram of keys narrows them down to a 2048th of their range)
             // the bin's tokens, in a list of this CTA's
             if (tid == 0) { s.list_n = 0; s.list_lo = 0xffffffffu; s.list_hi = 0u; }
             __syncthreads();
@@ -502,7 +506,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
             }
             const uint32_t count = at_bin.before.count;
             const u64 mass = at_bin.before.mass;
-            if (lo == hi) {                                  // one value
+            if (lo >= hi || level == 4) {                    // one value
                 turn ^= 1;
                 return Found{lo, (uint32_t)all, count, weight(value_of(lo)), mass};
             }
@@ -802,7 +806,9 @@ int sample_launch(SampleArgs a, cudaStream_t stream) {
     if (most == 0) return -1;
     auto chunk_of = [&](int c) { return ((a.vocab + c - 1) / c + 63) / 64 * 64; };
     int c = 1;
-    while (c < kMaxCluster && chunk_of(c) > 16384) c *= 2;
+    // Logits of a CTA: so many that two CTAs have room in an SM; fewer for few rows, for which the time of one row counts.
+    const int many = sizeof(T) == 2 && (int64_t)a.rows * kMaxCluster > 2 * 2 * 148 ? 32768 : 16384;
+    while (c < kMaxCluster && chunk_of(c) > many) c *= 2;
     a.cluster = c;
     a.chunk = chunk_of(c);
     a.shift = 46;
