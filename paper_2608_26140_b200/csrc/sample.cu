@@ -15,7 +15,6 @@
 //    them all with one another, where they are few, else by another histogram of their keys.  A search ends at a value; among the tokens that have
 //    it the index decides.
 #include <algorithm>
-#include <type_traits>
 
 #include "kernels.h"
 #include "launch.h"
@@ -32,6 +31,7 @@ constexpr int kBins = 2048;
 constexpr int kFew = 512;                // tokens of a bin that are compared with one another
 constexpr int kTop = 1024, kList = 2048; // largest top_k whose tokens are sorted; room for them and those that come with them
 constexpr int kMaxCluster = 8;
+constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kSteps = 64, kCopies = 16; // a table of 2^(-j / 64), a copy for every lane of half a warp: no two in one bank
 
 __device__ __forceinline__ uint32_t order_key(float f) {     // larger float, larger key; 0 and -0 are one
@@ -84,8 +84,8 @@ struct alignas(16) Scratch {
     uint32_t list_lo, list_hi;
     u64 reached[2];
 };
-struct Hist {                            // this CTA's counts and weights; a weight in two halves
-    uint32_t count[kBins], lo[kBins], hi[kBins];
+struct Hist {                            // this CTA's counts, or its weights in three parts of 16 bits: sums of 2^15 of them fit in 32, whose atomics return nothing
+    uint32_t part[3][kBins];
 };
 union Work {                             // one after the other
     Hist hist;
@@ -122,7 +122,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
 
     auto clear = [&] {
         __syncthreads();
-        for (int i = tid; i < kBins; i += kThreads) hist.count[i] = hist.lo[i] = hist.hi[i] = 0u;
+        for (int i = tid; i < kBins; i += kThreads) hist.part[0][i] = hist.part[1][i] = hist.part[2][i] = 0u;
         __syncthreads();
     };
     cluster_arrive_relaxed();                                // waited for before the first word to another CTA: it has begun
@@ -145,15 +145,10 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
     constexpr int VEC = 16 / sizeof(T);
     const int shift = (int)(reinterpret_cast<uintptr_t>(from) % 16 / sizeof(T));     // held[shift + i]: whole pieces of 16 bytes in both places
     const int pieces = (shift + n + VEC - 1) / VEC;          // the first and the last filled up with -inf
-    T* mine = held + shift;
+    const T* mine = held + shift;
     float top = -INFINITY, low = INFINITY;
+    float conf = 0.f, conf_top = -3.4028234663852886e38f;    // sum of exp(l - conf_top) over this thread's logits, conf_top the largest of them so far
     bool nan = false;
-    auto take = [&](float v) -> float {
-        if (v != v) { nan = true; v = -INFINITY; }
-        top = fmaxf(top, v);
-        if (v > -INFINITY) low = fminf(low, v);
-        return v;
-    };
     auto to_f = [](T v) -> float { if constexpr (sizeof(T) == 2) return __bfloat162float(v); else return v; };
     auto from_f = [](float v) -> T { if constexpr (sizeof(T) == 2) return __float2bfloat16(v); else return v; };
     auto unpack = [](const uint4& v, float (&x)[VEC]) {
@@ -164,32 +159,73 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
             else x[k] = __uint_as_float(w[k]);
         }
     };
+    auto ex2f = [](float x) {
+        float e;
+        asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(x));
+        return e;
+    };
+    // a piece as it came: NaN out, its share of largest, smallest and sum
+    auto take = [&](uint4& v) {
+        float x[VEC], high = -INFINITY;
+        unpack(v, x);
+        bool odd = false;
+#pragma unroll
+        for (int k = 0; k < VEC; ++k) odd |= x[k] != x[k];
+        if (odd) {
+            nan = true;
+            T* w = reinterpret_cast<T*>(&v);
+#pragma unroll
+            for (int k = 0; k < VEC; ++k) {
+                x[k] = x[k] != x[k] ? -INFINITY : x[k];
+                w[k] = from_f(x[k]);
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < VEC; ++k) {
+            high = fmaxf(high, x[k]);
+            low = fminf(low, x[k] > -INFINITY ? x[k] : INFINITY);
+        }
+        top = fmaxf(top, high);
+        if (a.confidence) {
+            if (high > conf_top) {
+                conf *= ex2f((conf_top - high) * kLog2e);
+                conf_top = high;
+            }
+#pragma unroll
+            for (int k = 0; k < VEC; ++k) conf += ex2f((x[k] - conf_top) * kLog2e);
+        }
+    };
+    // piece i of `held` is thread i % kThreads'
     {
-        const int lead = min(n, (VEC - shift) % VEC), body = (n - lead) / VEC, tail = lead + body * VEC;
-        for (int i = tid; i < lead; i += kThreads) mine[i] = from_f(take(to_f(from[i])));
-        for (int i = tail + tid; i < n; i += kThreads) mine[i] = from_f(take(to_f(from[i])));
-        if (tid < shift) held[tid] = from_f(-INFINITY);
-        if (shift + n + tid < pieces * VEC) mine[n + tid] = from_f(-INFINITY);
+        const int whole0 = shift ? 1 : 0, whole1 = (shift + n) / VEC;        // pieces that are all the row's
+        auto partial = [&](int i) {
+            uint4 v;
+            T* w = reinterpret_cast<T*>(&v);
+#pragma unroll
+            for (int k = 0; k < VEC; ++k) {
+                const int e = i * VEC + k - shift;
+                w[k] = e >= 0 && e < n ? from[e] : from_f(-INFINITY);
+            }
+            take(v);
+            reinterpret_cast<uint4*>(held)[i] = v;
+        };
+        if (whole0 && tid == 0) partial(0);
+        if (whole1 < pieces && whole1 >= whole0 && tid == whole1 % kThreads) partial(whole1);
+        const uint4* source = reinterpret_cast<const uint4*>(from - shift);  // (aligned; the first piece is not read here where it is not whole)
         constexpr int AHEAD = 4;
-        for (int i0 = tid; i0 < body; i0 += AHEAD * kThreads) {
+        for (int i0 = tid; i0 < whole1; i0 += AHEAD * kThreads) {
             uint4 v[AHEAD];
 #pragma unroll
-            for (int j = 0; j < AHEAD; ++j)
-                if (i0 + j * kThreads < body) v[j] = __ldcs(reinterpret_cast<const uint4*>(from + lead) + i0 + j * kThreads);
+            for (int j = 0; j < AHEAD; ++j) {
+                const int i = i0 + j * kThreads;
+                if (i >= whole0 && i < whole1) v[j] = __ldcs(source + i);
+            }
 #pragma unroll
             for (int j = 0; j < AHEAD; ++j) {
-                if (i0 + j * kThreads >= body) break;
-                float x[VEC];
-                unpack(v[j], x);
-                bool odd = false;
-#pragma unroll
-                for (int k = 0; k < VEC; ++k) { odd |= x[k] != x[k]; x[k] = take(x[k]); }
-                if (odd) {
-                    T* w = reinterpret_cast<T*>(&v[j]);
-#pragma unroll
-                    for (int k = 0; k < VEC; ++k) w[k] = from_f(x[k]);
-                }
-                *(reinterpret_cast<uint4*>(mine + lead) + i0 + j * kThreads) = v[j];
+                const int i = i0 + j * kThreads;
+                if (i < whole0 || i >= whole1) continue;
+                take(v[j]);
+                reinterpret_cast<uint4*>(held)[i] = v[j];
             }
         }
     }
@@ -224,6 +260,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
         }
         return v;
     };
+    const float own_top = top;
     cluster_wait();
     // A bound that top_k tokens reach at least: the largest logits of that many threads.  Two bounds hold: top_k of one CTA's threads, and a share of top_k in every CTA's.  (Of 31 logits a thread, those of 50 threads of 512: about 53
     // tokens of a CTA are as large; those of 7 threads in each of 8 CTAs, the least of them: 80 of the row.)
@@ -311,55 +348,41 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
     const float bins_per = (float)(kBins - 1) / reach;       // (infinite where all are equal)
     auto bin_of = [&](float d) { return d > 0.f ? (int)(__float_as_uint(fmaf(fminf(d, reach), bins_per, 8388608.f)) & (kBins - 1)) : 0; };      // to the nearest
 
-    // ---- counts and weights by bins; the sum for the confidence; what min_p leaves ----
-    float conf = 0.f;
+    // ---- counts and weights by bins, what min_p leaves ----
     u64 mass_min_p = 0ull;
     auto add_weight = [&](int bin, u64 w) {
-        const uint32_t w_lo = (uint32_t)w, was = atomicAdd(&hist.lo[bin], w_lo), w_hi = (uint32_t)(w >> 32) + (was + w_lo < was);
-        if (w_hi) atomicAdd(&hist.hi[bin], w_hi);
+#pragma unroll
+        for (int p = 0; p < 3; ++p) atomicAdd(&hist.part[p][bin], (uint32_t)(w >> (16 * p)) & (p < 2 ? 0xFFFFu : 0xFFFFFFFFu));
     };
-    auto add_conf = [&](float d) {
-        float e;
-        asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(d * -2.8853900817779268f));
-        conf += e;
-    };
-    // one pass over the logits, for what is asked for; four at a time, without a branch until their weights are there
-    auto pass = [&](auto with_conf, auto with_count, auto with_weight) {
+    // one pass over the logits, for counts or for weights; four at a time, without a branch until their weights are there
+    auto pass = [&](bool counts) {
         each([&](const float (&x)[VEC], int) {
 #pragma unroll
             for (int k0 = 0; k0 < VEC; k0 += 4) {
                 int bin[4];
-                u64 w[4];
-                uint32_t was[4];
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
                     const float d = behind(x[k0 + k]);
-                    if constexpr (with_conf.value) add_conf(d);
                     bin[k] = d <= reach ? bin_of(d) : -1;
-                    if constexpr (with_weight.value) w[k] = weight(bin[k] >= 0 ? x[k0 + k] : top);
                 }
+                if (counts) {
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    if constexpr (with_count.value)
-                        if (bin[k] >= 0) atomicAdd(&hist.count[bin[k]], 1u);
-                    if constexpr (with_weight.value) {
-                        was[k] = 0u;
-                        if (bin[k] >= 0) was[k] = atomicAdd(&hist.lo[bin[k]], (uint32_t)w[k]);
-                    }
+                    for (int k = 0; k < 4; ++k)
+                        if (bin[k] >= 0) atomicAdd(&hist.part[0][bin[k]], 1u);
+                    continue;
                 }
-                if constexpr (with_weight.value) {
+                u64 w[4];
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        const uint32_t hi = (uint32_t)(w[k] >> 32) + (was[k] + (uint32_t)w[k] < was[k]);
-                        if (bin[k] >= 0 && hi) atomicAdd(&hist.hi[bin[k]], hi);
-                        if (bin[k] >= 0 && w[k] >= least) mass_min_p += w[k];
+                for (int k = 0; k < 4; ++k) w[k] = weight(bin[k] >= 0 ? x[k0 + k] : top);
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    if (bin[k] >= 0) {
+                        add_weight(bin[k], w[k]);
+                        if (w[k] >= least) mass_min_p += w[k];
                     }
-                }
             }
         });
     };
-    using Yes = std::true_type;
-    using No = std::false_type;
     // sum of a value over the CTA, in every thread of warp 0
     auto cta_sum = [&](auto v, auto* at_warp) {
 #pragma unroll
@@ -390,41 +413,45 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
         return v + __shfl_sync(0xffffffffu, before, 0);
     };
 
-    // running sums over the cluster of this CTA's bins; box.slice: every CTA's whole sum
-    auto add_up = [&](int level, bool counts, bool weights) {
+    // running sums over the cluster of this CTA's bins, counts or weights (the others stay as they are); box.slice: every CTA's whole sum
+    auto add_up = [&](int level, bool counts) {
         cluster_sync_all();
         // a thread four bins of one CTA: the CTAs side by side
         const int peer = tid & (cluster - 1), i0 = tid / cluster * 4;
         static_assert(kBins == 4 * kThreads, "all bins of all CTAs at once");
         const Hist* h = of_peer(&hist, peer);
-        uint4 n4 = make_uint4(0u, 0u, 0u, 0u), lo4 = n4, hi4 = n4;
-        if (counts) n4 = *reinterpret_cast<const uint4*>(h->count + rank * slice + i0);
-        if (weights) {
-            lo4 = *reinterpret_cast<const uint4*>(h->lo + rank * slice + i0);
-            hi4 = *reinterpret_cast<const uint4*>(h->hi + rank * slice + i0);
+        auto four = [&](int p) { return *reinterpret_cast<const uint4*>(h->part[p] + rank * slice + i0); };
+        u64 m[4];
+        {
+            const uint4 x = four(0);
+            m[0] = x.x; m[1] = x.y; m[2] = x.z; m[3] = x.w;
+            if (!counts) {
+                const uint4 y = four(1), z = four(2);
+                m[0] += ((u64)y.x << 16) + ((u64)z.x << 32); m[1] += ((u64)y.y << 16) + ((u64)z.y << 32);
+                m[2] += ((u64)y.z << 16) + ((u64)z.z << 32); m[3] += ((u64)y.w << 16) + ((u64)z.w << 32);
+            }
         }
-        u64 m[4] = {(u64)hi4.x << 32 | lo4.x, (u64)hi4.y << 32 | lo4.y, (u64)hi4.z << 32 | lo4.z, (u64)hi4.w << 32 | lo4.w};
-        uint32_t c[4] = {n4.x, n4.y, n4.z, n4.w};
         for (int off = 1; off < cluster; off <<= 1)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                if (weights) m[j] += __shfl_xor_sync(0xffffffffu, m[j], off);
-                if (counts) c[j] += __shfl_xor_sync(0xffffffffu, c[j], off);
-            }
+            for (int j = 0; j < 4; ++j) m[j] += __shfl_xor_sync(0xffffffffu, m[j], off);
 #pragma unroll
-        for (int j = 1; j < 4; ++j) {
-            m[j] += m[j - 1];
-            c[j] += c[j - 1];
-        }
-        const u64 run_m = weights ? running(peer == 0 ? m[3] : 0ull) : 0ull;
-        const uint32_t run_c = counts ? (uint32_t)running(peer == 0 ? (u64)c[3] : 0ull) : 0u;
+        for (int j = 1; j < 4; ++j) m[j] += m[j - 1];
+        const u64 run = running(peer == 0 ? m[3] : 0ull);
+        Totals* of = totals + level * slice + i0;
         if (peer == 0) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) totals[level * slice + i0 + j] = Totals{run_m - m[3] + m[j], run_c - c[3] + c[j]};
+            for (int j = 0; j < 4; ++j) {
+                if (counts) of[j].count = (uint32_t)(run - m[3] + m[j]);
+                else of[j].mass = run - m[3] + m[j];
+            }
         }
         if (warp == kWarps - 1) {
-            const Totals all{__shfl_sync(0xffffffffu, run_m, 31), __shfl_sync(0xffffffffu, run_c, 31)};
-            if (lane < cluster) of_peer(&box, lane)->slice[level][rank] = all;
+            const u64 all = __shfl_sync(0xffffffffu, run, 31);
+            if (lane < cluster) {
+                Totals& t = of_peer(&box, lane)->slice[level][rank];
+                if (counts) t.count = (uint32_t)all;
+                else t.mass = all;
+            }
         }
         cluster_sync_all();
     };
@@ -539,17 +566,20 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
             clear();
             const uint32_t width = hi - lo;
             const int by = max(0, 21 - __clz(width));        // at most 2048 bins
-            each([&](const float (&x)[VEC], int) {
+            for (int counts = 1; counts >= 0; --counts) {
+                if (!counts) clear();
+                each([&](const float (&x)[VEC], int) {
 #pragma unroll
-                for (int k = 0; k < VEC; ++k) {
-                    const uint32_t key = order_key(x[k]);
-                    if (behind(x[k]) <= reach && key >= lo && key <= hi) {
-                        add_weight((hi - key) >> by, weight(x[k]));
-                        atomicAdd(&hist.count[(hi - key) >> by], 1u);
+                    for (int k = 0; k < VEC; ++k) {
+                        const uint32_t key = order_key(x[k]);
+                        if (behind(x[k]) <= reach && key >= lo && key <= hi) {
+                            if (counts) atomicAdd(&hist.part[0][(hi - key) >> by], 1u);
+                            else add_weight((hi - key) >> by, weight(x[k]));
+                        }
                     }
-                }
-            });
-            add_up(1, true, true);
+                });
+                add_up(1, counts);
+            }
             at_bin = locate(1, by_count, target, at_bin.before);
             const uint32_t b_lo = (uint32_t)at_bin.bin << by, b_hi = b_lo + ((1u << by) - 1u);
             const uint32_t top_key = hi;
@@ -570,33 +600,33 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
         if (a.confidence) a.confidence[row] = (float)((l == top ? 1.0 : exp((double)l - (double)top)) / total);
     };
 
-    auto share_conf = [&] {
-        const double c = cta_sum((double)conf, s.d);
-        if (tid < cluster) of_peer(&box, tid)->confidence[rank] = c;
-    };
     auto cluster_sum = [&](const auto (&v)[kMaxCluster], int n) {
         auto sum = v[0];
         sum = 0;
         for (int r = 0; r < n; ++r) sum += v[r];
         return sum;
     };
+    const bool endless = top == INFINITY;                    // (infinite logits share the confidence, which the running sums do not give)
+    if (a.confidence) {
+        double c = 0.0;
+        if (endless) each([&](const float (&x)[VEC], int) {
+#pragma unroll
+            for (int k = 0; k < VEC; ++k) c += x[k] == INFINITY;
+        });
+        else c = (double)conf * (double)ex2f((conf_top - top) * kLog2e);
+        c = cta_sum(c, s.d);
+        if (tid < cluster) of_peer(&box, tid)->confidence[rank] = c;
+    }
     auto total_of = [&] { return a.confidence ? cluster_sum(box.confidence, cluster) : 1.0; };
 
     // ---- a small top_k: its tokens in a list ----
-    bool had_conf = false;
     for (int attempt = quick ? 0 : 1; sampled && top_k <= kTop && attempt < 2; ++attempt) {
         int bin = -1;
         if (attempt == 1) {
             // by the counts of the bins
             if (quick) clear();                              // (too many tokens reach the bound)
-            if (a.confidence && !had_conf) {
-                pass(Yes(), Yes(), No());
-                share_conf();
-                had_conf = true;
-            } else {
-                pass(No(), Yes(), No());
-            }
-            add_up(0, true, false);
+            pass(true);
+            add_up(0, true);
             uint32_t count = 0u;
             for (int r = 0; r < cluster; ++r) count += box.slice[0][r].count;
             const Place p = locate(0, true, min((u64)top_k, (u64)count), Totals{0ull, 0u});
@@ -611,20 +641,14 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
             const int slot = atomicAdd(&s.list_n, 1);
             if (slot < room_of) to[slot] = (u64)order_key(l) << 32 | ~(uint32_t)(e0 + i);
         };
-        each([&](const float (&x)[VEC], int i0) {
+        if (attempt == 1 || own_top >= bound)                // (a thread has the same pieces as when they came)
+            each([&](const float (&x)[VEC], int i0) {
 #pragma unroll
-            for (int j = 0; j < VEC; ++j) {
-                const float d = behind(x[j]);
-                if (attempt == 0) {
-                    if (a.confidence) add_conf(d);
-                    if (x[j] >= bound && x[j] > -INFINITY) put(x[j], i0 + j);
-                } else if (d <= reach && bin_of(d) <= bin) {
-                    put(x[j], i0 + j);
+                for (int j = 0; j < VEC; ++j) {
+                    const float d = behind(x[j]);
+                    if (attempt == 0 ? x[j] >= bound && x[j] > -INFINITY : d <= reach && bin_of(d) <= bin) put(x[j], i0 + j);
                 }
-            }
-        });
-        if (a.confidence && !had_conf) share_conf();
-        had_conf = true;
+            });
         __syncthreads();
         if (tid < cluster) of_peer(&box, tid)->n[attempt][rank] = s.list_n;
         cluster_sync_all();
@@ -717,16 +741,14 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
     if (!greedy) {
         const bool counts = top_k > 0;
         if (counts) {
-            if (a.confidence && !had_conf) pass(Yes(), Yes(), Yes());
-            else pass(No(), Yes(), Yes());
-        } else {
-            if (a.confidence) pass(Yes(), No(), Yes());
-            else pass(No(), No(), Yes());
+            pass(true);
+            add_up(0, true);
+            clear();
         }
-        if (a.confidence && !had_conf) share_conf();
+        pass(false);
         const u64 left_here = cta_sum(mass_min_p, s.m[1]);
         if (tid < cluster) of_peer(&box, tid)->mass_min_p[rank] = left_here;
-        add_up(0, counts, true);
+        add_up(0, false);
         u64 sum = 0ull;
         uint32_t count = 0u;
         for (int r = 0; r < cluster; ++r) {
@@ -751,9 +773,6 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
         equal_all = f.equal;
         token_at = min((drawn - f.mass) / f.weight, (u64)(f.equal - 1u));
         prob = (double)f.weight / (double)kept;
-    } else if (a.confidence) {
-        pass(Yes(), No(), No());
-        share_conf();
     }
     if (equal_all == 1u) {
         each([&](const float (&x)[VEC], int i0) {
