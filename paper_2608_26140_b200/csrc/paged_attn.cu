@@ -38,6 +38,9 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t v) {
 __device__ __forceinline__ void cp_async16_or_zero(uint32_t dst, const void* src, bool on) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;\n" ::"r"(dst), "l"(src), "r"(on ? 16 : 0) : "memory");
 }
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;\n" ::"r"(dst), "l"(src) : "memory");
+}
 template <int N>
 __device__ __forceinline__ void ring_wait() { asm volatile("cp.async.wait_group %0;\n" ::"n"(N) : "memory"); }
 
@@ -137,7 +140,10 @@ __global__ void __launch_bounds__(PW * 32, 2) paged_attn_kernel(const PagedAttnA
     constexpr int PASS = 32 / PIECES, PASSES = PSTEP / PASS;
     const int row0 = lane / PIECES, piece = lane % PIECES;
     const uint32_t ring = smem_u32(smem) + warp * (PSTAGES * L::STAGE);
-    const uint32_t put = ring + row0 * D * 2 + ((piece ^ row0) << 4);        // of the pass i: the row i PASS further, swizzled by its number
+    constexpr int SWIZZLES = 8 / PASS;                       // a row's pieces are swizzled by its number modulo 8; the pass i is PASS rows further
+    uint32_t put[SWIZZLES];
+#pragma unroll
+    for (int i = 0; i < SWIZZLES; ++i) put[i] = ring + row0 * D * 2 + ((piece ^ row0 ^ (i * PASS)) << 4);
     const int mrow = lane & 7, mj = lane >> 3;               // ldmatrix: this lane's row of the matrix mj
     const uint32_t k_get = ((mj & 1) * 8 + mrow) * D * 2 + (((mj >> 1) ^ mrow) << 4);
     const uint32_t v_get = L::HALF + ((mj >> 1) * 8 + mrow) * D * 2 + (((mj & 1) ^ mrow) << 4);
@@ -186,32 +192,49 @@ __global__ void __launch_bounds__(PW * 32, 2) paged_attn_kernel(const PagedAttnA
                 const int key0 = key_lo + (warp + s * PW) * PSTEP, left = key_hi - key0;
                 const bool good = entry >= 0 && entry < a.pages.n_pages;
                 uint32_t there = (left >= PSTEP ? 0xFFFFu : (1u << left) - 1u) & ~drop;
-                const uint32_t known = __ballot_sync(0xffffffffu, good);
-                if (known != 0xffffffffu) {                  // keys in pages that are none do not count
-                    if ((there & ~known) != 0u && lane == 0) atomicOr(a.status, kFlagBadIndex);
+                const uint32_t known = whole ? (good ? 0xFFFFu : 0u) : __ballot_sync(0xffffffffu, good);
+                if ((there & ~known) != 0u) {                // keys in pages that are none do not count
+                    if (lane == 0) atomicOr(a.status, kFlagBadIndex);
                     there &= known;
                 }
                 if (lane == 0) there_of[warp][stage] = there;
                 const int64_t off = (good ? entry * a.pages.page_stride : 0) +
                                     (((int64_t)kvh << a.pages.log2_page) + ((key0 + (whole ? 0 : lane & 15)) & page_mask)) * D;
-                const uint32_t to = put + stage * L::STAGE;
+                if (whole && there == 0xFFFFu) {             // side by side
+                    const __nv_bfloat16 *kf = kp + off + row0 * D + piece * 8, *vf = vp + off + row0 * D + piece * 8;
 #pragma unroll
-                for (int i = 0; i < PASSES; ++i) {
-                    const int row = i * PASS + row0;
-                    const int64_t at = (whole ? off + row * D : __shfl_sync(0xffffffffu, off, row)) + piece * 8;
-                    const bool on = (there >> row) & 1u;
-                    const uint32_t dst = (to + i * PASS * D * 2) ^ (((i * PASS) & 7) << 4);
-                    cp_async16_or_zero(dst, kp + at, on);
-                    cp_async16_or_zero(dst + L::HALF, vp + at, on);
+                    for (int i = 0; i < PASSES; ++i) {
+                        const uint32_t dst = put[i % SWIZZLES] + stage * L::STAGE + i * PASS * D * 2;
+                        cp_async16(dst, kf + i * PASS * D);
+                        cp_async16(dst + L::HALF, vf + i * PASS * D);
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < PASSES; ++i) {
+                        const int row = i * PASS + row0;
+                        const int64_t at = (whole ? off + row * D : __shfl_sync(0xffffffffu, off, row)) + piece * 8;
+                        const bool on = (there >> row) & 1u;
+                        const uint32_t dst = put[i % SWIZZLES] + stage * L::STAGE + i * PASS * D * 2;
+                        cp_async16_or_zero(dst, kp + at, on);
+                        cp_async16_or_zero(dst + L::HALF, vp + at, on);
+                    }
                 }
             }
             cp_async_commit();
         };
         look_up(0);
-#pragma unroll
-        for (int s = 0; s < PSTAGES - 1; ++s) {
-            fetch(s, s);
-            look_up(s + 1);
+        {
+            const int e0 = entry;
+            const uint32_t d0 = drop;
+            look_up(1);                                      // (asked for before the first is used)
+            const int e1 = entry;
+            const uint32_t d1 = drop;
+            entry = e0; drop = d0;
+            fetch(0, 0);
+            entry = e1; drop = d1;
+            fetch(1, 1);
+            static_assert(PSTAGES == 3, "two stages ahead");
+            look_up(2);
         }
         __syncthreads();                                     // the queries are there
 
