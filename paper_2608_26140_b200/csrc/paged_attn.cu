@@ -41,6 +41,14 @@ __device__ __forceinline__ void cp_async16_or_zero(uint32_t dst, const void* src
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;\n" ::"r"(dst), "l"(src) : "memory");
 }
+// the products' first step: nothing to add to
+__device__ __forceinline__ void mma_bf16_16816_first(float* c, const uint32_t* a, uint32_t b0, uint32_t b1) {
+    asm volatile(
+        "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, "
+        "{%10,%10,%10,%10};\n"
+        : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
+}
 template <int N>
 __device__ __forceinline__ void ring_wait() { asm volatile("cp.async.wait_group %0;\n" ::"n"(N) : "memory"); }
 
@@ -247,11 +255,11 @@ __global__ void __launch_bounds__(PW * 32, 2) paged_attn_kernel(const PagedAttnA
                 for (int nt = 0; nt < NT; ++nt) qf[ks][nt] = qs[(ks * NT + nt) * 32 + lane];
         }
         float o[D / 16][NT][4];
-        float m[NT][2], l[NT][2];                            // references, denominators of rows 2 t, 2 t + 1
+        float2 m[NT], l[NT];                                 // references, denominators of rows 2 t, 2 t + 1
         unsigned unset = (1u << (2 * NT)) - 1u;              // rows without a reference yet (no key, or none with a logit above -inf)
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-            m[nt][0] = m[nt][1] = l[nt][0] = l[nt][1] = 0.f;
+            m[nt] = l[nt] = make_float2(0.f, 0.f);
 #pragma unroll
             for (int i = 0; i < D / 16; ++i)
 #pragma unroll
@@ -270,8 +278,6 @@ __global__ void __launch_bounds__(PW * 32, 2) paged_attn_kernel(const PagedAttnA
             // ---- S^T = K Q^T ----
             float sv[NT][4];
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) sv[nt][0] = sv[nt][1] = sv[nt][2] = sv[nt][3] = 0.f;
-#pragma unroll
             for (int ks = 0; ks < D / 16; ++ks) {
                 uint32_t fa[4];
                 ldmatrix_x4(fa[0], fa[1], fa[2], fa[3], st + (k_get ^ (ks << 5)));
@@ -280,18 +286,29 @@ __global__ void __launch_bounds__(PW * 32, 2) paged_attn_kernel(const PagedAttnA
                     uint2 q;
                     if constexpr (Q_REGS) q = qf[ks][nt];
                     else q = qs[(ks * NT + nt) * 32 + lane];
-                    mma_bf16_16816(sv[nt], fa, q.x, q.y);
+                    if (ks == 0) mma_bf16_16816_first(sv[nt], fa, q.x, q.y);
+                    else mma_bf16_16816(sv[nt], fa, q.x, q.y);
                 }
             }
-            float top = -INFINITY;
+            const float2 scale2 = make_float2(a.scale_log2e, a.scale_log2e);
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    sv[nt][j] = fmaf(sv[nt][j], a.scale_log2e, -m[nt][j & 1]);
-                    if (there != 0xFFFFu && !((there >> ((j >> 1) * 8 + g)) & 1u)) sv[nt][j] = -INFINITY;
-                    top = fmaxf(top, sv[nt][j]);
+                for (int j = 0; j < 4; j += 2) {
+                    const float2 y = __ffma2_rn(make_float2(sv[nt][j], sv[nt][j + 1]), scale2, make_float2(-m[nt].x, -m[nt].y));
+                    sv[nt][j] = y.x;
+                    sv[nt][j + 1] = y.y;
                 }
+            if (there != 0xFFFFu) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (!((there >> ((j >> 1) * 8 + g)) & 1u))
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt) sv[nt][j] = -INFINITY;
+            }
+            float top = fmaxf(fmaxf(sv[0][0], sv[0][1]), fmaxf(sv[0][2], sv[0][3]));
+#pragma unroll
+            for (int nt = 1; nt < NT; ++nt) top = fmaxf(fmaxf(fmaxf(fmaxf(top, sv[nt][0]), sv[nt][1]), sv[nt][2]), sv[nt][3]);
             if (__any_sync(0xffffffffu, top > kPagedRaise || unset != 0u)) {
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
@@ -305,8 +322,8 @@ __global__ void __launch_bounds__(PW * 32, 2) paged_attn_kernel(const PagedAttnA
                         if (x > 0.f || ((unset & bit) && x > -INFINITY)) {
                             const float f = unset & bit ? 0.f : ex2(-x);
                             unset &= ~bit;
-                            m[nt][r] += x;
-                            l[nt][r] *= f;
+                            if (r == 0) { m[nt].x += x; l[nt].x *= f; }
+                            else { m[nt].y += x; l[nt].y *= f; }
 #pragma unroll
                             for (int i = 0; i < D / 16; ++i) {
                                 o[i][nt][r] *= f;
@@ -322,8 +339,7 @@ __global__ void __launch_bounds__(PW * 32, 2) paged_attn_kernel(const PagedAttnA
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
                 const float p0 = ex2(sv[nt][0]), p1 = ex2(sv[nt][1]), p2 = ex2(sv[nt][2]), p3 = ex2(sv[nt][3]);
-                l[nt][0] += p0 + p2;
-                l[nt][1] += p1 + p3;
+                l[nt] = __fadd2_rn(l[nt], __fadd2_rn(make_float2(p0, p1), make_float2(p2, p3)));
                 pf[nt][0] = transpose8x8(pack_bf16(p0, p1));
                 pf[nt][1] = transpose8x8(pack_bf16(p2, p3));
             }
@@ -341,12 +357,12 @@ __global__ void __launch_bounds__(PW * 32, 2) paged_attn_kernel(const PagedAttnA
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int r = 0; r < 2; ++r) {
-                float x = l[nt][r];
+                float x = r ? l[nt].y : l[nt].x;
                 x += __shfl_xor_sync(0xffffffffu, x, 4);
                 x += __shfl_xor_sync(0xffffffffu, x, 8);
                 x += __shfl_xor_sync(0xffffffffu, x, 16);
                 if (g == 0) {
-                    stat[0][warp][nt * 8 + 2 * t + r] = (unset >> (2 * nt + r)) & 1u ? -INFINITY : m[nt][r];
+                    stat[0][warp][nt * 8 + 2 * t + r] = (unset >> (2 * nt + r)) & 1u ? -INFINITY : r ? m[nt].y : m[nt].x;
                     stat[1][warp][nt * 8 + 2 * t + r] = x;
                 }
             }
