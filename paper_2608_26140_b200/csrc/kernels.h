@@ -301,6 +301,8 @@ struct PagedAttnArgs {
     float* part;                    // scratch of paged_attention_scratch_bytes()
     unsigned int* arrived;          // kKv8Counters words that are zero between launches
     uint32_t* status;
+    int group;                      // set by the launcher: query heads of a KV head
+    unsigned group_inverse;         // 2^32 / group, rounded up; 0: divide
 };
 size_t paged_attention_scratch_bytes(int head_dim);
 int launch_paged_attention(const PagedAttnArgs& a, cudaStream_t stream);    // kernels launched, or -1

@@ -75,11 +75,20 @@ __global__ void __launch_bounds__(PW * 32, 2) paged_attn_kernel(const PagedAttnA
     __shared__ long long sums[PW];
     __shared__ long long at_request[2];                      // (request, first unit of it) that this CTA begins with
     __shared__ int is_last;
+    __shared__ float4 factor[8 * NT];
+    __shared__ float lse2_of[8 * NT];
+    static_assert(PW == 4, "a factor for every warp");
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
     pdl_wait();
     pdl_launch_dependents();
-    const int hkv = a.n_kv_heads, G = a.n_heads / hkv, R = a.n * G, tiles = (R + L::ROWS - 1) / L::ROWS, per_request = hkv * tiles;
+    const int hkv = a.n_kv_heads, G = a.group, R = a.n * G, tiles = (R + L::ROWS - 1) / L::ROWS, per_request = hkv * tiles;
     uint2* qs = reinterpret_cast<uint2*>(smem + L::SMEM - L::QS);
+
+    // where row r of KV head kvh of request b lies: query row r / G, head kvh G + r % G
+    auto place_of = [&](int b, int kvh, int r) {
+        const int i = a.group_inverse ? (int)__umulhi((unsigned)r, a.group_inverse) : G == 1 ? r : r / G;
+        return (int64_t)(b * (int64_t)a.n + i) * a.n_heads + kvh * G + (r - i * G);
+    };
 
     // ---- this CTA's share of the units ----
     auto len_of = [&](int b) { return a.lens ? min(max(a.lens[b], 0), a.ctx_len) : a.ctx_len; };
@@ -173,19 +182,7 @@ __global__ void __launch_bounds__(PW * 32, 2) paged_attn_kernel(const PagedAttnA
         const int steps = max(0, (key_hi - key_lo + PSTEP - 1) / PSTEP), my_steps = (steps - warp + PW - 1) / PW;
         const int32_t* table = a.pages.table + (int64_t)b * a.pages.table_stride;
 
-        // ---- queries as fragments, the rows dealt out to the warps ----
-        __syncthreads();                                     // nobody reads the last item's any more
-        for (int f = warp; f < (D / 16) * NT; f += PW) {
-            const int ks = f / NT, r = tile * L::ROWS + (f % NT) * 8 + g;
-            uint2 q = make_uint2(0u, 0u);
-            if (r < R) {
-                const uint32_t* from = reinterpret_cast<const uint32_t*>(static_cast<const __nv_bfloat16*>(a.q) +
-                                                                         ((int64_t)(b * (int64_t)a.n + r / G) * a.n_heads + kvh * G + r % G) * D + ks * 16);
-                q = make_uint2(__ldg(from + t), __ldg(from + t + 4));
-            }
-            qs[f * 32 + lane] = q;
-        }
-
+        __syncthreads();                                     // nobody reads the last item's results or queries any more
         // ---- the ring ----
         int entry = 0;                                       // page of this lane's key of the next step to be fetched
         uint32_t drop = 0u;
@@ -244,6 +241,17 @@ __global__ void __launch_bounds__(PW * 32, 2) paged_attn_kernel(const PagedAttnA
             static_assert(PSTAGES == 3, "two stages ahead");
             look_up(2);
         }
+        // ---- queries as fragments, the rows dealt out to the warps ----
+        for (int f = warp; f < (D / 16) * NT; f += PW) {
+            const int ks = f / NT, r = tile * L::ROWS + (f % NT) * 8 + g;
+            uint2 q = make_uint2(0u, 0u);
+            if (r < R) {
+                const uint32_t* from = reinterpret_cast<const uint32_t*>(static_cast<const __nv_bfloat16*>(a.q) + place_of(b, kvh, r) * D + ks * 16);
+                q = make_uint2(__ldg(from + t), __ldg(from + t + 4));
+            }
+            qs[f * 32 + lane] = q;
+        }
+
         __syncthreads();                                     // the queries are there
 
         constexpr bool Q_REGS = NT * D <= 256;
@@ -380,75 +388,104 @@ __global__ void __launch_bounds__(PW * 32, 2) paged_attn_kernel(const PagedAttnA
         const bool all_of_it = unit == item_lo && seg_hi == item_hi;
         constexpr int TPR = D / 4;                           // threads of a row, 4 values each
         auto give = [&](int row, int c, const float4& v, float lse2) {
-            const int r = tile * L::ROWS + row;
-            const int64_t at = (int64_t)(b * (int64_t)a.n + r / G) * a.n_heads + kvh * G + r % G;
+            const int64_t at = place_of(b, kvh, tile * L::ROWS + row);
             *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(a.o) + at * D + c * 4) = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
             if (a.lse && c == 0) a.lse[at] = lse2 * 0.6931471805599453f;
         };
+        // what a warp's sums of a row are multiplied by, and the log2 of the denominator
+        if (tid < L::ROWS) {
+            float mx = -INFINITY, den = 0.f, f[PW];
+#pragma unroll
+            for (int w = 0; w < PW; ++w) mx = fmaxf(mx, stat[0][w][tid]);
+#pragma unroll
+            for (int w = 0; w < PW; ++w) {
+                f[w] = stat[0][w][tid] == -INFINITY ? 0.f : ex2(stat[0][w][tid] - mx);   // (a warp that met no key has sums of zero)
+                den = fmaf(f[w], stat[1][w][tid], den);
+            }
+            const float inv = den == 0.f ? 0.f : 1.f / den;
+            factor[tid] = make_float4(f[0] * inv, f[1] * inv, f[2] * inv, f[3] * inv);
+            lse2_of[tid] = den == 0.f ? -INFINITY : mx + log2f(den);
+        }
+        __syncthreads();
         // parts: [2 CTA + (whether the item began with it)][row][D], then [..][row] log2 of the denominators
         float* part_o = a.part;
         float* part_l = a.part + (int64_t)2 * gridDim.x * L::ROWS * D;
         const int64_t my_part = (int64_t)(2 * blockIdx.x + (unit == item_lo)) * L::ROWS;
-        for (int i = tid; i < L::ROWS * TPR; i += PW * 32) {
+        const int rows = min(L::ROWS, R - tile * L::ROWS);
+        for (int i = tid; i < rows * TPR; i += PW * 32) {
             const int row = i / TPR, c = i % TPR;
-            if (tile * L::ROWS + row >= R) break;
-            float mx = -INFINITY;
-#pragma unroll
-            for (int w = 0; w < PW; ++w) mx = fmaxf(mx, stat[0][w][row]);
-            float den = 0.f;
+            const float4 f4 = factor[row];
+            const float f[PW] = {f4.x, f4.y, f4.z, f4.w};
             float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
             for (int w = 0; w < PW; ++w) {
-                const float mw = stat[0][w][row];
-                if (mw == -INFINITY) continue;               // a warp that met no key
-                const float f = ex2(mw - mx);
                 const float4 x = *reinterpret_cast<const float4*>(os + (w * L::ROWS + row) * (D + 4) + c * 4);
-                den = fmaf(f, stat[1][w][row], den);
-                v.x = fmaf(f, x.x, v.x); v.y = fmaf(f, x.y, v.y); v.z = fmaf(f, x.z, v.z); v.w = fmaf(f, x.w, v.w);
+                v.x = fmaf(f[w], x.x, v.x); v.y = fmaf(f[w], x.y, v.y); v.z = fmaf(f[w], x.z, v.z); v.w = fmaf(f[w], x.w, v.w);
             }
-            const float inv = den == 0.f ? 0.f : 1.f / den;
-            v.x *= inv; v.y *= inv; v.z *= inv; v.w *= inv;
-            const float lse2 = den == 0.f ? -INFINITY : mx + log2f(den);
             if (all_of_it) {
-                give(row, c, v, lse2);
+                give(row, c, v, lse2_of[row]);
             } else {
                 *reinterpret_cast<float4*>(part_o + (my_part + row) * D + c * 4) = v;
-                if (c == 0) part_l[my_part + row] = lse2;
+                if (c == 0) part_l[my_part + row] = lse2_of[row];
             }
         }
         if (!all_of_it) {
             // ---- the last of the item's CTAs adds the parts up, in their order ----
             const int c0 = (int)(((item_lo + 1) * ctas - 1) / total), c1 = (int)((item_hi * ctas - 1) / total);
-            __threadfence();
+            auto part_of = [&](int q) { return (int64_t)(2 * q + (q == c0)) * L::ROWS; };
             __syncthreads();
             if (tid == 0) {
                 unsigned* arrived = a.arrived + c0;          // an item that goes on past a CTA is the last one that begins there
+                __threadfence();                             // (the other threads' parts too: they are behind the barrier)
                 is_last = atomicAdd(arrived, 1u) == (unsigned)(c1 - c0);
                 if (is_last) *arrived = 0u;
+                __threadfence();
             }
             __syncthreads();
             if (is_last) {
-                __threadfence();
-                for (int i = tid; i < L::ROWS * TPR; i += PW * 32) {
-                    const int row = i / TPR, c = i % TPR;
-                    if (tile * L::ROWS + row >= R) break;
-                    Sum sum;
+                if (tid < rows) {                            // largest and sum of the denominators of a row
+                    float mx = -INFINITY, den = 0.f;
                     for (int q0 = c0; q0 <= c1; q0 += 8) {
-                        float x[8];
-                        float4 w[8];
+                        float x[8], most = mx;
 #pragma unroll
                         for (int p = 0; p < 8; ++p) {
+                            x[p] = q0 + p <= c1 ? __ldcg(part_l + part_of(q0 + p) + tid) : -INFINITY;
+                            most = fmaxf(most, x[p]);
+                        }
+                        if (mx != -INFINITY) den *= ex2(mx - most);
+                        mx = most;
+#pragma unroll
+                        for (int p = 0; p < 8; ++p)
+                            if (x[p] != -INFINITY) den += ex2(x[p] - mx);        // (a NaN comes through)
+                    }
+                    factor[tid] = make_float4(mx, den == 0.f ? 0.f : 1.f / den, 0.f, 0.f);
+                    lse2_of[tid] = den == 0.f ? -INFINITY : mx + log2f(den);
+                }
+                __syncthreads();
+                for (int i = tid; i < rows * TPR; i += PW * 32) {
+                    const int row = i / TPR, c = i % TPR;
+                    const float mx = factor[row].x, inv = factor[row].y;
+                    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+                    for (int q0 = c0; q0 <= c1; q0 += 4) {
+                        float x[4];
+                        float4 w[4];
+#pragma unroll
+                        for (int p = 0; p < 4; ++p) {
                             x[p] = -INFINITY;
                             if (q0 + p <= c1) {
-                                const int64_t at = (int64_t)(2 * (q0 + p) + (q0 + p == c0)) * L::ROWS + row;
+                                const int64_t at = part_of(q0 + p) + row;
                                 x[p] = __ldcg(part_l + at);
                                 w[p] = __ldcg(reinterpret_cast<const float4*>(part_o + at * D + c * 4));
                             }
                         }
 #pragma unroll
-                        for (int p = 0; p < 8; ++p) sum.add(x[p], w[p]);
+                        for (int p = 0; p < 4; ++p) {
+                            if (x[p] == -INFINITY) continue;
+                            const float f = ex2(x[p] - mx) * inv;
+                            v.x = fmaf(f, w[p].x, v.x); v.y = fmaf(f, w[p].y, v.y); v.z = fmaf(f, w[p].z, v.z); v.w = fmaf(f, w[p].w, v.w);
+                        }
                     }
-                    give(row, c, sum.mean(), sum.lse2());
+                    give(row, c, v, lse2_of[row]);
                 }
             }
         }
@@ -457,7 +494,7 @@ __global__ void __launch_bounds__(PW * 32, 2) paged_attn_kernel(const PagedAttnA
 }
 
 template <int D, int NT>
-int paged_launch(const PagedAttnArgs& a, cudaStream_t stream) {
+int paged_launch(PagedAttnArgs a, cudaStream_t stream) {
     using L = PagedLayout<D, NT>;
     static PerDevice<bool> ready;
     int device = 0;
@@ -466,7 +503,10 @@ int paged_launch(const PagedAttnArgs& a, cudaStream_t stream) {
             ok = cudaFuncSetAttribute(paged_attn_kernel<D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, L::SMEM) == cudaSuccess;
         }))
         return -1;
-    const int R = a.n * (a.n_heads / a.n_kv_heads), tiles = (R + L::ROWS - 1) / L::ROWS;
+    a.group = a.n_heads / a.n_kv_heads;
+    const int R = a.n * a.group, tiles = (R + L::ROWS - 1) / L::ROWS;
+    // r / group as the upper half of a product, exact while r group stays below 2^32
+    a.group_inverse = a.group > 1 && (int64_t)R * a.group < ((int64_t)1 << 32) ? (unsigned)((((int64_t)1 << 32) + a.group - 1) / a.group) : 0u;
     const int64_t units = (int64_t)std::max(1, (a.ctx_len + kUnit - 1) / kUnit) * tiles * a.batch * a.n_kv_heads;
     const int ctas = (int)std::min<int64_t>(kPlaces, std::max<int64_t>(1, units / kMinUnits));
     return launch_pdl(paged_attn_kernel<D, NT>, dim3(ctas), dim3(PW * 32), L::SMEM, stream, a) == cudaSuccess ? 1 : -1;
