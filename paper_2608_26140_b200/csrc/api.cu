@@ -238,6 +238,7 @@ acache_status run_paged_attention(acache_ctx* c, const acache_paged_kv* kv, int3
     a.arrived = wsp<unsigned int>(c, c->o_arrived);
     a.status = wsp<uint32_t>(c, c->o_status);
     const int nl = launch_paged_attention(a, st);
+    if (nl == -2) return fail(c, ACACHE_ERR_UNSUPPORTED_SHAPE, "keys / 64 times row tiles, KV heads and requests do not fit in 31 bits");
     if (nl < 0) return check_cuda(c, "paged attention") == ACACHE_OK ? fail(c, ACACHE_ERR_CUDA, "paged attention launch failed") : ACACHE_ERR_CUDA;
     c->launches += nl;
     return check_cuda(c, "paged attention");

@@ -305,7 +305,7 @@ struct PagedAttnArgs {
     unsigned group_inverse;         // 2^32 / group, rounded up; 0: divide
 };
 size_t paged_attention_scratch_bytes(int head_dim);
-int launch_paged_attention(const PagedAttnArgs& a, cudaStream_t stream);    // kernels launched, or -1
+int launch_paged_attention(const PagedAttnArgs& a, cudaStream_t stream);    // kernels launched, -1: failed, -2: too much for one call
 
 // ---- sample.cu ----------------------------------------------------------------------------
 constexpr int kSampleMaxVocab = 1 << 18;

@@ -13,6 +13,7 @@
 // A warp streams 16 keys a step through a ring of its own in shared memory (cp.async, whole rows side by side, the page's number asked for a
 // step ahead), swizzled so that ldmatrix meets different banks.  Keys that do not count are not read: their places are zero.
 #include <algorithm>
+#include <climits>
 
 #include "kernels.h"
 #include "kv8.cuh"
@@ -72,11 +73,10 @@ __global__ void __launch_bounds__(PW * 32, 2) paged_attn_kernel(const PagedAttnA
     extern __shared__ __align__(128) unsigned char smem[];
     __shared__ float stat[2][PW][8 * NT];                    // references, denominators
     __shared__ uint32_t there_of[PW][PSTAGES];               // a stage's keys that count
-    __shared__ long long sums[PW];
-    __shared__ long long at_request[2];                      // (request, first unit of it) that this CTA begins with
+    __shared__ unsigned sums[PW], at_request[2];             // (request, first unit of it) that this CTA begins with
     __shared__ int is_last;
     __shared__ float4 factor[8 * NT];
-    __shared__ float lse2_of[8 * NT];
+    __shared__ float lse2_of[8 * NT], lse_of[L::RING / (D * 4)];
     static_assert(PW == 4, "a factor for every warp");
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
     pdl_wait();
@@ -92,40 +92,42 @@ __global__ void __launch_bounds__(PW * 32, 2) paged_attn_kernel(const PagedAttnA
 
     // ---- this CTA's share of the units ----
     auto len_of = [&](int b) { return a.lens ? min(max(a.lens[b], 0), a.ctx_len) : a.ctx_len; };
-    int64_t total, mine_lo, mine_hi;
+    unsigned base, rest;                                     // CTA c takes base units, the first `rest` ones one more
     int ctas;                                                // that have work
-    auto share = [&](int64_t units) {
-        total = units;
-        ctas = (int)min((int64_t)gridDim.x, max((int64_t)1, units / kMinUnits));
-        mine_lo = units * blockIdx.x / ctas;
-        mine_hi = units * (blockIdx.x + 1) / ctas;
+    auto first_of = [&](int c) { return (unsigned)c * base + min((unsigned)c, rest); };
+    auto cta_of = [&](unsigned unit) { return unit < rest * (base + 1u) ? unit / (base + 1u) : rest + (unit - rest * (base + 1u)) / base; };
+    auto share = [&](unsigned units) {
+        ctas = (int)min(gridDim.x, max(1u, units / kMinUnits));
+        base = units / (unsigned)ctas;
+        rest = units - base * (unsigned)ctas;
     };
     int b;
-    int64_t b_lo;                                            // first unit of request b
+    unsigned b_lo;                                           // first unit of request b
     if (!a.lens) {
-        const int64_t u = (int64_t)units_of(a.ctx_len) * per_request;
+        const unsigned u = (unsigned)units_of(a.ctx_len) * per_request;
         share(u * a.batch);
         if ((int)blockIdx.x >= ctas) return;
-        b = (int)(mine_lo / u);
+        b = (int)(first_of(blockIdx.x) / u);
         b_lo = u * b;
     } else {
         // the threads count the units of equal runs of requests; the one whose run holds the first unit of the share finds its request
         const int run = (a.batch + PW * 32 - 1) / (PW * 32), r0 = min(tid * run, a.batch), r1 = min(r0 + run, a.batch);
-        int64_t sum = 0;
+        unsigned sum = 0u;
+#pragma unroll 1
         for (int r = r0; r < r1; ++r) {
             const int len = a.lens[r];
             if (blockIdx.x == 0 && (len < 0 || len > a.ctx_len)) atomicOr(a.status, kFlagBadIndex);
-            sum += (int64_t)units_of(len_of(r)) * per_request;
+            sum += (unsigned)units_of(min(max(len, 0), a.ctx_len)) * per_request;
         }
-        int64_t upto = sum;
+        unsigned upto = sum;
 #pragma unroll
         for (int off = 1; off < 32; off <<= 1) {
-            const int64_t v = __shfl_up_sync(0xffffffffu, upto, off);
+            const unsigned v = __shfl_up_sync(0xffffffffu, upto, off);
             if (lane >= off) upto += v;
         }
         if (lane == 31) sums[warp] = upto;
         __syncthreads();
-        int64_t all = 0;
+        unsigned all = 0u;
 #pragma unroll
         for (int w = 0; w < PW; ++w) {
             if (w == warp) upto += all;
@@ -133,22 +135,24 @@ __global__ void __launch_bounds__(PW * 32, 2) paged_attn_kernel(const PagedAttnA
         }
         share(all);
         if ((int)blockIdx.x >= ctas) return;
-        int64_t lo = upto - sum;
-        if (lo <= mine_lo && mine_lo < upto) {
+        unsigned lo = upto - sum;
+        const unsigned mine = first_of(blockIdx.x);
+        if (lo <= mine && mine < upto) {
             int r = r0;
+#pragma unroll 1
             for (; r < r1 - 1; ++r) {
-                const int64_t u = (int64_t)units_of(len_of(r)) * per_request;
-                if (mine_lo < lo + u) break;
+                const unsigned u = (unsigned)units_of(len_of(r)) * per_request;
+                if (mine < lo + u) break;
                 lo += u;
             }
-            at_request[0] = r;
+            at_request[0] = (unsigned)r;
             at_request[1] = lo;
         }
         __syncthreads();
         b = (int)at_request[0];
         b_lo = at_request[1];
     }
-    if (mine_hi <= mine_lo) return;
+    const unsigned mine_hi = first_of(blockIdx.x + 1);
 
     const int page_mask = (1 << a.pages.log2_page) - 1;
     const bool whole = a.pages.log2_page >= 4;               // a step's keys lie in one page
@@ -165,32 +169,33 @@ __global__ void __launch_bounds__(PW * 32, 2) paged_attn_kernel(const PagedAttnA
     const uint32_t k_get = ((mj & 1) * 8 + mrow) * D * 2 + (((mj >> 1) ^ mrow) << 4);
     const uint32_t v_get = L::HALF + ((mj >> 1) * 8 + mrow) * D * 2 + (((mj & 1) ^ mrow) << 4);
 
-    int64_t unit = mine_lo;
+    unsigned unit = first_of(blockIdx.x);
     while (unit < mine_hi) {
         // ---- the item and this CTA's keys of it ----
-        int len = len_of(b), units = units_of(len);
-        while (unit >= b_lo + (int64_t)units * per_request) {
-            b_lo += (int64_t)units * per_request;
+        int len = len_of(b);
+        unsigned units = units_of(len);
+        while (unit >= b_lo + units * per_request) {
+            b_lo += units * per_request;
             ++b;
             len = len_of(b);
             units = units_of(len);
         }
-        const int item = (int)((unit - b_lo) / units), tile = item % tiles, kvh = item / tiles;
-        const int64_t item_lo = b_lo + (int64_t)item * units, item_hi = item_lo + units;
-        const int64_t seg_hi = min(item_hi, mine_hi);
+        const int item = (int)((unit - b_lo) / units), kvh = tiles == 1 ? item : item / tiles, tile = item - kvh * tiles;
+        const unsigned item_lo = b_lo + (unsigned)item * units, item_hi = item_lo + units, seg_hi = min(item_hi, mine_hi);
         const int key_lo = (int)(unit - item_lo) * kUnit, key_hi = min(len, (int)(seg_hi - item_lo) * kUnit);
         const int steps = max(0, (key_hi - key_lo + PSTEP - 1) / PSTEP), my_steps = (steps - warp + PW - 1) / PW;
         const int32_t* table = a.pages.table + (int64_t)b * a.pages.table_stride;
 
         __syncthreads();                                     // nobody reads the last item's results or queries any more
         // ---- the ring ----
-        int entry = 0;                                       // page of this lane's key of the next step to be fetched
-        uint32_t drop = 0u;
-        auto look_up = [&](int s) {
+        // page of this lane's key, and the bits of keys that do not exist, of the next two steps to be fetched
+        int entry = 0, entry2 = 0;
+        uint32_t drop = 0u, drop2 = 0u;
+        auto look_up = [&](int s, int& e, uint32_t& d) {
             if (s >= my_steps) return;
             const int key0 = key_lo + (warp + s * PW) * PSTEP, key = key0 + (whole ? 0 : lane & 15);
-            entry = key < key_hi ? __ldg(table + (key >> a.pages.log2_page)) : 0;
-            drop = a.key_drop ? __ldg(a.key_drop + (int64_t)b * a.drop_words + (key0 >> 5)) >> (key0 & 16) : 0u;
+            e = key < key_hi ? __ldg(table + (key >> a.pages.log2_page)) : 0;
+            d = a.key_drop ? __ldg(a.key_drop + (int64_t)b * a.drop_words + (key0 >> 5)) >> (key0 & 16) : 0u;
         };
         auto fetch = [&](int s, int stage) {
             if (s < my_steps) {
@@ -227,31 +232,34 @@ __global__ void __launch_bounds__(PW * 32, 2) paged_attn_kernel(const PagedAttnA
             }
             cp_async_commit();
         };
-        look_up(0);
-        {
-            const int e0 = entry;
-            const uint32_t d0 = drop;
-            look_up(1);                                      // (asked for before the first is used)
-            const int e1 = entry;
-            const uint32_t d1 = drop;
-            entry = e0; drop = d0;
-            fetch(0, 0);
-            entry = e1; drop = d1;
-            fetch(1, 1);
-            static_assert(PSTAGES == 3, "two stages ahead");
-            look_up(2);
-        }
+        look_up(0, entry, drop);
+        look_up(1, entry2, drop2);
+        int ahead = 0;                                       // the next step to be fetched
+        auto advance = [&](int stage) {
+            fetch(ahead, stage);
+            entry = entry2; drop = drop2;
+            look_up(ahead + 2, entry2, drop2);
+            ++ahead;
+        };
+#pragma unroll 1
+        while (ahead < PSTAGES - 1) advance(ahead);
         // ---- queries as fragments, the rows dealt out to the warps ----
-        for (int f = warp; f < (D / 16) * NT; f += PW) {
-            const int ks = f / NT, r = tile * L::ROWS + (f % NT) * 8 + g;
-            uint2 q = make_uint2(0u, 0u);
-            if (r < R) {
-                const uint32_t* from = reinterpret_cast<const uint32_t*>(static_cast<const __nv_bfloat16*>(a.q) + place_of(b, kvh, r) * D + ks * 16);
-                q = make_uint2(__ldg(from + t), __ldg(from + t + 4));
+        constexpr int FRAGS = (D / 16) * NT, PER_WARP = (FRAGS + PW - 1) / PW;
+        {
+            uint2 q[PER_WARP];
+#pragma unroll
+            for (int i = 0; i < PER_WARP; ++i) {
+                const int f = warp + i * PW, r = tile * L::ROWS + (f % NT) * 8 + g;
+                q[i] = make_uint2(0u, 0u);
+                if (f < FRAGS && r < R) {
+                    const uint32_t* from = reinterpret_cast<const uint32_t*>(static_cast<const __nv_bfloat16*>(a.q) + place_of(b, kvh, r) * D + f / NT * 16);
+                    q[i] = make_uint2(__ldg(from + t), __ldg(from + t + 4));
+                }
             }
-            qs[f * 32 + lane] = q;
+#pragma unroll
+            for (int i = 0; i < PER_WARP; ++i)
+                if (warp + i * PW < FRAGS) qs[(warp + i * PW) * 32 + lane] = q[i];
         }
-
         __syncthreads();                                     // the queries are there
 
         constexpr bool Q_REGS = NT * D <= 256;
@@ -279,8 +287,7 @@ __global__ void __launch_bounds__(PW * 32, 2) paged_attn_kernel(const PagedAttnA
             ring_wait<PSTAGES - 2>();
             __syncwarp();                                    // this step's stage is there for every lane, and every lane is done with the last one's
             const uint32_t there = there_of[warp][stage];
-            fetch(s + PSTAGES - 1, stage == 0 ? PSTAGES - 1 : stage - 1);
-            look_up(s + PSTAGES);
+            advance(stage == 0 ? PSTAGES - 1 : stage - 1);
             stage = stage == PSTAGES - 1 ? 0 : stage + 1;
             if (there == 0u) continue;
             // ---- S^T = K Q^T ----
@@ -431,61 +438,69 @@ __global__ void __launch_bounds__(PW * 32, 2) paged_attn_kernel(const PagedAttnA
         }
         if (!all_of_it) {
             // ---- the last of the item's CTAs adds the parts up, in their order ----
-            const int c0 = (int)(((item_lo + 1) * ctas - 1) / total), c1 = (int)((item_hi * ctas - 1) / total);
+            const int c0 = (int)cta_of(item_lo), c1 = (int)cta_of(item_hi - 1u);
             auto part_of = [&](int q) { return (int64_t)(2 * q + (q == c0)) * L::ROWS; };
             __syncthreads();
             if (tid == 0) {
                 unsigned* arrived = a.arrived + c0;          // an item that goes on past a CTA is the last one that begins there
-                __threadfence();                             // (the other threads' parts too: they are behind the barrier)
-                is_last = atomicAdd(arrived, 1u) == (unsigned)(c1 - c0);
+                unsigned before;                             // (the other threads' parts are behind the barrier, and so told with this one's)
+                asm volatile("atom.add.acq_rel.gpu.global.u32 %0, [%1], 1;" : "=r"(before) : "l"(arrived) : "memory");
+                is_last = before == (unsigned)(c1 - c0);
                 if (is_last) *arrived = 0u;
-                __threadfence();
             }
             __syncthreads();
             if (is_last) {
-                if (tid < rows) {                            // largest and sum of the denominators of a row
-                    float mx = -INFINITY, den = 0.f;
-                    for (int q0 = c0; q0 <= c1; q0 += 8) {
-                        float x[8], most = mx;
+                // This runs once: short loops (code that is met for the first time costs more than what it does), and the parts come as copies
+                // into the ring's place, as many at a time as it holds, so that one wait stands for all of them.
+                constexpr int HELD = L::RING / (L::ROWS * D * 4);
+                float* held = os;                            // [part][row][D]
+                float4 v[(L::ROWS * TPR) / (PW * 32)];
+                float den[(L::ROWS * TPR) / (PW * 32)], top_l[(L::ROWS * TPR) / (PW * 32)];
 #pragma unroll
-                        for (int p = 0; p < 8; ++p) {
-                            x[p] = q0 + p <= c1 ? __ldcg(part_l + part_of(q0 + p) + tid) : -INFINITY;
-                            most = fmaxf(most, x[p]);
-                        }
-                        if (mx != -INFINITY) den *= ex2(mx - most);
-                        mx = most;
-#pragma unroll
-                        for (int p = 0; p < 8; ++p)
-                            if (x[p] != -INFINITY) den += ex2(x[p] - mx);        // (a NaN comes through)
-                    }
-                    factor[tid] = make_float4(mx, den == 0.f ? 0.f : 1.f / den, 0.f, 0.f);
-                    lse2_of[tid] = den == 0.f ? -INFINITY : mx + log2f(den);
+                for (int k = 0; k < (L::ROWS * TPR) / (PW * 32); ++k) {
+                    v[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+                    den[k] = 0.f;
+                    top_l[k] = -INFINITY;
                 }
-                __syncthreads();
-                for (int i = tid; i < rows * TPR; i += PW * 32) {
-                    const int row = i / TPR, c = i % TPR;
-                    const float mx = factor[row].x, inv = factor[row].y;
-                    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-                    for (int q0 = c0; q0 <= c1; q0 += 4) {
-                        float x[4];
-                        float4 w[4];
+#pragma unroll 1
+                for (int q0 = c0; q0 <= c1; q0 += HELD) {
+                    const int n_here = min(HELD, c1 + 1 - q0), chunks = rows * TPR;
+#pragma unroll 1
+                    for (int p = warp; p < n_here; p += PW) {
+                        const float* from = part_o + part_of(q0 + p) * D;
+#pragma unroll 1
+                        for (int i = lane; i < chunks; i += 32) cp_async16(smem_u32(held + p * (L::ROWS * D) + i * 4), from + i * 4);
+                    }
+                    cp_async_commit();
+                    for (int i = tid; i < n_here * L::ROWS; i += PW * 32)
+                        if (i % L::ROWS < rows) lse_of[i] = __ldcg(part_l + part_of(q0 + i / L::ROWS) + i % L::ROWS);
+                    ring_wait<0>();
+                    __syncthreads();
+#pragma unroll 1
+                    for (int p = 0; p < n_here; ++p) {
 #pragma unroll
-                        for (int p = 0; p < 4; ++p) {
-                            x[p] = -INFINITY;
-                            if (q0 + p <= c1) {
-                                const int64_t at = part_of(q0 + p) + row;
-                                x[p] = __ldcg(part_l + at);
-                                w[p] = __ldcg(reinterpret_cast<const float4*>(part_o + at * D + c * 4));
-                            }
-                        }
-#pragma unroll
-                        for (int p = 0; p < 4; ++p) {
-                            if (x[p] == -INFINITY) continue;
-                            const float f = ex2(x[p] - mx) * inv;
-                            v.x = fmaf(f, w[p].x, v.x); v.y = fmaf(f, w[p].y, v.y); v.z = fmaf(f, w[p].z, v.z); v.w = fmaf(f, w[p].w, v.w);
+                        for (int k = 0; k < (L::ROWS * TPR) / (PW * 32); ++k) {
+                            const int i = tid + k * PW * 32;
+                            if (i >= chunks) break;
+                            const float x = lse_of[p * L::ROWS + i / TPR];
+                            if (x == -INFINITY) continue;    // no keys
+                            const float4 w = *reinterpret_cast<const float4*>(held + p * (L::ROWS * D) + i * 4);
+                            const float most = fmaxf(top_l[k], x), fo = top_l[k] == -INFINITY ? 0.f : ex2(top_l[k] - most), f = ex2(x - most);       // (a NaN comes through by f)
+                            top_l[k] = most;
+                            den[k] = fmaf(den[k], fo, f);
+                            v[k].x = fmaf(v[k].x, fo, f * w.x); v[k].y = fmaf(v[k].y, fo, f * w.y);
+                            v[k].z = fmaf(v[k].z, fo, f * w.z); v[k].w = fmaf(v[k].w, fo, f * w.w);
                         }
                     }
-                    give(row, c, v, lse2_of[row]);
+                    __syncthreads();
+                }
+#pragma unroll
+                for (int k = 0; k < (L::ROWS * TPR) / (PW * 32); ++k) {
+                    const int i = tid + k * PW * 32;
+                    if (i >= rows * TPR) break;
+                    const float inv = den[k] == 0.f ? 0.f : 1.f / den[k];
+                    give(i / TPR, i % TPR, make_float4(v[k].x * inv, v[k].y * inv, v[k].z * inv, v[k].w * inv),
+                         den[k] == 0.f ? -INFINITY : top_l[k] + log2f(den[k]));
                 }
             }
         }
@@ -508,6 +523,7 @@ int paged_launch(PagedAttnArgs a, cudaStream_t stream) {
     // r / group as the upper half of a product, exact while r group stays below 2^32
     a.group_inverse = a.group > 1 && (int64_t)R * a.group < ((int64_t)1 << 32) ? (unsigned)((((int64_t)1 << 32) + a.group - 1) / a.group) : 0u;
     const int64_t units = (int64_t)std::max(1, (a.ctx_len + kUnit - 1) / kUnit) * tiles * a.batch * a.n_kv_heads;
+    if (units > INT_MAX) return -2;                        // counted in 32 bits
     const int ctas = (int)std::min<int64_t>(kPlaces, std::max<int64_t>(1, units / kMinUnits));
     return launch_pdl(paged_attn_kernel<D, NT>, dim3(ctas), dim3(PW * 32), L::SMEM, stream, a) == cudaSuccess ? 1 : -1;
 }
