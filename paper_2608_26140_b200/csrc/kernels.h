@@ -303,6 +303,7 @@ struct PagedAttnArgs {
     uint32_t* status;
     int group;                      // set by the launcher: query heads of a KV head
     unsigned group_inverse;         // 2^32 / group, rounded up; 0: divide
+    int cluster;                    // CTAs of an item, in a cluster; 0: items in one line, cut into equal pieces
 };
 size_t paged_attention_scratch_bytes(int head_dim);
 int launch_paged_attention(const PagedAttnArgs& a, cudaStream_t stream);    // kernels launched, -1: failed, -2: too much for one call

@@ -19,6 +19,7 @@
 #include "kv8.cuh"
 #include "launch.h"
 #include "per_device.h"
+#include "tc_ptx.cuh"
 
 namespace acache {
 namespace {
@@ -61,7 +62,8 @@ struct PagedLayout {
     static constexpr int RING = PW * PSTAGES * STAGE;
     static constexpr int MERGE = PW * ROWS * (D + 4) * 4;    // the warps' results, in the ring's place
     static constexpr int QS = (D / 16) * NT * 32 * 8;        // the queries as fragments
-    static constexpr int SMEM = (RING > MERGE ? RING : MERGE) + QS;
+    static constexpr int RESULT = ROWS * D * 4;              // behind them, what a cluster's other CTAs read
+    static constexpr int SMEM = (RING > MERGE + RESULT ? RING : MERGE + RESULT) + QS;
 };
 
 // Units of a request's items (row tile and KV head): one for an empty request too, which has outputs like any other.
@@ -102,8 +104,18 @@ __global__ void __launch_bounds__(PW * 32, 2) paged_attn_kernel(const PagedAttnA
         rest = units - base * (unsigned)ctas;
     };
     int b;
-    unsigned b_lo;                                           // first unit of request b
-    if (!a.lens) {
+    unsigned b_lo = 0u;                                      // first unit of request b
+    unsigned unit, mine_hi;
+    int cluster_item = 0;                                    // in a cluster: the item of request b that its CTAs share
+    if (a.cluster) {
+        const int item = blockIdx.x / a.cluster, rank = blockIdx.x % a.cluster;
+        b = item / per_request;
+        cluster_item = item - b * per_request;
+        const unsigned units = units_of(len_of(b));
+        unit = cluster_item * units + units * rank / a.cluster;
+        mine_hi = cluster_item * units + units * (rank + 1) / a.cluster;
+        if (a.lens && cluster_item == 0 && rank == 0 && tid == 0 && a.lens[b] != len_of(b)) atomicOr(a.status, kFlagBadIndex);
+    } else if (!a.lens) {
         const unsigned u = (unsigned)units_of(a.ctx_len) * per_request;
         share(u * a.batch);
         if ((int)blockIdx.x >= ctas) return;
@@ -152,7 +164,10 @@ __global__ void __launch_bounds__(PW * 32, 2) paged_attn_kernel(const PagedAttnA
         b = (int)at_request[0];
         b_lo = at_request[1];
     }
-    const unsigned mine_hi = first_of(blockIdx.x + 1);
+    if (!a.cluster) {
+        unit = first_of(blockIdx.x);
+        mine_hi = first_of(blockIdx.x + 1);
+    }
 
     const int page_mask = (1 << a.pages.log2_page) - 1;
     const bool whole = a.pages.log2_page >= 4;               // a step's keys lie in one page
@@ -169,18 +184,17 @@ __global__ void __launch_bounds__(PW * 32, 2) paged_attn_kernel(const PagedAttnA
     const uint32_t k_get = ((mj & 1) * 8 + mrow) * D * 2 + (((mj >> 1) ^ mrow) << 4);
     const uint32_t v_get = L::HALF + ((mj >> 1) * 8 + mrow) * D * 2 + (((mj & 1) ^ mrow) << 4);
 
-    unsigned unit = first_of(blockIdx.x);
-    while (unit < mine_hi) {
+    for (;;) {
         // ---- the item and this CTA's keys of it ----
         int len = len_of(b);
         unsigned units = units_of(len);
-        while (unit >= b_lo + units * per_request) {
+        while (!a.cluster && unit >= b_lo + units * per_request) {
             b_lo += units * per_request;
             ++b;
             len = len_of(b);
             units = units_of(len);
         }
-        const int item = (int)((unit - b_lo) / units), kvh = tiles == 1 ? item : item / tiles, tile = item - kvh * tiles;
+        const int item = a.cluster ? cluster_item : (int)((unit - b_lo) / units), kvh = tiles == 1 ? item : item / tiles, tile = item - kvh * tiles;
         const unsigned item_lo = b_lo + (unsigned)item * units, item_hi = item_lo + units, seg_hi = min(item_hi, mine_hi);
         const int key_lo = (int)(unit - item_lo) * kUnit, key_hi = min(len, (int)(seg_hi - item_lo) * kUnit);
         const int steps = max(0, (key_hi - key_lo + PSTEP - 1) / PSTEP), my_steps = (steps - warp + PW - 1) / PW;
@@ -392,7 +406,7 @@ __global__ void __launch_bounds__(PW * 32, 2) paged_attn_kernel(const PagedAttnA
                 for (int j = 0; j < 4; ++j)
                     os[(warp * L::ROWS + nt * 8 + 2 * t + (j & 1)) * (D + 4) + i * 16 + (j >> 1) * 8 + g] = o[i][nt][j];
         __syncthreads();
-        const bool all_of_it = unit == item_lo && seg_hi == item_hi;
+        const bool all_of_it = a.cluster ? a.cluster == 1 : unit == item_lo && seg_hi == item_hi;
         constexpr int TPR = D / 4;                           // threads of a row, 4 values each
         auto give = [&](int row, int c, const float4& v, float lse2) {
             const int64_t at = place_of(b, kvh, tile * L::ROWS + row);
@@ -431,10 +445,36 @@ __global__ void __launch_bounds__(PW * 32, 2) paged_attn_kernel(const PagedAttnA
             }
             if (all_of_it) {
                 give(row, c, v, lse2_of[row]);
+            } else if (a.cluster) {
+                *reinterpret_cast<float4*>(os + L::MERGE / 4 + row * D + c * 4) = v;
             } else {
                 *reinterpret_cast<float4*>(part_o + (my_part + row) * D + c * 4) = v;
                 if (c == 0) part_l[my_part + row] = lse2_of[row];
             }
+        }
+        if (a.cluster > 1) {
+            // ---- the CTAs of the cluster add their results up, each for a share of the values, in the order of their keys ----
+            cluster_sync_all();
+            const uint32_t res_at = smem_u32(os) + L::MERGE, lse_at = smem_u32(lse2_of);
+            for (int i = tid + blockIdx.x % a.cluster * PW * 32; i < rows * TPR; i += a.cluster * PW * 32) {
+                const int row = i / TPR, c = i % TPR;
+                float x[8];
+                float4 w[8];
+#pragma unroll
+                for (int p = 0; p < 8; ++p) {
+                    x[p] = -INFINITY;
+                    if (p < a.cluster) {
+                        x[p] = ld_peer(mapa_u32(lse_at + row * 4, p));
+                        w[p] = ld_peer4(mapa_u32(res_at + (row * D + c * 4) * 4, p));
+                    }
+                }
+                Sum sum;
+#pragma unroll
+                for (int p = 0; p < 8; ++p) sum.add(x[p], w[p]);
+                give(row, c, sum.mean(), sum.lse2());
+            }
+            cluster_sync_all();                              // nobody leaves while its results are read
+            return;
         }
         if (!all_of_it) {
             // ---- the last of the item's CTAs adds the parts up, in their order ----
@@ -505,6 +545,7 @@ __global__ void __launch_bounds__(PW * 32, 2) paged_attn_kernel(const PagedAttnA
             }
         }
         unit = seg_hi;
+        if (a.cluster || unit >= mine_hi) return;
     }
 }
 
@@ -524,8 +565,34 @@ int paged_launch(PagedAttnArgs a, cudaStream_t stream) {
     a.group_inverse = a.group > 1 && (int64_t)R * a.group < ((int64_t)1 << 32) ? (unsigned)((((int64_t)1 << 32) + a.group - 1) / a.group) : 0u;
     const int64_t units = (int64_t)std::max(1, (a.ctx_len + kUnit - 1) / kUnit) * tiles * a.batch * a.n_kv_heads;
     if (units > INT_MAX) return -2;                        // counted in 32 bits
+    // Two ways to share the work.  In one line of units every CTA has as much to do, but a result in parts costs a trip through memory and
+    // back (5.5 us); a cluster for each item joins its CTAs' parts in 1.6 us, and divides no work among items.  A unit takes 0.37 us (1 us with 32 rows a CTA),
+    // or its share of the memory's bandwidth.  One token of one request, 4 KV heads, 1664 keys: 9.1 and 6.7 us.
+    const int64_t items = (int64_t)tiles * a.batch * a.n_kv_heads, u = units / items;
     const int ctas = (int)std::min<int64_t>(kPlaces, std::max<int64_t>(1, units / kMinUnits));
-    return launch_pdl(paged_attn_kernel<D, NT>, dim3(ctas), dim3(PW * 32), L::SMEM, stream, a) == cudaSuccess ? 1 : -1;
+    auto unit_us = [&](int64_t active) { return std::max(NT == 4 ? 1.0 : 0.37, 1.5 * D / 128 * std::min<int64_t>(active, kPlaces) / kPlaces); };
+    double best = (units + ctas - 1) / ctas * unit_us(ctas) + 5.5;
+    a.cluster = 0;
+    for (int c = 1; c <= 8 && c <= u && items * c <= 4 * kPlaces; c *= 2) {
+        const double t = (items * c + kPlaces - 1) / kPlaces * ((u + c - 1) / c * unit_us(items * c) * (a.lens ? 1.3 : 1.0) + (c > 1 ? 1.6 : 0.0));
+        if (t < best) {
+            best = t;
+            a.cluster = c;
+        }
+    }
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(a.cluster ? (unsigned)items * a.cluster : ctas);
+    cfg.blockDim = dim3(PW * 32);
+    cfg.dynamicSmemBytes = L::SMEM;
+    cfg.stream = stream;
+    cudaLaunchAttribute at[2];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = a.cluster; at[1].val.clusterDim.y = 1; at[1].val.clusterDim.z = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = a.cluster > 1 ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, paged_attn_kernel<D, NT>, a) == cudaSuccess ? 1 : -1;
 }
 template <int D>
 int paged_dispatch(const PagedAttnArgs& a, cudaStream_t stream) {
