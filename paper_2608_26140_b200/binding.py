@@ -224,6 +224,12 @@ def _check_tensor(t, dtype, shape):
         raise ValueError(f"a tensor {tuple(t.shape)} of {t.dtype} on {t.device} where contiguous {tuple(shape)} of {dtype} on a GPU is wanted")
 
 
+def _checked(t, dtype, shape):
+    """The address of a tensor of that type and shape."""
+    _check_tensor(t, dtype, shape)
+    return t.data_ptr()
+
+
 def _dense(t, strides):
     """All dimensions but the first as in a contiguous tensor; the stride of a dimension of one element says nothing."""
     return t.numel() == 0 or all(n == 1 or have == want for n, have, want in zip(t.shape[1:], t.stride()[1:], strides))
@@ -231,8 +237,14 @@ def _dense(t, strides):
 
 def _stream() -> int:
     """The current stream of the current device (torch.cuda.current_stream() builds an object around it: 3.3 us a call, this 0.2)."""
-    import torch
-    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+    global _raw_stream, _device
+    if _raw_stream is None:
+        import torch
+        _raw_stream, _device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
+    return _raw_stream(_device())
+
+
+_raw_stream = _device = None
 
 
 class Context:
@@ -245,6 +257,10 @@ class Context:
         self.desc = ModelDesc(hidden, n_heads, n_kv_heads, head_dim, ffn, rms_eps, int(bool(qkv_bias)),
                               max_batch, max_ctx, max_affix, max_rows, max_masked, max_vocab, max_block)
         self.heads = (n_heads, n_kv_heads, head_dim)
+        self.dtypes = (torch.bfloat16, torch.float32, torch.int32)
+        self._row_args = [(r, C.byref(r)) for r in (Rows(), Rows(), Rows())]
+        how = Sampling()
+        self._sampling_arg = (how, C.byref(how))
         h = C.c_void_p()
         st = self.lib.acache_create(C.byref(self.desc), C.byref(h))
         if st != OK:
@@ -460,51 +476,77 @@ class Context:
         self._check(self.lib.acache_layer_step_kv8(self.h, C.byref(w), C.byref(req), C.byref(cache), _ptr(x), int(x_is_compact),
                                                    float(ratio), int(flags), _ptr(scores), _ptr(anchor_idx), _ptr(y), _stream()))
 
+    # (As above: most of a small call is spent here, so each property is asked for once and what the call takes by reference is kept.)
     def paged_append(self, cache: PagedKV, ctx_len, k, v, lens=None, pos=None, counts=None, rope=None, q=None, q_out=None):
         """Rows k, v [B, n, Hkv, d] (bf16; rows and requests may lie apart) as tokens lens[b] .. or pos [B, n] (int32), turned by rope = (cos, sin)
         [>= ctx_len, d / 2] (fp32) on the way; counts [B]: rows of each request; q [B, n, H, d] turned likewise to q_out."""
-        import torch
-        B, n = k.shape[0], k.shape[1]
+        bf16, f32, i32 = self.dtypes
+        H, hkv, d = self.heads
+        shape = k.shape
+        B, n = shape[0], shape[1]
         self._cache_fits(cache, B)
-        if v.shape != k.shape:
-            raise ValueError(f"k {tuple(k.shape)} and v {tuple(v.shape)} differ in shape")
-        at_k, at_v = self._rows_at(k, B, n, self.heads[1]), self._rows_at(v, B, n, self.heads[1])
-        at_q = None if q is None else self._rows_at(q, B, n, self.heads[0])
-        if (q is None) != (q_out is None):
-            raise ValueError("q and q_out go together")
-        if q_out is not None:
-            _check_tensor(q_out, torch.bfloat16, q.shape)
-        for t, shape in ((lens, (B,)), (counts, (B,)), (pos, (B, n))):
-            if t is not None:
-                _check_tensor(t, torch.int32, shape)
+        if v.shape != shape:
+            raise ValueError(f"k {tuple(shape)} and v {tuple(v.shape)} differ in shape")
+        (row_k, ref_k), (row_v, ref_v), (row_q, ref_q) = self._row_args
+        self._rows_at(row_k, k, shape, hkv)
+        self._rows_at(row_v, v, shape, hkv)
+        to_q = None
+        if q is None:
+            ref_q = None
+            if q_out is not None:
+                raise ValueError("q and q_out go together")
+        else:
+            shape_q = q.shape
+            if q_out is None or shape_q[0] != B or shape_q[1] != n:
+                raise ValueError("q and q_out go together, and with k")
+            self._rows_at(row_q, q, shape_q, H)
+            if q_out.shape != shape_q or q_out.dtype is not bf16 or not q_out.is_cuda or not q_out.is_contiguous():
+                _check_tensor(q_out, bf16, shape_q)
+            to_q = q_out.data_ptr()
+        if lens is not None:
+            _check_tensor(lens, i32, (B,))
+            lens = lens.data_ptr()
+        if counts is not None:
+            _check_tensor(counts, i32, (B,))
+            counts = counts.data_ptr()
+        if pos is not None:
+            _check_tensor(pos, i32, (B, n))
+            pos = pos.data_ptr()
         cos = sin = None
         if rope is not None:
             cos, sin = rope
-            for t in rope:
-                _check_tensor(t, torch.float32, (t.shape[0], self.heads[2] // 2))
-                if t.shape[0] < ctx_len:
-                    raise ValueError(f"a rope table of {t.shape[0]} rows for a context of {ctx_len}")
-        self._check(self.lib.acache_paged_append(self.h, C.byref(cache), B, ctx_len, at_k, at_v, at_q, _ptr(q_out), n, _ptr(lens), _ptr(pos),
-                                                 _ptr(counts), _ptr(cos), _ptr(sin), _stream()))
+            at = cos.shape
+            if at[0] < ctx_len:
+                raise ValueError(f"a rope table of {at[0]} rows for a context of {ctx_len}")
+            _check_tensor(cos, f32, (at[0], d // 2))
+            _check_tensor(sin, f32, at)
+            cos, sin = cos.data_ptr(), sin.data_ptr()
+        st = self.lib.acache_paged_append(self.h, C.byref(cache), B, ctx_len, ref_k, ref_v, ref_q, to_q, n, lens, pos, counts, cos, sin, _stream())
+        if st:
+            self._check(st)
 
     def paged_attention(self, cache: PagedKV, ctx_len, q, o, lse=None, lens=None, key_drop=None):
         """q, o: bf16 [B, n, H, d]; lse: fp32 [B, n, H]; lens: int32 [B]; key_drop: int32 [B, ceil(ctx_len / 32)] (pack_key_drop)."""
-        import torch
+        bf16, f32, i32 = self.dtypes
         shape = q.shape
         B, n, H, d = shape
         self._cache_fits(cache, B)
         if H != self.heads[0] or d != self.heads[2]:
             raise ValueError(f"q {tuple(shape)} is not [B, n, H, d]")
-        _check_tensor(q, torch.bfloat16, shape)
-        _check_tensor(o, torch.bfloat16, shape)
+        _check_tensor(q, bf16, shape)
+        _check_tensor(o, bf16, shape)
         if lse is not None:
-            _check_tensor(lse, torch.float32, shape[:3])
+            _check_tensor(lse, f32, (B, n, H))
+            lse = lse.data_ptr()
         if lens is not None:
-            _check_tensor(lens, torch.int32, (B,))
+            _check_tensor(lens, i32, (B,))
+            lens = lens.data_ptr()
         if key_drop is not None:
-            _check_tensor(key_drop, torch.int32, (B, -(-ctx_len // 32)))
-        self._check(self.lib.acache_paged_attention(self.h, C.byref(cache), B, n, ctx_len, q.data_ptr(), _ptr(lens), _ptr(key_drop),
-                                                    o.data_ptr(), _ptr(lse), _stream()))
+            _check_tensor(key_drop, i32, (B, -(-ctx_len // 32)))
+            key_drop = key_drop.data_ptr()
+        st = self.lib.acache_paged_attention(self.h, C.byref(cache), B, n, ctx_len, q.data_ptr(), lens, key_drop, o.data_ptr(), lse, _stream())
+        if st:
+            self._check(st)
 
     def recompute_paged(self, w: LayerWeights, req: Request, cache: PagedKV, x, x_is_compact, anchor_idx, k, y, lens=None):
         """The rows of R through the layer, over a cache in pages; lens: int32 [B], the tokens of each request with them."""
@@ -518,18 +560,24 @@ class Context:
     def sample_tokens(self, logits, u, token, prob=None, confidence=None, temperature=None, top_k=None, top_p=None, min_p=None, rows_per_setting=1):
         """logits: bf16 or fp32 [rows, vocab] (rows may lie apart); u: fp32 [rows]; token: int32 [rows]; prob, confidence: fp32 [rows]; temperature,
         top_p, min_p (fp32) and top_k (int32): one for every rows_per_setting rows."""
-        import torch
+        bf16, f32, i32 = self.dtypes
         rows, vocab = logits.shape
-        if logits.dtype not in (torch.bfloat16, torch.float32) or not logits.is_cuda or (vocab > 1 and logits.stride(1) != 1):
-            raise ValueError(f"logits of {logits.dtype} on {logits.device}, strides {logits.stride()}: bf16 or fp32 rows on a GPU are wanted")
-        _check_tensor(token, torch.int32, (rows,))
-        for t in (prob, confidence):
-            if t is not None:
-                _check_tensor(t, torch.float32, (rows,))
+        apart, one = logits.stride()
+        kind = logits.dtype
+        if (kind is not bf16 and kind is not f32) or not logits.is_cuda or (vocab > 1 and one != 1):
+            raise ValueError(f"logits of {kind} on {logits.device}, strides {(apart, one)}: bf16 or fp32 rows on a GPU are wanted")
+        _check_tensor(token, i32, (rows,))
+        if prob is not None:
+            _check_tensor(prob, f32, (rows,))
+            prob = prob.data_ptr()
+        if confidence is not None:
+            _check_tensor(confidence, f32, (rows,))
+            confidence = confidence.data_ptr()
         how = self._sampling(rows, u, temperature, top_k, top_p, min_p, rows_per_setting)
-        self._check(self.lib.acache_sample_tokens(self.h, logits.data_ptr(), 0 if logits.dtype is torch.bfloat16 else 1, rows, vocab,
-                                                  logits.stride(0) if rows > 1 else vocab, how, u.data_ptr(), token.data_ptr(), _ptr(prob),
-                                                  _ptr(confidence), _stream()))
+        st = self.lib.acache_sample_tokens(self.h, logits.data_ptr(), 0 if kind is bf16 else 1, rows, vocab, apart if rows > 1 else vocab, how, u.data_ptr(),
+                                           token.data_ptr(), prob, confidence, _stream())
+        if st:
+            self._check(st)
 
     def predict_sample(self, h, h_rows, block_rows, batch, n_blk, final_norm_g, w_lm, vocab, logits, u, threshold, token, confidence, commit,
                        temperature=None, top_k=None, top_p=None, min_p=None, rows_per_setting=1):
@@ -542,31 +590,34 @@ class Context:
                                                    _ptr(logits), how, _ptr(u), float(threshold), _ptr(token), _ptr(confidence), _ptr(commit),
                                                    _stream()))
 
-    @staticmethod
-    def _sampling(rows, u, temperature, top_k, top_p, min_p, rows_per_setting):
-        import torch
-        _check_tensor(u, torch.float32, (rows,))
-        per = (-(-rows // max(rows_per_setting, 1)),)
-        for t, dtype in ((temperature, torch.float32), (top_p, torch.float32), (min_p, torch.float32), (top_k, torch.int32)):
-            if t is not None:
-                _check_tensor(t, dtype, per)
-        return C.byref(Sampling(_ptr(temperature), _ptr(top_p), _ptr(min_p), _ptr(top_k), rows_per_setting))
+    def _sampling(self, rows, u, temperature, top_k, top_p, min_p, rows_per_setting):
+        bf16, f32, i32 = self.dtypes
+        _check_tensor(u, f32, (rows,))
+        per = (rows,) if rows_per_setting == 1 else (-(-rows // max(rows_per_setting, 1)),)
+        how, ref = self._sampling_arg
+        how.temperature = None if temperature is None else _checked(temperature, f32, per)
+        how.top_p = None if top_p is None else _checked(top_p, f32, per)
+        how.min_p = None if min_p is None else _checked(min_p, f32, per)
+        how.top_k = None if top_k is None else _checked(top_k, i32, per)
+        how.rows_per_setting = rows_per_setting
+        return ref
 
-    def _rows_at(self, t, B, n, heads):
-        """Where rows [B, n, heads, d] lie; the heads of a row side by side."""
-        import torch
-        d = self.heads[2]
-        if t.shape != (B, n, heads, d) or t.dtype is not torch.bfloat16 or not t.is_cuda:
-            raise ValueError(f"rows {tuple(t.shape)} of {t.dtype} on {t.device} are not bf16 [B, n, {heads}, {d}] on a GPU")
+    def _rows_at(self, to, t, shape, heads):
+        """Puts where rows t [B, n, heads, d] lie into a Rows; the heads of a row side by side."""
+        B, n, h, d = shape
         batch, row, head, one = t.stride()
+        if h != heads or d != self.heads[2] or t.dtype is not self.dtypes[0] or not t.is_cuda:
+            raise ValueError(f"rows {tuple(shape)} of {t.dtype} on {t.device} are not bf16 [B, n, {heads}, {self.heads[2]}] on a GPU")
         if (head != d and heads > 1) or one != 1:
             raise ValueError("the heads of a row lie side by side")
-        return C.byref(Rows(t.data_ptr(), batch if B > 1 else 0, row if n > 1 else heads * d))
+        to.p = t.data_ptr()
+        to.batch_stride = batch if B > 1 else 0
+        to.row_stride = row if n > 1 else heads * d
 
     def _cache_fits(self, cache, batch):
         """What a call would read or write past the cache's tensors for (a KV8 filled in by hand is the caller's affair)."""
         m = cache.made_of
-        if m is not None and (m[0] < batch or m[1:] != (self.heads[1], self.heads[2], True)):
+        if m is not None and (m[0] < batch or m[1] != self.heads[1] or m[2] != self.heads[2] or not m[3]):
             raise ValueError(f"a cache of {m[0]} requests, {m[1]} KV heads of {m[2]}, {'not ' if not m[3] else ''}all on a GPU, "
                              f"for {batch} requests and {self.heads[1]} KV heads of {self.heads[2]}")
 
