@@ -3,7 +3,7 @@
 //   k'_i = k_i cos_i - k_{i + d/2} sin_i,   k'_{i + d/2} = k_{i + d/2} cos_i + k_i sin_i   (i < d / 2; the table's row: the token's position)
 //
 // in fp32, rounded once; queries likewise, values as they are.  A CTA takes a row: a thread the same eight pairs of every
-// eighth (fourth, with head dimension 64) head, so that its angles are read once.  What is read depends on nothing but the row's
+// sixteenth (of 64 values, thirty-second) head, so that its angles are read once.  What is read depends on nothing but the row's
 // number and is asked for before the position and the page are known.
 #include "common.cuh"
 #include "kernels.h"
@@ -12,7 +12,10 @@
 namespace acache {
 namespace {
 
-constexpr int kAppendThreads = 256;
+// Threads of a CTA, heads that a thread asks for at once and CTAs of an SM: what is in flight is what counts, until writes of too many rows at a time
+// get in each other's way.  us for 16 x 922 rows by list and for 16 x 2560 rows with 32 heads of queries (floors 74 and 308): 256 threads, 4, no
+// bound 143 and 372; 256, 3, 4 103 and 309; 128, 2, 8 91 and 323; 128, 3, 8 87 and 316; 128, 6, 5 100 and 309; 64, 3, 14 90 and 331.
+constexpr int kAppendThreads = 128, kAppendAhead = 3, kAppendCtas = 8;
 
 struct Pair { uint4 lo, hi; };           // elements c .. c + 7 and d / 2 + c .. of a head
 
@@ -24,10 +27,10 @@ __device__ __forceinline__ uint32_t turn_hi(uint32_t a, uint32_t b, float2 c, fl
 }
 
 template <int D>
-__global__ void __launch_bounds__(kAppendThreads) paged_append_kernel(const PagedAppendArgs a) {
+__global__ void __launch_bounds__(kAppendThreads, kAppendCtas) paged_append_kernel(const PagedAppendArgs a) {
     constexpr int SLOTS = D / 16;        // threads of a head
     constexpr int HEADS = kAppendThreads / SLOTS;
-    constexpr int AHEAD = 4;             // heads of a thread that are asked for at once
+    constexpr int AHEAD = kAppendAhead;
     const int b = blockIdx.y, i = blockIdx.x, tid = threadIdx.x, c = tid % SLOTS * 8, head0 = tid / SLOTS;
     pdl_wait();
     pdl_launch_dependents();
