@@ -15,6 +15,7 @@
 //    them all with one another, where they are few, else by another histogram of their keys.  A search ends at a value; among the tokens that have
 //    it the index decides.
 #include <algorithm>
+#include <type_traits>
 
 #include "kernels.h"
 #include "launch.h"
@@ -26,7 +27,7 @@ namespace {
 
 using u64 = unsigned long long;
 
-constexpr int kThreads = 512, kWarps = kThreads / 32;
+constexpr int kMaxWarps = 16;
 constexpr int kBins = 2048;
 constexpr int kFew = 512;                // tokens of a bin that are compared with one another
 constexpr int kTop = 1024, kList = 2048; // largest top_k whose tokens are sorted; room for them and those that come with them
@@ -41,6 +42,14 @@ __device__ __forceinline__ uint32_t order_key(float f) {     // larger float, la
 }
 __device__ __forceinline__ float value_of(uint32_t key) { return __uint_as_float((key & 0x80000000u) ? key & 0x7FFFFFFFu : ~key); }
 
+// a thread's values
+template <class V, int N>
+struct Few {
+    static constexpr int kSize = N;
+    V at[N];
+    __device__ __forceinline__ V& operator[](int i) { return at[i]; }
+    __device__ __forceinline__ const V& operator[](int i) const { return at[i]; }
+};
 // the same place in another CTA of the cluster
 template <class T>
 __device__ __forceinline__ T* of_peer(T* p, int rank) {
@@ -76,10 +85,10 @@ struct Inbox {
 struct alignas(16) Scratch {
     Inbox box;
     double power[kSteps][kCopies];
-    float f[2][kWarps];
-    double d[kWarps];
-    u64 m[2][kWarps];
-    uint32_t c[kWarps];
+    float f[2][kMaxWarps];
+    double d[kMaxWarps];
+    u64 m[2][kMaxWarps];
+    uint32_t c[kMaxWarps];
     int list_n;
     uint32_t list_lo, list_hi;
     u64 reached[2];
@@ -98,17 +107,15 @@ union Work {                             // one after the other
     } few;
 };
 
-template <class T>
-struct SampleSmem {
-    static constexpr size_t kSorted = kList * sizeof(u64);                   // the sorted list, in the row's place
-    static size_t bytes(int chunk, int cluster) {
-        return sizeof(Work) + sizeof(Scratch) + 2 * (kBins / cluster) * sizeof(Totals) +
-               std::max(kSorted, (chunk + 32) * sizeof(T));
-    }
-};
+// kHold: the row's part stays in shared memory; else it is read again (from L2) for every pass that needs it.
+template <class T, bool kHold>
+size_t sample_smem(int chunk, int cluster) {
+    return sizeof(Work) + sizeof(Scratch) + 2 * (kBins / cluster) * sizeof(Totals) + (kHold ? (chunk + 32) * sizeof(T) : 0);
+}
 
-template <class T>
-__global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a) {
+template <class T, int kThreads, bool kHold>
+__global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const SampleArgs a) {
+    constexpr int kWarps = kThreads / 32, kPer = kFew / kThreads;            // kPer: values a thread sorts, kThreads apart
     extern __shared__ __align__(16) unsigned char smem[];
     const int cluster = a.cluster, row = blockIdx.x / cluster, rank = blockIdx.x % cluster;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -126,7 +133,11 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
         __syncthreads();
     };
     cluster_arrive_relaxed();                                // waited for before the first word to another CTA: it has begun
-    for (int i = tid; i < kSteps * kCopies; i += kThreads) s.power[i / kCopies][i % kCopies] = exp2(-(double)(i / kCopies) / kSteps);
+    if (tid < kSteps) {
+        const double x = exp2(-(double)tid / kSteps);
+#pragma unroll 1
+        for (int i = 0; i < kCopies; ++i) s.power[tid][i] = x;
+    }
     pdl_wait();
     pdl_launch_dependents();
 
@@ -145,7 +156,6 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
     constexpr int VEC = 16 / sizeof(T);
     const int shift = (int)(reinterpret_cast<uintptr_t>(from) % 16 / sizeof(T));     // held[shift + i]: whole pieces of 16 bytes in both places
     const int pieces = (shift + n + VEC - 1) / VEC;          // the first and the last filled up with -inf
-    const T* mine = held + shift;
     float top = -INFINITY, low = INFINITY;
     float conf = 0.f, conf_top = -3.4028234663852886e38f;    // sum of exp(l - conf_top) over this thread's logits, conf_top the largest of them so far
     bool nan = false;
@@ -195,79 +205,102 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
             for (int k = 0; k < VEC; ++k) conf += ex2f((x[k] - conf_top) * kLog2e);
         }
     };
-    // piece i of `held` is thread i % kThreads'
-    {
-        const int whole0 = shift ? 1 : 0, whole1 = (shift + n) / VEC;        // pieces that are all the row's
-        auto partial = [&](int i) {
-            uint4 v;
-            T* w = reinterpret_cast<T*>(&v);
+    // Piece i is thread i % kThreads', here and in every later pass.
+    const int whole0 = shift ? 1 : 0, whole1 = (shift + n) / VEC;            // pieces that are all the row's
+    const uint4* source = reinterpret_cast<const uint4*>(from - shift);      // (aligned; the first piece is not read here where it is not whole)
+    auto partial = [&](int i) {
+        uint4 v;
+        T* w = reinterpret_cast<T*>(&v);
 #pragma unroll
-            for (int k = 0; k < VEC; ++k) {
-                const int e = i * VEC + k - shift;
-                w[k] = e >= 0 && e < n ? from[e] : from_f(-INFINITY);
-            }
+        for (int k = 0; k < VEC; ++k) {
+            const int e = i * VEC + k - shift;
+            w[k] = e >= 0 && e < n ? from[e] : from_f(-INFINITY);
+        }
+        return v;
+    };
+    {
+        auto alone = [&](int i) {
+            uint4 v = partial(i);
             take(v);
-            reinterpret_cast<uint4*>(held)[i] = v;
+            if (kHold) reinterpret_cast<uint4*>(held)[i] = v;
         };
-        if (whole0 && tid == 0) partial(0);
-        if (whole1 < pieces && whole1 >= whole0 && tid == whole1 % kThreads) partial(whole1);
-        const uint4* source = reinterpret_cast<const uint4*>(from - shift);  // (aligned; the first piece is not read here where it is not whole)
+        if (whole0 && tid == 0) alone(0);
+        if (whole1 < pieces && whole1 >= whole0 && tid == whole1 % kThreads) alone(whole1);
         constexpr int AHEAD = 4;
         for (int i0 = tid; i0 < whole1; i0 += AHEAD * kThreads) {
             uint4 v[AHEAD];
 #pragma unroll
             for (int j = 0; j < AHEAD; ++j) {
                 const int i = i0 + j * kThreads;
-                if (i >= whole0 && i < whole1) v[j] = __ldcs(source + i);
+                if (i >= whole0 && i < whole1) v[j] = kHold ? __ldcs(source + i) : __ldcg(source + i);
             }
 #pragma unroll
             for (int j = 0; j < AHEAD; ++j) {
                 const int i = i0 + j * kThreads;
                 if (i < whole0 || i >= whole1) continue;
                 take(v[j]);
-                reinterpret_cast<uint4*>(held)[i] = v[j];
+                if (kHold) reinterpret_cast<uint4*>(held)[i] = v[j];
             }
         }
     }
     if (nan) atomicOr(a.status, kFlagNonFinite);
     // each piece of 16 bytes to f(logits, index of the first)
     auto each = [&](auto&& f) {
+#pragma unroll 1
         for (int i = tid; i < pieces; i += kThreads) {
             float x[VEC];
-            unpack(reinterpret_cast<const uint4*>(held)[i], x);
+            if (kHold) {
+                unpack(reinterpret_cast<const uint4*>(held)[i], x);
+            } else {
+                unpack(i >= whole0 && i < whole1 ? __ldcg(source + i) : partial(i), x);
+                if (nan)
+#pragma unroll
+                    for (int k = 0; k < VEC; ++k) x[k] = x[k] != x[k] ? -INFINITY : x[k];
+            }
             f(x, i * VEC - shift);
         }
     };
-    // a value a thread, the largest to the first thread; room: threads that have one (a power of two, 32 and more)
-    auto sorted = [&](auto v, int room, auto* exchange) {
+    // values kThreads apart, the largest first; room: how many there are (a power of two, 32 and more)
+    auto sort = [&](auto& v, int room, auto* exchange) {
+        constexpr int P = std::remove_reference_t<decltype(v)>::kSize;
 #pragma unroll
-        for (int size = 2; size <= kThreads; size *= 2) {
+        for (int size = 2; size <= kThreads * P; size *= 2) {
             if (size > room) break;
 #pragma unroll
             for (int step = size / 2; step; step /= 2) {
-                decltype(v) other;
-                if (step >= 32) {
+                auto other = v;
+                if (step >= kThreads) {
+#pragma unroll
+                    for (int j = 0; j < P; ++j) other[j] = v[j ^ (step / kThreads)];
+                } else if (step >= 32) {
                     __syncthreads();
-                    exchange[tid] = v;
+#pragma unroll
+                    for (int j = 0; j < P; ++j) exchange[j * kThreads + tid] = v[j];
                     __syncthreads();
-                    other = exchange[tid ^ step];
+#pragma unroll
+                    for (int j = 0; j < P; ++j) other[j] = exchange[j * kThreads + (tid ^ step)];
                 } else {
-                    other = __shfl_xor_sync(0xffffffffu, v, step);
+#pragma unroll
+                    for (int j = 0; j < P; ++j) other[j] = __shfl_xor_sync(0xffffffffu, v[j], step);
                 }
-                const bool larger = ((tid & size) == 0) == ((tid & step) == 0);
-                v = (v > other) == larger ? v : other;
+#pragma unroll
+                for (int j = 0; j < P; ++j) {
+                    const int i = j * kThreads + tid;
+                    const bool larger = ((i & size) == 0) == ((i & step) == 0);
+                    v[j] = (v[j] > other[j]) == larger ? v[j] : other[j];
+                }
             }
         }
-        return v;
     };
     const float own_top = top;
     cluster_wait();
     // A bound that top_k tokens reach at least: the largest logits of that many threads.  Two bounds hold: top_k of one CTA's threads, and a share of top_k in every CTA's.  (Of 31 logits a thread, those of 50 threads of 512: about 53
     // tokens of a CTA are as large; those of 7 threads in each of 8 CTAs, the least of them: 80 of the row.)
     if (quick) {
-        const uint32_t key = sorted(order_key(top), kThreads, work.few.merged);
-        if (tid == top_k - 1) s.f[0][0] = value_of(key);
-        if (tid == (top_k + cluster - 1) / cluster - 1) s.f[0][1] = value_of(key);
+        Few<uint32_t, 1> key{{order_key(top)}};
+        sort(key, kThreads, work.few.merged);
+        if (tid == top_k - 1) s.f[0][0] = value_of(key[0]);
+        if (tid == (top_k + cluster - 1) / cluster - 1) s.f[0][1] = value_of(key[0]);
         __syncthreads();
         if (tid < cluster) {
             of_peer(&box, tid)->bound[rank] = top_k <= kThreads ? s.f[0][0] : -INFINITY;
@@ -416,33 +449,34 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
     // running sums over the cluster of this CTA's bins, counts or weights (the others stay as they are); box.slice: every CTA's whole sum
     auto add_up = [&](int level, bool counts) {
         cluster_sync_all();
-        // a thread four bins of one CTA: the CTAs side by side
-        const int peer = tid & (cluster - 1), i0 = tid / cluster * 4;
-        static_assert(kBins == 4 * kThreads, "all bins of all CTAs at once");
+        // a thread kMine bins of one CTA: the CTAs side by side
+        constexpr int kMine = kBins / kThreads;
+        const int peer = tid & (cluster - 1), i0 = tid / cluster * kMine;
         const Hist* h = of_peer(&hist, peer);
-        auto four = [&](int p) { return *reinterpret_cast<const uint4*>(h->part[p] + rank * slice + i0); };
-        u64 m[4];
-        {
+        u64 m[kMine];
+#pragma unroll
+        for (int q = 0; q < kMine; q += 4) {
+            auto four = [&](int p) { return *reinterpret_cast<const uint4*>(h->part[p] + rank * slice + i0 + q); };
             const uint4 x = four(0);
-            m[0] = x.x; m[1] = x.y; m[2] = x.z; m[3] = x.w;
+            m[q] = x.x; m[q + 1] = x.y; m[q + 2] = x.z; m[q + 3] = x.w;
             if (!counts) {
                 const uint4 y = four(1), z = four(2);
-                m[0] += ((u64)y.x << 16) + ((u64)z.x << 32); m[1] += ((u64)y.y << 16) + ((u64)z.y << 32);
-                m[2] += ((u64)y.z << 16) + ((u64)z.z << 32); m[3] += ((u64)y.w << 16) + ((u64)z.w << 32);
+                m[q] += ((u64)y.x << 16) + ((u64)z.x << 32); m[q + 1] += ((u64)y.y << 16) + ((u64)z.y << 32);
+                m[q + 2] += ((u64)y.z << 16) + ((u64)z.z << 32); m[q + 3] += ((u64)y.w << 16) + ((u64)z.w << 32);
             }
         }
         for (int off = 1; off < cluster; off <<= 1)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) m[j] += __shfl_xor_sync(0xffffffffu, m[j], off);
+            for (int j = 0; j < kMine; ++j) m[j] += __shfl_xor_sync(0xffffffffu, m[j], off);
 #pragma unroll
-        for (int j = 1; j < 4; ++j) m[j] += m[j - 1];
-        const u64 run = running(peer == 0 ? m[3] : 0ull);
+        for (int j = 1; j < kMine; ++j) m[j] += m[j - 1];
+        const u64 run = running(peer == 0 ? m[kMine - 1] : 0ull);
         Totals* of = totals + level * slice + i0;
         if (peer == 0) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                if (counts) of[j].count = (uint32_t)(run - m[3] + m[j]);
-                else of[j].mass = run - m[3] + m[j];
+            for (int j = 0; j < kMine; ++j) {
+                if (counts) of[j].count = (uint32_t)(run - m[kMine - 1] + m[j]);
+                else of[j].mass = run - m[kMine - 1] + m[j];
             }
         }
         if (warp == kWarps - 1) {
@@ -546,19 +580,32 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
                     merged[first + i] = work.few.key[turn][r_of * room_of + i];
                 __syncthreads();
                 turn ^= 1;
-                static_assert(kFew == kThreads, "a thread has a key");
                 int room = 32;
                 while (room < all) room *= 2;
-                const uint32_t key = sorted(tid < all ? merged[tid] : 0u, room, work.few.own);
-                const u64 w = tid < all ? weight(value_of(key)) : 0ull;
-                const u64 run = running(w) + mass;           // with this key
-                const u64 before = by_count ? (u64)(count + tid) : run - w, upto = by_count ? (u64)(count + tid + 1) : run;
-                __syncthreads();
-                work.few.upto[tid] = run;
-                if (tid < all && before < target && target <= upto) s.list_lo = key;
+                Few<uint32_t, kPer> key;
+#pragma unroll
+                for (int j = 0; j < kPer; ++j) key[j] = j * kThreads + tid < all ? merged[j * kThreads + tid] : 0u;
+                sort(key, room, work.few.own);
+                u64 run = mass;
+#pragma unroll
+                for (int j = 0; j < kPer; ++j) {
+                    const int i = j * kThreads + tid;
+                    const u64 w = i < all ? weight(value_of(key[j])) : 0ull;
+                    const u64 with = running(w) + run;
+                    const u64 before = by_count ? (u64)(count + i) : with - w, upto = by_count ? (u64)(count + i + 1) : with;
+                    work.few.upto[i] = with;
+                    if (i < all && before < target && target <= upto) s.list_lo = key[j];
+                    for (int v = 0; j + 1 < kPer && v < kWarps; ++v) run += s.m[0][v];
+                }
                 __syncthreads();
                 const uint32_t found = s.list_lo;
-                const int larger = __syncthreads_count(tid < all && key > found), equal = __syncthreads_count(tid < all && key == found);
+                int larger = 0, equal = 0;
+#pragma unroll
+                for (int j = 0; j < kPer; ++j) {
+                    const bool one = j * kThreads + tid < all;
+                    larger += __syncthreads_count(one && key[j] > found);
+                    equal += __syncthreads_count(one && key[j] == found);
+                }
                 return Found{found, (uint32_t)equal, count + larger, weight(value_of(found)), larger ? work.few.upto[larger - 1] : mass};
             }
             // too many: a histogram of their keys, the largest first
@@ -660,76 +707,72 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
         if (longest > room_of) continue;
         if (rank != 0) return;                               // nobody writes to its memory, or reads there, any more
         const double total = total_of();
-        u64* list = reinterpret_cast<u64*>(held);
-        {
-            const int r_of = warp % cluster;
-            int first = 0;
-            for (int r = 0; r < r_of; ++r) first += box.n[attempt][r];
-            for (int i = warp / cluster * 32 + lane; i < box.n[attempt][r_of]; i += kWarps / cluster * 32) list[first + i] = work.top[r_of * room_of + i];
-        }
-        __syncthreads();
-        u64 w[kList / kThreads], word[kList / kThreads];
-        constexpr int PER = kList / kThreads;
-        int per = 1;
-        if (all <= kThreads) {
+        // sorted, kThreads apart
+        constexpr int kMost = kList / kThreads;
+        Few<u64, kMost> word;
+        int per = kPer;
+        if (all <= kFew) {
+            Few<u64, kPer> some;
+#pragma unroll
+            for (int j = 0; j < kPer; ++j) {
+                int i = j * kThreads + tid, r = 0;
+                while (r < cluster && i >= box.n[attempt][r]) i -= box.n[attempt][r++];
+                some[j] = r < cluster ? work.top[r * room_of + i] : 0ull;
+            }
             int room = 32;
             while (room < all) room *= 2;
-            word[0] = sorted(tid < all ? list[tid] : 0ull, room, work.top);
+            sort(some, room, work.top);
+#pragma unroll
+            for (int j = 0; j < kPer; ++j) word[j] = some[j];
         } else {
-            int room = kThreads;
-            while (room < all) room *= 2;
-            per = room / kThreads;
-            for (int i = all + tid; i < room; i += kThreads) list[i] = 0ull;
-            for (int size = 2; size <= room; size *= 2)
+            per = kMost;
+            for (int i = tid; i < kList; i += kThreads)
+                if (i % room_of >= box.n[attempt][i / room_of]) work.top[i] = 0ull;
+#pragma unroll 1
+            for (int size = 2; size <= kList; size *= 2)
+#pragma unroll 1
                 for (int step = size / 2; step; step /= 2) {
                     __syncthreads();
-                    for (int i = tid; i < room / 2; i += kThreads) {
+                    for (int i = tid; i < kList / 2; i += kThreads) {
                         const int x = 2 * i - (i & (step - 1)), y = x + step;
-                        const u64 u = list[x], v = list[y];
-                        if ((u < v) == ((x & size) == 0)) { list[x] = v; list[y] = u; }      // the largest first
+                        const u64 u = work.top[x], v = work.top[y];
+                        if ((u < v) == ((x & size) == 0)) { work.top[x] = v; work.top[y] = u; }      // the largest first
                     }
                 }
             __syncthreads();
 #pragma unroll
-            for (int j = 0; j < PER; ++j)
-                if (j < per) word[j] = list[tid * per + j];
+            for (int j = 0; j < kMost; ++j) word[j] = work.top[j * kThreads + tid];
         }
-        // running sums of the weights of the first top_k
-        u64 sum = 0ull;
+        // running sums of the weights of the first top_k: upto, with this token
+        u64 w[kMost], upto[kMost], kept = 0ull;
 #pragma unroll
-        for (int j = 0; j < PER; ++j) {
-            w[j] = 0ull;
-            if (j < per && tid * per + j < min(top_k, all)) {
+        for (int j = 0; j < kMost; ++j) {
+            w[j] = upto[j] = 0ull;
+            if (j >= per) continue;
+            if (j * kThreads + tid < min(top_k, all)) {
                 const float l = value_of((uint32_t)(word[j] >> 32));
                 if (behind(l) <= reach) w[j] = weight(l);
             }
-            sum += w[j];
+            upto[j] = running(w[j]) + kept;
+            for (int v = 0; v < kWarps; ++v) kept += s.m[0][v];
         }
-        const u64 run = running(sum) - sum;
-        u64 kept = 0ull;
-        for (int v = 0; v < kWarps; ++v) kept += s.m[0][v];
         // the sum at the first token where it comes to what top_p keeps; [1]: before the first that min_p does not leave
         const u64 enough = top_p < 1.f ? enough_of(kept) : kept;
         if (tid == 0) s.reached[1] = kept;
         __syncthreads();
-        u64 r0 = run;
 #pragma unroll
-        for (int j = 0; j < PER; ++j) {
-            const u64 r1 = r0 + w[j];
-            if (r0 < enough && enough <= r1) s.reached[0] = r1;
-            if (r0 < r1 && w[j] < least) atomicMin(&s.reached[1], r0);
-            r0 = r1;
+        for (int j = 0; j < kMost; ++j) {
+            if (w[j] == 0ull) continue;
+            if (upto[j] - w[j] < enough && enough <= upto[j]) s.reached[0] = upto[j];
+            if (w[j] < least) atomicMin(&s.reached[1], upto[j] - w[j]);
         }
         __syncthreads();
         kept = min(s.reached[0], s.reached[1]);
         const u64 target = drawn_of(kept) + 1ull;
-        r0 = run;
 #pragma unroll
-        for (int j = 0; j < PER; ++j) {
-            const u64 r1 = r0 + w[j];
-            if (r0 < target && target <= r1) give((int)~(uint32_t)word[j], value_of((uint32_t)(word[j] >> 32)), (double)w[j] / (double)kept, total);
-            r0 = r1;
-        }
+        for (int j = 0; j < kMost; ++j)
+            if (w[j] != 0ull && upto[j] - w[j] < target && target <= upto[j])
+                give((int)~(uint32_t)word[j], value_of((uint32_t)(word[j] >> 32)), (double)w[j] / (double)kept, total);
         return;
     }
     if (sampled && top_k <= kTop) clear();                   // the list was too long
@@ -785,7 +828,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
 
     // ---- among the tokens of the value, the one with that many before it ----
     const int seg = (n + kThreads - 1) / kThreads * 32, j0 = min(warp * seg, n), j1 = min(j0 + seg, n);
-    auto has_it = [&](int i) { return order_key(to_f(mine[i])) == token_key; };
+    auto has_it = [&](int i) { return order_key(to_f(kHold ? held[shift + i] : from[i])) == token_key; };      // (NaN has a key that nothing else has)
     uint32_t equal = 0u;
     for (int i = j0 + lane; i < j1; i += 32) equal += has_it(i);
     equal = __reduce_add_sync(0xffffffffu, equal);
@@ -811,23 +854,21 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
     }
 }
 
-template <class T>
-int sample_launch(SampleArgs a, cudaStream_t stream) {
-    static PerDevice<int> ready;
+template <class T, int kThreads, bool kHold>
+int sample_launch(SampleArgs a, int most, cudaStream_t stream) {
+    static PerDevice<bool> ready;
     int device = 0;
     cudaGetDevice(&device);
-    const int most = ready.of(device, [](int& bytes) {
-        int optin = 0, dev = 0;
-        cudaGetDevice(&dev);
-        cudaDeviceGetAttribute(&optin, cudaDevAttrMaxSharedMemoryPerBlockOptin, dev);
-        bytes = cudaFuncSetAttribute(sample_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, optin) == cudaSuccess ? optin : 0;
-    });
-    if (most == 0) return -1;
+    if (!ready.of(device, [](bool& ok) {
+            int optin = 0, dev = 0;
+            cudaGetDevice(&dev);
+            cudaDeviceGetAttribute(&optin, cudaDevAttrMaxSharedMemoryPerBlockOptin, dev);
+            ok = cudaFuncSetAttribute(sample_kernel<T, kThreads, kHold>, cudaFuncAttributeMaxDynamicSharedMemorySize, optin) == cudaSuccess;
+        }))
+        return -1;
     auto chunk_of = [&](int c) { return ((a.vocab + c - 1) / c + 63) / 64 * 64; };
     int c = 1;
-    // Logits of a CTA: so many that two CTAs have room in an SM; fewer for few rows, for which the time of one row counts.
-    const int many = sizeof(T) == 2 && (int64_t)a.rows * kMaxCluster > 2 * 2 * 148 ? 32768 : 16384;
-    while (c < kMaxCluster && chunk_of(c) > many) c *= 2;
+    while (c < kMaxCluster && chunk_of(c) > most) c *= 2;
     a.cluster = c;
     a.chunk = chunk_of(c);
     a.shift = 46;
@@ -835,9 +876,8 @@ int sample_launch(SampleArgs a, cudaStream_t stream) {
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3(a.rows * c);
     cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = SampleSmem<T>::bytes(a.chunk, c);
+    cfg.dynamicSmemBytes = sample_smem<T, kHold>(a.chunk, c);
     cfg.stream = stream;
-    if (cfg.dynamicSmemBytes > (size_t)most) return -1;
     cudaLaunchAttribute at[2];
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at[0].val.programmaticStreamSerializationAllowed = 1;
@@ -845,14 +885,21 @@ int sample_launch(SampleArgs a, cudaStream_t stream) {
     at[1].val.clusterDim.x = c; at[1].val.clusterDim.y = 1; at[1].val.clusterDim.z = 1;
     cfg.attrs = at;
     cfg.numAttrs = 2;
-    return cudaLaunchKernelEx(&cfg, sample_kernel<T>, a) == cudaSuccess ? 1 : -1;
+    return cudaLaunchKernelEx(&cfg, sample_kernel<T, kThreads, kHold>, a) == cudaSuccess ? 1 : -1;
+}
+template <class T>
+int sample_dispatch(const SampleArgs& a, cudaStream_t stream) {
+    constexpr int kMost = 16384;                             // logits of a CTA
+    const int64_t ctas = (int64_t)a.rows * std::min<int64_t>(kMaxCluster, (a.vocab + kMost - 1) / kMost);
+    if (ctas > 2 * 148) return sample_launch<T, 256, false>(a, kMost, stream);
+    return sample_launch<T, 512, true>(a, kMost, stream);
 }
 
 }  // namespace
 
 int launch_sample(const SampleArgs& a, cudaStream_t stream) {
     if (a.rows == 0) return 0;
-    return a.bf16 ? sample_launch<__nv_bfloat16>(a, stream) : sample_launch<float>(a, stream);
+    return a.bf16 ? sample_dispatch<__nv_bfloat16>(a, stream) : sample_dispatch<float>(a, stream);
 }
 
 }  // namespace acache
