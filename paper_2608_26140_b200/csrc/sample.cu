@@ -15,7 +15,6 @@
 //    them all with one another, where they are few, else by another histogram of their keys.  A search ends at a value; among the tokens that have
 //    it the index decides.
 #include <algorithm>
-#include <type_traits>
 
 #include "kernels.h"
 #include "launch.h"
@@ -27,7 +26,7 @@ namespace {
 
 using u64 = unsigned long long;
 
-constexpr int kMaxWarps = 16;
+constexpr int kThreads = 512, kWarps = kThreads / 32;
 constexpr int kBins = 2048;
 constexpr int kFew = 512;                // tokens of a bin that are compared with one another
 constexpr int kTop = 1024, kList = 2048; // largest top_k whose tokens are sorted; room for them and those that come with them
@@ -42,14 +41,6 @@ __device__ __forceinline__ uint32_t order_key(float f) {     // larger float, la
 }
 __device__ __forceinline__ float value_of(uint32_t key) { return __uint_as_float((key & 0x80000000u) ? key & 0x7FFFFFFFu : ~key); }
 
-// a thread's values
-template <class V, int N>
-struct Few {
-    static constexpr int kSize = N;
-    V at[N];
-    __device__ __forceinline__ V& operator[](int i) { return at[i]; }
-    __device__ __forceinline__ const V& operator[](int i) const { return at[i]; }
-};
 // the same place in another CTA of the cluster
 template <class T>
 __device__ __forceinline__ T* of_peer(T* p, int rank) {
@@ -85,10 +76,10 @@ struct Inbox {
 struct alignas(16) Scratch {
     Inbox box;
     double power[kSteps][kCopies];
-    float f[2][kMaxWarps];
-    double d[kMaxWarps];
-    u64 m[2][kMaxWarps];
-    uint32_t c[kMaxWarps];
+    float f[2][kWarps];
+    double d[kWarps];
+    u64 m[2][kWarps];
+    uint32_t c[kWarps];
     int list_n;
     uint32_t list_lo, list_hi;
     u64 reached[2];
@@ -113,9 +104,8 @@ size_t sample_smem(int chunk, int cluster) {
     return sizeof(Work) + sizeof(Scratch) + 2 * (kBins / cluster) * sizeof(Totals) + (kHold ? (chunk + 32) * sizeof(T) : 0);
 }
 
-template <class T, int kThreads, bool kHold>
-__global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const SampleArgs a) {
-    constexpr int kWarps = kThreads / 32, kPer = kFew / kThreads;            // kPer: values a thread sorts, kThreads apart
+template <class T, bool kHold>
+__global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a) {
     extern __shared__ __align__(16) unsigned char smem[];
     const int cluster = a.cluster, row = blockIdx.x / cluster, rank = blockIdx.x % cluster;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -174,8 +164,10 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
         asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(x));
         return e;
     };
+    int top_piece = 0;                                       // where `top` is, and the largest logit of this thread's other pieces
+    float next_top = -INFINITY;
     // a piece as it came: NaN out, its share of largest, smallest and sum
-    auto take = [&](uint4& v) {
+    auto take = [&](uint4& v, int i) {
         float x[VEC], high = -INFINITY;
         unpack(v, x);
         bool odd = false;
@@ -195,7 +187,11 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
             high = fmaxf(high, x[k]);
             low = fminf(low, x[k] > -INFINITY ? x[k] : INFINITY);
         }
-        top = fmaxf(top, high);
+        next_top = fmaxf(next_top, fminf(top, high));
+        if (high > top) {
+            top = high;
+            top_piece = i;
+        }
         if (a.confidence) {
             if (high > conf_top) {
                 conf *= ex2f((conf_top - high) * kLog2e);
@@ -221,7 +217,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
     {
         auto alone = [&](int i) {
             uint4 v = partial(i);
-            take(v);
+            take(v, i);
             if (kHold) reinterpret_cast<uint4*>(held)[i] = v;
         };
         if (whole0 && tid == 0) alone(0);
@@ -238,69 +234,59 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
             for (int j = 0; j < AHEAD; ++j) {
                 const int i = i0 + j * kThreads;
                 if (i < whole0 || i >= whole1) continue;
-                take(v[j]);
+                take(v[j], i);
                 if (kHold) reinterpret_cast<uint4*>(held)[i] = v[j];
             }
         }
     }
     if (nan) atomicOr(a.status, kFlagNonFinite);
-    // each piece of 16 bytes to f(logits, index of the first)
+    // a piece to f(logits, index of the first)
+    auto one = [&](int i, auto&& f) {
+        float x[VEC];
+        if (kHold) {
+            unpack(reinterpret_cast<const uint4*>(held)[i], x);
+        } else {
+            unpack(i >= whole0 && i < whole1 ? __ldcg(source + i) : partial(i), x);
+            if (nan)
+#pragma unroll
+                for (int k = 0; k < VEC; ++k) x[k] = x[k] != x[k] ? -INFINITY : x[k];
+        }
+        f(x, i * VEC - shift);
+    };
     auto each = [&](auto&& f) {
 #pragma unroll 1
-        for (int i = tid; i < pieces; i += kThreads) {
-            float x[VEC];
-            if (kHold) {
-                unpack(reinterpret_cast<const uint4*>(held)[i], x);
-            } else {
-                unpack(i >= whole0 && i < whole1 ? __ldcg(source + i) : partial(i), x);
-                if (nan)
-#pragma unroll
-                    for (int k = 0; k < VEC; ++k) x[k] = x[k] != x[k] ? -INFINITY : x[k];
-            }
-            f(x, i * VEC - shift);
-        }
+        for (int i = tid; i < pieces; i += kThreads) one(i, f);
     };
-    // values kThreads apart, the largest first; room: how many there are (a power of two, 32 and more)
-    auto sort = [&](auto& v, int room, auto* exchange) {
-        constexpr int P = std::remove_reference_t<decltype(v)>::kSize;
+    // a value a thread, the largest to the first thread; room: threads that have one (a power of two, 32 and more)
+    auto sorted = [&](auto v, int room, auto* exchange) {
 #pragma unroll
-        for (int size = 2; size <= kThreads * P; size *= 2) {
+        for (int size = 2; size <= kThreads; size *= 2) {
             if (size > room) break;
 #pragma unroll
             for (int step = size / 2; step; step /= 2) {
-                auto other = v;
-                if (step >= kThreads) {
-#pragma unroll
-                    for (int j = 0; j < P; ++j) other[j] = v[j ^ (step / kThreads)];
-                } else if (step >= 32) {
+                decltype(v) other;
+                if (step >= 32) {
                     __syncthreads();
-#pragma unroll
-                    for (int j = 0; j < P; ++j) exchange[j * kThreads + tid] = v[j];
+                    exchange[tid] = v;
                     __syncthreads();
-#pragma unroll
-                    for (int j = 0; j < P; ++j) other[j] = exchange[j * kThreads + (tid ^ step)];
+                    other = exchange[tid ^ step];
                 } else {
-#pragma unroll
-                    for (int j = 0; j < P; ++j) other[j] = __shfl_xor_sync(0xffffffffu, v[j], step);
+                    other = __shfl_xor_sync(0xffffffffu, v, step);
                 }
-#pragma unroll
-                for (int j = 0; j < P; ++j) {
-                    const int i = j * kThreads + tid;
-                    const bool larger = ((i & size) == 0) == ((i & step) == 0);
-                    v[j] = (v[j] > other[j]) == larger ? v[j] : other[j];
-                }
+                const bool larger = ((tid & size) == 0) == ((tid & step) == 0);
+                v = (v > other) == larger ? v : other;
             }
         }
+        return v;
     };
     const float own_top = top;
     cluster_wait();
     // A bound that top_k tokens reach at least: the largest logits of that many threads.  Two bounds hold: top_k of one CTA's threads, and a share of top_k in every CTA's.  (Of 31 logits a thread, those of 50 threads of 512: about 53
     // tokens of a CTA are as large; those of 7 threads in each of 8 CTAs, the least of them: 80 of the row.)
     if (quick) {
-        Few<uint32_t, 1> key{{order_key(top)}};
-        sort(key, kThreads, work.few.merged);
-        if (tid == top_k - 1) s.f[0][0] = value_of(key[0]);
-        if (tid == (top_k + cluster - 1) / cluster - 1) s.f[0][1] = value_of(key[0]);
+        const uint32_t key = sorted(order_key(top), kThreads, work.few.merged);
+        if (tid == top_k - 1) s.f[0][0] = value_of(key);
+        if (tid == (top_k + cluster - 1) / cluster - 1) s.f[0][1] = value_of(key);
         __syncthreads();
         if (tid < cluster) {
             of_peer(&box, tid)->bound[rank] = top_k <= kThreads ? s.f[0][0] : -INFINITY;
@@ -582,30 +568,16 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
                 turn ^= 1;
                 int room = 32;
                 while (room < all) room *= 2;
-                Few<uint32_t, kPer> key;
-#pragma unroll
-                for (int j = 0; j < kPer; ++j) key[j] = j * kThreads + tid < all ? merged[j * kThreads + tid] : 0u;
-                sort(key, room, work.few.own);
-                u64 run = mass;
-#pragma unroll
-                for (int j = 0; j < kPer; ++j) {
-                    const int i = j * kThreads + tid;
-                    const u64 w = i < all ? weight(value_of(key[j])) : 0ull;
-                    const u64 with = running(w) + run;
-                    const u64 before = by_count ? (u64)(count + i) : with - w, upto = by_count ? (u64)(count + i + 1) : with;
-                    work.few.upto[i] = with;
-                    if (i < all && before < target && target <= upto) s.list_lo = key[j];
-                    for (int v = 0; j + 1 < kPer && v < kWarps; ++v) run += s.m[0][v];
-                }
+                static_assert(kFew == kThreads, "a thread has a key");
+                const uint32_t key = sorted(tid < all ? merged[tid] : 0u, room, work.few.own);
+                const u64 w = tid < all ? weight(value_of(key)) : 0ull;
+                const u64 run = running(w) + mass;           // with this key
+                const u64 before = by_count ? (u64)(count + tid) : run - w, upto = by_count ? (u64)(count + tid + 1) : run;
+                work.few.upto[tid] = run;
+                if (tid < all && before < target && target <= upto) s.list_lo = key;
                 __syncthreads();
                 const uint32_t found = s.list_lo;
-                int larger = 0, equal = 0;
-#pragma unroll
-                for (int j = 0; j < kPer; ++j) {
-                    const bool one = j * kThreads + tid < all;
-                    larger += __syncthreads_count(one && key[j] > found);
-                    equal += __syncthreads_count(one && key[j] == found);
-                }
+                const int larger = __syncthreads_count(tid < all && key > found), equal = __syncthreads_count(tid < all && key == found);
                 return Found{found, (uint32_t)equal, count + larger, weight(value_of(found)), larger ? work.few.upto[larger - 1] : mass};
             }
             // too many: a histogram of their keys, the largest first
@@ -688,14 +660,19 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
             const int slot = atomicAdd(&s.list_n, 1);
             if (slot < room_of) to[slot] = (u64)order_key(l) << 32 | ~(uint32_t)(e0 + i);
         };
-        if (attempt == 1 || own_top >= bound)                // (a thread has the same pieces as when they came)
-            each([&](const float (&x)[VEC], int i0) {
+        if (attempt == 1 || own_top >= bound) {
+            // (few threads have a token that reaches the bound, and those in one of their pieces, as a rule)
+            const bool whole_share = attempt == 1 || next_top >= bound;
+#pragma unroll 1
+            for (int i = whole_share ? tid : top_piece; i < pieces; i += whole_share ? kThreads : pieces)
+                one(i, [&](const float (&x)[VEC], int i0) {
 #pragma unroll
-                for (int j = 0; j < VEC; ++j) {
-                    const float d = behind(x[j]);
-                    if (attempt == 0 ? x[j] >= bound && x[j] > -INFINITY : d <= reach && bin_of(d) <= bin) put(x[j], i0 + j);
-                }
-            });
+                    for (int j = 0; j < VEC; ++j) {
+                        const float d = behind(x[j]);
+                        if (attempt == 0 ? x[j] >= bound && x[j] > -INFINITY : d <= reach && bin_of(d) <= bin) put(x[j], i0 + j);
+                    }
+                });
+        }
         __syncthreads();
         if (tid < cluster) of_peer(&box, tid)->n[attempt][rank] = s.list_n;
         cluster_sync_all();
@@ -709,21 +686,14 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
         const double total = total_of();
         // sorted, kThreads apart
         constexpr int kMost = kList / kThreads;
-        Few<u64, kMost> word;
-        int per = kPer;
-        if (all <= kFew) {
-            Few<u64, kPer> some;
-#pragma unroll
-            for (int j = 0; j < kPer; ++j) {
-                int i = j * kThreads + tid, r = 0;
-                while (r < cluster && i >= box.n[attempt][r]) i -= box.n[attempt][r++];
-                some[j] = r < cluster ? work.top[r * room_of + i] : 0ull;
-            }
+        u64 word[kMost];
+        int per = 1;
+        if (all <= kThreads) {
+            int i = tid, r = 0;
+            while (r < cluster && i >= box.n[attempt][r]) i -= box.n[attempt][r++];
             int room = 32;
             while (room < all) room *= 2;
-            sort(some, room, work.top);
-#pragma unroll
-            for (int j = 0; j < kPer; ++j) word[j] = some[j];
+            word[0] = sorted(r < cluster ? work.top[r * room_of + i] : 0ull, room, work.top);
         } else {
             per = kMost;
             for (int i = tid; i < kList; i += kThreads)
@@ -854,7 +824,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
     }
 }
 
-template <class T, int kThreads, bool kHold>
+template <class T, bool kHold>
 int sample_launch(SampleArgs a, int most, cudaStream_t stream) {
     static PerDevice<bool> ready;
     int device = 0;
@@ -863,7 +833,7 @@ int sample_launch(SampleArgs a, int most, cudaStream_t stream) {
             int optin = 0, dev = 0;
             cudaGetDevice(&dev);
             cudaDeviceGetAttribute(&optin, cudaDevAttrMaxSharedMemoryPerBlockOptin, dev);
-            ok = cudaFuncSetAttribute(sample_kernel<T, kThreads, kHold>, cudaFuncAttributeMaxDynamicSharedMemorySize, optin) == cudaSuccess;
+            ok = cudaFuncSetAttribute(sample_kernel<T, kHold>, cudaFuncAttributeMaxDynamicSharedMemorySize, optin) == cudaSuccess;
         }))
         return -1;
     auto chunk_of = [&](int c) { return ((a.vocab + c - 1) / c + 63) / 64 * 64; };
@@ -885,14 +855,17 @@ int sample_launch(SampleArgs a, int most, cudaStream_t stream) {
     at[1].val.clusterDim.x = c; at[1].val.clusterDim.y = 1; at[1].val.clusterDim.z = 1;
     cfg.attrs = at;
     cfg.numAttrs = 2;
-    return cudaLaunchKernelEx(&cfg, sample_kernel<T, kThreads, kHold>, a) == cudaSuccess ? 1 : -1;
+    return cudaLaunchKernelEx(&cfg, sample_kernel<T, kHold>, a) == cudaSuccess ? 1 : -1;
 }
+// Logits of a CTA: up to 16384 for few rows, for which the time of one row counts; twice as many once their CTAs take more than a round, as
+// what a step costs by itself is then spread over more of them (512 rows of 126464 bf16 310 and 240 us).  So many fp32 logits would leave
+// room for one CTA in an SM, and are read again from L2 (512 rows 281 us; held, in halves, 335; 40 rows 82 where held bf16 ones take 68).
 template <class T>
 int sample_dispatch(const SampleArgs& a, cudaStream_t stream) {
-    constexpr int kMost = 16384;                             // logits of a CTA
+    constexpr int kMost = 16384;
     const int64_t ctas = (int64_t)a.rows * std::min<int64_t>(kMaxCluster, (a.vocab + kMost - 1) / kMost);
-    if (ctas > 2 * 148) return sample_launch<T, 256, false>(a, kMost, stream);
-    return sample_launch<T, 512, true>(a, kMost, stream);
+    if (ctas <= 2 * 148) return sample_launch<T, true>(a, kMost, stream);
+    return sample_launch<T, sizeof(T) == 2>(a, 2 * kMost, stream);
 }
 
 }  // namespace
