@@ -510,10 +510,17 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
             if (tid == 0) { s.list_n = 0; s.list_lo = 0xffffffffu; s.list_hi = 0u; }
             __syncthreads();
             const int bin = at_bin.bin;
+            // Logits of the bin lie less than a bin from its middle, whatever was rounded: the others are sorted out by two comparisons.
+            float from_l = -INFINITY, to_l = INFINITY;
+            if (!keys && bins_per < 1e30f && top < INFINITY) {
+                from_l = __double2float_rd((double)top - 2.0 * (bin + 1) / (double)bins_per);
+                to_l = __double2float_ru((double)top - 2.0 * (bin - 1) / (double)bins_per);
+            }
             uint32_t k_lo = 0xffffffffu, k_hi = 0u;
             each([&](const float (&x)[VEC], int) {
 #pragma unroll
                 for (int k = 0; k < VEC; ++k) {
+                    if (!(x[k] >= from_l && x[k] <= to_l)) continue;
                     const float d = behind(x[k]);
                     const uint32_t key = order_key(x[k]);
                     if (d <= reach && (keys ? key >= lo && key <= hi : bin_of(d) == bin)) {
@@ -797,31 +804,46 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
     }
 
     // ---- among the tokens of the value, the one with that many before it ----
-    const int seg = (n + kThreads - 1) / kThreads * 32, j0 = min(warp * seg, n), j1 = min(j0 + seg, n);
-    auto has_it = [&](int i) { return order_key(to_f(kHold ? held[shift + i] : from[i])) == token_key; };      // (NaN has a key that nothing else has)
-    uint32_t equal = 0u;
-    for (int i = j0 + lane; i < j1; i += 32) equal += has_it(i);
-    equal = __reduce_add_sync(0xffffffffu, equal);
+    // how many a warp's pieces have, round by round, which is the order of their indices
+    const float value = value_of(token_key);
+    uint32_t* count_of = work.few.own;                       // [round][warp]
+    const int rounds = (pieces + kThreads - 1) / kThreads;
+    auto has = [&](int i) {                                  // tokens of piece i, a bit each
+        uint32_t bits = 0u;
+        if (i < pieces && own_top >= value) one(i, [&](const float (&x)[VEC], int) {
+#pragma unroll
+            for (int k = 0; k < VEC; ++k) bits |= x[k] == value && x[k] > -INFINITY ? 1u << k : 0u;
+        });
+        return bits;
+    };
     __syncthreads();
-    if (lane == 0) s.c[warp] = equal;
-    __syncthreads();
-    if (tid < cluster) {
-        uint32_t all = 0u;
-        for (int w = 0; w < kWarps; ++w) all += s.c[w];
-        of_peer(&box, tid)->equal[rank] = all;
+    uint32_t here = 0u;
+#pragma unroll 1
+    for (int j = 0; j < rounds; ++j) {
+        const uint32_t c = __reduce_add_sync(0xffffffffu, __popc(has(j * kThreads + tid)));
+        if (lane == 0) count_of[j * kWarps + warp] = c;
+        here += c;
     }
+    here = cta_sum(lane == 0 ? here : 0u, s.c);
+    if (tid < cluster) of_peer(&box, tid)->equal[rank] = here;
     cluster_sync_all();
     if (greedy) total = total_of();
     u64 before = cluster_sum(box.equal, rank);
-    for (int w = 0; w < warp; ++w) before += s.c[w];
-    if (before <= token_at && token_at < before + equal) {   // one warp of the cluster
-        for (int i = j0; i < j1; i += 32) {
-            const bool eq = i + lane < j1 && has_it(i + lane);
-            const uint32_t eqs = __ballot_sync(0xffffffffu, eq);
-            if (eq && before + __popc(eqs & ((1u << lane) - 1u)) == token_at) give(e0 + i + lane, value_of(token_key), prob, total);
-            before += __popc(eqs);
-        }
+    if (token_at < before || token_at >= before + box.equal[rank]) return;
+    int group = 0;                                           // the round and warp that have it
+    for (; before + count_of[group] <= token_at; ++group) before += count_of[group];
+    if (group % kWarps != warp) return;
+    const int i = group / kWarps * kThreads + tid;
+    uint32_t bits = has(i), upto = __popc(bits);
+#pragma unroll
+    for (int off = 1; off < 32; off <<= 1) {
+        const uint32_t x = __shfl_up_sync(0xffffffffu, upto, off);
+        if (lane >= off) upto += x;
     }
+    const int nth = (int)(token_at - before) - (int)(upto - __popc(bits));      // of this lane's
+    if (nth < 0 || nth >= __popc(bits)) return;
+    for (int k = 0; k < nth; ++k) bits &= bits - 1u;
+    give(e0 + i * VEC - shift + __ffs(bits) - 1, value, prob, total);
 }
 
 template <class T, bool kHold>
