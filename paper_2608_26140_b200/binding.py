@@ -59,7 +59,7 @@ class KV8(C.Structure):
 class PagedKV(C.Structure):
     _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("page_stride", C.c_int64), ("n_pages", C.c_int32), ("page", C.c_int32),
                 ("table", C.c_void_p), ("table_stride", C.c_int32)]
-    made_of = None      # of the tensors that Context.paged_kv made it over: requests, KV heads, head dimension, all on a GPU
+    made_of = None      # of the tensors that Context.paged_kv made it over: requests, KV heads, head dimension, all on one GPU, which
 
 
 class Rows(C.Structure):
@@ -235,6 +235,12 @@ def _dense(t, strides):
     return t.numel() == 0 or all(n == 1 or have == want for n, have, want in zip(t.shape[1:], t.stride()[1:], strides))
 
 
+def _current_device() -> int:
+    if _raw_stream is None:
+        _stream()
+    return _device()
+
+
 def _stream() -> int:
     """The current stream of the current device (torch.cuda.current_stream() builds an object around it: 3.3 us a call, this 0.2)."""
     global _raw_stream, _device
@@ -248,7 +254,7 @@ _raw_stream = _device = None
 
 
 class Context:
-    """One layer shape + workspace.  Mirrors the C entry points one to one."""
+    """One layer shape + workspace.  Mirrors the C entry points one to one.  A context is used from one thread at a time."""
 
     def __init__(self, hidden, n_heads, n_kv_heads, head_dim, ffn, rms_eps, qkv_bias,
                  max_batch, max_ctx, max_affix, max_rows, max_masked, device="cuda:0", max_vocab=0, max_block=0):
@@ -350,7 +356,8 @@ class Context:
         if (hkv, d) != self.heads[1:]:
             raise ValueError(f"pages of {hkv} KV heads of {d} for a context of {self.heads[1]} of {self.heads[2]}")
         c = PagedKV(_ptr(k_pages), _ptr(v_pages), k_pages.stride(0) if n_pages > 1 else hkv * page * d, n_pages, page, _ptr(table), table.shape[1])
-        c.made_of = (table.shape[0], hkv, d, all(t.is_cuda for t in (k_pages, v_pages, table)))
+        devices = {t.get_device() for t in (k_pages, v_pages, table)}
+        c.made_of = (table.shape[0], hkv, d, all(t.is_cuda for t in (k_pages, v_pages, table)) and len(devices) == 1, devices.pop())
         return c
 
     @staticmethod
@@ -484,7 +491,7 @@ class Context:
         H, hkv, d = self.heads
         shape = k.shape
         B, n = shape[0], shape[1]
-        self._cache_fits(cache, B)
+        self._pages_fit(cache, B)
         if v.shape != shape:
             raise ValueError(f"k {tuple(shape)} and v {tuple(v.shape)} differ in shape")
         (row_k, ref_k), (row_v, ref_v), (row_q, ref_q) = self._row_args
@@ -530,7 +537,7 @@ class Context:
         bf16, f32, i32 = self.dtypes
         shape = q.shape
         B, n, H, d = shape
-        self._cache_fits(cache, B)
+        self._pages_fit(cache, B)
         if H != self.heads[0] or d != self.heads[2]:
             raise ValueError(f"q {tuple(shape)} is not [B, n, H, d]")
         _check_tensor(q, bf16, shape)
@@ -551,7 +558,7 @@ class Context:
     def recompute_paged(self, w: LayerWeights, req: Request, cache: PagedKV, x, x_is_compact, anchor_idx, k, y, lens=None):
         """The rows of R through the layer, over a cache in pages; lens: int32 [B], the tokens of each request with them."""
         import torch
-        self._cache_fits(cache, req.batch)
+        self._pages_fit(cache, req.batch)
         if lens is not None:
             _check_tensor(lens, torch.int32, (req.batch,))
         self._check(self.lib.acache_recompute_paged(self.h, C.byref(w), C.byref(req), C.byref(cache), _ptr(x), int(x_is_compact), _ptr(anchor_idx), k,
@@ -564,8 +571,8 @@ class Context:
         rows, vocab = logits.shape
         apart, one = logits.stride()
         kind = logits.dtype
-        if (kind is not bf16 and kind is not f32) or not logits.is_cuda or (vocab > 1 and one != 1):
-            raise ValueError(f"logits of {kind} on {logits.device}, strides {(apart, one)}: bf16 or fp32 rows on a GPU are wanted")
+        if (kind is not bf16 and kind is not f32) or logits.get_device() != _current_device() or (vocab > 1 and one != 1):
+            raise ValueError(f"logits of {kind} on {logits.device}, strides {(apart, one)}: bf16 or fp32 rows on the current GPU are wanted")
         _check_tensor(token, i32, (rows,))
         if prob is not None:
             _check_tensor(prob, f32, (rows,))
@@ -614,10 +621,17 @@ class Context:
         to.batch_stride = batch if B > 1 else 0
         to.row_stride = row if n > 1 else heads * d
 
+    def _pages_fit(self, cache, batch):
+        """As _cache_fits; and the pages are on the current device, where the call runs."""
+        m = cache.made_of
+        if m is not None and (m[0] < batch or m[1] != self.heads[1] or m[2] != self.heads[2] or not m[3] or m[4] != _current_device()):
+            raise ValueError(f"pages of {m[0]} requests, {m[1]} KV heads of {m[2]}, {'' if m[3] else 'not all '}on GPU {m[4]}, "
+                             f"for {batch} requests and {self.heads[1]} KV heads of {self.heads[2]} on GPU {_current_device()}")
+
     def _cache_fits(self, cache, batch):
         """What a call would read or write past the cache's tensors for (a KV8 filled in by hand is the caller's affair)."""
         m = cache.made_of
-        if m is not None and (m[0] < batch or m[1] != self.heads[1] or m[2] != self.heads[2] or not m[3]):
+        if m is not None and (m[0] < batch or m[1:] != (self.heads[1], self.heads[2], True)):
             raise ValueError(f"a cache of {m[0]} requests, {m[1]} KV heads of {m[2]}, {'not ' if not m[3] else ''}all on a GPU, "
                              f"for {batch} requests and {self.heads[1]} KV heads of {self.heads[2]}")
 

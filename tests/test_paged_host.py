@@ -87,7 +87,7 @@ def test_the_handle_wants_pools_that_go_together():
     ctx.heads = (4, 2, 64)
     pool, table = torch.zeros((5, 2, 16, 64), dtype=torch.bfloat16), torch.zeros((3, 4), dtype=torch.int32)
     c = ctx.paged_kv(pool, pool.clone(), table)
-    assert (c.page_stride, c.n_pages, c.page, c.table_stride) == (2 * 16 * 64, 5, 16, 4) and c.made_of == (3, 2, 64, False)
+    assert (c.page_stride, c.n_pages, c.page, c.table_stride) == (2 * 16 * 64, 5, 16, 4) and c.made_of == (3, 2, 64, False, -1)
     apart = torch.zeros((5, 3, 16, 64), dtype=torch.bfloat16)[:, :2]
     assert ctx.paged_kv(apart, torch.zeros((5, 3, 16, 64), dtype=torch.bfloat16)[:, 1:], table).page_stride == 3 * 16 * 64
     for bad in ((pool, pool[:3], table), (pool, apart, table), (pool.float(), pool, table), (pool, pool, table.long()), (pool, pool, table.t()), (pool, pool, table[0]),
