@@ -240,6 +240,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
         }
     }
     if (nan) atomicOr(a.status, kFlagNonFinite);
+    bool endless = false;                                    // infinite logits: those are read as 0, all others as -inf, which has the same limits
     // a piece to f(logits, index of the first)
     auto one = [&](int i, auto&& f) {
         float x[VEC];
@@ -251,6 +252,9 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
 #pragma unroll
                 for (int k = 0; k < VEC; ++k) x[k] = x[k] != x[k] ? -INFINITY : x[k];
         }
+        if (endless)
+#pragma unroll
+            for (int k = 0; k < VEC; ++k) x[k] = x[k] == INFINITY ? 0.f : -INFINITY;
         f(x, i * VEC - shift);
     };
     auto each = [&](auto&& f) {
@@ -279,7 +283,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
         }
         return v;
     };
-    const float own_top = top;
+    float own_top = top;
     cluster_wait();
     // A bound that top_k tokens reach at least: the largest logits of that many threads.  Two bounds hold: top_k of one CTA's threads, and a share of top_k in every CTA's.  (Of 31 logits a thread, those of 50 threads of 512: about 53
     // tokens of a CTA are as large; those of 7 threads in each of 8 CTAs, the least of them: 80 of the row.)
@@ -339,19 +343,25 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
         return;
     }
 
+    endless = top == INFINITY;
+    if (endless) {
+        own_top = own_top == INFINITY ? 0.f : -INFINITY;
+        next_top = next_top == INFINITY ? 0.f : -INFINITY;
+        bound = bound == INFINITY ? 0.f : -INFINITY;
+        top = low = 0.f;
+    }
     const double unit = (double)(1ull << a.shift);
     const double rate = 1.4426950408889634074 / (double)temperature;         // log2 of a weight per logit
     const u64 least = (u64)ceil((double)min_p * unit);
-    // half of the distance from the largest, which may be infinite (the whole of it would pass fp32's range between finite logits)
+    // half of the distance from the largest (the whole of it may pass fp32's range)
     const float half_top = 0.5f * top;
-    auto behind = [&](float l) { return l == top ? 0.f : fmaf(-0.5f, l, half_top); };
+    auto behind = [&](float l) { return fmaf(-0.5f, l, half_top); };
     // 2^-y in units, for y up to shift + 1: y = j / 64 + r, the table's 2^(-j / 64) times 2^-r by its series, of which |r ln 2|^6 / 720 < 2^-54 is left
     // out; the last addition rounds to whole units
     auto weight = [&](float l) -> u64 {
-        const double y = l == top ? 0.0 : ((double)top - (double)l) * rate;
         constexpr double kRound = 1.5 * 70368744177664.0;                    // 1.5 * 2^46: what is added to it is rounded to 1 / 64
         constexpr double kLn2 = -0.69314718055994530942;
-        const double t = y + kRound, r = y - (t - kRound);
+        const double d = (double)top - (double)l, t = fma(d, rate, kRound), r = fma(d, rate, -(t - kRound));
         const int j = __double2loint(t);
         const double at = s.power[j & (kSteps - 1)][lane & (kCopies - 1)];
         const double scaled = __hiloint2double(__double2hiint(at) + ((a.shift - (j >> 6)) << 20), __double2loint(at));
@@ -395,10 +405,11 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
                 for (int k = 0; k < 4; ++k) w[k] = weight(bin[k] >= 0 ? x[k0 + k] : top);
 #pragma unroll
                 for (int k = 0; k < 4; ++k)
-                    if (bin[k] >= 0) {
-                        add_weight(bin[k], w[k]);
-                        if (w[k] >= least) mass_min_p += w[k];
-                    }
+                    if (bin[k] >= 0) add_weight(bin[k], w[k]);
+                if (least)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        if (bin[k] >= 0 && w[k] >= least) mass_min_p += w[k];
             }
         });
     };
@@ -512,7 +523,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
             const int bin = at_bin.bin;
             // Logits of the bin lie less than a bin from its middle, whatever was rounded: the others are sorted out by two comparisons.
             float from_l = -INFINITY, to_l = INFINITY;
-            if (!keys && bins_per < 1e30f && top < INFINITY) {
+            if (!keys && bins_per < 1e30f) {
                 from_l = __double2float_rd((double)top - 2.0 * (bin + 1) / (double)bins_per);
                 to_l = __double2float_ru((double)top - 2.0 * (bin - 1) / (double)bins_per);
             }
@@ -623,7 +634,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
     auto give = [&](int token, float l, double prob, double total) {
         a.token[row] = token;
         if (a.prob) a.prob[row] = (float)prob;
-        if (a.confidence) a.confidence[row] = (float)((l == top ? 1.0 : exp((double)l - (double)top)) / total);
+        if (a.confidence) a.confidence[row] = (float)(exp((double)l - (double)top) / total);
     };
 
     auto cluster_sum = [&](const auto (&v)[kMaxCluster], int n) {
@@ -632,12 +643,11 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
         for (int r = 0; r < n; ++r) sum += v[r];
         return sum;
     };
-    const bool endless = top == INFINITY;                    // (infinite logits share the confidence, which the running sums do not give)
     if (a.confidence) {
         double c = 0.0;
-        if (endless) each([&](const float (&x)[VEC], int) {
+        if (endless) each([&](const float (&x)[VEC], int) {                  // (the running sums say nothing then)
 #pragma unroll
-            for (int k = 0; k < VEC; ++k) c += x[k] == INFINITY;
+            for (int k = 0; k < VEC; ++k) c += x[k] == 0.f;
         });
         else c = (double)conf * (double)ex2f((conf_top - top) * kLog2e);
         c = cta_sum(c, s.d);
