@@ -183,10 +183,10 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
             }
         }
 #pragma unroll
-        for (int k = 0; k < VEC; ++k) {
-            high = fmaxf(high, x[k]);
-            low = fminf(low, x[k] > -INFINITY ? x[k] : INFINITY);
-        }
+        for (int k = 0; k < VEC; ++k) high = fmaxf(high, x[k]);
+        if (!greedy && !quick)                               // (who else needs the range of the bins takes all that weights allow)
+#pragma unroll
+            for (int k = 0; k < VEC; ++k) low = fminf(low, x[k] > -INFINITY ? x[k] : INFINITY);
         next_top = fmaxf(next_top, fminf(top, high));
         if (high > top) {
             top = high;
@@ -344,6 +344,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
     }
 
     endless = top == INFINITY;
+    if (greedy || quick) low = -INFINITY;
     if (endless) {
         own_top = own_top == INFINITY ? 0.f : -INFINITY;
         next_top = next_top == INFINITY ? 0.f : -INFINITY;
