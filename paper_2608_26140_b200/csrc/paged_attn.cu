@@ -9,9 +9,14 @@
 //
 // The work of all requests, KV heads and row tiles is one line of units of 64 keys, cut into equal pieces, one a CTA, whatever
 // the requests' lengths (they are known on the device only).  A CTA that does not have all keys of an item leaves a partial result
-// and the last one to arrive adds the parts up, in their order.
-// A warp streams 16 keys a step through a ring of its own in shared memory (cp.async, whole rows side by side, the page's number asked for a
-// step ahead), swizzled so that ldmatrix meets different banks.  Keys that do not count are not read: their places are zero.
+// and the last one to arrive adds the parts up, in their order.  Where there is too little for that, a cluster of CTAs has an item to itself.
+// A warp streams 16 keys a step through a ring of its own in shared memory (cp.async, whole rows side by side, the page's number asked for two
+// steps ahead), swizzled so that ldmatrix meets different banks.  Keys that do not count are not read: their places are zero.
+//
+// Up to 8 rows HBM bounds it: one token of 2 requests over 65537 keys of 32 heads (2148 MB) 314 us, 6.8 TB/s; of 64 requests over up to 8191 keys of
+// 4 KV heads (794 MB) 127 us, 6.3 TB/s.  32 rows of 16 requests over 2560 keys of 32 heads, of which 2048 are the same pages for all, 108 us: 371 instructions
+// a step, two warps a scheduler that wait for one another's results (issue slots 33 %, tensor pipe 37 % busy), 6.2 TB/s from L2.  One token of one
+// request over 1664 keys 7.5 us: four trips to memory one behind the other (arguments, page, keys, result) and a cluster's exchange.
 #include <algorithm>
 #include <climits>
 
@@ -566,8 +571,9 @@ int paged_launch(PagedAttnArgs a, cudaStream_t stream) {
     const int64_t units = (int64_t)std::max(1, (a.ctx_len + kUnit - 1) / kUnit) * tiles * a.batch * a.n_kv_heads;
     if (units > INT_MAX) return -2;                        // counted in 32 bits
     // Two ways to share the work.  In one line of units every CTA has as much to do, but a result in parts costs a trip through memory and
-    // back (5.5 us); a cluster for each item joins its CTAs' parts in 1.6 us, and divides no work among items.  A unit takes 0.37 us (1 us with 32 rows a CTA),
-    // or its share of the memory's bandwidth.  One token of one request, 4 KV heads, 1664 keys: 9.1 and 6.7 us.
+    // back (5.5 us); a cluster for each item joins its CTAs' parts in 1.6 us, but is as long as its item (lengths on the device: a third longer than
+    // an equal share, say).  A unit takes 0.37 us (1 us with 32 rows a CTA), or its share of the memory's bandwidth.  One token of one request, 4 KV heads,
+    // 1664 keys: 9.1 us in one line, 7.5 in clusters; 5 rows of 7 requests, 251 keys: 10.5 and 6.7.
     const int64_t items = (int64_t)tiles * a.batch * a.n_kv_heads, u = units / items;
     const int ctas = (int)std::min<int64_t>(kPlaces, std::max<int64_t>(1, units / kMinUnits));
     auto unit_us = [&](int64_t active) { return std::max(NT == 4 ? 1.0 : 0.37, 1.5 * D / 128 * std::min<int64_t>(active, kPlaces) / kPlaces); };

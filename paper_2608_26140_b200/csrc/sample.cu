@@ -5,15 +5,22 @@
 //   passes u times the sum S of all that are kept.
 //
 // A weight is a whole number of 2^-shift (46 bits behind the point for up to 2^16 tokens, one less for every doubling), so that sums are exact and do not
-// depend on their order; what is below half of that is never drawn.  The row lies in the shared memory of a cluster of CTAs, read once; what a CTA
-// finds out it writes to the others, and every CTA takes every decision by itself, so that a step of a search costs one or two barriers
-// of the cluster.  The logits are counted by bins that part them evenly from the largest to the smallest whose weight counts.
-//  - With a top_k of up to kTop (and room in the list) the tokens of the bins that hold the first top_k go into a list; one CTA sorts it, adds up their weights
-//    and decides.  No other weight is formed.
-//  - Else the bins have weights too (32-bit atomics on the two halves of a sum: adding 64 bits at once took five times as long).  Each of the searches (the
-//    k-th token, the one at which top_p is reached, the one that is drawn) goes to a bin, then over the tokens of that bin: by comparing
-//    them all with one another, where they are few, else by another histogram of their keys.  A search ends at a value; among the tokens that have
-//    it the index decides.
+// depend on their order; what is below half of that is never drawn.  A row belongs to a cluster of CTAs, which keep it in shared memory or read it
+// again from L2; what one finds out it writes to the others, and every CTA takes every decision by itself, so that a step of a search costs
+// one or two barriers of the cluster.
+//  - A top_k of up to kTop: while the row comes in every thread keeps its largest logit, and of those a bound follows that at least top_k tokens
+//    reach and few others.  They go into a list of the first CTA, which sorts it, adds up their weights and decides.  No other weight is formed.
+//    (Where too many reach the bound, those of the bins that hold the first top_k are taken.)
+//  - Else the weights of all tokens are added up by bins, which part the logits evenly from the largest to the smallest that counts: in three parts of
+//    16 bits, as 32-bit atomics that return nothing take a seventh of the time of 64-bit ones.  Each of the searches (the k-th token, the one at
+//    which top_p is reached, the one that is drawn) goes to a bin, then over the tokens of that bin: sorted, where they are few, else by
+//    another histogram of their keys.  A search ends at a value; among the tokens that have it the index decides.
+// The sum for the confidence is kept while the row comes in, against each thread's largest logit so far.
+//
+// What bounds it: 512 rows of 126464 fp32 logits, each with settings of its own, 233 us (floor 40), 128 bf16 rows with top_p 100 us, one row with top_k
+// and top_p 10.7 us.  The chain of steps of a row, two CTAs an SM: of the 50 us that a CTA of 31616 bf16 logits takes without a top_k, 17 are the weights (conflicts
+// of the atomics: random bins meet about four to a bank), 5 the row, 14 two searches, the rest barriers and sums; a word to another CTA is there after 0.6 us,
+// a barrier of the cluster takes 0.25.  Issue slots are busy for half of the time.
 #include <algorithm>
 
 #include "kernels.h"
@@ -285,8 +292,9 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
     };
     float own_top = top;
     cluster_wait();
-    // A bound that top_k tokens reach at least: the largest logits of that many threads.  Two bounds hold: top_k of one CTA's threads, and a share of top_k in every CTA's.  (Of 31 logits a thread, those of 50 threads of 512: about 53
-    // tokens of a CTA are as large; those of 7 threads in each of 8 CTAs, the least of them: 80 of the row.)
+    // A bound that top_k tokens reach at least: the largest logits of that many threads.  Two bounds hold: top_k of one CTA's threads, and a share of
+    // top_k in every CTA's.  (Of 31 logits a thread, those of 50 threads of 512: about 53 tokens of a CTA are as large; those of 7 threads in
+    // each of 8 CTAs, the least of them: 80 of the row.)
     if (quick) {
         const uint32_t key = sorted(order_key(top), kThreads, work.few.merged);
         if (tid == top_k - 1) s.f[0][0] = value_of(key);
@@ -890,9 +898,9 @@ int sample_launch(SampleArgs a, int most, cudaStream_t stream) {
     cfg.numAttrs = 2;
     return cudaLaunchKernelEx(&cfg, sample_kernel<T, kHold>, a) == cudaSuccess ? 1 : -1;
 }
-// Logits of a CTA: up to 16384 for few rows, for which the time of one row counts; twice as many once their CTAs take more than a round, as
-// what a step costs by itself is then spread over more of them (512 rows of 126464 bf16 310 and 240 us).  So many fp32 logits would leave
-// room for one CTA in an SM, and are read again from L2 (512 rows 281 us; held, in halves, 335; 40 rows 82 where held bf16 ones take 68).
+// Logits of a CTA: up to 16384 for few rows, for which the time of one row counts (8 rows of 126464 bf16 32 us, and 43 with twice as many); twice as many
+// once their CTAs take more than a round, as what a step costs by itself is then spread over more of them (128 rows 101 us, and 143; 40 rows
+// 53 and 62).  So many fp32 logits would leave room for one CTA in an SM, and are read again from L2 (512 rows 241 us; held 328, held in halves 315).
 template <class T>
 int sample_dispatch(const SampleArgs& a, cudaStream_t stream) {
     constexpr int kMost = 16384;
