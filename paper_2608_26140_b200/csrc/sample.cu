@@ -12,7 +12,7 @@
 //    reach and few others.  They go into a list of the first CTA, which sorts it, adds up their weights and decides.  No other weight is formed.
 //    (Where too many reach the bound, those of the bins that hold the first top_k are taken.)
 //  - Else the weights of all tokens are added up by bins, which part the logits evenly from the largest to the smallest that counts: in three parts of
-//    16 bits, as 32-bit atomics that return nothing take a seventh of the time of 64-bit ones.  Each of the searches (the k-th token, the one at
+//    16 bits, as a 32-bit atomic that returns nothing takes a twentieth of a 64-bit one's time.  Each of the searches (the k-th token, the one at
 //    which top_p is reached, the one that is drawn) goes to a bin, then over the tokens of that bin: sorted, where they are few, else by
 //    another histogram of their keys.  A search ends at a value; among the tokens that have it the index decides.
 // The sum for the confidence is kept while the row comes in, against each thread's largest logit so far.
