@@ -224,9 +224,10 @@ def _check_tensor(t, dtype, shape):
         raise ValueError(f"a tensor {tuple(t.shape)} of {t.dtype} on {t.device} where contiguous {tuple(shape)} of {dtype} on a GPU is wanted")
 
 
-def _checked(t, dtype, shape):
-    """The address of a tensor of that type and shape."""
-    _check_tensor(t, dtype, shape)
+def _at(t, dtype, shape, device):
+    """The address of a contiguous tensor of that type and shape on that GPU."""
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != device or not t.is_contiguous():
+        raise ValueError(f"a tensor {tuple(t.shape)} of {t.dtype} on {t.device} where contiguous {tuple(shape)} of {dtype} on GPU {device} is wanted")
     return t.data_ptr()
 
 
@@ -276,6 +277,7 @@ class Context:
         nbytes = self.lib.acache_workspace_bytes(self.h)
         with torch.cuda.device(self.device):
             self.workspace = torch.empty(nbytes + 256, dtype=torch.uint8, device=self.device)
+            self.gpu = self.workspace.get_device()
             base = self.workspace.data_ptr()
             self._ws_ptr = (base + 255) & ~255
             self._check(self.lib.acache_set_workspace(self.h, self._ws_ptr, nbytes, _stream()))
@@ -491,12 +493,12 @@ class Context:
         H, hkv, d = self.heads
         shape = k.shape
         B, n = shape[0], shape[1]
-        self._pages_fit(cache, B)
+        device = self._pages_fit(cache, B)
         if v.shape != shape:
             raise ValueError(f"k {tuple(shape)} and v {tuple(v.shape)} differ in shape")
         (row_k, ref_k), (row_v, ref_v), (row_q, ref_q) = self._row_args
-        self._rows_at(row_k, k, shape, hkv)
-        self._rows_at(row_v, v, shape, hkv)
+        self._rows_at(row_k, k, shape, hkv, device)
+        self._rows_at(row_v, v, shape, hkv, device)
         to_q = None
         if q is None:
             ref_q = None
@@ -506,28 +508,21 @@ class Context:
             shape_q = q.shape
             if q_out is None or shape_q[0] != B or shape_q[1] != n:
                 raise ValueError("q and q_out go together, and with k")
-            self._rows_at(row_q, q, shape_q, H)
-            if q_out.shape != shape_q or q_out.dtype is not bf16 or not q_out.is_cuda or not q_out.is_contiguous():
-                _check_tensor(q_out, bf16, shape_q)
-            to_q = q_out.data_ptr()
+            self._rows_at(row_q, q, shape_q, H, device)
+            to_q = _at(q_out, bf16, shape_q, device)
         if lens is not None:
-            _check_tensor(lens, i32, (B,))
-            lens = lens.data_ptr()
+            lens = _at(lens, i32, (B,), device)
         if counts is not None:
-            _check_tensor(counts, i32, (B,))
-            counts = counts.data_ptr()
+            counts = _at(counts, i32, (B,), device)
         if pos is not None:
-            _check_tensor(pos, i32, (B, n))
-            pos = pos.data_ptr()
+            pos = _at(pos, i32, (B, n), device)
         cos = sin = None
         if rope is not None:
             cos, sin = rope
             at = cos.shape
             if at[0] < ctx_len:
                 raise ValueError(f"a rope table of {at[0]} rows for a context of {ctx_len}")
-            _check_tensor(cos, f32, (at[0], d // 2))
-            _check_tensor(sin, f32, at)
-            cos, sin = cos.data_ptr(), sin.data_ptr()
+            cos, sin = _at(cos, f32, (at[0], d // 2), device), _at(sin, f32, at, device)
         st = self.lib.acache_paged_append(self.h, C.byref(cache), B, ctx_len, ref_k, ref_v, ref_q, to_q, n, lens, pos, counts, cos, sin, _stream())
         if st:
             self._check(st)
@@ -537,30 +532,26 @@ class Context:
         bf16, f32, i32 = self.dtypes
         shape = q.shape
         B, n, H, d = shape
-        self._pages_fit(cache, B)
+        device = self._pages_fit(cache, B)
         if H != self.heads[0] or d != self.heads[2]:
             raise ValueError(f"q {tuple(shape)} is not [B, n, H, d]")
-        _check_tensor(q, bf16, shape)
-        _check_tensor(o, bf16, shape)
+        q, o = _at(q, bf16, shape, device), _at(o, bf16, shape, device)
         if lse is not None:
-            _check_tensor(lse, f32, (B, n, H))
-            lse = lse.data_ptr()
+            lse = _at(lse, f32, (B, n, H), device)
         if lens is not None:
-            _check_tensor(lens, i32, (B,))
-            lens = lens.data_ptr()
+            lens = _at(lens, i32, (B,), device)
         if key_drop is not None:
-            _check_tensor(key_drop, i32, (B, -(-ctx_len // 32)))
-            key_drop = key_drop.data_ptr()
-        st = self.lib.acache_paged_attention(self.h, C.byref(cache), B, n, ctx_len, q.data_ptr(), lens, key_drop, o.data_ptr(), lse, _stream())
+            key_drop = _at(key_drop, i32, (B, -(-ctx_len // 32)), device)
+        st = self.lib.acache_paged_attention(self.h, C.byref(cache), B, n, ctx_len, q, lens, key_drop, o, lse, _stream())
         if st:
             self._check(st)
 
     def recompute_paged(self, w: LayerWeights, req: Request, cache: PagedKV, x, x_is_compact, anchor_idx, k, y, lens=None):
         """The rows of R through the layer, over a cache in pages; lens: int32 [B], the tokens of each request with them."""
         import torch
-        self._pages_fit(cache, req.batch)
+        device = self._pages_fit(cache, req.batch)
         if lens is not None:
-            _check_tensor(lens, torch.int32, (req.batch,))
+            lens = _at(lens, torch.int32, (req.batch,), device)
         self._check(self.lib.acache_recompute_paged(self.h, C.byref(w), C.byref(req), C.byref(cache), _ptr(x), int(x_is_compact), _ptr(anchor_idx), k,
                                                     _ptr(lens), _ptr(y), _stream()))
 
@@ -571,18 +562,18 @@ class Context:
         rows, vocab = logits.shape
         apart, one = logits.stride()
         kind = logits.dtype
-        if (kind is not bf16 and kind is not f32) or logits.get_device() != _current_device() or (vocab > 1 and one != 1):
+        device = self._on_device()
+        if (kind is not bf16 and kind is not f32) or logits.get_device() != device or (vocab > 1 and one != 1):
             raise ValueError(f"logits of {kind} on {logits.device}, strides {(apart, one)}: bf16 or fp32 rows on the current GPU are wanted")
-        _check_tensor(token, i32, (rows,))
+        token = _at(token, i32, (rows,), device)
         if prob is not None:
-            _check_tensor(prob, f32, (rows,))
-            prob = prob.data_ptr()
+            prob = _at(prob, f32, (rows,), device)
         if confidence is not None:
-            _check_tensor(confidence, f32, (rows,))
-            confidence = confidence.data_ptr()
-        how = self._sampling(rows, u, temperature, top_k, top_p, min_p, rows_per_setting)
-        st = self.lib.acache_sample_tokens(self.h, logits.data_ptr(), 0 if kind is bf16 else 1, rows, vocab, apart if rows > 1 else vocab, how, u.data_ptr(),
-                                           token.data_ptr(), prob, confidence, _stream())
+            confidence = _at(confidence, f32, (rows,), device)
+        u = _at(u, f32, (rows,), device)
+        how = self._sampling(rows, device, temperature, top_k, top_p, min_p, rows_per_setting)
+        st = self.lib.acache_sample_tokens(self.h, logits.data_ptr(), 0 if kind is bf16 else 1, rows, vocab, apart if rows > 1 else vocab, how, u,
+                                           token, prob, confidence, _stream())
         if st:
             self._check(st)
 
@@ -591,42 +582,51 @@ class Context:
         """predict_commit with drawn tokens; logits: fp32 [batch * n_blk, vocab] out; u: fp32 [batch, n_blk]; settings as sample_tokens."""
         import torch
         rows = batch * n_blk
-        _check_tensor(logits, torch.float32, (rows, vocab))
-        how = self._sampling(rows, u.view(-1), temperature, top_k, top_p, min_p, rows_per_setting)
+        device = self._on_device()
+        logits, u = _at(logits, torch.float32, (rows, vocab), device), _at(u.view(-1), torch.float32, (rows,), device)
+        how = self._sampling(rows, device, temperature, top_k, top_p, min_p, rows_per_setting)
         self._check(self.lib.acache_predict_sample(self.h, _ptr(h), h_rows, _ptr(block_rows), batch, n_blk, _ptr(final_norm_g), _ptr(w_lm), vocab,
-                                                   _ptr(logits), how, _ptr(u), float(threshold), _ptr(token), _ptr(confidence), _ptr(commit),
+                                                   logits, how, u, float(threshold), _ptr(token), _ptr(confidence), _ptr(commit),
                                                    _stream()))
 
-    def _sampling(self, rows, u, temperature, top_k, top_p, min_p, rows_per_setting):
+    def _sampling(self, rows, device, temperature, top_k, top_p, min_p, rows_per_setting):
         bf16, f32, i32 = self.dtypes
-        _check_tensor(u, f32, (rows,))
         per = (rows,) if rows_per_setting == 1 else (-(-rows // max(rows_per_setting, 1)),)
         how, ref = self._sampling_arg
-        how.temperature = None if temperature is None else _checked(temperature, f32, per)
-        how.top_p = None if top_p is None else _checked(top_p, f32, per)
-        how.min_p = None if min_p is None else _checked(min_p, f32, per)
-        how.top_k = None if top_k is None else _checked(top_k, i32, per)
+        how.temperature = None if temperature is None else _at(temperature, f32, per, device)
+        how.top_p = None if top_p is None else _at(top_p, f32, per, device)
+        how.min_p = None if min_p is None else _at(min_p, f32, per, device)
+        how.top_k = None if top_k is None else _at(top_k, i32, per, device)
         how.rows_per_setting = rows_per_setting
         return ref
 
-    def _rows_at(self, to, t, shape, heads):
+    def _rows_at(self, to, t, shape, heads, device):
         """Puts where rows t [B, n, heads, d] lie into a Rows; the heads of a row side by side."""
         B, n, h, d = shape
         batch, row, head, one = t.stride()
-        if h != heads or d != self.heads[2] or t.dtype is not self.dtypes[0] or not t.is_cuda:
-            raise ValueError(f"rows {tuple(shape)} of {t.dtype} on {t.device} are not bf16 [B, n, {heads}, {self.heads[2]}] on a GPU")
+        if h != heads or d != self.heads[2] or t.dtype is not self.dtypes[0] or t.get_device() != device:
+            raise ValueError(f"rows {tuple(shape)} of {t.dtype} on {t.device} are not bf16 [B, n, {heads}, {self.heads[2]}] on GPU {device}")
         if (head != d and heads > 1) or one != 1:
             raise ValueError("the heads of a row lie side by side")
         to.p = t.data_ptr()
         to.batch_stride = batch if B > 1 else 0
         to.row_stride = row if n > 1 else heads * d
 
+    def _on_device(self):
+        """The current device, on which a call runs, and the context's scratch has to be."""
+        device = _current_device()
+        if device != self.gpu:
+            raise ValueError(f"a context on GPU {self.gpu} while GPU {device} is the current one")
+        return device
+
     def _pages_fit(self, cache, batch):
-        """As _cache_fits; and the pages are on the current device, where the call runs."""
+        """As _cache_fits; and the pages are on the current device, which is returned."""
+        device = self._on_device()
         m = cache.made_of
-        if m is not None and (m[0] < batch or m[1] != self.heads[1] or m[2] != self.heads[2] or not m[3] or m[4] != _current_device()):
+        if m is not None and (m[0] < batch or m[1] != self.heads[1] or m[2] != self.heads[2] or not m[3] or m[4] != device):
             raise ValueError(f"pages of {m[0]} requests, {m[1]} KV heads of {m[2]}, {'' if m[3] else 'not all '}on GPU {m[4]}, "
-                             f"for {batch} requests and {self.heads[1]} KV heads of {self.heads[2]} on GPU {_current_device()}")
+                             f"for {batch} requests and {self.heads[1]} KV heads of {self.heads[2]} on GPU {device}")
+        return device
 
     def _cache_fits(self, cache, batch):
         """What a call would read or write past the cache's tensors for (a KV8 filled in by hand is the caller's affair)."""

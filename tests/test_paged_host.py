@@ -94,3 +94,29 @@ def test_the_handle_wants_pools_that_go_together():
                 (pool.transpose(2, 3), pool.transpose(2, 3), table), (pool[:, :1], pool[:, :1], table)):
         with pytest.raises(ValueError):
             ctx.paged_kv(*bad)
+
+
+def test_calls_want_one_device(monkeypatch):
+    """The context's, the pages' and every tensor's: the current one, where the call runs."""
+    ctx = ab.Context.__new__(ab.Context)
+    ctx.heads, ctx.dtypes, ctx.gpu = (4, 2, 64), (torch.bfloat16, torch.float32, torch.int32), 0
+    ctx._row_args = [(ab.Rows(), None) for _ in range(3)]
+    cache = ab.PagedKV()
+    cache.made_of = (3, 2, 64, True, 1)
+    q, k, lens = torch.zeros((3, 1, 4, 64), dtype=torch.bfloat16), torch.zeros((3, 1, 2, 64), dtype=torch.bfloat16), torch.zeros(3, dtype=torch.int32)
+    logits, u, token = torch.zeros((2, 10)), torch.zeros(2), torch.zeros(2, dtype=torch.int32)
+    calls = (lambda: ctx.paged_attention(cache, 16, q, q.clone()), lambda: ctx.paged_append(cache, 16, k, k.clone(), lens=lens))
+    samples = (lambda: ctx.sample_tokens(logits, u, token), lambda: ctx.predict_sample(None, 1, None, 2, 1, None, None, 10, logits, u, 0.9, None, None, None))
+    monkeypatch.setattr(ab, "_current_device", lambda: 1)
+    for call in calls + samples:
+        with pytest.raises(ValueError, match="a context on GPU 0 while GPU 1 is"):
+            call()
+    ctx.gpu = 1
+    for call in calls + samples:                                 # tensors on the CPU
+        with pytest.raises(ValueError, match="on cpu"):
+            call()
+    monkeypatch.setattr(ab, "_current_device", lambda: 0)
+    ctx.gpu = 0
+    for call in calls:
+        with pytest.raises(ValueError, match="on GPU 1"):
+            call()
