@@ -35,6 +35,7 @@ constexpr int PSTAGES = 3;
 constexpr int kUnit = PW * PSTEP;        // keys of a unit of work
 constexpr int kMinUnits = 2;             // fewest units that are worth a CTA
 constexpr int kPlaces = 2 * 148;         // CTAs that run at a time
+static_assert(kPlaces <= kKv8Counters, "a counter for every CTA that an item may begin in");
 constexpr float kPagedRaise = 8.f;       // M moves when a logit passes it by this (log2): P and sums stay within 2^8 of what they are with M the largest
 
 __device__ __forceinline__ uint32_t transpose8x8(uint32_t v) {
