@@ -312,17 +312,25 @@ __global__ void __launch_bounds__(PW * 32, 2) paged_attn_kernel(const PagedAttnA
             if (there == 0u) continue;
             // ---- S^T = K Q^T ----
             float sv[NT][4];
-#pragma unroll
-            for (int ks = 0; ks < D / 16; ++ks) {
-                uint32_t fa[4];
-                ldmatrix_x4(fa[0], fa[1], fa[2], fa[3], st + (k_get ^ (ks << 5)));
+            uint32_t fa[2][4];
+            uint2 fq[2][NT];
+            auto get = [&](int ks) {
+                ldmatrix_x4(fa[ks & 1][0], fa[ks & 1][1], fa[ks & 1][2], fa[ks & 1][3], st + (k_get ^ (ks << 5)));
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
-                    uint2 q;
-                    if constexpr (Q_REGS) q = qf[ks][nt];
-                    else q = qs[(ks * NT + nt) * 32 + lane];
-                    if (ks == 0) mma_bf16_16816_first(sv[nt], fa, q.x, q.y);
-                    else mma_bf16_16816(sv[nt], fa, q.x, q.y);
+                    if constexpr (Q_REGS) fq[ks & 1][nt] = qf[ks][nt];
+                    else fq[ks & 1][nt] = qs[(ks * NT + nt) * 32 + lane];
+                }
+            };
+            get(0);
+#pragma unroll
+            for (int ks = 0; ks < D / 16; ++ks) {
+                if (ks + 1 < D / 16) get(ks + 1);
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                    const uint2 q = fq[ks & 1][nt];
+                    if (ks == 0) mma_bf16_16816_first(sv[nt], fa[ks & 1], q.x, q.y);
+                    else mma_bf16_16816(sv[nt], fa[ks & 1], q.x, q.y);
                 }
             }
             const float2 scale2 = make_float2(a.scale_log2e, a.scale_log2e);
@@ -380,10 +388,11 @@ __global__ void __launch_bounds__(PW * 32, 2) paged_attn_kernel(const PagedAttnA
             }
 #pragma unroll
             for (int i = 0; i < D / 16; ++i) {
-                uint32_t fa[4];
-                ldmatrix_x4_trans(fa[0], fa[1], fa[2], fa[3], st + (v_get ^ (i << 5)));
+                if (i == 0) ldmatrix_x4_trans(fa[0][0], fa[0][1], fa[0][2], fa[0][3], st + v_get);
+                if (i + 1 < D / 16)
+                    ldmatrix_x4_trans(fa[(i + 1) & 1][0], fa[(i + 1) & 1][1], fa[(i + 1) & 1][2], fa[(i + 1) & 1][3], st + (v_get ^ ((i + 1) << 5)));
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt) mma_bf16_16816(o[i][nt], fa, pf[nt][0], pf[nt][1]);
+                for (int nt = 0; nt < NT; ++nt) mma_bf16_16816(o[i][nt], fa[i & 1], pf[nt][0], pf[nt][1]);
             }
         }
 
