@@ -7,8 +7,8 @@
 // so that up to 8 rows (the query heads of a KV head, times the tokens) cost one matrix instruction for every 16 keys and 16 d; P only has
 // to be transposed in 8 x 8 blocks (movmatrix).  P is rounded to bf16, as V is: 2^-8 of each probability at most; its sum is not.
 //
-// The work of all requests, KV heads and row tiles is one line of units of 64 keys, cut into equal pieces, one a CTA, whatever
-// the requests' lengths (they are known on the device only).  A CTA that does not have all keys of an item leaves a partial result
+// The work of all requests, KV heads and row tiles is one line of units of 64 keys (and a few behind each item's for what it costs by itself), cut into
+// equal pieces, one a CTA, whatever the requests' lengths (they are known on the device only).  A CTA that does not have all keys of an item leaves a partial result
 // and the last one to arrive adds the parts up, in their order.  Where there is too little for that, a cluster of CTAs has an item to itself.
 // A warp streams 16 keys a step through a ring of its own in shared memory (cp.async, whole rows side by side, the page's number asked for two
 // steps ahead), swizzled so that ldmatrix meets different banks.  Keys that do not count are not read: their places are zero.
@@ -34,6 +34,11 @@ constexpr int PSTEP = 16;                // keys of a warp's step
 constexpr int PSTAGES = 3;
 constexpr int kUnit = PW * PSTEP;        // keys of a unit of work
 constexpr int kMinUnits = 2;             // fewest units that are worth a CTA
+// What an item costs besides its keys (start, queries, joining the warps; 4.5 us beside units of 1.5), in units.  Without it a CTA may get a whole run of short
+// requests' items, each of one unit: one token and 32 rows of 32 requests over 40 to 4000 keys of 32 heads 270 and 502 us; with 2 units 145 and 237, 3 141 and
+// 197, 5 141 and 157, 8 140 and 158; 64 requests over 300 keys 62, 41, 40.5, 41.5, 43.
+template <int NT>
+constexpr unsigned kItemUnits = NT > 2 ? 5u : 3u;
 constexpr int kPlaces = 2 * 148;         // CTAs that run at a time
 static_assert(kPlaces <= kKv8Counters, "a counter for every CTA that an item may begin in");
 constexpr float kPagedRaise = 8.f;       // M moves when a logit passes it by this (log2): P and sums stay within 2^8 of what they are with M the largest
@@ -89,6 +94,7 @@ __global__ void __launch_bounds__(PW * 32, 2) paged_attn_kernel(const PagedAttnA
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
     pdl_wait();
     pdl_launch_dependents();
+    const unsigned extra = a.cluster ? 0u : kItemUnits<NT>;     // units behind an item's that stand for no keys
     const int hkv = a.n_kv_heads, G = a.group, R = a.n * G, tiles = (R + L::ROWS - 1) / L::ROWS, per_request = hkv * tiles;
     uint2* qs = reinterpret_cast<uint2*>(smem + L::SMEM - L::QS);
 
@@ -122,7 +128,7 @@ __global__ void __launch_bounds__(PW * 32, 2) paged_attn_kernel(const PagedAttnA
         mine_hi = cluster_item * units + units * (rank + 1) / a.cluster;
         if (a.lens && cluster_item == 0 && rank == 0 && tid == 0 && a.lens[b] != len_of(b)) atomicOr(a.status, kFlagBadIndex);
     } else if (!a.lens) {
-        const unsigned u = (unsigned)units_of(a.ctx_len) * per_request;
+        const unsigned u = (units_of(a.ctx_len) + extra) * per_request;
         share(u * a.batch);
         if ((int)blockIdx.x >= ctas) return;
         b = (int)(first_of(blockIdx.x) / u);
@@ -135,7 +141,7 @@ __global__ void __launch_bounds__(PW * 32, 2) paged_attn_kernel(const PagedAttnA
         for (int r = r0; r < r1; ++r) {
             const int len = a.lens[r];
             if (blockIdx.x == 0 && (len < 0 || len > a.ctx_len)) atomicOr(a.status, kFlagBadIndex);
-            sum += (unsigned)units_of(min(max(len, 0), a.ctx_len)) * per_request;
+            sum += (units_of(min(max(len, 0), a.ctx_len)) + extra) * per_request;
         }
         unsigned upto = sum;
 #pragma unroll
@@ -159,7 +165,7 @@ __global__ void __launch_bounds__(PW * 32, 2) paged_attn_kernel(const PagedAttnA
             int r = r0;
 #pragma unroll 1
             for (; r < r1 - 1; ++r) {
-                const unsigned u = (unsigned)units_of(len_of(r)) * per_request;
+                const unsigned u = (units_of(len_of(r)) + extra) * per_request;
                 if (mine < lo + u) break;
                 lo += u;
             }
@@ -194,14 +200,19 @@ __global__ void __launch_bounds__(PW * 32, 2) paged_attn_kernel(const PagedAttnA
         // ---- the item and this CTA's keys of it ----
         int len = len_of(b);
         unsigned units = units_of(len);
-        while (!a.cluster && unit >= b_lo + units * per_request) {
-            b_lo += units * per_request;
+        while (!a.cluster && unit >= b_lo + (units + extra) * per_request) {
+            b_lo += (units + extra) * per_request;
             ++b;
             len = len_of(b);
             units = units_of(len);
         }
-        const int item = a.cluster ? cluster_item : (int)((unit - b_lo) / units), kvh = tiles == 1 ? item : item / tiles, tile = item - kvh * tiles;
-        const unsigned item_lo = b_lo + (unsigned)item * units, item_hi = item_lo + units, seg_hi = min(item_hi, mine_hi);
+        const int item = a.cluster ? cluster_item : (int)((unit - b_lo) / (units + extra)), kvh = tiles == 1 ? item : item / tiles, tile = item - kvh * tiles;
+        const unsigned item_lo = b_lo + (unsigned)item * (units + extra), item_hi = item_lo + units, seg_hi = min(item_hi, mine_hi);
+        if (!a.cluster && unit >= item_hi) {                 // the others have all its keys
+            unit = item_hi + extra;
+            if (unit >= mine_hi) return;
+            continue;
+        }
         const int key_lo = (int)(unit - item_lo) * kUnit, key_hi = min(len, (int)(seg_hi - item_lo) * kUnit);
         const int steps = max(0, (key_hi - key_lo + PSTEP - 1) / PSTEP), my_steps = (steps - warp + PW - 1) / PW;
         const int32_t* table = a.pages.table + (int64_t)b * a.pages.table_stride;
@@ -559,7 +570,7 @@ __global__ void __launch_bounds__(PW * 32, 2) paged_attn_kernel(const PagedAttnA
                 }
             }
         }
-        unit = seg_hi;
+        unit = seg_hi == item_hi ? item_hi + extra : seg_hi;
         if (a.cluster || unit >= mine_hi) return;
     }
 }
@@ -578,15 +589,14 @@ int paged_launch(PagedAttnArgs a, cudaStream_t stream) {
     const int R = a.n * a.group, tiles = (R + L::ROWS - 1) / L::ROWS;
     // r / group as the upper half of a product, exact while r group stays below 2^32
     a.group_inverse = a.group > 1 && (int64_t)R * a.group < ((int64_t)1 << 32) ? (unsigned)((((int64_t)1 << 32) + a.group - 1) / a.group) : 0u;
-    const int64_t units = (int64_t)std::max(1, (a.ctx_len + kUnit - 1) / kUnit) * tiles * a.batch * a.n_kv_heads;
+    const int64_t items = (int64_t)tiles * a.batch * a.n_kv_heads, u = std::max(1, (a.ctx_len + kUnit - 1) / kUnit), units = (u + kItemUnits<NT>) * items;
     if (units > INT_MAX) return -2;                        // counted in 32 bits
     // Two ways to share the work.  In one line of units every CTA has as much to do, but a result in parts costs a trip through memory and
     // back (5.5 us); a cluster for each item joins its CTAs' parts in 1.6 us, but is as long as its item (lengths on the device: a third longer than
     // an equal share, say).  A unit takes 0.37 us (1 us with 32 rows a CTA), or its share of the memory's bandwidth.  One token of one request, 4 KV heads,
     // 1664 keys: 9.1 us in one line, 7.5 in clusters; 5 rows of 7 requests, 251 keys: 10.5 and 6.7.
-    const int64_t items = (int64_t)tiles * a.batch * a.n_kv_heads, u = units / items;
     const int ctas = (int)std::min<int64_t>(kPlaces, std::max<int64_t>(1, units / kMinUnits));
-    auto unit_us = [&](int64_t active) { return std::max(NT == 4 ? 1.0 : 0.37, 1.5 * D / 128 * std::min<int64_t>(active, kPlaces) / kPlaces); };
+    auto unit_us = [&](int64_t active) { return std::max(NT > 2 ? 0.8 : 0.37, 1.5 * D / 128 * std::min<int64_t>(active, kPlaces) / kPlaces); };
     double best = (units + ctas - 1) / ctas * unit_us(ctas) + 5.5;
     a.cluster = 0;
     for (int c = 1; c <= 8 && c <= u && items * c <= 4 * kPlaces; c *= 2) {
@@ -615,6 +625,7 @@ int paged_dispatch(const PagedAttnArgs& a, cudaStream_t stream) {
     const int R = a.n * (a.n_heads / a.n_kv_heads);
     if (R <= 8) return paged_launch<D, 1>(a, stream);
     if (R <= 16) return paged_launch<D, 2>(a, stream);
+    if (R <= 24) return paged_launch<D, 3>(a, stream);
     return paged_launch<D, 4>(a, stream);
 }
 
