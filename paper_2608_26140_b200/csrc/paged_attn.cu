@@ -592,15 +592,20 @@ int paged_launch(PagedAttnArgs a, cudaStream_t stream) {
     const int64_t items = (int64_t)tiles * a.batch * a.n_kv_heads, u = std::max(1, (a.ctx_len + kUnit - 1) / kUnit), units = (u + kItemUnits<NT>) * items;
     if (units > INT_MAX) return -2;                        // counted in 32 bits
     // Two ways to share the work.  In one line of units every CTA has as much to do, but a result in parts costs a trip through memory and
-    // back (5.5 us); a cluster for each item joins its CTAs' parts in 1.6 us, but is as long as its item (lengths on the device: a third longer than
-    // an equal share, say).  A unit takes 0.37 us (1 us with 32 rows a CTA), or its share of the memory's bandwidth.  One token of one request, 4 KV heads,
-    // 1664 keys: 9.1 us in one line, 7.5 in clusters; 5 rows of 7 requests, 251 keys: 10.5 and 6.7.
+    // back (5 us, and the last CTA's time with each part); a cluster for each item joins its CTAs' parts in 1.6 us, but is as long as its item (lengths on
+    // the device: a quarter longer than an equal share, say).  A unit of 128 columns takes a CTA 0.8 us alone on its SM and 1.3 beside another, or its share
+    // of the memory's bandwidth.  One token of one request, 4 KV heads, 1664 keys: 9.1 us in one line, 7.5 in clusters; 5 rows of 7 requests, 251 keys: 10.5
+    // and 6.7; 32 rows of one request, 4 KV heads of 64, 8000 keys: 40 and 17; one token of 32 requests, 4 KV heads, 40 to 2000 keys: 15 and 15.
+    constexpr double kColumns = D / 128.0;
     const int ctas = (int)std::min<int64_t>(kPlaces, std::max<int64_t>(1, units / kMinUnits));
-    auto unit_us = [&](int64_t active) { return std::max(NT > 2 ? 0.8 : 0.37, 1.5 * D / 128 * std::min<int64_t>(active, kPlaces) / kPlaces); };
-    double best = (units + ctas - 1) / ctas * unit_us(ctas) + 5.5;
+    auto unit_us = [&](int64_t active) {
+        return kColumns * std::max(active > kPlaces / 2 ? 1.3 : 0.8, 1.5 * std::min<int64_t>(active, kPlaces) / kPlaces);
+    };
+    const double parts = ctas > items ? (double)ctas / items : 0.0;
+    double best = (units + ctas - 1) / ctas * unit_us(ctas) + 6.0 + parts * 0.28 * NT * kColumns;
     a.cluster = 0;
     for (int c = 1; c <= 8 && c <= u && items * c <= 4 * kPlaces; c *= 2) {
-        const double t = (items * c + kPlaces - 1) / kPlaces * ((u + c - 1) / c * unit_us(items * c) * (a.lens ? 1.3 : 1.0) + (c > 1 ? 1.6 : 0.0));
+        const double t = (items * c + kPlaces - 1) / kPlaces * ((u + c - 1) / c * unit_us(items * c) * (a.lens ? 1.25 : 1.0) + (c > 1 ? 2.6 : 1.0));
         if (t < best) {
             best = t;
             a.cluster = c;

@@ -92,3 +92,31 @@ def test_more_work_than_a_call_takes_is_refused():
     with pytest.raises(ab.AcacheError) as e:                  # 2^24 units x 2 tiles x 2 KV heads x 64 requests
         ctx.paged_attention(ctx.paged_kv(k, v, table), 1 << 30, q, torch.empty_like(q))
     assert e.value.status == ab.ERR_UNSUPPORTED_SHAPE and ctx.launch_count() == launches
+
+
+@pytest.mark.parametrize("heads,batch,n,ctx_len,page", [("mha32", 20, 1, 1500, 64), ("mha32", 12, 24, 1301, 16), ("mha4-64", 90, 20, 2001, 128), ("gqa4-64", 200, 12, 1100, 4), ("mha32", 9, 30, 640, 32)])
+@pytest.mark.parametrize("how", ["two long", "one long, last", "all short", "all empty"])
+def test_short_requests_between_long_ones(heads, batch, n, ctx_len, page, how):
+    """Pieces that hold many items, and pieces that begin behind an item's last key; a request of none too."""
+    H, hkv, d = HEADS[heads]
+    gen = torch.Generator(device=DEV).manual_seed(batch * 3 + n)
+    k, v, few = pool_of(gen, heads, 4, ctx_len, page)
+    table = few[torch.arange(batch, device=DEV) % 4].contiguous()
+    lens = np.array([(1, 40, 64, 130, 0, 65)[b % 6] for b in range(batch)])
+    if how == "two long":
+        lens[[2, batch // 2]] = ctx_len, ctx_len - 3
+    elif how == "one long, last":
+        lens[-1] = ctx_len
+    elif how == "all empty":
+        lens[:] = 0
+    q = random(gen, batch, n, H, d)
+    o, lse = torch.full_like(q, 7.0), torch.full((batch, n, H), 7.0, device=DEV)
+    ctx = context(heads, batch)
+    ctx.paged_attention(ctx.paged_kv(k, v, table), ctx_len, q, o, lse=lse, lens=torch.tensor(lens, dtype=torch.int32, device=DEV))
+    looked_at = sorted({0, 1, 2, 3, 4, 5, batch // 2, batch - 2, batch - 1})
+    at = torch.tensor(looked_at, device=DEV)
+    check(o[at], lse[at], reference(q[at], k, v, table[at], [np.arange(lens[b]) for b in looked_at]))
+    assert ctx.poll_status() == 0
+    empty = torch.tensor(lens == 0, device=DEV)
+    assert torch.equal(o[empty], torch.zeros_like(o[empty])) and torch.isneginf(lse[empty]).all()
+    assert torch.isfinite(lse[~empty]).all() and torch.isfinite(o).all()
