@@ -38,6 +38,7 @@ constexpr int kBins = 2048;
 constexpr int kFew = 512;                // tokens of a bin that are compared with one another
 constexpr int kTop = 1024, kList = 2048; // largest top_k whose tokens are sorted; room for them and those that come with them
 constexpr int kMaxCluster = 8;
+constexpr int kMostLogits = 65536;       // of a CTA: sums of as many parts of 16 bits fit in 32
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kSteps = 64, kCopies = 16; // a table of 2^(-j / 64), a copy for every lane of half a warp: no two in one bank
 
@@ -91,7 +92,7 @@ struct alignas(16) Scratch {
     uint32_t list_lo, list_hi;
     u64 reached[2];
 };
-struct Hist {                            // this CTA's counts, or its weights in three parts of 16 bits: sums of 2^15 of them fit in 32, whose atomics return nothing
+struct Hist {                            // this CTA's counts, or its weights in three parts of 16 bits, whose sums fit in 32 bits: atomics that return nothing
     uint32_t part[3][kBins];
 };
 union Work {                             // one after the other
@@ -106,9 +107,9 @@ union Work {                             // one after the other
 };
 
 // kHold: the row's part stays in shared memory; else it is read again (from L2) for every pass that needs it.
-template <class T, bool kHold>
-size_t sample_smem(int chunk, int cluster) {
-    return sizeof(Work) + sizeof(Scratch) + 2 * (kBins / cluster) * sizeof(Totals) + (kHold ? (chunk + 32) * sizeof(T) : 0);
+template <class T>
+size_t sample_smem(int chunk, int cluster, bool hold) {
+    return sizeof(Work) + sizeof(Scratch) + 2 * (kBins / cluster) * (sizeof(u64) + sizeof(uint32_t)) + (hold ? (chunk + 32) * sizeof(T) : 0);
 }
 
 template <class T, bool kHold>
@@ -120,8 +121,9 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
     Work& work = *reinterpret_cast<Work*>(smem);
     Hist& hist = work.hist;
     Scratch& s = *reinterpret_cast<Scratch*>(&work + 1);
-    Totals* totals = reinterpret_cast<Totals*>(&s + 1);                      // [2][slice]
-    T* held = reinterpret_cast<T*>(totals + 2 * slice);
+    u64* masses = reinterpret_cast<u64*>(&s + 1);            // running sums of this CTA's bins, and of a histogram of keys: [2][slice]
+    uint32_t* numbers = reinterpret_cast<uint32_t*>(masses + 2 * slice);
+    T* held = reinterpret_cast<T*>(numbers + 2 * slice);
     Inbox& box = s.box;
 
     auto clear = [&] {
@@ -204,8 +206,14 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
                 conf *= ex2f((conf_top - high) * kLog2e);
                 conf_top = high;
             }
+            float e[VEC];                                    // (added up by themselves: fewer roundings of the large sum)
 #pragma unroll
-            for (int k = 0; k < VEC; ++k) conf += ex2f((x[k] - conf_top) * kLog2e);
+            for (int k = 0; k < VEC; ++k) e[k] = ex2f((x[k] - conf_top) * kLog2e);
+#pragma unroll
+            for (int half = VEC / 2; half; half /= 2)
+#pragma unroll
+                for (int k = 0; k < half; ++k) e[k] += e[k + half];
+            conf += e[0];
         }
     };
     // Piece i is thread i % kThreads', here and in every later pass.
@@ -477,12 +485,11 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
 #pragma unroll
         for (int j = 1; j < kMine; ++j) m[j] += m[j - 1];
         const u64 run = running(peer == 0 ? m[kMine - 1] : 0ull);
-        Totals* of = totals + level * slice + i0;
         if (peer == 0) {
 #pragma unroll
             for (int j = 0; j < kMine; ++j) {
-                if (counts) of[j].count = (uint32_t)(run - m[kMine - 1] + m[j]);
-                else of[j].mass = run - m[kMine - 1] + m[j];
+                if (counts) numbers[level * slice + i0 + j] = (uint32_t)(run - m[kMine - 1] + m[j]);
+                else masses[level * slice + i0 + j] = run - m[kMine - 1] + m[j];
             }
         }
         if (warp == kWarps - 1) {
@@ -506,11 +513,11 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
             before.mass += t.mass;
         }
         if (rank == owner) {
-            const Totals* of = totals + level * slice;
+            const u64* mass = masses + level * slice;
+            const uint32_t* number = numbers + level * slice;
             for (int i = tid; i < slice; i += kThreads) {
-                Totals t0 = i > 0 ? of[i - 1] : Totals{0ull, 0u}, t1 = of[i];
-                t0 = Totals{before.mass + t0.mass, before.count + t0.count};
-                t1 = Totals{before.mass + t1.mass, before.count + t1.count};
+                const Totals t0{before.mass + (i > 0 ? mass[i - 1] : 0ull), before.count + (i > 0 ? number[i - 1] : 0u)};
+                const Totals t1{before.mass + mass[i], before.count + number[i]};
                 const u64 from_here = by_count ? (u64)t0.count : t0.mass, to_here = by_count ? (u64)t1.count : t1.mass;
                 if ((from_here < target || i == 0) && (target <= to_here || i == slice - 1))     // (whatever the target, some bin is found)
                     for (int r = 0; r < cluster; ++r) of_peer(&box, r)->place = Place{t0, t1, owner * slice + i};
@@ -825,7 +832,8 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
     // ---- among the tokens of the value, the one with that many before it ----
     // how many a warp's pieces have, round by round, which is the order of their indices
     const float value = value_of(token_key);
-    uint32_t* count_of = work.few.own;                       // [round][warp]
+    uint32_t* count_of = reinterpret_cast<uint32_t*>(&work); // [round][warp]
+    static_assert(((kMostLogits + 2 * VEC) / VEC / kThreads + 1) * kWarps * sizeof(uint32_t) <= sizeof(Work), "a word for every round and warp");
     const int rounds = (pieces + kThreads - 1) / kThreads;
     auto has = [&](int i) {                                  // tokens of piece i, a bit each
         uint32_t bits = 0u;
@@ -865,8 +873,10 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
     give(e0 + i * VEC - shift + __ffs(bits) - 1, value, prob, total);
 }
 
+int chunk_of(int vocab, int c) { return ((vocab + c - 1) / c + 63) / 64 * 64; }
+
 template <class T, bool kHold>
-int sample_launch(SampleArgs a, int most, cudaStream_t stream) {
+int sample_launch(SampleArgs a, int c, cudaStream_t stream) {
     static PerDevice<bool> ready;
     int device = 0;
     cudaGetDevice(&device);
@@ -877,17 +887,14 @@ int sample_launch(SampleArgs a, int most, cudaStream_t stream) {
             ok = cudaFuncSetAttribute(sample_kernel<T, kHold>, cudaFuncAttributeMaxDynamicSharedMemorySize, optin) == cudaSuccess;
         }))
         return -1;
-    auto chunk_of = [&](int c) { return ((a.vocab + c - 1) / c + 63) / 64 * 64; };
-    int c = 1;
-    while (c < kMaxCluster && chunk_of(c) > most) c *= 2;
     a.cluster = c;
-    a.chunk = chunk_of(c);
+    a.chunk = chunk_of(a.vocab, c);
     a.shift = 46;
     while (((int64_t)a.vocab << a.shift) > (int64_t)1 << 62) --a.shift;      // the sum of all weights stays below 2^63
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3(a.rows * c);
     cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = sample_smem<T, kHold>(a.chunk, c);
+    cfg.dynamicSmemBytes = sample_smem<T>(a.chunk, c, kHold);
     cfg.stream = stream;
     cudaLaunchAttribute at[2];
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -898,15 +905,23 @@ int sample_launch(SampleArgs a, int most, cudaStream_t stream) {
     cfg.numAttrs = 2;
     return cudaLaunchKernelEx(&cfg, sample_kernel<T, kHold>, a) == cudaSuccess ? 1 : -1;
 }
-// Logits of a CTA: up to 16384 for few rows, for which the time of one row counts (8 rows of 126464 bf16 32 us, and 43 with twice as many); twice as many
-// once their CTAs take more than a round, as what a step costs by itself is then spread over more of them (128 rows 101 us, and 143; 40 rows
-// 53 and 62).  So many fp32 logits would leave room for one CTA in an SM, and are read again from L2 (512 rows 241 us; held 328, held in halves 315).
+// CTAs of a row: as many as pay while there are SMs for them, one each down to 4096 logits a CTA, two an SM down to 8192 (clusters of 8 find no more than 256 places
+// at a time); us on average over settings, 32000 bf16 logits by 1, 2, 4, 8 CTAs: one row 22, 16, 13, 12; 37 rows 32, 24.6, 22.4, 32; 128 rows 32, 32, 42, 70.  With more
+// rows than that a step's cost is spread over up to 40960 logits a CTA, up to twice as many with 4 CTAs: 300 bf16 rows of 151936 by 8 CTAs 234, by 4 183, of 262144 312
+// and 261, fp32 379 and 321.  (Fewer CTAs wait for the row whose settings take longest: 512 fp32 rows of 126464 with settings of their own by 4 CTAs 236, by 2 254.)
+// The row stays in shared memory where that leaves room for two CTAs in an SM, or there are so few that no two need share one, else it is read again from L2: 300 bf16
+// rows of 8000 held with room for one CTA 45, read again 37; 5 fp32 rows of 151936 23.5 and 28, 16 rows 37.5 and 35.
 template <class T>
 int sample_dispatch(const SampleArgs& a, cudaStream_t stream) {
-    constexpr int kMost = 16384;
-    const int64_t ctas = (int64_t)a.rows * std::min<int64_t>(kMaxCluster, (a.vocab + kMost - 1) / kMost);
-    if (ctas <= 2 * 148) return sample_launch<T, true>(a, kMost, stream);
-    return sample_launch<T, sizeof(T) == 2>(a, 2 * kMost, stream);
+    constexpr size_t kHalfSm = 113 * 1024;
+    int c = 1;
+    for (; c < kMaxCluster; c *= 2) {
+        const int chunk = chunk_of(a.vocab, c);
+        const int64_t ctas = (int64_t)a.rows * 2 * c;
+        if (!(chunk > kMostLogits || (chunk > 40960 && (c < 4 || ctas <= 2 * 148)) || (chunk > 8192 && ctas <= 256) || (chunk > 4096 && ctas <= 128))) break;
+    }
+    const bool hold = sample_smem<T>(chunk_of(a.vocab, c), c, true) <= kHalfSm || (int64_t)a.rows * c <= 64;
+    return hold ? sample_launch<T, true>(a, c, stream) : sample_launch<T, false>(a, c, stream);
 }
 
 }  // namespace

@@ -1,4 +1,4 @@
-"""Sampling of so many rows that other kernels are used (bf16 rows in larger parts, fp32 rows that are read again instead of held), against 64 bits as
+"""Sampling of so many rows that other kernels are used (rows in larger parts, read again instead of held), against 64 bits as
 in test_gpu_sample.py."""
 import math
 
@@ -69,3 +69,33 @@ def test_a_row_gives_the_same_alone_and_among_others(ctx, dtype):  # noqa: F811
     for r in (0, 17, 63):
         ctx.sample_tokens(logits[r:r + 1], u[r:r + 1], one, prob=one_prob, temperature=T[r:r + 1], top_p=p[r:r + 1])
         assert one[0] == token[r] and one_prob[0] == prob[r]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,vocab", [(1, 8191), (5, 4097), (16, 32003), (33, 262144), (64, 50257), (65, 8200), (129, 40961), (257, 9000), (70, 151937), (130, 65537)])
+def test_rows_cut_in_every_way(ctx, rows, vocab, dtype):  # noqa: F811
+    rng = np.random.default_rng(rows)
+    logits, u = draw(rng, rows, vocab, dtype), rng.random(rows)
+    pick = lambda *v: [v[i % len(v)] for i in range(rows)]  # noqa: E731
+    check(ctx, logits, u, temperature=pick(1.0, 0.6, 2.5, 0.0), top_k=pick(0, 0, 30, 900, 3000), top_p=pick(1.0, 0.9, 0.4), min_p=pick(0.0, 0.0, 0.0, 0.05))
+
+
+@pytest.mark.parametrize("dtype,rows,vocab", [(torch.float32, 33, 262144), (torch.bfloat16, 300, 80000), (torch.float32, 257, 65536)])
+def test_sums_that_fill_their_words(ctx, dtype, rows, vocab):  # noqa: F811
+    """All but one token weigh a unit less than the largest, so that each of a weight's parts is as large as it can be; in whole numbers."""
+    shift = 46 if vocab <= 65536 else 45 if vocab <= 131072 else 44
+    logits = torch.zeros((rows, vocab), device=DEV, dtype=dtype)
+    logits[:, 77] = 1.0
+    temperature = torch.full((rows,), 2.0 ** shift, device=DEV)
+    unit, less = 1 << shift, (1 << shift) - 1                # 2^shift exp(-2^-shift) = 2^shift - 1 + 2^-(shift + 1)
+    u = torch.linspace(0.0, 1.0, rows, device=DEV)
+    u[-1] = 0.999999
+    token, prob = torch.empty(rows, dtype=torch.int32, device=DEV), torch.empty(rows, device=DEV)
+    ctx.sample_tokens(logits, u, token, prob=prob, temperature=temperature)
+    kept = unit + (vocab - 1) * less
+    for r, share in enumerate(u.tolist()):
+        drawn = int(share * float(kept))
+        i = 0 if drawn < unit else 1 + (drawn - unit) // less          # in the order of falling logits
+        assert int(token[r]) == (77 if i == 0 else i - 1 if i - 1 < 77 else i), (r, share)
+        assert abs(float(prob[r]) * kept / (unit if i == 0 else less) - 1) <= 2.0 ** -24
+    assert ctx.poll_status() == 0
