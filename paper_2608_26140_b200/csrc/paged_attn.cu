@@ -13,10 +13,10 @@
 // A warp streams 16 keys a step through a ring of its own in shared memory (cp.async, whole rows side by side, the page's number asked for two
 // steps ahead), swizzled so that ldmatrix meets different banks.  Keys that do not count are not read: their places are zero.
 //
-// Up to 8 rows HBM bounds it: one token of 2 requests over 65537 keys of 32 heads (2148 MB) 314 us, 6.8 TB/s; of 64 requests over up to 8191 keys of
-// 4 KV heads (794 MB) 127 us, 6.3 TB/s.  32 rows of 16 requests over 2560 keys of 32 heads, of which 2048 are the same pages for all, 108 us: 371 instructions
-// a step, two warps a scheduler that wait for one another's results (issue slots 33 %, tensor pipe 37 % busy), 6.2 TB/s from L2.  One token of one
-// request over 1664 keys 7.5 us: four trips to memory one behind the other (arguments, page, keys, result) and a cluster's exchange.
+// Up to 8 rows HBM bounds it: one token of 2 requests over 65537 keys of 32 heads (2148 MB) 305 us, 7.0 TB/s; of 64 requests over up to 8191 keys of
+// 4 KV heads (794 MB) 121 us, 6.6 TB/s.  32 rows of 16 requests over 2560 keys of 32 heads, of which 2048 are the same pages for all, 103 us (8 rows 57, 16 69, 24
+// 87): a step takes a warp 2000 clocks, two warps a scheduler that wait for their own results (issue slots 33 %, tensor pipe 41 % busy), 6.5 TB/s from L2; starts and ends
+// of items are a fifth.  The fragments of a step's next product are asked for before the last one's products (108 without).  One token of one request over 1664 keys 7.5 us: four trips to memory one behind the other (arguments, page, keys, result) and a cluster's exchange.
 #include <algorithm>
 #include <climits>
 
@@ -630,7 +630,7 @@ int paged_dispatch(const PagedAttnArgs& a, cudaStream_t stream) {
     const int R = a.n * (a.n_heads / a.n_kv_heads);
     if (R <= 8) return paged_launch<D, 1>(a, stream);
     if (R <= 16) return paged_launch<D, 2>(a, stream);
-    if (R <= 24) return paged_launch<D, 3>(a, stream);
+    if (R <= 24) return paged_launch<D, 3>(a, stream);       // (24 rows as 32: 100 us for 87)
     return paged_launch<D, 4>(a, stream);
 }
 
