@@ -473,8 +473,8 @@ acache_status acache_predict_commit(acache_ctx *ctx, const void *h, int32_t h_ro
                                     int32_t *commit, acache_stream_t stream);
 
 /* acache_predict_commit with tokens drawn from the logits (acache_sample_tokens) instead of the arg max; the commit rule is the same, on the drawn
- * token's confidence.  logits: DEVICE fp32 [B * n_blk, vocab] out (the LM head's sums, not rounded further); how: a setting per row, or with
- * rows_per_setting = n_blk per request; u: DEVICE fp32 [B, n_blk].  With T = 0 token and commit are acache_predict_commit's. */
+ * token's confidence; a row without a token (-1) is not committed.  logits: DEVICE fp32 [B * n_blk, vocab] out (the LM head's sums, not rounded
+ * further); how: a setting per row, or with rows_per_setting = n_blk per request; u: DEVICE fp32 [B, n_blk].  With T = 0 token and commit are acache_predict_commit's. */
 acache_status acache_predict_sample(acache_ctx *ctx, const void *h, int32_t h_rows, const int32_t *block_rows, int32_t batch, int32_t n_blk,
                                     const void *final_norm_g, const void *w_lm, int32_t vocab, float *logits, const acache_sampling *how,
                                     const float *u, float threshold, int32_t *token, float *confidence, int32_t *commit,
@@ -592,9 +592,11 @@ acache_status acache_probe_select(acache_ctx *ctx, int32_t n_layers, const acach
 /* Eq. 3 applied to the sequence: among the block's positions block_pos[b, i] whose token id is still
  * mask_id, those with confidence[b, i] > threshold receive token[b, i]; if a request has masked
  * positions but none qualifies, its single most confident masked position does (lowest i on ties).
- * Positions already decoded are left alone whatever their confidence.
+ * Positions already decoded are left alone whatever their confidence, and so are those without a
+ * token (token[b, i] below 0), which stay masked.
  *   token_ids: DEVICE int32 [B, ctx_len], updated in place; block_pos: DEVICE int32 [B, n_blk] absolute
- *   positions; token, confidence: DEVICE [B, n_blk] as written by acache_predict_commit for those rows;
+ *   positions; token, confidence: DEVICE [B, n_blk] as written by acache_predict_commit or
+ *   acache_predict_sample for those rows;
  *   remaining: DEVICE int32 [B], masked positions left in the block after the update.
  * A position outside [0, ctx_len) raises ACACHE_FLAG_BAD_INDEX and is skipped. */
 acache_status acache_commit_update(acache_ctx *ctx, int32_t *token_ids, int32_t ctx_len, const int32_t *block_pos,

@@ -1055,7 +1055,7 @@ acache_status predict_impl(acache_ctx* ctx, const void* h, int32_t h_rows, const
     if (how) {
         const acache_status s = run_sample(ctx, logits, ACACHE_F32, batch * n_blk, vocab, vocab, how, u, token, nullptr, confidence, stream);
         if (s != ACACHE_OK) return s;
-        nl = launch_commit(confidence, batch, n_blk, threshold, commit, stream);
+        nl = launch_commit(token, confidence, batch, n_blk, threshold, commit, stream);
     } else {
         nl = launch_predict_commit(g, batch, n_blk, threshold, token, confidence, commit, stream);
     }

@@ -897,22 +897,24 @@ __global__ void __launch_bounds__(LR_THREADS) logit_reduce_kernel(const GemmArgs
 }
 
 // One warp per request: commit the rows above the threshold, or the single most confident row
-// (lowest index on ties) if there is none.
-__global__ void __launch_bounds__(32) commit_kernel(const float* __restrict__ confidence, int n_blk, float threshold,
-                                                    int32_t* __restrict__ commit) {
+// (lowest index on ties) if there is none; never a row that has no token (-1).
+__global__ void __launch_bounds__(32) commit_kernel(const int32_t* __restrict__ token, const float* __restrict__ confidence, int n_blk,
+                                                    float threshold, int32_t* __restrict__ commit) {
     pdl_wait();
     pdl_launch_dependents();
     const int b = blockIdx.x, lane = threadIdx.x;
+    const int32_t* t = token + (int64_t)b * n_blk;
     const float* c = confidence + (int64_t)b * n_blk;
     int32_t* out = commit + (int64_t)b * n_blk;
     int any = 0, best = 0x7fffffff;
     float bestc = -INFINITY;
     for (int i = lane; i < n_blk; i += 32) {
         const float v = __ldcg(c + i);
-        const int f = v > threshold;
+        const bool has = __ldcg(t + i) >= 0;
+        const int f = has && v > threshold;
         out[i] = f;
         any |= f;
-        if (v > bestc) { bestc = v; best = i; }
+        if (has && v > bestc) { bestc = v; best = i; }
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
@@ -1232,13 +1234,15 @@ int launch_predict_commit(const GemmArgs& g, int batch, int n_blk, float thresho
     if (g.M == 0) return 0;
     const GemmLaunch gl = plan_gemm(g);
     if (launch_pdl(logit_reduce_kernel, dim3(g.M), dim3(LR_THREADS), 0, stream, g, gl.p, gl.split, token, confidence) != cudaSuccess) return -1;
-    const int nl = launch_commit(confidence, batch, n_blk, threshold, commit, stream);
+    const int nl = launch_commit(token, confidence, batch, n_blk, threshold, commit, stream);
     return nl < 0 ? -1 : 1 + nl;
 }
 
-int launch_commit(const float* confidence, int batch, int n_blk, float threshold, int32_t* commit, cudaStream_t stream) {
+int launch_commit(const int32_t* token, const float* confidence, int batch, int n_blk, float threshold, int32_t* commit,
+                  cudaStream_t stream) {
     if (batch == 0 || n_blk == 0) return 0;
-    return launch_pdl(commit_kernel, dim3(batch), dim3(32), 0, stream, confidence, n_blk, threshold, commit) == cudaSuccess ? 1 : -1;
+    const cudaError_t e = launch_pdl(commit_kernel, dim3(batch), dim3(32), 0, stream, token, confidence, n_blk, threshold, commit);
+    return e == cudaSuccess ? 1 : -1;
 }
 
 }  // namespace acache

@@ -173,8 +173,9 @@ int launch_gemm(const GemmArgs& g, cudaStream_t stream);      // kernels launche
 // commit[b, i] = conf > threshold, and if no row of request b qualifies, its most confident row.
 int launch_predict_commit(const GemmArgs& g, int batch, int n_blk, float threshold, int32_t* token, float* confidence,
                           int32_t* commit, cudaStream_t stream);
-// The commit rule alone; kernels launched, or -1.
-int launch_commit(const float* confidence, int batch, int n_blk, float threshold, int32_t* commit, cudaStream_t stream);
+// The commit rule alone, a row without a token (-1) left out; kernels launched, or -1.
+int launch_commit(const int32_t* token, const float* confidence, int batch, int n_blk, float threshold, int32_t* commit,
+                  cudaStream_t stream);
 
 // ---- attn.cu ----------------------------------------------------------------------------
 struct AttnArgs {

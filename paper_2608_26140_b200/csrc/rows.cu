@@ -154,7 +154,7 @@ __global__ void __launch_bounds__(32) commit_update_kernel(int32_t* __restrict__
     float best_c = -INFINITY;
     for (int i0 = 0; i0 < n_blk; i0 += 32) {
         const int i = i0 + lane;
-        bool masked = false, hit = false;
+        bool masked = false, can = false, hit = false;       // can: masked, and there is a token for it
         float c = -INFINITY;
         int pos = 0;
         if (i < n_blk) {
@@ -164,15 +164,17 @@ __global__ void __launch_bounds__(32) commit_update_kernel(int32_t* __restrict__
             } else {
                 masked = ids[pos] == mask_id;
                 c = confidence[(int64_t)b * n_blk + i];
-                hit = masked && c > threshold;
-                if (hit) ids[pos] = token[(int64_t)b * n_blk + i];
+                const int32_t tok = token[(int64_t)b * n_blk + i];
+                can = masked && tok >= 0;
+                hit = can && c > threshold;
+                if (hit) ids[pos] = tok;
             }
         }
         n_masked += __popc(__ballot_sync(0xffffffffu, masked));
         n_commit += __popc(__ballot_sync(0xffffffffu, hit));
-        // most confident masked row of this chunk, lowest index on ties
-        float cc = masked ? c : -INFINITY;
-        int ci = masked ? i : 0x7fffffff;
+        // most confident masked row of this chunk that has a token, lowest index on ties
+        float cc = can ? c : -INFINITY;
+        int ci = can ? i : 0x7fffffff;
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) {
             const float oc = __shfl_xor_sync(0xffffffffu, cc, o);
