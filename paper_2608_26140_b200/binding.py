@@ -231,6 +231,16 @@ def _at(t, dtype, shape, device):
     return t.data_ptr()
 
 
+def _room(t, dtype, n, device, name):
+    """The address of a contiguous tensor of that type with room for n elements on that GPU.  None and addresses pass: the call itself refuses
+    a NULL where it needs more, and an address is the caller's affair."""
+    if t is None or isinstance(t, int):
+        return t
+    if t.dtype is not dtype or t.get_device() != device or t.numel() < n or not t.is_contiguous():
+        raise ValueError(f"{name}: a tensor {tuple(t.shape)} of {t.dtype} on {t.device} where a contiguous one of {n} or more of {dtype} on GPU {device} is wanted")
+    return t.data_ptr()
+
+
 def _dense(t, strides):
     """All dimensions but the first as in a contiguous tensor; the stride of a dimension of one element says nothing."""
     return t.numel() == 0 or all(n == 1 or have == want for n, have, want in zip(t.shape[1:], t.stride()[1:], strides))
@@ -579,15 +589,19 @@ class Context:
 
     def predict_sample(self, h, h_rows, block_rows, batch, n_blk, final_norm_g, w_lm, vocab, logits, u, threshold, token, confidence, commit,
                        temperature=None, top_k=None, top_p=None, min_p=None, rows_per_setting=1):
-        """predict_commit with drawn tokens; logits: fp32 [batch * n_blk, vocab] out; u: fp32 [batch, n_blk]; settings as sample_tokens."""
-        import torch
+        """predict_commit with drawn tokens; logits: fp32 [batch * n_blk, vocab] out; u: fp32 [batch, n_blk]; settings as sample_tokens.  h: bf16
+        [batch, h_rows, D]; block_rows, token, commit: int32, confidence: fp32 [batch, n_blk]; final_norm_g: bf16 [D]; w_lm: bf16 [vocab, D]."""
+        bf16, f32, i32 = self.dtypes
         rows = batch * n_blk
         device = self._on_device()
-        logits, u = _at(logits, torch.float32, (rows, vocab), device), _at(u.view(-1), torch.float32, (rows,), device)
+        logits, u = _at(logits, f32, (rows, vocab), device), _at(u.view(-1), f32, (rows,), device)
         how = self._sampling(rows, device, temperature, top_k, top_p, min_p, rows_per_setting)
-        self._check(self.lib.acache_predict_sample(self.h, _ptr(h), h_rows, _ptr(block_rows), batch, n_blk, _ptr(final_norm_g), _ptr(w_lm), vocab,
-                                                   logits, how, u, float(threshold), _ptr(token), _ptr(confidence), _ptr(commit),
-                                                   _stream()))
+        D = self.desc.hidden
+        self._check(self.lib.acache_predict_sample(
+            self.h, _room(h, bf16, batch * h_rows * D, device, "h"), h_rows, _room(block_rows, i32, rows, device, "block_rows"), batch, n_blk,
+            _room(final_norm_g, bf16, D, device, "final_norm_g"), _room(w_lm, bf16, vocab * D, device, "w_lm"), vocab, logits, how, u, float(threshold),
+            _room(token, i32, rows, device, "token"), _room(confidence, f32, rows, device, "confidence"), _room(commit, i32, rows, device, "commit"),
+            _stream()))
 
     def _sampling(self, rows, device, temperature, top_k, top_p, min_p, rows_per_setting):
         bf16, f32, i32 = self.dtypes

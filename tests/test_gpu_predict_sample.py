@@ -61,3 +61,19 @@ def test_a_row_without_a_token_is_not_committed(n_blk, threshold):
     assert torch.equal(ids[:, 1::2], torch.where(want, token, 999)) and (ids[:, ::2] == 999).all()
     assert torch.equal(left, (n_blk - want.sum(1)).to(torch.int32))
     assert head.ctx.poll_status() == 0
+
+
+def test_tensors_that_do_not_fit_are_refused_before_any_launch():
+    head = Head(640, 2, 3, 5)
+    token, conf, commit = head.out()
+    good = dict(h=head.h, h_rows=3, block_rows=head.rows, batch=2, n_blk=3, final_norm_g=head.gain, w_lm=head.w_lm, vocab=640, logits=head.logits, u=head.u, threshold=0.5,
+                token=token, confidence=conf, commit=commit)
+    launches = head.ctx.launch_count()
+    for bad in (dict(token=token.long()), dict(token=token.cpu()), dict(token=token[:1]), dict(confidence=conf.double()), dict(confidence=conf.view(-1)[:5]), dict(commit=commit[:1]),
+                dict(commit=commit.cpu()), dict(h=head.h.cpu()), dict(h=head.h.float()), dict(h=head.h[:1]), dict(h=head.h.transpose(0, 1)), dict(block_rows=head.rows.long()),
+                dict(block_rows=head.rows[:1]), dict(final_norm_g=head.gain.float()), dict(w_lm=head.w_lm[:639]), dict(w_lm=head.w_lm.cpu())):
+        with pytest.raises(ValueError):
+            head.ctx.predict_sample(**{**good, **bad})
+    assert head.ctx.launch_count() == launches
+    head.ctx.predict_sample(**good)
+    assert head.ctx.launch_count() > launches and head.ctx.poll_status() == 0 and (token >= 0).all()
