@@ -44,6 +44,8 @@ class ModelDesc(C.Structure):
 class LayerWeights(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("attn_norm_g", "wq", "wk", "wv", "bq", "bk", "bv", "wo",
                                           "mlp_norm_g", "w_gate", "w_up", "w_down")]
+    tensors = None      # by name, as Context.weights was given them
+    fit = None          # the layer shape and device that they were found to fit
 
 
 class KV(C.Structure):
@@ -75,6 +77,7 @@ class Request(C.Structure):
                 ("affix_len", C.c_int32), ("masked_pos", C.c_void_p), ("n_masked", C.c_int32),
                 ("extra_rows", C.c_void_p), ("n_extra", C.c_int32), ("rope_cos", C.c_void_p),
                 ("rope_sin", C.c_void_p), ("token_ids", C.c_void_p), ("n_embed", C.c_int32)]
+    tensors = None      # extra_rows, rope_cos, rope_sin, token_ids, as Context.request was given them
 
 
 class AcacheError(RuntimeError):
@@ -320,6 +323,7 @@ class Context:
         lw = LayerWeights()
         for name, _ in LayerWeights._fields_:
             setattr(lw, name, _ptr(w.get(name)))
+        lw.tensors = {name: w.get(name) for name, _ in LayerWeights._fields_}
         return lw
 
     @staticmethod
@@ -386,8 +390,10 @@ class Context:
                 token_ids=None, n_embed=0) -> Request:
         nm = 0 if masked_pos is None else int(masked_pos.shape[1])
         ne = 0 if extra_rows is None else int(extra_rows.shape[1])
-        return Request(batch, ctx_len, affix_start, affix_len, _ptr(masked_pos) if nm else None, nm,
-                       _ptr(extra_rows) if ne else None, ne, _ptr(rope_cos), _ptr(rope_sin), _ptr(token_ids), n_embed)
+        req = Request(batch, ctx_len, affix_start, affix_len, _ptr(masked_pos) if nm else None, nm,
+                      _ptr(extra_rows) if ne else None, ne, _ptr(rope_cos), _ptr(rope_sin), _ptr(token_ids), n_embed)
+        req.tensors = extra_rows if ne else None, rope_cos, rope_sin, token_ids
+        return req
 
     # ---- entry points ----
     def launch_count(self) -> int:
@@ -557,13 +563,23 @@ class Context:
             self._check(st)
 
     def recompute_paged(self, w: LayerWeights, req: Request, cache: PagedKV, x, x_is_compact, anchor_idx, k, y, lens=None):
-        """The rows of R through the layer, over a cache in pages; lens: int32 [B], the tokens of each request with them."""
-        import torch
-        device = self._pages_fit(cache, req.batch)
+        """The rows of R through the layer, over a cache in pages; lens: int32 [B], the tokens of each request with them.  x: bf16 [B, ctx_len, D], or
+        [B, k + e, D] if x_is_compact, or the table that the request's token_ids look up; anchor_idx: int32 [B, k]; y: bf16 [B, k + e, D]."""
+        bf16, f32, i32 = self.dtypes
+        B = req.batch
+        device = self._pages_fit(cache, B)
         if lens is not None:
-            lens = _at(lens, torch.int32, (req.batch,), device)
-        self._check(self.lib.acache_recompute_paged(self.h, C.byref(w), C.byref(req), C.byref(cache), _ptr(x), int(x_is_compact), _ptr(anchor_idx), k,
-                                                    _ptr(lens), _ptr(y), _stream()))
+            lens = _at(lens, i32, (B,), device)
+        self._weights_fit(w, device)
+        self._request_fits(req, device, not x_is_compact)
+        D, rows = self.desc.hidden, k + req.n_extra
+        x = _room(x, bf16, (B * rows if x_is_compact else req.n_embed if req.token_ids else B * req.ctx_len) * D, device, "x")
+        if k > 0:
+            anchor_idx = _room(anchor_idx, i32, B * k, device, "anchor_idx")
+        if k <= 0 or anchor_idx is not None:                     # (else the call is refused for the anchors)
+            y = _room(y, bf16, B * rows * D, device, "y")
+        self._check(self.lib.acache_recompute_paged(self.h, C.byref(w), C.byref(req), C.byref(cache), x, int(x_is_compact), _ptr(anchor_idx), k, lens,
+                                                    _ptr(y), _stream()))
 
     def sample_tokens(self, logits, u, token, prob=None, confidence=None, temperature=None, top_k=None, top_p=None, min_p=None, rows_per_setting=1):
         """logits: bf16 or fp32 [rows, vocab] (rows may lie apart); u: fp32 [rows]; token: int32 [rows]; prob, confidence: fp32 [rows]; temperature,
@@ -641,6 +657,35 @@ class Context:
             raise ValueError(f"pages of {m[0]} requests, {m[1]} KV heads of {m[2]}, {'' if m[3] else 'not all '}on GPU {m[4]}, "
                              f"for {batch} requests and {self.heads[1]} KV heads of {self.heads[2]} on GPU {device}")
         return device
+
+    def _weights_fit(self, w, device):
+        """As _pages_fit, for weights that Context.weights made (addresses put in by hand are the caller's affair)."""
+        d, bf16 = self.desc, self.dtypes[0]
+        key = (d.hidden, d.ffn, d.qkv_bias, self.heads, device)
+        if w.tensors is None or w.fit == key:
+            return
+        H, hkv, dim = self.heads
+        D, q, kv = d.hidden, H * dim, hkv * dim
+        sizes = dict(attn_norm_g=D, wq=q * D, wk=kv * D, wv=kv * D, wo=D * q, mlp_norm_g=D, w_gate=d.ffn * D, w_up=d.ffn * D, w_down=D * d.ffn)
+        if d.qkv_bias:
+            sizes.update(bq=q, bk=kv, bv=kv)
+        for name, n in sizes.items():
+            t = w.tensors.get(name)
+            if t is not None and getattr(w, name) == _ptr(t):
+                _room(t, bf16, n, device, name)
+        w.fit = key
+
+    def _request_fits(self, req, device, looks_up):
+        """As _weights_fit, for a request; looks_up: whether token_ids are used."""
+        if req.tensors is None:
+            return
+        bf16, f32, i32 = self.dtypes
+        extra, cos, sin, ids = req.tensors
+        table = req.ctx_len * (self.heads[2] // 2)
+        for t, name, kind, n in ((extra, "extra_rows", i32, req.batch * req.n_extra), (cos, "rope_cos", f32, table), (sin, "rope_sin", f32, table),
+                                 (ids if looks_up else None, "token_ids", i32, req.batch * req.ctx_len)):
+            if t is not None and getattr(req, name) == _ptr(t):
+                _room(t, kind, n, device, name)
 
     def _cache_fits(self, cache, batch):
         """What a call would read or write past the cache's tensors for (a KV8 filled in by hand is the caller's affair)."""
