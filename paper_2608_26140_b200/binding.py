@@ -62,6 +62,7 @@ class PagedKV(C.Structure):
     _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("page_stride", C.c_int64), ("n_pages", C.c_int32), ("page", C.c_int32),
                 ("table", C.c_void_p), ("table_stride", C.c_int32)]
     made_of = None      # of the tensors that Context.paged_kv made it over: requests, KV heads, head dimension, all on one GPU, which
+    tensors = None      # those tensors: the pools and the table live as long as this does
 
 
 class Rows(C.Structure):
@@ -361,7 +362,7 @@ class Context:
 
     def paged_kv(self, k_pages, v_pages, table) -> PagedKV:
         """Cache in pages over bf16 pools [n_pages, Hkv, page, d] and a table int32 [B, entries]: the pages of each request in order.  Pages may
-        lie further apart than they take."""
+        lie further apart than they take.  The cache keeps the three tensors."""
         import torch
         n_pages, hkv, page, d = k_pages.shape
         for p in (k_pages, v_pages):
@@ -374,6 +375,7 @@ class Context:
         c = PagedKV(_ptr(k_pages), _ptr(v_pages), k_pages.stride(0) if n_pages > 1 else hkv * page * d, n_pages, page, _ptr(table), table.shape[1])
         devices = {t.get_device() for t in (k_pages, v_pages, table)}
         c.made_of = (table.shape[0], hkv, d, all(t.is_cuda for t in (k_pages, v_pages, table)) and len(devices) == 1, devices.pop())
+        c.tensors = (k_pages, v_pages, table)
         return c
 
     @staticmethod
