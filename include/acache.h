@@ -428,6 +428,7 @@ acache_status acache_paged_append(acache_ctx *ctx, acache_paged_kv *kv, int32_t 
  * taken as the nearer end; so does a page that is none of the pool's, whose keys do not exist.
  *   q, o: DEVICE bf16 [B, n_rows, H, d], any number of rows (every 32 rows of a KV head, n_rows H / Hkv, read the keys once); lse: DEVICE fp32
  *   [B, n_rows, H], natural logarithm, may be NULL (with it, results over several caches can be put together).
+ * Tiles of 32 rows times KV heads times requests times (ctx_len / 64 + 6) have to stay below 2^31 (ACACHE_ERR_UNSUPPORTED_SHAPE).
  * Logits, softmax and sums in fp32; a probability is rounded to bf16 where it meets its value. */
 acache_status acache_paged_attention(acache_ctx *ctx, const acache_paged_kv *kv, int32_t batch, int32_t n_rows, int32_t ctx_len,
                                      const void *q, const int32_t *lens, const uint32_t *key_drop, void *o, float *lse,

@@ -225,6 +225,14 @@ bool rows_ok(const acache_ctx* c, const acache_rows* r, int heads, int32_t batch
            (n <= 1 || r->row_stride >= (int64_t)heads * c->d.head_dim);
 }
 
+acache_status check_paged_attention(acache_ctx* c, int32_t batch, int32_t n, int32_t ctx_len) {
+    const acache_model_desc& d = c->d;
+    if (n < 0 || (int64_t)n * (d.n_heads / d.n_kv_heads) > (1 << 30)) return fail(c, ACACHE_ERR_INVALID_ARG, "n_rows %d is negative or too large", n);
+    if (!paged_attention_fits(batch, n, ctx_len, d.n_heads, d.n_kv_heads))
+        return fail(c, ACACHE_ERR_UNSUPPORTED_SHAPE, "keys / 64 times row tiles, KV heads and requests do not fit in 31 bits");
+    return ACACHE_OK;
+}
+
 acache_status run_paged_attention(acache_ctx* c, const acache_paged_kv* kv, int32_t batch, int32_t n, int32_t ctx_len, const void* q, void* o,
                                   float* lse, const int32_t* lens, const uint32_t* key_drop, cudaStream_t st) {
     const acache_model_desc& d = c->d;
@@ -238,7 +246,6 @@ acache_status run_paged_attention(acache_ctx* c, const acache_paged_kv* kv, int3
     a.arrived = wsp<unsigned int>(c, c->o_arrived);
     a.status = wsp<uint32_t>(c, c->o_status);
     const int nl = launch_paged_attention(a, st);
-    if (nl == -2) return fail(c, ACACHE_ERR_UNSUPPORTED_SHAPE, "keys / 64 times row tiles, KV heads and requests do not fit in 31 bits");
     if (nl < 0) return check_cuda(c, "paged attention") == ACACHE_OK ? fail(c, ACACHE_ERR_CUDA, "paged attention launch failed") : ACACHE_ERR_CUDA;
     c->launches += nl;
     return check_cuda(c, "paged attention");
@@ -980,8 +987,7 @@ acache_status acache_paged_attention(acache_ctx* ctx, const acache_paged_kv* kv,
     if (!ctx) return ACACHE_ERR_INVALID_ARG;
     acache_status s = check_paged(ctx, kv, batch, ctx_len);
     if (s != ACACHE_OK) return s;
-    if (n_rows < 0 || (int64_t)n_rows * (ctx->d.n_heads / ctx->d.n_kv_heads) > (1 << 30))
-        return fail(ctx, ACACHE_ERR_INVALID_ARG, "n_rows %d is negative or too large", n_rows);
+    if ((s = check_paged_attention(ctx, batch, n_rows, ctx_len)) != ACACHE_OK) return s;
     if (batch == 0 || n_rows == 0) return ACACHE_OK;
     if (!q || !o || !aligned16(q) || !aligned16(o)) return fail(ctx, ACACHE_ERR_INVALID_ARG, "q / o NULL or misaligned");
     return run_paged_attention(ctx, kv, batch, n_rows, ctx_len, q, o, lse, lens, key_drop, stream);
@@ -994,6 +1000,7 @@ acache_status acache_recompute_paged(acache_ctx* ctx, const acache_layer_weights
     acache_status s = check_request(ctx, req, nullptr, k, true);
     if (s != ACACHE_OK) return s;
     if ((s = check_paged(ctx, kv, req->batch, req->ctx_len)) != ACACHE_OK) return s;
+    if ((s = check_paged_attention(ctx, req->batch, k + req->n_extra, req->ctx_len)) != ACACHE_OK) return s;
     if ((s = check_weights(ctx, w, false)) != ACACHE_OK) return s;
     if (req->batch * (k + req->n_extra) == 0) return ACACHE_OK;
     if (!x || !y || !aligned16(x) || !aligned16(y)) return fail(ctx, ACACHE_ERR_INVALID_ARG, "x / y NULL or misaligned");

@@ -307,7 +307,8 @@ struct PagedAttnArgs {
     int cluster;                    // CTAs of an item, in a cluster; 0: items in one line, cut into equal pieces
 };
 size_t paged_attention_scratch_bytes(int head_dim);
-int launch_paged_attention(const PagedAttnArgs& a, cudaStream_t stream);    // kernels launched, -1: failed, -2: too much for one call
+bool paged_attention_fits(int batch, int n, int ctx_len, int n_heads, int n_kv_heads);     // whether its units can be counted in 32 bits
+int launch_paged_attention(const PagedAttnArgs& a, cudaStream_t stream);    // kernels launched, or -1; for what fits
 
 // ---- sample.cu ----------------------------------------------------------------------------
 constexpr int kSampleMaxVocab = 1 << 18;

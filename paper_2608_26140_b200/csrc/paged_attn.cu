@@ -590,7 +590,6 @@ int paged_launch(PagedAttnArgs a, cudaStream_t stream) {
     // r / group as the upper half of a product, exact while r group stays below 2^32
     a.group_inverse = a.group > 1 && (int64_t)R * a.group < ((int64_t)1 << 32) ? (unsigned)((((int64_t)1 << 32) + a.group - 1) / a.group) : 0u;
     const int64_t items = (int64_t)tiles * a.batch * a.n_kv_heads, u = std::max(1, (a.ctx_len + kUnit - 1) / kUnit), units = (u + kItemUnits<NT>) * items;
-    if (units > INT_MAX) return -2;                        // counted in 32 bits
     // Two ways to share the work.  In one line of units every CTA has as much to do, but a result in parts costs a trip through memory and
     // back (5 us, and the last CTA's time with each part); a cluster for each item joins its CTAs' parts in 1.6 us, but is as long as its item (lengths on
     // the device: a quarter longer than an equal share, say).  A unit of 128 columns takes a CTA 0.8 us alone on its SM and 1.3 beside another, or its share
@@ -625,18 +624,32 @@ int paged_launch(PagedAttnArgs a, cudaStream_t stream) {
     cfg.numAttrs = a.cluster > 1 ? 2 : 1;
     return cudaLaunchKernelEx(&cfg, paged_attn_kernel<D, NT>, a) == cudaSuccess ? 1 : -1;
 }
+// row tiles of 8 in a CTA for R rows of a KV head (24 rows as 32: 100 us for 87)
+int tile_of(int64_t R) { return R <= 8 ? 1 : R <= 16 ? 2 : R <= 24 ? 3 : 4; }
+
 template <int D>
 int paged_dispatch(const PagedAttnArgs& a, cudaStream_t stream) {
-    const int R = a.n * (a.n_heads / a.n_kv_heads);
-    if (R <= 8) return paged_launch<D, 1>(a, stream);
-    if (R <= 16) return paged_launch<D, 2>(a, stream);
-    if (R <= 24) return paged_launch<D, 3>(a, stream);       // (24 rows as 32: 100 us for 87)
-    return paged_launch<D, 4>(a, stream);
+    switch (tile_of((int64_t)a.n * (a.n_heads / a.n_kv_heads))) {
+        case 1: return paged_launch<D, 1>(a, stream);
+        case 2: return paged_launch<D, 2>(a, stream);
+        case 3: return paged_launch<D, 3>(a, stream);
+        default: return paged_launch<D, 4>(a, stream);
+    }
 }
 
 }  // namespace
 
 size_t paged_attention_scratch_bytes(int head_dim) { return (size_t)2 * kPlaces * 32 * (head_dim + 1) * sizeof(float); }
+
+bool paged_attention_fits(int batch, int n, int ctx_len, int n_heads, int n_kv_heads) {
+    const int64_t R = (int64_t)n * (n_heads / n_kv_heads);
+    const int rows = 8 * tile_of(R);
+    int64_t units = (R + rows - 1) / rows * batch;
+    if (units > INT_MAX) return false;                       // (step by step: no product passes 64 bits)
+    units *= n_kv_heads;
+    if (units > INT_MAX) return false;
+    return units * (std::max(1, (ctx_len + kUnit - 1) / kUnit) + (rows > 16 ? kItemUnits<4> : kItemUnits<1>)) <= INT_MAX;
+}
 
 int launch_paged_attention(const PagedAttnArgs& a, cudaStream_t stream) {
     if (a.batch == 0 || a.n == 0) return 0;
