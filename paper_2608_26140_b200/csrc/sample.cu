@@ -67,7 +67,7 @@ struct Place {                           // a bin, what is before it, and with i
 };
 struct Found {                           // where a search ended: a value, how many have it, its weight, and what comes before it
     uint32_t key, equal;
-    uint32_t count;
+    uint32_t count;                      // (of a search by count only)
     u64 weight, mass;
 };
 // What the CTAs of a cluster tell one another, each in the others' memory before a barrier: reading there takes a thousand clocks.
@@ -503,21 +503,23 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
         cluster_sync_all();
     };
 
-    // the first bin at which the running count (or weight), `before` the first one, comes to `target`: the CTA that has it tells the others
-    auto locate = [&](int level, bool by_count, u64 target, Totals before) -> Place {
+    // The first bin at which the running count (or weight), `before` the first one, comes to `target`: the CTA that has it tells the others.  The sum that
+    // is not searched by is there only if `both` have been added up; else it is not looked at, and the place's is zero.
+    auto locate = [&](int level, bool by_count, bool both, u64 target, Totals before) -> Place {
+        const bool counts = by_count || both, weights = !by_count || both;
         int owner = 0;
         for (; owner < cluster - 1; ++owner) {
-            const Totals t = box.slice[level][owner];
-            if ((by_count ? (u64)(before.count + t.count) : before.mass + t.mass) >= target) break;
-            before.count += t.count;
-            before.mass += t.mass;
+            const Totals& t = box.slice[level][owner];
+            const Totals with{before.mass + (weights ? t.mass : 0ull), before.count + (counts ? t.count : 0u)};
+            if ((by_count ? (u64)with.count : with.mass) >= target) break;
+            before = with;
         }
         if (rank == owner) {
             const u64* mass = masses + level * slice;
             const uint32_t* number = numbers + level * slice;
             for (int i = tid; i < slice; i += kThreads) {
-                const Totals t0{before.mass + (i > 0 ? mass[i - 1] : 0ull), before.count + (i > 0 ? number[i - 1] : 0u)};
-                const Totals t1{before.mass + mass[i], before.count + number[i]};
+                const Totals t0{before.mass + (weights && i > 0 ? mass[i - 1] : 0ull), before.count + (counts && i > 0 ? number[i - 1] : 0u)};
+                const Totals t1{before.mass + (weights ? mass[i] : 0ull), before.count + (counts ? number[i] : 0u)};
                 const u64 from_here = by_count ? (u64)t0.count : t0.mass, to_here = by_count ? (u64)t1.count : t1.mass;
                 if ((from_here < target || i == 0) && (target <= to_here || i == slice - 1))     // (whatever the target, some bin is found)
                     for (int r = 0; r < cluster; ++r) of_peer(&box, r)->place = Place{t0, t1, owner * slice + i};
@@ -526,10 +528,10 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
         cluster_sync_all();
         return box.place;
     };
-    // the value at which the running count (or weight) comes to `target`
+    // The value at which the running count (or weight) comes to `target`.  By count: what comes before is counted and weighed; by weight: weighed only.
     int turn = 0;
     auto find = [&](bool by_count, u64 target) -> Found {
-        Place at_bin = locate(0, by_count, target, Totals{0ull, 0u});
+        Place at_bin = locate(0, by_count, by_count, target, Totals{0ull, 0u});
         uint32_t lo = 0u, hi = 0xffffffffu;                  // keys of the bin, once it is one of keys
         bool keys = false;
         for (int level = 0;; ++level) {                      // (a histogram of keys narrows them down to a 2048th of their range)
@@ -619,8 +621,8 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
             clear();
             const uint32_t width = hi - lo;
             const int by = max(0, 21 - __clz(width));        // at most 2048 bins
-            for (int counts = 1; counts >= 0; --counts) {
-                if (!counts) clear();
+            for (int counts = by_count; counts >= 0; --counts) {
+                if (by_count && !counts) clear();
                 each([&](const float (&x)[VEC], int) {
 #pragma unroll
                     for (int k = 0; k < VEC; ++k) {
@@ -633,7 +635,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
                 });
                 add_up(1, counts);
             }
-            at_bin = locate(1, by_count, target, at_bin.before);
+            at_bin = locate(1, by_count, by_count, target, at_bin.before);
             const uint32_t b_lo = (uint32_t)at_bin.bin << by, b_hi = b_lo + ((1u << by) - 1u);
             const uint32_t top_key = hi;
             hi = top_key - b_lo;
@@ -681,7 +683,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
             add_up(0, true);
             uint32_t count = 0u;
             for (int r = 0; r < cluster; ++r) count += box.slice[0][r].count;
-            const Place p = locate(0, true, min((u64)top_k, (u64)count), Totals{0ull, 0u});
+            const Place p = locate(0, true, false, min((u64)top_k, (u64)count), Totals{0ull, 0u});
             if (p.upto.count > kList) break;
             bin = p.bin;
         }
@@ -799,10 +801,10 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
         uint32_t count = 0u;
         for (int r = 0; r < cluster; ++r) {
             sum += box.slice[0][r].mass;
-            count += box.slice[0][r].count;
+            if (counts) count += box.slice[0][r].count;
         }
         total = total_of();
-        if (top_k > 0 && (uint32_t)top_k < count) {
+        if (counts && (uint32_t)top_k < count) {
             const Found f = find(true, (u64)top_k);
             sum = f.mass + f.weight * ((u64)top_k - f.count);
         }
