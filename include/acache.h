@@ -475,7 +475,9 @@ acache_status acache_predict_commit(acache_ctx *ctx, const void *h, int32_t h_ro
 
 /* acache_predict_commit with tokens drawn from the logits (acache_sample_tokens) instead of the arg max; the commit rule is the same, on the drawn
  * token's confidence; a row without a token (-1) is not committed.  logits: DEVICE fp32 [B * n_blk, vocab] out (the LM head's sums, not rounded
- * further); how: a setting per row, or with rows_per_setting = n_blk per request; u: DEVICE fp32 [B, n_blk].  With T = 0 token and commit are acache_predict_commit's. */
+ * further); how: a setting per row, or with rows_per_setting = n_blk per request; u: DEVICE fp32 [B, n_blk].  With T = 0 the token is
+ * acache_predict_commit's, where no logit is a NaN.  The two calls add up their confidences in fp32 in orders of their own, within 2^-14 of one
+ * another: of rows that lie that close to the threshold, or to the largest of their request, one call may commit what the other does not. */
 acache_status acache_predict_sample(acache_ctx *ctx, const void *h, int32_t h_rows, const int32_t *block_rows, int32_t batch, int32_t n_blk,
                                     const void *final_norm_g, const void *w_lm, int32_t vocab, float *logits, const acache_sampling *how,
                                     const float *u, float threshold, int32_t *token, float *confidence, int32_t *commit,

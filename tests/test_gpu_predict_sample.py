@@ -77,3 +77,28 @@ def test_tensors_that_do_not_fit_are_refused_before_any_launch():
     assert head.ctx.launch_count() == launches
     head.ctx.predict_sample(**good)
     assert head.ctx.launch_count() > launches and head.ctx.poll_status() == 0 and (token >= 0).all()
+
+
+def committed(conf, threshold):
+    over = conf > threshold
+    first = torch.arange(conf.shape[1], device=DEV) == conf.argmax(1)[:, None]
+    return torch.where(over.any(1, keepdim=True), over, first).to(torch.int32)
+
+
+@pytest.mark.parametrize("V,B,n_blk", [(16640, 9, 32), (640, 2, 40)])
+def test_without_a_temperature(V, B, n_blk):
+    """Tokens are the arg max's, and each call's commits follow from its own confidences, also at thresholds that one of those equals.
+
+    How far the confidences may differ, in roundings of 2^-24.  An exponential is off by 4 + 2.4 |x| of them (2 + 1.17 |x| units in the last place), |x| on
+    average over a row's weight at most ln(262144) = 12.5: 34.  One call adds 128 terms in a row (128) with 4 corrections of 6 (24) and joins some 14 such sums by
+    two exponentials, two products and an addition each (112); the other adds 36 in a row, behind up to 32 corrections of 6 (228).  560 in all, below 2^-14."""
+    head = Head(V, B, n_blk, V)
+    zero = torch.zeros(B, device=DEV)
+    conf = head.sample(0.5, temperature=zero, rows_per_setting=n_blk)[1]
+    for t in (0.9, 0.3, 0.0, float(conf[0, 0]), float(conf[-1, -1]), float(conf.max()), float(conf.min())):
+        token, conf, commit = head.sample(t, temperature=zero, rows_per_setting=n_blk)
+        arg = head.out()
+        head.ctx.predict_commit(head.h, n_blk, head.rows, B, n_blk, head.gain, head.w_lm, V, t, *arg)
+        assert torch.equal(token, arg[0]) and torch.equal(token.view(-1), head.logits.argmax(1).to(torch.int32))
+        assert ((conf - arg[1]).abs() <= 2 ** -14 * arg[1]).all()
+        assert torch.equal(commit, committed(conf, t)) and torch.equal(arg[2], committed(arg[1], t))
