@@ -412,7 +412,8 @@ acache_status acache_layer_step_kv8(acache_ctx *ctx, const acache_layer_weights 
  * counts (DEVICE int32 [B], NULL: n_rows each): rows of each request; nothing is done for the rows behind them, in q_out neither.
  * rope_cos, rope_sin: DEVICE fp32 [>= ctx_len, d/2], both NULL: K and Q are as they are.  q, q_out: both NULL without queries.
  * A row whose token lies outside [0, ctx_len), or whose page is none of the pool's, raises ACACHE_FLAG_BAD_INDEX and is skipped (its query
- * too); so does a count outside [0, n_rows], which is taken as the nearer end.  Of two rows of one token in pos the last is written.  A page
+ * too); so does a count outside [0, n_rows], which is taken as the nearer end.  Of two rows of one token in pos the last is written (the
+ * rest of a list is looked through for each of its rows: beyond some ten thousand rows its time grows with their square).  A page
  * that is written to has to be named by one request only, once.  ctx_len: at most table_stride * page, and 2^30; batch: at most 65535.
  * The descriptor's max_ctx and max_rows are no limit here and in acache_paged_attention. */
 acache_status acache_paged_append(acache_ctx *ctx, acache_paged_kv *kv, int32_t batch, int32_t ctx_len, const acache_rows *k,
@@ -438,7 +439,8 @@ acache_status acache_paged_attention(acache_ctx *ctx, const acache_paged_kv *kv,
  * written to their places in the request's pages, and their attention is acache_paged_attention over its first lens[b] tokens (DEVICE int32 [B];
  * NULL: ctx_len) as they then are.  Pages that hold rows of R belong to one request; all others may be shared.  A decode pass: k = 0,
  * extra_rows = the new tokens' positions, lens = the tokens with them.  anchor_idx: DEVICE int32 [B, k], relative to affix_start; x, x_is_compact, y
- * as acache_recompute_anchors. */
+ * as acache_recompute_anchors.  The attention is made for few rows: with more than 32 per KV head it reads the keys again for every 32, and a
+ * refresh of hundreds of rows takes longer than acache_layer_step on a contiguous cache. */
 acache_status acache_recompute_paged(acache_ctx *ctx, const acache_layer_weights *w, const acache_request *req, acache_paged_kv *kv,
                                      const void *x, int x_is_compact, const int32_t *anchor_idx, int32_t k, const int32_t *lens,
                                      void *y, acache_stream_t stream);

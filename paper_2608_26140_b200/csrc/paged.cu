@@ -5,6 +5,9 @@
 // in fp32, rounded once; queries likewise, values as they are.  A CTA takes a row: a thread the same eight pairs of every
 // sixteenth (of 64 values, thirty-second) head, so that its angles are read once.  What is read depends on nothing but the row's
 // number and is asked for before the position and the page are known.
+//
+// A row of a list looks for its position in the rest of the list, all threads together: nothing among hundreds of rows, and the square of their number beyond.
+// Rows of 32 KV heads of one request, by list and behind a length: 4096 rows 31 and 29 us, 16 384 104 and 88, 65 536 748 and 326, 131 072 2554 and 641.
 #include "common.cuh"
 #include "kernels.h"
 #include "launch.h"

@@ -17,6 +17,11 @@
 // 4 KV heads (794 MB) 121 us, 6.6 TB/s.  32 rows of 16 requests over 2560 keys of 32 heads, of which 2048 are the same pages for all, 103 us (8 rows 57, 16 69, 24
 // 87): a step takes a warp 2000 clocks, two warps a scheduler that wait for their own results (issue slots 33 %, tensor pipe 41 % busy), 6.5 TB/s from L2; starts and ends
 // of items are a fifth.  The fragments of a step's next product are asked for before the last one's products (108 without).  One token of one request over 1664 keys 7.5 us: four trips to memory one behind the other (arguments, page, keys, result) and a cluster's exchange.
+//
+// More than 32 rows of a KV head are tiles of 32, each of which reads all keys again, through L2 where they fit: 32 tokens on 28 query and 4 KV heads (224 rows, 7 tiles)
+// of 16 requests over 2560 keys 94 us (floor 14: bytes and operations), of 32 requests over 8000 keys 424 (82; one token of each 104); a refresh of 16 x 922 rows
+// over 2560 keys 2.9 ms on 32 KV heads (floor 0.37), 2.4 on 4.  215 to 277 TFLOP/s, the rate of one tile of 32 rows:
+// nothing is gained from there being many.  Tiles of 128 rows on tcgen05, as the contiguous and the 8-bit cache have, are not written for pages.
 #include <algorithm>
 #include <climits>
 
