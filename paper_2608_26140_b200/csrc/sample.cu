@@ -17,7 +17,7 @@
 //    another histogram of their keys.  A search ends at a value; among the tokens that have it the index decides.
 // The sum for the confidence is kept while the row comes in, against each thread's largest logit so far.
 //
-// What bounds it: 512 rows of 126464 fp32 logits, each with settings of its own, 236 us (floor 40), 128 bf16 rows with top_p 100 us, one row with top_k
+// What bounds it: 512 rows of 126464 fp32 logits, each with settings of its own, 233 us (floor 40), 128 bf16 rows with top_p 101 us, one row with top_k
 // and top_p 11.0 us.  The chain of steps of a row, two CTAs an SM: of the 50 us that a CTA of 31616 bf16 logits takes without a top_k, 17 are the weights (conflicts
 // of the atomics: random bins meet about four to a bank), 5 the row, 14 two searches, the rest barriers and sums; a word to another CTA is there after 0.6 us,
 // a barrier of the cluster takes 0.25.  Issue slots are busy for half of the time.
